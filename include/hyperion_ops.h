@@ -208,6 +208,100 @@ HYP_API int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int
                                 int32_t max_pages_per_seq, const int32_t* cu_q, const int32_t* ctx_lens, void* out,
                                 void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators over the paged cache for serving (none of them has a counterpart in the paper).  Queries are already
+ * rotated fp16 rows, q 16-byte aligned, q_stride (elements) a multiple of 8; out fp16 [rows, n_q_heads * D], 16-byte
+ * aligned; kv_pages 16-byte aligned.  Scores, softmax state and sums are fp32; the softmax weights enter the value
+ * product as fp16 relative to a running maximum.
+ * Decode calls take ctx_lens as hyp_op_attn_decode does: the new token sits at position ctx_lens[b] and its key and value
+ * are already in the cache.  ctx_lens[b] = -1 marks a row that has nothing of its own to see (padding of a batch);
+ * a row that sees nothing at all gives zeros.  Cache slots behind a sequence's end may hold anything.  Lengths are read
+ * on the device and clamped to what the table's row can name; table entries behind a sequence's end are not read.
+ * All lengths and tables may change between replays of a captured graph; the shapes and sizes passed by value may not.
+ * Scratch is caller-owned, 16-byte aligned, needs no initialisation and keeps nothing between calls; two calls whose
+ * kernels can overlap need a scratch each.  Pointers belong to the current device.  The first attention call on a process
+ * allocates one device word for error reporting (bounded waits): make it before capturing a graph.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Modification of the scores s = q . k / sqrt(D) of query position i and key position j, in this order:
+ *   softcap > 0      s = softcap * tanh(s / softcap)
+ *   slopes           s = s - slopes[h] * |i - j|                         (query head h)
+ *   visible keys     j <= i and (window == 0 or i - j < window), or j < prefix_lens[b]
+ * The prefix is visible to every row, those before its end included (as far as it is in the cache). */
+typedef struct {
+  float softcap;              /* 0 = none                                                              */
+  int32_t window;             /* 0 = none                                                              */
+  const float* slopes;        /* DEVICE fp32 [n_q_heads] or NULL                                       */
+  const int32_t* prefix_lens; /* DEVICE int32 [n_seqs] or NULL                                         */
+} hyp_attn_mod;
+
+/* hyp_op_attn_decode with modified scores; only the pages that hold visible keys are read.
+ * scratch: hyp_op_attn_mod_scratch_bytes(...) bytes (0 on bad arguments).
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
+HYP_API size_t hyp_op_attn_mod_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
+HYP_API int hyp_op_attn_decode_mod(const hyp_attn_shape* shape, const hyp_attn_mod* mod, int32_t n_seqs, const void* q,
+                                   int64_t q_stride, const void* kv_pages, const int32_t* block_table,
+                                   int32_t max_pages_per_seq, const int32_t* ctx_lens, void* scratch, size_t scratch_bytes,
+                                   void* out, void* stream);
+
+/* hyp_op_attn_prefill with modified scores (either head size runs on the tcgen05 tensor cores).  Sequences without new
+ * rows (cu_q[i] = cu_q[i + 1]) are allowed.  Rows at or behind cu_q[n_seqs] are left as they were.
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (more than 65535 row tiles), HYP_ECUDA. */
+HYP_API int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_attn_mod* mod, int32_t n_seqs, int32_t M,
+                                    const void* q, int64_t q_stride, const void* kv_pages, const int32_t* block_table,
+                                    int32_t max_pages_per_seq, const int32_t* cu_q, const int32_t* ctx_lens, void* out,
+                                    void* stream);
+
+/* Decode attention that also sums the weight every cached position receives:
+ *   w_out[b, kvh, j] = decay * w_in[b, kvh, j] + sum over the query heads h of kvh of p[b, h, j]      j < ctx_lens[b]
+ *   w_out[b, kvh, ctx_lens[b]] = sum over h of p[b, h, ctx_lens[b]]                       (the new token's sum starts here)
+ * with p the softmax weights of hyp_op_attn_decode.  Entries behind the new token are left as they were.
+ *   weights_in  DEVICE fp32 [n_seqs, n_kv_heads, weights_stride], or NULL (all zero)
+ *   weights_out the same shape; may be weights_in itself, must not overlap it otherwise
+ *   weights_stride >= 16 * max_pages_per_seq
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
+HYP_API size_t hyp_op_attn_scored_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
+HYP_API int hyp_op_attn_decode_scored(const hyp_attn_shape* shape, int32_t n_seqs, const void* q, int64_t q_stride,
+                                      const void* kv_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                                      const int32_t* ctx_lens, float decay, const float* weights_in, float* weights_out,
+                                      int64_t weights_stride, void* scratch, size_t scratch_bytes, void* out, void* stream);
+
+/* Cut every sequence's cache to n_keep tokens.  Per sequence and KV head, of n_cached[b] > n_keep tokens stay the first
+ * n_sink, the last n_recent and, of the others, those of the largest weight (ties: the lowest position; NaN counts as
+ * -infinity); a sequence with n_cached[b] <= n_keep keeps all.  The kept tokens' keys, values and weights move, in their
+ * order, to slots 0, 1, ... of the destination.  (Keys keep the rotation of their original position: the caller goes on
+ * counting positions from there when it rotates the next query and key.)
+ *   n_cached   DEVICE int32 [n_seqs]: tokens in the cache
+ *   weights_in DEVICE fp32 [n_seqs, n_kv_heads, weights_stride], weights_stride >= 16 * max_pages_per_seq
+ *   dst_pages, dst_table [n_seqs, dst_pages_per_seq]: where the kept rows go.  Either kv_pages and block_table themselves
+ *              (in place: the pages behind the new length become free), or pages that are not among the source pages
+ *              (of the same pool or of another one); 16 * dst_pages_per_seq >= n_keep
+ *   kept       DEVICE int32 [n_seqs, n_kv_heads, n_keep]: the old slot of every kept token, -1 behind the new length
+ *   new_lens   DEVICE int32 [n_seqs]: min(n_cached, n_keep); not n_cached itself
+ *   weights_out DEVICE fp32 [n_seqs, n_kv_heads, weights_out_stride]: the kept tokens' weights; may be weights_in itself
+ *              (equal strides); entries behind the new length are left as they were, and so are such cache rows
+ * n_keep >= 1, n_sink + n_recent <= n_keep.  Errors: HYP_EINVAL, HYP_ECUDA. */
+HYP_API int hyp_op_kv_evict(const hyp_attn_shape* shape, int32_t n_seqs, const void* kv_pages, const int32_t* block_table,
+                            int32_t max_pages_per_seq, const int32_t* n_cached, const float* weights_in,
+                            int64_t weights_stride, int32_t n_keep, int32_t n_sink, int32_t n_recent, void* dst_pages,
+                            const int32_t* dst_table, int32_t dst_pages_per_seq, int32_t* kept, int32_t* new_lens,
+                            float* weights_out, int64_t weights_out_stride, void* stream);
+
+/* Decode attention of a batch whose groups of sequences share a long prefix: group g holds the sequences cu_group[g] ..
+ * cu_group[g+1]-1, its prefix's prefix_lens[g] tokens are kept once, in the pages of prefix_table[g]; block_table and
+ * ctx_lens describe what every sequence has behind the prefix (its own token t sits at position prefix_lens[g] + t).
+ * The prefix is read once per group (per 128 / (n_q_heads / n_kv_heads) sequences), not once per sequence.
+ *   cu_group int32 [n_groups + 1] ascending from 0 to n_seqs, empty groups allowed; prefix_table int32
+ *   [n_groups, max_prefix_pages]; prefix_lens int32 [n_groups], 0 allowed
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, more than 2^31 CTAs), HYP_ECUDA. */
+HYP_API size_t hyp_op_attn_shared_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t n_groups,
+                                                int32_t max_prefix_pages, int32_t max_pages_per_seq);
+HYP_API int hyp_op_attn_decode_shared(const hyp_attn_shape* shape, int32_t n_seqs, const void* q, int64_t q_stride,
+                                      const void* kv_pages, int32_t n_groups, const int32_t* cu_group,
+                                      const int32_t* prefix_table, int32_t max_prefix_pages, const int32_t* prefix_lens,
+                                      const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
+                                      void* scratch, size_t scratch_bytes, void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,417 @@
+// Decode attention with modified scores, decode attention that sums the weights each cached position receives, and
+// shared-prefix decode attention (see attn_paged.cuh and attn_tile.cuh for the two CTA bodies).
+#include "attn_tile.cuh"
+#include "cache_ops.cuh"
+#include "gemm_tc.cuh"
+
+namespace hyp {
+
+namespace {
+
+constexpr int PD_WARPS = 4;      // decode kernels
+template <int D>
+constexpr int pd_slots() { return D == 128 ? 2 : 4; }  // 64 KB of ring: three CTAs per SM
+
+template <int D, int G, int MODE>
+__global__ void __launch_bounds__(PD_WARPS * 32) paged_decode_kernel(PagedArgs a) {
+  extern __shared__ __align__(128) uint8_t pd_smem[];
+  __shared__ uint64_t bars[PD_WARPS * pd_slots<D>()];
+  pdl_wait();     // queries, lengths and cache rows may come from the kernel launched just before
+  pdl_trigger();  // after the wait: nothing of this operator runs before its inputs exist
+  paged_body<D, G, MODE, PD_WARPS, pd_slots<D>()>(a, pd_smem, bars, blockIdx.x, gridDim.x, blockIdx.y, blockIdx.z, threadIdx.x,
+                                                  [] { __syncthreads(); });
+}
+
+// Joins the partial rows of one (sequence, query head) and writes fp16.
+template <int D>
+__global__ void paged_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots, __half* __restrict__ out) {
+  pdl_wait();
+  pdl_trigger();
+  const size_t row = blockIdx.x;  // b * Hq + h
+  out[row * D + threadIdx.x] = __float2half_rn(paged_merge_element<D>(acc, ml, row * n_slots, n_slots, threadIdx.x));
+}
+
+// Second kernel of the scored operator.  grid (key chunks, Hkv, n_seqs): every CTA joins the splits' (maximum,
+// denominator) of its G query heads, turns its chunk of scores into weights and adds them to the running sums; the
+// CTA of chunk 0 also joins the value sums.
+constexpr int SC_THREADS = 256, SC_KEYS = 1024;
+template <int D, int G>
+__global__ void __launch_bounds__(SC_THREADS)
+scored_finish_kernel(PagedArgs a, float decay, const float* __restrict__ w_in, float* __restrict__ w_out, long long w_stride,
+                     __half* __restrict__ out) {
+  __shared__ float s_m[G], s_inv[G];
+  pdl_wait();
+  pdl_trigger();
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
+  const int k_begin = blockIdx.x * SC_KEYS;
+  if (blockIdx.x > 0 && k_begin >= total) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const size_t row0 = (size_t)b * a.Hq + kvh * G;
+  if (warp < G) {
+    const float* ml = a.ml + (row0 + warp) * a.n_slots * 2;
+    float mx = PG_NEG, l = 0.f;
+    for (int s = lane; s < a.n_slots; s += 32) mx = fmaxf(mx, ml[2 * s]);
+    mx = warp_max(mx);
+    for (int s = lane; s < a.n_slots; s += 32) l += ml[2 * s + 1] * ex2_approx(ml[2 * s] - mx);
+    l = warp_sum(l);
+    if (lane == 0) {
+      s_m[warp] = mx;
+      s_inv[warp] = l != 0.f ? 1.f / l : 0.f;
+    }
+  }
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int e = threadIdx.x; e < G * D; e += SC_THREADS) {
+      const int gq = e / D, dd = e % D;
+      out[(row0 + gq) * D + dd] = __float2half_rn(paged_merge_element<D>(a.acc, a.ml, (row0 + gq) * a.n_slots, a.n_slots, dd));
+    }
+  const float* wi = w_in ? w_in + ((long long)b * a.Hkv + kvh) * w_stride : nullptr;
+  float* wo = w_out + ((long long)b * a.Hkv + kvh) * w_stride;
+  for (int k = k_begin + threadIdx.x; k < min(total, k_begin + SC_KEYS); k += SC_THREADS) {
+    float w = 0.f;
+#pragma unroll
+    for (int gq = 0; gq < G; ++gq) w += ex2_approx(a.scores[(row0 + gq) * a.score_stride + k] - s_m[gq]) * s_inv[gq];
+    wo[k] = (wi && k < total - 1) ? fmaf(decay, wi[k], w) : w;  // the new token's sum starts here
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// shared prefix: one launch holds the CTAs of both parts, so that the tensor-core work on the prefixes runs beside the
+// streaming of the sequences' own pages; a second one joins the partial rows.
+// ---------------------------------------------------------------------------------------------
+struct SharedArgs {
+  PagedArgs own;              // slots prefix_splits ..
+  const int32_t* cu_group;
+  const int32_t* prefix_table;
+  int prefix_stride;
+  const int32_t* prefix_lens;
+  int n_groups, prefix_splits, own_splits, prefix_ctas;
+};
+constexpr int SH_WARPS = AT_THREADS / 32;
+template <int D>
+constexpr int sh_slots() { return D == 128 ? 2 : 4; }
+template <int D>
+constexpr int sh_smem() {
+  return AtGeom<D>::SMEM > paged_smem_bytes<D, SH_WARPS>(sh_slots<D>()) ? AtGeom<D>::SMEM : paged_smem_bytes<D, SH_WARPS>(sh_slots<D>());
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(AT_THREADS, 2)
+shared_decode_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
+  extern __shared__ __align__(128) uint8_t sh_smem_raw[];
+  __shared__ TileShared ts;
+  __shared__ uint64_t bars[SH_WARPS * sh_slots<D>()];
+  pdl_wait();
+  pdl_trigger();
+  if ((int)blockIdx.x >= a.prefix_ctas) {
+    const int i = blockIdx.x - a.prefix_ctas;
+    paged_body<D, G, PAGED_PLAIN, SH_WARPS, sh_slots<D>()>(a.own, sh_smem_raw, bars, i % a.own_splits, a.own_splits,
+                                                          (i / a.own_splits) % a.own.Hkv, i / (a.own_splits * a.own.Hkv),
+                                                          threadIdx.x, [] { __syncthreads(); });
+    return;
+  }
+  constexpr int T = AT_ROWS / G;
+  const int split = blockIdx.x % a.prefix_splits, kvh = (blockIdx.x / a.prefix_splits) % a.own.Hkv;
+  const int tile = blockIdx.x / (a.prefix_splits * a.own.Hkv);
+  int group, first, q0, len;
+  at_locate(a.cu_group, a.n_groups, T, tile, group, first, q0, len);
+  if (group < 0) return;
+  const int plen = min(max(a.prefix_lens[group], 0), a.prefix_stride * PG_PT);
+  const int all_tiles = (plen + AT_KEYS - 1) / AT_KEYS;
+  const int per = (all_tiles + a.prefix_splits - 1) / a.prefix_splits;
+  TileWork wk;
+  wk.head0 = kvh * G;
+  wk.kvh = kvh;
+  wk.row0 = first + q0;
+  wk.rows = min(T, len - q0);
+  wk.table = a.prefix_table + (long long)group * a.prefix_stride;
+  wk.key_end = plen;
+  wk.n_first = 0;
+  wk.second = split * per;
+  wk.n_tiles = max(0, min(per, all_tiles - split * per));
+  auto slot_of = [&](int t, int gh) { return ((size_t)(wk.row0 + t) * a.own.Hq + wk.head0 + gh) * a.own.n_slots + split; };
+  if (wk.n_tiles == 0) {  // the whole CTA: an empty share still has to say so
+    const int t = threadIdx.x / G, gh = threadIdx.x % G;
+    if (threadIdx.x < AT_ROWS && t < wk.rows) *reinterpret_cast<float2*>(a.own.ml + slot_of(t, gh) * 2) = make_float2(PG_NEG, 0.f);
+    return;
+  }
+  tile_body<D, false, false>(
+      &tm_q, &tm_kv, sh_smem_raw, ts, wk, G, a.own.Hkv, 0.f, nullptr, a.own.err,
+      [&](int, int& pos) {
+        pos = plen - 1;
+        return TileRow{0, plen - 1, 0};
+      },
+      [&](int t, int gh, bool valid, float m_ref, float l, auto load) {
+        const size_t row = slot_of(t, gh);
+        float* dst = a.own.acc + row * D;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t v[16], w[16];
+          load(c, v, w);
+          if (valid) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+              reinterpret_cast<uint4*>(dst + c)[4 + i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            }
+          }
+        }
+        if (valid) *reinterpret_cast<float2*>(a.own.ml + row * 2) = make_float2(m_ref, l);
+      });
+}
+
+// ---------------------------------------------------------------------------------------------
+// prefill with modified scores
+// ---------------------------------------------------------------------------------------------
+struct PrefillModArgs {
+  __half* out;
+  const int32_t* cu_q;
+  const int32_t* ctx;
+  const int32_t* table;
+  int table_stride, n_seqs, Hq, Hkv, G;
+  float softcap;
+  int window;
+  const float* slopes;
+  const int32_t* prefix;
+  int* err;
+};
+
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(AT_THREADS, 2)
+prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, PrefillModArgs a) {
+  extern __shared__ __align__(128) uint8_t pm_smem[];
+  __shared__ TileShared ts;
+  pdl_wait();
+  pdl_trigger();
+  const int T = AT_ROWS / a.G;
+  const int kvh = blockIdx.x;  // heads vary fastest: every head's heaviest tile is scheduled before any lighter one
+  int seq, first, q0, len;
+  // the last tiles of a sequence see the most keys: they go first
+  at_locate(a.cu_q, a.n_seqs, T, (int)gridDim.y - 1 - (int)blockIdx.y, seq, first, q0, len);
+  if (seq < 0) return;
+  const int ctx = max(a.ctx[seq], 0);
+  const int have = min(ctx + len, a.table_stride * PG_PT);  // tokens in the cache, the new rows included
+  const int pre = a.prefix ? min(max(a.prefix[seq], 0), have) : 0;
+  const int window = a.window > 0 ? a.window : 0x40000000;
+  TileWork wk;
+  wk.head0 = kvh * a.G;
+  wk.kvh = kvh;
+  wk.row0 = first + q0;
+  wk.rows = min(T, len - q0);
+  wk.table = a.table + (long long)seq * a.table_stride;
+  wk.key_end = have;
+  const int lo = max(ctx + q0 - window + 1, 0), hi = min(ctx + q0 + wk.rows, have);  // keys of the tile's rows: [lo, hi), [0, pre)
+  wk.n_first = (pre + AT_KEYS - 1) / AT_KEYS;
+  wk.second = max(lo / AT_KEYS, wk.n_first);
+  wk.n_tiles = wk.n_first + max((hi + AT_KEYS - 1) / AT_KEYS - wk.second, 0);
+  tile_body<D, CAP, BIAS>(
+      &tm_q, &tm_kv, pm_smem, ts, wk, a.G, a.Hkv, a.softcap, a.slopes, a.err,
+      [&](int t, int& pos) {
+        pos = ctx + q0 + t;
+        return TileRow{max(pos - window + 1, 0), min(pos, have - 1), pre};
+      },
+      [&](int t, int gh, bool valid, float, float l, auto load) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        __half* orow = a.out + ((size_t)(wk.row0 + t) * a.Hq + wk.head0 + gh) * D;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t v[16], w[16];
+          load(c, v, w);
+          if (valid) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              pk[i] = pack_f16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+              pk[8 + i] = pack_f16(__uint_as_float(w[2 * i]) * inv, __uint_as_float(w[2 * i + 1]) * inv);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              reinterpret_cast<uint4*>(orow + c)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+          }
+        }
+      });
+}
+
+PagedArgs paged_args(const CacheView& c, const __half* q, long long q_stride, float* scratch, int n_slots, int slot0, int* err) {
+  PagedArgs a{};
+  a.q = q; a.q_stride = q_stride;
+  a.pool = c.pool; a.table = c.table; a.table_stride = c.table_stride; a.ctx = c.ctx;
+  a.Hq = c.Hq; a.Hkv = c.Hkv;
+  a.acc = scratch;
+  a.ml = scratch + (size_t)c.n_seqs * c.Hq * n_slots * c.D;
+  a.n_slots = n_slots; a.slot0 = slot0;
+  a.err = err;
+  return a;
+}
+
+template <int D, int G, int MODE>
+int launch_paged(const PagedArgs& a, int n_splits, int n_seqs, cudaStream_t st) {
+  constexpr int smem = paged_smem_bytes<D, PD_WARPS>(pd_slots<D>());
+  const int rc = allow_smem<paged_decode_kernel<D, G, MODE>>(smem);
+  if (rc) return rc;
+  HYP_CUDA_TRY(launch_pdl<2>(paged_decode_kernel<D, G, MODE>, dim3(n_splits, a.Hkv, n_seqs), dim3(PD_WARPS * 32), (size_t)smem, st, a));
+  return 1;
+}
+
+template <int D>
+int launch_merge(const PagedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
+  HYP_CUDA_TRY(launch_pdl<2>(paged_merge_kernel<D>, dim3(n_seqs * a.Hq), dim3(D), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
+  return 1;
+}
+
+#define HYP_DG_DISPATCH(F)                                                            \
+  do {                                                                                \
+    const int G_ = c.Hq / c.Hkv;                                                      \
+    if (c.D == 128 && G_ == 1) return F(128, 1);                                      \
+    if (c.D == 128 && G_ == 2) return F(128, 2);                                      \
+    if (c.D == 128 && G_ == 4) return F(128, 4);                                      \
+    if (c.D == 128 && G_ == 8) return F(128, 8);                                      \
+    if (c.D == 64 && G_ == 1) return F(64, 1);                                        \
+    if (c.D == 64 && G_ == 2) return F(64, 2);                                        \
+    if (c.D == 64 && G_ == 4) return F(64, 4);                                        \
+    if (c.D == 64 && G_ == 8) return F(64, 8);                                        \
+    return HYP_EINVAL;                                                                \
+  } while (0)
+
+template <int D, int G>
+int decode_mod_dg(const PagedArgs& a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
+  const int rc = launch_paged<D, G, PAGED_MOD>(a, n_splits, n_seqs, st);
+  if (rc < 0) return rc;
+  const int rc2 = launch_merge<D>(a, n_seqs, out, st);
+  return rc2 < 0 ? rc2 : rc + rc2;
+}
+
+template <int D, int G>
+int decode_scored_dg(const PagedArgs& a, int n_splits, int n_seqs, float decay, const float* w_in, float* w_out, long long w_stride,
+                     __half* out, cudaStream_t st) {
+  const int rc = launch_paged<D, G, PAGED_SCORED>(a, n_splits, n_seqs, st);
+  if (rc < 0) return rc;
+  const int chunks = (a.table_stride * PG_PT + SC_KEYS - 1) / SC_KEYS;
+  HYP_CUDA_TRY(launch_pdl<2>(scored_finish_kernel<D, G>, dim3(chunks, a.Hkv, n_seqs), dim3(SC_THREADS), (size_t)0, st, a, decay, w_in,
+                             w_out, w_stride, out));
+  return rc + 1;
+}
+
+template <int D, int G>
+int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
+  constexpr int smem = sh_smem<D>();
+  const int rc = allow_smem<shared_decode_kernel<D, G>>(smem);
+  if (rc) return rc;
+  const unsigned grid = (unsigned)(a.prefix_ctas + a.own_splits * a.own.Hkv * n_seqs);
+  HYP_CUDA_TRY(launch_pdl<2>(shared_decode_kernel<D, G>, dim3(grid), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
+  const int rc2 = launch_merge<D>(a.own, n_seqs, out, st);
+  return rc2 < 0 ? rc2 : 1 + rc2;
+}
+
+template <int D, bool CAP, bool BIAS>
+int prefill_mod_launch(const CUtensorMap& mq, const CUtensorMap& mkv, const PrefillModArgs& a, int M, cudaStream_t st) {
+  constexpr int smem = AtGeom<D>::SMEM;
+  const int rc = allow_smem<prefill_mod_kernel<D, CAP, BIAS>>(smem);
+  if (rc) return rc;
+  const int T = AT_ROWS / a.G;
+  const int tiles = M / T + a.n_seqs;  // every sequence adds at most one ragged tile
+  if (tiles > 65535) return HYP_ECAPACITY;
+  HYP_CUDA_TRY(launch_pdl<2>(prefill_mod_kernel<D, CAP, BIAS>, dim3(a.Hkv, tiles), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
+  return 1;
+}
+
+}  // namespace
+
+int paged_splits(int n_seqs, int Hkv, int max_pages) {
+  // about four waves of three CTAs per SM at the longest length the table allows, so that ragged batches even out;
+  // at least two pages per warp, so that the ring has something to run ahead of
+  const int groups = n_seqs * Hkv;
+  int want = (12 * sm_count() + groups - 1) / groups;
+  const int cap = (max_pages + 2 * PD_WARPS - 1) / (2 * PD_WARPS);
+  if (want > cap) want = cap;
+  if (want > 64) want = 64;
+  return want < 1 ? 1 : want;
+}
+
+size_t paged_scratch_floats(int n_seqs, int Hq, int D, int n_slots) { return (size_t)n_seqs * Hq * n_slots * (D + 2); }
+
+int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half* q, long long q_stride, float* scratch,
+                      __half* out, int* err, cudaStream_t st) {
+  const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride);
+  PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
+  a.softcap = mod.softcap; a.window = mod.window; a.slopes = mod.slopes; a.prefix = mod.prefix_lens;
+#define HYP_F(DD, GG) decode_mod_dg<DD, GG>(a, ns, c.n_seqs, out, st)
+  HYP_DG_DISPATCH(HYP_F);
+#undef HYP_F
+}
+
+int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride, float decay, const float* w_in, float* w_out,
+                         long long w_stride, float* scratch, __half* out, int* err, cudaStream_t st) {
+  const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride);
+  PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
+  a.score_stride = c.table_stride * PG_PT;
+  a.scores = scratch + paged_scratch_floats(c.n_seqs, c.Hq, c.D, ns);
+#define HYP_F(DD, GG) decode_scored_dg<DD, GG>(a, ns, c.n_seqs, decay, w_in, w_out, w_stride, out, st)
+  HYP_DG_DISPATCH(HYP_F);
+#undef HYP_F
+}
+
+SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int n_groups, int prefix_pages, int own_pages) {
+  SharedPlan p;
+  const int T = AT_ROWS / (Hq / Hkv);
+  p.row_tiles = n_seqs / T + n_groups;  // every group adds at most one ragged tile
+  const int slots = 2 * sm_count();     // resident CTAs
+  const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
+  p.prefix_splits = slots / (full * Hkv);
+  const int most = (prefix_pages * PG_PT + 2 * AT_KEYS - 1) / (2 * AT_KEYS);  // at least two key tiles each
+  if (p.prefix_splits > most) p.prefix_splits = most;
+  if (p.prefix_splits > 32) p.prefix_splits = 32;
+  if (p.prefix_splits < 1) p.prefix_splits = 1;
+  const int groups = n_seqs * Hkv;
+  p.own_splits = (4 * slots + groups - 1) / groups;
+  const int cap = (own_pages + 2 * SH_WARPS - 1) / (2 * SH_WARPS);
+  if (p.own_splits > cap) p.own_splits = cap;
+  if (p.own_splits > 32) p.own_splits = 32;
+  if (p.own_splits < 1) p.own_splits = 1;
+  return p;
+}
+
+int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride, int n_groups, const int32_t* cu_group,
+                         const int32_t* prefix_table, int prefix_stride, const int32_t* prefix_lens, float* scratch,
+                         __half* out, int* err, cudaStream_t st) {
+  const SharedPlan p = shared_plan(c.n_seqs, c.Hq, c.Hkv, n_groups, prefix_stride, c.table_stride);
+  SharedArgs a{};
+  a.own = paged_args(c, q, q_stride, scratch, p.prefix_splits + p.own_splits, p.prefix_splits, err);
+  a.cu_group = cu_group; a.prefix_table = prefix_table; a.prefix_stride = prefix_stride; a.prefix_lens = prefix_lens;
+  a.n_groups = n_groups; a.prefix_splits = p.prefix_splits; a.own_splits = p.own_splits;
+  a.prefix_ctas = p.prefix_splits * c.Hkv * p.row_tiles;
+  CUtensorMap mq, mkv;
+  int rc = tc_make_q_map(&mq, q, c.n_seqs, q_stride, c.Hq, c.Hq / c.Hkv, c.D);
+  if (!rc) rc = tc_make_pool_map(&mkv, c.pool, c.D);
+  if (rc) return rc;
+#define HYP_F(DD, GG) decode_shared_dg<DD, GG>(mq, mkv, a, c.n_seqs, out, st)
+  HYP_DG_DISPATCH(HYP_F);
+#undef HYP_F
+}
+
+int launch_prefill_mod(const CacheView& c, const hyp_attn_mod& mod, int M, const __half* q, long long q_stride,
+                       const int32_t* cu_q, __half* out, int* err, cudaStream_t st) {
+  PrefillModArgs a{};
+  a.out = out; a.cu_q = cu_q; a.ctx = c.ctx; a.table = c.table; a.table_stride = c.table_stride;
+  a.n_seqs = c.n_seqs; a.Hq = c.Hq; a.Hkv = c.Hkv; a.G = c.Hq / c.Hkv;
+  a.softcap = mod.softcap; a.window = mod.window; a.slopes = mod.slopes; a.prefix = mod.prefix_lens;
+  a.err = err;
+  CUtensorMap mq, mkv;
+  int rc = tc_make_q_map(&mq, q, M, q_stride, c.Hq, a.G, c.D);
+  if (!rc) rc = tc_make_pool_map(&mkv, c.pool, c.D);
+  if (rc) return rc;
+  const bool cap = mod.softcap > 0.f, bias = mod.slopes != nullptr;
+#define HYP_F(DD)                                                                        \
+  if (c.D == DD) {                                                                       \
+    if (cap && bias) return prefill_mod_launch<DD, true, true>(mq, mkv, a, M, st);       \
+    if (cap) return prefill_mod_launch<DD, true, false>(mq, mkv, a, M, st);              \
+    if (bias) return prefill_mod_launch<DD, false, true>(mq, mkv, a, M, st);             \
+    return prefill_mod_launch<DD, false, false>(mq, mkv, a, M, st);                      \
+  }
+  HYP_F(128) HYP_F(64)
+#undef HYP_F
+  return HYP_EINVAL;
+}
+
+}  // namespace hyp

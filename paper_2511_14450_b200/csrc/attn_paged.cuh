@@ -1,0 +1,297 @@
+// Split decode attention over the paged cache, as a CTA body shared by the operators that need one query row per
+// sequence: attention with modified scores, attention that keeps its scores, and the sequences' own part of
+// shared-prefix attention.
+//
+// A CTA takes one (split, KV head, sequence): the visible pages of the sequence go round-robin over the splits and,
+// inside the CTA, over the warps; every warp streams its pages through its own ring of bulk copies (16 keys and 16 values of
+// one head are contiguous in the cache and already chunk-permuted for ldmatrix), forms the scores of the page's 16
+// keys for the G query heads that share the KV head (rows of one mma.sync.m16n8k16 operand), keeps its own running
+// maximum and denominator and its own O += P V.  No CTA-wide synchronisation inside the loop.  Bound by HBM: a page
+// of one head is 8 KB (head_dim 128) for 32 MMAs.
+// The CTA's result is one partial row per query head: sum of weighted values (fp32), maximum (log2 units), denominator.
+#pragma once
+#include "attn_common.cuh"
+#include "sm100_common.cuh"
+
+namespace hyp {
+
+constexpr int PG_PT = 16;           // tokens per page
+constexpr float PG_NEG = -1e30f;    // "no key seen yet": below every score that finite fp16 operands can form
+constexpr float PG_LOG2E = 1.4426950408889634f;
+
+enum PagedMode : int { PAGED_PLAIN = 0, PAGED_SCORED = 1, PAGED_MOD = 2 };
+
+struct PagedArgs {
+  const __half* q;            // row b at q + b * q_stride, head h at + h * D
+  long long q_stride;
+  const __half* pool;         // one block's page pool
+  const int32_t* table;       // [n_seqs, table_stride] page ids
+  int table_stride;
+  const int32_t* ctx;         // [n_seqs] tokens before the new one; -1 = nothing to see
+  int Hq, Hkv;
+  float* acc;                 // partial rows: ((b * Hq + h) * n_slots + slot0 + split) * D
+  float* ml;                  // the same rows' (maximum, denominator)
+  int n_slots, slot0;
+  int* err;
+  float* scores;              // PAGED_SCORED: [n_seqs * Hq][score_stride] scores in log2 units
+  int score_stride;
+  float softcap;              // PAGED_MOD: 0 = none
+  int window;                 // PAGED_MOD: 0 = none
+  const float* slopes;        // PAGED_MOD: [Hq] or null
+  const int32_t* prefix;      // PAGED_MOD: [n_seqs] or null
+};
+
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// cap * tanh(x) in log2 units from y = 2 x log2(e): tanh x = 1 - 2 / (1 + e^(2x)).  Saturates cleanly (e^(2x) = inf
+// gives +cap, 0 gives -cap); absolute error ~ 2^-22 * cap, where the hardware tanh (2^-11) would put a capped score
+// of 50 off by 0.02 and its weight off by 2 %.
+__device__ __forceinline__ float softcap_log2(float y, float cap_l2) {
+  return fmaf(-2.f * cap_l2, rcp_approx(1.f + ex2_approx(y)), cap_l2);
+}
+
+template <int D, int WARPS>
+constexpr int paged_smem_bytes(int slots) { return WARPS * slots * 2 * PG_PT * D * 2; }
+
+// `smem`: 128-byte aligned shared memory, paged_smem_bytes<D, WARPS>(SLOTS) bytes; `bars`: WARPS * SLOTS mbarriers.
+// WARPS warps of the CTA call this (warp = 0 .. WARPS - 1); `bar_sync` joins exactly those warps.
+template <int D, int G, int MODE, int WARPS, int SLOTS, typename Sync>
+__device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, uint64_t* bars, int split, int n_splits, int kvh,
+                                           int b, int tid, Sync bar_sync) {
+  constexpr int KS = D / 16, DN = D / 8, CPR = D / 8;
+  constexpr int PAGE_BYTES = PG_PT * D * 2;
+  constexpr int SLOT_BYTES = 2 * PAGE_BYTES;  // keys, then values
+  constexpr int THREADS = WARPS * 32;
+  static_assert(paged_smem_bytes<D, WARPS>(SLOTS) >= (2 * WARPS * 8 + WARPS * G * D) * 4, "the combine buffers reuse the ring");
+  const int warp = tid >> 5, lane = tid & 31;
+  const int g = lane >> 2, tq = lane & 3;
+
+  // visible keys: [lo, total) behind the query, and [0, pre)
+  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
+  int lo = 0, pre = 0;
+  if (MODE == PAGED_MOD) {
+    if (a.window > 0) lo = max(total - a.window, 0);
+    if (a.prefix) pre = min(max(a.prefix[b], 0), total);
+  }
+  const int n_pages = (total + PG_PT - 1) / PG_PT;
+  const int n_pre = MODE == PAGED_MOD ? (pre + PG_PT - 1) / PG_PT : 0;
+  const int p_lo = MODE == PAGED_MOD ? max(lo / PG_PT, n_pre) : 0;
+  const int n_vis = n_pre + max(n_pages - p_lo, 0);
+  auto page_index = [&](int i) {  // this warp's i-th page
+    const int v = split + n_splits * (warp + WARPS * i);
+    return MODE == PAGED_MOD ? (v < n_pre ? v : v - n_pre + p_lo) : v;
+  };
+  const int first = split + n_splits * warp, stride_p = n_splits * WARPS;
+  const int my_n = first < n_vis ? (n_vis - first + stride_p - 1) / stride_p : 0;
+
+  const int32_t* bt = a.table + (long long)b * a.table_stride;
+  const size_t page_elems = kv_page_elems(a.Hkv, PG_PT, D);
+  const size_t v_off = (size_t)a.Hkv * PG_PT * D;
+  const uint32_t my_bars = smem_u32(bars) + 8u * (warp * SLOTS);
+  const uint32_t my_ring = smem_u32(smem) + (uint32_t)(warp * SLOTS) * SLOT_BYTES;
+  // page ids: lane l holds the id of this warp's page base + l, for the 32 pages being issued and the 32 after them
+  auto load_ids = [&](int base) { return base + lane < my_n ? bt[page_index(base + lane)] : 0; };
+  int32_t ids_cur = load_ids(0), ids_next = load_ids(32);
+  auto issue = [&](int i, int slot) {  // all lanes call, i ascending
+    if (i > 0 && (i & 31) == 0) {
+      ids_cur = ids_next;
+      ids_next = load_ids(i + 32);
+    }
+    const int page = __shfl_sync(0xffffffffu, ids_cur, i & 31);
+    if (lane == 0) {
+      const __half* src = a.pool + (size_t)page * page_elems + (size_t)kvh * PG_PT * D;
+      const uint32_t dst = my_ring + slot * SLOT_BYTES, bar = my_bars + 8u * slot;
+      mbar_expect_tx(bar, SLOT_BYTES);
+      bulk_load(dst, src, PAGE_BYTES, bar);
+      bulk_load(dst + PAGE_BYTES, src + v_off, PAGE_BYTES, bar);
+    }
+  };
+  if (lane == 0) {
+    for (int s = 0; s < SLOTS; ++s) mbar_init(my_bars + 8u * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  for (int s = 0; s < SLOTS && s < my_n; ++s) issue(s, s);
+
+  // query heads kvh*G .. kvh*G+G-1 as operand rows 0..G-1 (rows G..15 are zero)
+  uint32_t qf[KS][2];  // [k step][k half]; only the "row g" halves of the fragment are non-zero
+  {
+    const __half* qrow = a.q + (long long)b * a.q_stride + (size_t)(kvh * G + (g < G ? g : 0)) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks][0] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + 16 * ks + 2 * tq) : 0u;
+      qf[ks][1] = g < G ? *reinterpret_cast<const uint32_t*>(qrow + 16 * ks + 8 + 2 * tq) : 0u;
+    }
+  }
+  const float sl2 = rsqrtf((float)D) * PG_LOG2E;
+  float cap_l2 = 0.f, cap_y = 0.f, slope_l2 = 0.f;
+  if (MODE == PAGED_MOD) {
+    if (a.softcap > 0.f) {
+      cap_l2 = a.softcap * PG_LOG2E;
+      cap_y = 2.f * sl2 / a.softcap;
+    }
+    if (a.slopes && g < G) slope_l2 = a.slopes[kvh * G + g] * PG_LOG2E;
+  }
+  float* srow = MODE == PAGED_SCORED ? a.scores + ((size_t)b * a.Hq + kvh * G + (g < G ? g : 0)) * a.score_stride : nullptr;
+
+  float o[DN][2];  // row g of each 8-wide output column tile (rows 8..15 are padding and dropped)
+#pragma unroll
+  for (int i = 0; i < DN; ++i) o[i][0] = o[i][1] = 0.f;
+  float m_run = PG_NEG, l_run = 0.f;
+
+  bool ok = true;
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int i = 0; i < my_n; ++i) {
+    if (!mbar_wait(my_bars + 8u * slot, phase, nullptr)) { ok = false; break; }
+    const uint32_t kt = my_ring + slot * SLOT_BYTES, vt = kt + PAGE_BYTES;
+    const int k0 = page_index(i) * PG_PT;
+    auto visible = [&](int key) { return MODE == PAGED_MOD ? key < total && (key >= lo || key < pre) : key < total; };
+    // slots that nobody may see can hold anything: their values are zeroed (a weight of 0 times infinity is not 0)
+    const bool partial = k0 + PG_PT > total || (MODE == PAGED_MOD && k0 < lo && k0 + PG_PT > pre);
+    if (partial) {
+      for (int e = lane; e < PG_PT * CPR; e += 32)
+        if (!visible(k0 + e / CPR))
+          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (uint32_t)e * 16u), "r"(0u) : "memory");
+      __syncwarp();
+    }
+
+    // scores of the page's 16 keys: two 8-key column tiles
+    float s[2][4];
+    s[0][0] = s[0][1] = s[0][2] = s[0][3] = 0.f;
+    s[1][0] = s[1][1] = s[1][2] = s[1][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int r = (lane & 7) + ((lane >> 4) << 3);
+      const int c = 2 * ks + ((lane >> 3) & 1);
+      uint32_t b0, b1, b2, b3;
+      ldsm_x4(kt + tile_off<D>(r, c), b0, b1, b2, b3);
+      mma_f16_16816(s[0], qf[ks][0], 0u, qf[ks][1], 0u, b0, b1);
+      mma_f16_16816(s[1], qf[ks][0], 0u, qf[ks][1], 0u, b2, b3);
+    }
+    const int key0 = k0 + 2 * tq;
+    float mx = m_run;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int key = key0 + 8 * nt + e;
+        float v;
+        if (MODE == PAGED_MOD) {
+          v = a.softcap > 0.f ? softcap_log2(s[nt][e] * cap_y, cap_l2) : s[nt][e] * sl2;
+          v = fmaf(slope_l2, (float)(key - (total - 1)), v);
+        } else {
+          v = s[nt][e] * sl2;
+        }
+        v = visible(key) ? v : PG_NEG;
+        s[nt][e] = v;
+        mx = fmaxf(mx, v);
+      }
+    if (MODE == PAGED_SCORED && g < G) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+        *reinterpret_cast<float2*>(srow + key0 + 8 * nt) = make_float2(s[nt][0], s[nt][1]);
+    }
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    const float corr = ex2_approx(m_run - mx);
+    m_run = mx;
+    float p[2][2];
+    float sum = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        p[nt][e] = visible(key0 + 8 * nt + e) ? ex2_approx(s[nt][e] - mx) : 0.f;
+        sum += p[nt][e];
+      }
+    l_run = l_run * corr + sum;
+    const uint32_t pa0 = pack_f16(p[0][0], p[0][1]), pa2 = pack_f16(p[1][0], p[1][1]);
+#pragma unroll
+    for (int dp = 0; dp < DN / 2; ++dp) {
+      const int r = (lane & 7) + (((lane >> 3) & 1) << 3);
+      const int c = 2 * dp + (lane >> 4);
+      uint32_t b0, b1, b2, b3;
+      ldsm_x4_t(vt + tile_off<D>(r, c), b0, b1, b2, b3);
+      float c0[4] = {o[2 * dp][0] * corr, o[2 * dp][1] * corr, 0.f, 0.f};
+      float c1[4] = {o[2 * dp + 1][0] * corr, o[2 * dp + 1][1] * corr, 0.f, 0.f};
+      mma_f16_16816(c0, pa0, 0u, pa2, 0u, b0, b1);
+      mma_f16_16816(c1, pa0, 0u, pa2, 0u, b2, b3);
+      o[2 * dp][0] = c0[0]; o[2 * dp][1] = c0[1];
+      o[2 * dp + 1][0] = c1[0]; o[2 * dp + 1][1] = c1[1];
+    }
+    __syncwarp();  // every lane's reads of the slot are done; hand it back to the copy engine
+    if (i + SLOTS < my_n) {
+      if (partial) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      issue(i + SLOTS, slot);
+    }
+    if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+  }
+  if (!ok) {
+    if (lane == 0) atomicCAS(a.err, 0, 21);
+    for (int s = 0; s < SLOTS; ++s) mbar_wait(my_bars + 8u * s, 0, nullptr), mbar_wait(my_bars + 8u * s, 1, nullptr);
+  }
+  bar_sync();  // every warp is done with its ring: the space is reused below
+
+  // combine the warps: (m, l) per head, then rescaled O
+  l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
+  l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+  float* sm_m = reinterpret_cast<float*>(smem);  // [WARPS][8]
+  float* sm_l = sm_m + WARPS * 8;                // [WARPS][8]
+  float* sm_o = sm_l + WARPS * 8;                // [WARPS][G][D]
+  if (g < G) {
+    if (tq == 0) {
+      sm_m[warp * 8 + g] = m_run;
+      sm_l[warp * 8 + g] = l_run;
+    }
+#pragma unroll
+    for (int dn = 0; dn < DN; ++dn)
+      *reinterpret_cast<float2*>(sm_o + (warp * G + g) * D + 8 * dn + 2 * tq) = make_float2(o[dn][0], o[dn][1]);
+  }
+  bar_sync();
+  for (int e = tid; e < G * D; e += THREADS) {
+    const int gq = e / D, dd = e % D;
+    float mx = PG_NEG;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, sm_m[w * 8 + gq]);
+    float l = 0.f, acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float wgt = ex2_approx(sm_m[w * 8 + gq] - mx);
+      l += wgt * sm_l[w * 8 + gq];
+      acc += wgt * sm_o[(w * G + gq) * D + dd];
+    }
+    const size_t row = ((size_t)b * a.Hq + kvh * G + gq) * a.n_slots + a.slot0 + split;
+    a.acc[row * D + dd] = acc;
+    if (dd == 0) *reinterpret_cast<float2*>(a.ml + row * 2) = make_float2(mx, l);
+  }
+}
+
+// Joins the n_slots partial rows of one query head.  A row whose denominator is 0 has seen nothing: its values are not
+// read.  Returns the joined value of element dd; a query with nothing to see gives 0.
+template <int D>
+__device__ __forceinline__ float paged_merge_element(const float* acc, const float* ml, size_t row0, int n_slots, int dd) {
+  float mx = PG_NEG;
+  for (int s = 0; s < n_slots; ++s) mx = fmaxf(mx, ml[(row0 + s) * 2]);
+  float l = 0.f, v = 0.f;
+  for (int s = 0; s < n_slots; ++s) {
+    const float2 x = *reinterpret_cast<const float2*>(ml + (row0 + s) * 2);
+    if (x.y != 0.f) {  // NaN is carried on
+      const float wgt = ex2_approx(x.x - mx);
+      l += wgt * x.y;
+      v += wgt * acc[(row0 + s) * D + dd];
+    }
+  }
+  return l != 0.f ? v / l : 0.f;
+}
+
+}  // namespace hyp

@@ -1,0 +1,392 @@
+// Attention of a tile of 128 query rows against a run of paged keys on the tcgen05 tensor cores, as a CTA body.
+//
+// The 128 rows are 128 / G tokens (prefill) or sequences (shared prefix) times the G query heads that share one KV head,
+// so a KV head's keys and values pass once for all its query heads.  Keys / values go by in tiles of 64 tokens
+// (4 pages), two tiles in flight.
+//   warp 0   lanes 0-15 issue TMA: the query tile once (3-D box: 64 dims x G heads x 128 / G rows, 128-byte swizzle),
+//            then per tile one 2-D box per page and 64-wide half of head_dim for keys and for values.  The cache keeps
+//            a token's row chunk-permuted inside each 128-byte half, so a box of 16 rows x 128 bytes lands as a ready
+//            128-byte-swizzled operand.
+//   warp 1   issues tcgen05.mma: S_b = Q K^T (128 x 64) into one of two score buffers in tensor memory and, once the
+//            softmax warps have written the weights, O += P V (P from tensor memory).  The scores of tile j + 2 are
+//            issued right behind the value product of tile j, so the tensor core works ahead of the softmax.  In the
+//            tile that holds the end of the sequence it first zeroes the values behind the end (0 times garbage
+//            infinity is not 0).
+//   warps 2-5  softmax, one thread per query row (tensor-memory lane); the reference maximum is moved, and O rescaled,
+//            only when a row of the warp has outgrown it by 2^8.
+// Every barrier exists once per buffer (phase = tile / 2), every wait is bounded, failure unwinds through a shared flag.
+#pragma once
+#include "attn_paged.cuh"
+#include "tcgen05.cuh"
+
+namespace hyp {
+
+constexpr int AT_ROWS = 128, AT_KEYS = 64, AT_THREADS = 192;
+
+template <int D>
+struct AtGeom {
+  static constexpr int HALVES = D / 64;
+  static constexpr int Q_BYTES = HALVES * 128 * 64 * 2;
+  static constexpr int STAGE = AT_KEYS * D * 2;                  // one tile of keys (or values)
+  static constexpr int SMEM = Q_BYTES + 4 * STAGE + 1024;        // queries, keys[2], values[2], alignment
+};
+
+// What one CTA works on.  Key tile j of the walk is tile j of the sequence for j < n_first, else j - n_first + second.
+struct TileWork {
+  int head0;                  // first query head of the group: kvh * G
+  int kvh;
+  int row0;                   // first row of the query matrix
+  int rows;                   // rows (tokens or sequences) in the tile, <= 128 / G
+  const int32_t* table;       // page ids
+  int key_end;                // keys at or behind it exist for nobody (bounds the pages that are read)
+  int n_first, second, n_tiles;
+};
+// Which keys a row sees: [lo, hi] and [0, pre); for the distance bias `pos` is the row's position.
+struct TileRow {
+  int lo, hi, pre;
+};
+struct TileScore {
+  float softcap;              // CAP
+  float slope_l2;             // BIAS: this thread's slope times log2(e)
+};
+
+struct TileShared {
+  uint64_t bars[16];
+  uint32_t tmem_slot;
+  int abort_word;
+};
+
+__device__ __forceinline__ void at_tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void at_tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void at_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// MMA whose A operand is read from tensor memory (lane = row, two fp16 k-values per 32-bit column).
+__device__ __forceinline__ void at_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// MN-major operand of D (MN) x 16 (K) fp16, 128-byte swizzle: the 64-wide pieces of a page are 4 x 2 KB apart, 8-row
+// groups along K are 1024 B apart.
+__device__ __forceinline__ uint64_t at_desc_mn(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((4 * 2048) >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// Softmax of one 64-key tile for one query row: see the head of the file.
+template <int D, bool CAP, bool BIAS, bool MASKED>
+__device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, const TileRow& rw,
+                                           const TileScore& sc, int j, uint32_t o_prev, uint32_t o_parity,
+                                           volatile int* abort_flag, float& m_ref, float& l) {
+  const float sl2 = rsqrtf((float)D) * PG_LOG2E;
+  const float sl = CAP || BIAS ? 1.f : sl2;  // what the exponent still has to be multiplied with
+  uint32_t sv[AT_KEYS];
+  float mx = PG_NEG;
+#pragma unroll
+  for (int c = 0; c < AT_KEYS; c += 16) tmem_ld16(tmem_sb + lane_off + c, reinterpret_cast<uint32_t(&)[16]>(sv[c]));
+  tmem_ld_wait();
+  if (CAP || BIAS) {
+    const float cap_l2 = sc.softcap * PG_LOG2E, cap_y = CAP ? 2.f * sl2 / sc.softcap : 0.f;
+#pragma unroll
+    for (int i = 0; i < AT_KEYS; ++i) {
+      float t = __uint_as_float(sv[i]);
+      t = CAP ? softcap_log2(t * cap_y, cap_l2) : t * sl2;
+      if (BIAS) t = fmaf(-sc.slope_l2, fabsf((float)(key0 + i - pos)), t);
+      sv[i] = __float_as_uint(t);
+    }
+  }
+  auto visible = [&](int key) { return !MASKED || (key >= rw.lo && key <= rw.hi) || key < rw.pre; };
+  {  // four independent chains: one or two warps per scheduler leave little else to hide the latency behind
+    float m4[4] = {PG_NEG, PG_NEG, PG_NEG, PG_NEG};
+#pragma unroll
+    for (int i = 0; i < AT_KEYS; ++i) m4[i & 3] = fmaxf(m4[i & 3], visible(key0 + i) ? __uint_as_float(sv[i]) : PG_NEG);
+    mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sl;  // sl > 0
+  }
+  if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
+    const float new_ref = fmaxf(m_ref, mx);
+    if (j > 0) {
+      // O must hold every earlier tile before it is scaled
+      if (!__all_sync(0xffffffffu, mbar_wait(o_prev, o_parity, abort_flag))) return false;
+      tc_fence_after();
+      const float corr = ex2_approx(m_ref - new_ref);
+      l *= corr;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t v[16], w[16];
+        tmem_ld16(tmem_o + lane_off + c, v);
+        tmem_ld16(tmem_o + lane_off + c + 16, w);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
+          w[i] = __float_as_uint(__uint_as_float(w[i]) * corr);
+        }
+        at_tmem_st16(tmem_o + lane_off + c, v);
+        at_tmem_st16(tmem_o + lane_off + c + 16, w);
+      }
+    }
+    m_ref = new_ref;
+  }
+  const float neg_ref = -m_ref;
+  float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < AT_KEYS; c += 32) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      float p0 = ex2_approx(fmaf(__uint_as_float(sv[c + i]), sl, neg_ref));
+      float p1 = ex2_approx(fmaf(__uint_as_float(sv[c + i + 1]), sl, neg_ref));
+      if (MASKED) {
+        p0 = visible(key0 + c + i) ? p0 : 0.f;
+        p1 = visible(key0 + c + i + 1) ? p1 : 0.f;
+      }
+      l4[(i >> 1) & 3] += p0 + p1;
+      pk[i >> 1] = pack_f16(p0, p1);
+    }
+    at_tmem_st16(tmem_sb + lane_off + 32 + (c >> 1), pk);  // key k of the tile: 16-bit half k & 1 of column 32 + k / 2
+  }
+  l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+  at_tmem_st_wait();
+  return true;
+}
+
+// The whole CTA (192 threads) calls this.  `store(row, head_in_group, valid, m_ref, l, load)` is called by the softmax
+// threads at the end: load(c, v) reads 32 columns of the thread's O row from tensor memory (all lanes call it).
+template <int D, bool CAP, bool BIAS, typename RowFn, typename StoreFn>
+__device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtensorMap* tm_kv, uint8_t* smem_raw, TileShared& sh,
+                                          const TileWork& wk, int G, int Hkv, float softcap, const float* slopes, int* err,
+                                          RowFn row_fn, StoreFn store) {
+  using Geo = AtGeom<D>;
+  constexpr uint32_t IDESC_S = (1u << 4) | ((uint32_t)(AT_KEYS >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sQ = base, sK = base + Geo::Q_BYTES, sV = sK + 2 * Geo::STAGE;
+  // barriers: one per buffer b = tile & 1 (add 8 * b); phase of tile j = j / 2
+  const uint32_t bar0 = smem_u32(sh.bars);
+  const uint32_t q_full = bar0, k_full = bar0 + 16, v_full = bar0 + 32, s_full = bar0 + 80, p_full = bar0 + 96, o_done = bar0 + 112;
+  volatile int* abort_flag = &sh.abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_tiles = wk.n_tiles;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 16; ++i) mbar_init(bar0 + 8u * i, (i == 12 || i == 13) ? 128u : 1u);  // p_full: every softmax thread
+    sh.abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_slot)), "r"(256));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // columns 0-63 / 64-127: the two score buffers (P over the upper half of each); from 128: O
+  const uint32_t tmem_s = sh.tmem_slot, tmem_o = sh.tmem_slot + 128u;
+  auto key_tile = [&](int j) { return j < wk.n_first ? j : j - wk.n_first + wk.second; };
+
+  if (warp == 0) {
+    // ---------------- TMA producer: one box per lane and tile ----------------
+    // lanes 0-7 bring the keys, 8-15 the values; within each, lane = page (0-3) x 64-wide half of head_dim
+    if (lane == 0) {
+      mbar_expect_tx(q_full, Geo::Q_BYTES);
+      for (int h = 0; h < Geo::HALVES; ++h) at_tma_load_3d(sQ + h * 128 * 64 * 2, tm_q, h * 64, wk.head0, wk.row0, q_full);
+    }
+    const int is_v = lane >> 3, p = (lane >> 1) & 3, h = lane & 1;
+    if (lane < 16 && h < Geo::HALVES) {
+      const uint32_t full = is_v ? v_full : k_full;
+      const uint32_t empty = is_v ? o_done : s_full;  // a stage is free once the product that read it has drained
+      const uint32_t dst = is_v ? sV + (h * 4 + p) * 2048 : sK + h * (AT_KEYS * 128) + p * 2048;
+      const int last_page = (wk.key_end - 1) / PG_PT;
+      // Key lanes and value lanes advance independently (their stages drain at different times), so no lane may
+      // block in a wait the others have to reconverge with: every lane polls its own barrier once per turn.
+      bool ok = true;
+      int j = 0;
+      uint32_t idle = 0;
+      uint64_t t_idle = 0;
+      while (j < n_tiles) {
+        const uint32_t b = (uint32_t)(j & 1);
+        if (j < 2 || mbar_try(empty + 8 * b, (uint32_t)(((j >> 1) - 1) & 1))) {
+          const int pi = min(4 * key_tile(j) + p, last_page);  // past the last page: any valid page (its keys are masked)
+          const int row0 = ((wk.table[pi] * 2 + is_v) * Hkv + wk.kvh) * PG_PT;
+          if ((lane & 7) == 0) mbar_expect_tx(full + 8 * b, Geo::STAGE);  // a copy may land first: the count goes negative meanwhile
+          tma_load_2d(dst + b * Geo::STAGE, tm_kv, h * 64, row0, full + 8 * b);
+          ++j;
+          idle = 0;
+        } else if ((++idle & 1023u) == 0) {
+          const uint64_t now = globaltimer();
+          if (idle == 1024u) t_idle = now;
+          if (*abort_flag || now - t_idle > WAIT_LIMIT_NS) { ok = false; break; }
+        }
+      }
+      if (!ok && (lane & 7) == 0) {
+        *abort_flag = 1;
+        atomicCAS(err, 0, 22);
+      }
+      // no copy may be in flight when the CTA leaves: at the end of a clean run these have long completed
+      for (int i = max(0, j - 2); i < j && (lane & 7) == 0; ++i)
+        mbar_wait(full + 8 * (uint32_t)(i & 1), (uint32_t)((i >> 1) & 1), nullptr);
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer: the warp waits together, lane 0 issues ----------------
+    bool ok = mbar_wait(q_full, 0, abort_flag);
+    const uint64_t dq = smem_desc(sQ), dk = smem_desc(sK), dv = at_desc_mn(sV);
+    auto scores = [&](int j) -> bool {
+      const uint32_t b = (uint32_t)(j & 1);
+      const bool got = mbar_wait(k_full + 8 * b, (uint32_t)((j >> 1) & 1), abort_flag);
+      if (!__all_sync(0xffffffffu, got)) return false;
+      tc_fence_after();
+      if (lane == 0) {
+        const uint64_t dkb = dk + (uint64_t)(b * (Geo::STAGE >> 4));
+#pragma unroll
+        for (int kb = 0; kb < Geo::HALVES; ++kb)
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks)
+            tc_mma(tmem_s + 64u * b, dq + (uint64_t)(kb * ((128 * 64 * 2) >> 4) + ks * 2),
+                   dkb + (uint64_t)(kb * ((AT_KEYS * 128) >> 4) + ks * 2), IDESC_S, (kb | ks) ? 1u : 0u);
+        tc_commit(s_full + 8 * b);  // also frees the key stage
+      }
+      __syncwarp();
+      return true;
+    };
+    ok = __all_sync(0xffffffffu, ok);
+    ok = ok && scores(0);
+    if (ok && n_tiles > 1) ok = scores(1);
+    for (int j = 0; j < n_tiles && ok; ++j) {
+      const uint32_t b = (uint32_t)(j & 1), ph = (uint32_t)((j >> 1) & 1);
+      const bool got = mbar_wait(p_full + 8 * b, ph, abort_flag) && mbar_wait(v_full + 8 * b, ph, abort_flag);
+      if (!__all_sync(0xffffffffu, got)) { ok = false; break; }
+      const int left = wk.key_end - key_tile(j) * AT_KEYS;
+      if (left < AT_KEYS) {  // the end of the sequence lies in this tile
+        for (int e = lane; e < Geo::HALVES * (AT_KEYS - left) * 8; e += 32) {
+          const int h = e / ((AT_KEYS - left) * 8), r = left + (e % ((AT_KEYS - left) * 8)) / 8, c = e & 7;
+          const uint32_t dst = sV + b * Geo::STAGE + (uint32_t)(h * AT_KEYS + r) * 128u + (uint32_t)c * 16u;
+          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(dst), "r"(0u) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+      tc_fence_after();
+      if (lane == 0) {
+        // O += P V: 4 pages of 16 keys; P sits in tensor memory (8 columns per page)
+        const uint64_t dvb = dv + (uint64_t)(b * (Geo::STAGE >> 4));
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          at_mma_ta(tmem_o, tmem_s + 64u * b + 32u + (uint32_t)(8 * p), dvb + (uint64_t)(p * (2048 >> 4)), IDESC_PV,
+                    (j > 0 || p > 0) ? 1u : 0u);
+        tc_commit(o_done + 8 * b);  // also frees the value stage
+      }
+      __syncwarp();
+      // the scores of tile j + 2 reuse this tile's buffer: issued behind its value product
+      if (j + 2 < n_tiles) ok = scores(j + 2);
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      atomicCAS(err, 0, 23);
+    }
+  } else {
+    // ---------------- softmax / epilogue: thread = query row = tensor-memory lane ----------------
+    const int q = warp & 3;
+    const int r = 32 * q + lane;
+    const uint32_t lane_off = (uint32_t)(32 * q) << 16;
+    const int t = r / G, gh = r % G;
+    const bool valid = t < wk.rows;
+    const bool warp_idle = (32 * q) / G >= wk.rows;  // no row of this warp exists: its weights are never used
+    int pos;
+    const TileRow rw = row_fn(min(t, wk.rows - 1), pos);  // rows past the end are clamped: computed, never stored
+    TileScore sc{softcap, 0.f};
+    if (BIAS) sc.slope_l2 = slopes[wk.head0 + gh] * PG_LOG2E;
+    float m_ref = PG_NEG, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n_tiles && ok; ++j) {
+      const uint32_t b = (uint32_t)(j & 1);
+      ok = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * b, (uint32_t)((j >> 1) & 1), abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (!warp_idle) {
+        const int key0 = key_tile(j) * AT_KEYS;
+        // the value product of tile j - 1: buffer (j - 1) & 1, phase (j - 1) / 2
+        const uint32_t o_prev = o_done + 8 * (b ^ 1), o_parity = (uint32_t)(((j - 1) >> 1) & 1);
+        const bool whole = (key0 >= rw.lo && key0 + AT_KEYS - 1 <= rw.hi) || key0 + AT_KEYS <= rw.pre;
+        if (__any_sync(0xffffffffu, !whole))
+          ok = at_softmax<D, CAP, BIAS, true>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, m_ref, l);
+        else
+          ok = at_softmax<D, CAP, BIAS, false>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, m_ref, l);
+        if (!ok) break;
+      }
+      tc_fence_before();
+      mbar_arrive(p_full + 8 * b);
+    }
+    // the last value product (a commit follows every earlier one too)
+    if (ok && !mbar_wait(o_done + 8 * ((n_tiles - 1) & 1), (uint32_t)(((n_tiles - 1) >> 1) & 1), abort_flag)) ok = false;
+    ok = __all_sync(0xffffffffu, ok);
+    tc_fence_after();
+    if (ok && !warp_idle)
+      store(min(t, wk.rows - 1), gh, valid, m_ref, l, [&](int c, uint32_t (&v)[16], uint32_t (&w)[16]) {
+        tmem_ld16(tmem_o + lane_off + c, v);
+        tmem_ld16(tmem_o + lane_off + c + 16, w);
+        tmem_ld_wait();
+      });
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      atomicCAS(err, 0, 24);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem_slot), "r"(256));
+  }
+}
+
+// Which row tile of `tile_rows` rows is tile t?  Sets run from cu[i] to cu[i + 1] and are cut into tiles one by one.
+// Every warp finds it for itself, 32 sets at a time; set = -1: no such tile.
+__device__ __forceinline__ void at_locate(const int32_t* cu, int n_sets, int tile_rows, int t, int& set, int& first, int& q0, int& len) {
+  const int lane = threadIdx.x & 31;
+  set = -1;
+  first = q0 = len = 0;
+  int before = 0;
+  for (int i0 = 0; i0 < n_sets; i0 += 32) {
+    const int i = i0 + lane;
+    const int c0 = i < n_sets ? cu[i] : 0;
+    const int my_len = i < n_sets ? max(cu[i + 1] - c0, 0) : 0;
+    const int nt = (my_len + tile_rows - 1) / tile_rows;
+    int incl = nt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, t < before + incl);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      set = i0 + src;
+      first = __shfl_sync(0xffffffffu, c0, src);
+      len = __shfl_sync(0xffffffffu, my_len, src);
+      q0 = (t - before - __shfl_sync(0xffffffffu, incl - nt, src)) * tile_rows;
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+
+}  // namespace hyp

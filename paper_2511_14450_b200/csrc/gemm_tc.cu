@@ -848,6 +848,43 @@ int tc_make_kv_map(CUtensorMap* map, const void* kv_layer, size_t n_pages, int H
   return HYP_OK;
 }
 
+// Query rows [rows][Hq][D] (row stride `stride` elements) seen as {D, Hq, rows}: boxes of 64 dims x G heads x 128 / G rows.
+int tc_make_q_map(CUtensorMap* map, const void* q, int rows, long long stride, int Hq, int G, int D) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return HYP_ECUDA;
+  if (D % 64 || G < 1 || 128 % G || Hq % G || rows < 1 || stride % 8 || ((uintptr_t)q & 15) != 0) return HYP_EINVAL;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64u, (cuuint32_t)G, (cuuint32_t)(128 / G)};
+  const cuuint32_t estr[3] = {1u, 1u, 1u};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)q, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_last_cuda_error((int)r);
+    return HYP_ECUDA;
+  }
+  return HYP_OK;
+}
+
+// A block's page pool as rows of head_dim: boxes of 16 rows x 64 dims, no swizzle (the cache's rows carry it).  The
+// pool's size is not known to the operators; the map covers every row that a 32-bit row coordinate can name.
+int tc_make_pool_map(CUtensorMap* map, const void* pool, int D) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return HYP_ECUDA;
+  if (D % 64 || ((uintptr_t)pool & 15) != 0) return HYP_EINVAL;
+  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)0x7ffffff0u};
+  const cuuint64_t strides[1] = {(cuuint64_t)D * 2};
+  const cuuint32_t box[2] = {64u, 16u};
+  const cuuint32_t estr[2] = {1u, 1u};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, (void*)pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_last_cuda_error((int)r);
+    return HYP_ECUDA;
+  }
+  return HYP_OK;
+}
+
 // Activations: 128-row boxes for the tile kernels, 16/32/64-row boxes for the swapped-operand kernel.
 int tc_make_act(TcAct* a, const void* ptr, int rows, int K, bool f16) {
   a->ptr = ptr; a->rows = rows; a->K = K; a->f16 = f16;

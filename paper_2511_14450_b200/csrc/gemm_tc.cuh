@@ -50,6 +50,9 @@ int tc_make_act(TcAct* a, const void* ptr, int rows, int K, bool f16 = false);
 
 // Tensor map over one block's KV page pool for the tcgen05 prefill attention (head_dim 128).
 int tc_make_kv_map(CUtensorMap* map, const void* kv_layer, size_t n_pages, int Hkv, int D);
+// Tensor maps of the row-tile attention: query rows by heads, and a page pool of either head size.
+int tc_make_q_map(CUtensorMap* map, const void* q, int rows, long long stride, int Hq, int G, int D);
+int tc_make_pool_map(CUtensorMap* map, const void* pool, int D);
 // Prefill attention on tcgen05 (head_dim 128); q_map = TcAct::map of the rotated-query buffer.
 int& attn_prefill_tc_enabled();
 int launch_attn_prefill_tc(const CUtensorMap& q_map, const CUtensorMap& kv_map, __half* attn_out, const BatchMeta& bm,

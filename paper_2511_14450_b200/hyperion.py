@@ -42,6 +42,10 @@ class hyp_attn_shape(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
+class hyp_attn_mod(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("prefix_lens", C.c_void_p)]
+
+
 class HyperionError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -103,6 +107,24 @@ SIGNATURES = {
     "hyp_op_attn_prefill": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                                       C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                       C.c_void_p]),
+    "hyp_op_attn_mod_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32]),
+    "hyp_op_attn_decode_mod": (C.c_int, [C.POINTER(hyp_attn_shape), C.POINTER(hyp_attn_mod), C.c_int32, C.c_void_p, C.c_int64,
+                                         C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p,
+                                         C.c_void_p]),
+    "hyp_op_attn_prefill_mod": (C.c_int, [C.POINTER(hyp_attn_shape), C.POINTER(hyp_attn_mod), C.c_int32, C.c_int32, C.c_void_p,
+                                          C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p]),
+    "hyp_op_attn_scored_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32]),
+    "hyp_op_attn_decode_scored": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                            C.c_int32, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                            C.c_size_t, C.c_void_p, C.c_void_p]),
+    "hyp_op_kv_evict": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                  C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "hyp_op_attn_shared_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "hyp_op_attn_decode_shared": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
+                                            C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                            C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
     "hyp_strerror": (C.c_char_p, [C.c_int]),
     "hyp_last_cuda_error": (C.c_int, []),
 }
@@ -387,6 +409,173 @@ def hyp_op_attn_prefill(shape3, q, kv_pages, block_table, cu_q, ctx_lens, out, s
     _check(lib().hyp_op_attn_prefill(C.byref(sh), ctx_lens.shape[0], q.shape[0], _ptr(q), q.stride(0), _ptr(kv_pages),
                                      _ptr(block_table), block_table.stride(0), _ptr(cu_q), _ptr(ctx_lens), _ptr(out),
                                      _stream_handle(stream)), "hyp_op_attn_prefill")
+
+
+# --------------------------------------------------------------------------------------------
+# operators over the paged cache (hyperion_ops.h).  These check their tensors: type, device, shape, strides; a call that
+# does not fit raises HYP_EINVAL before anything is launched, and a call on tensors of another device than the current one
+# runs there (on that device's current stream unless one is given).
+# --------------------------------------------------------------------------------------------
+def _refuse(where: str, why: str):
+    err = HyperionError(HYP_EINVAL, where)
+    err.args = (f"{where}: {why} ({HYP_EINVAL})",)
+    raise err
+
+
+def _need(where, name, t, dtype, shape, device):
+    """A dense tensor of this type and shape (None in the shape: any size) on this device."""
+    if t.dtype != dtype or t.device != device or t.dim() != len(shape) or not t.is_contiguous():
+        _refuse(where, f"{name} must be a contiguous {dtype} tensor of {len(shape)} dimensions on {device}")
+    for have, want in zip(t.shape, shape):
+        if want is not None and have != want:
+            _refuse(where, f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
+
+
+def _need_query(where, shape3, q, out, kv_pages):
+    import torch
+    hq, hkv, d = shape3
+    if q.dtype != torch.float16 or not q.is_cuda or q.dim() != 2 or q.shape[1] < hq * d or q.stride(1) != 1:
+        _refuse(where, "q must be a CUDA fp16 matrix [rows, >= n_q_heads * head_dim] with dense rows")
+    if q.shape[0] > 1 and q.stride(0) < q.shape[1]:
+        _refuse(where, "the rows of q overlap")
+    _need(where, "out", out, torch.float16, (q.shape[0], hq * d), q.device)
+    _need(where, "kv_pages", kv_pages, torch.float16, (None, 2, hkv, 16, d), q.device)
+
+
+def _query_stride(q, shape3):
+    return q.stride(0) if q.shape[0] > 1 else (shape3[0] * shape3[2] + 7) // 8 * 8
+
+
+def _scratch_args(where, scratch, device):
+    if scratch.device != device or not scratch.is_contiguous():
+        _refuse(where, f"scratch must be a contiguous tensor on {device}")
+    return scratch.data_ptr(), scratch.numel() * scratch.element_size()
+
+
+def _call_on(device, fn, where, args, stream):
+    import torch
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream_handle(stream)), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream_handle(stream)), where)
+
+
+class AttnMod:
+    """hyp_attn_mod with its device tensors: softcap (0 = none), window (0 = none), slopes fp32 [n_q_heads] or None,
+    prefix_lens int32 [n_seqs] or None.  Keeps the tensors alive; make it once and use it in every call."""
+
+    def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_lens=None):
+        self.slopes, self.prefix_lens = slopes, prefix_lens
+        self.struct = hyp_attn_mod(softcap, window, None if slopes is None else slopes.data_ptr(),
+                                   None if prefix_lens is None else prefix_lens.data_ptr())
+
+    def check(self, where, shape3, n_seqs, device):
+        import torch
+        if self.slopes is not None:
+            _need(where, "slopes", self.slopes, torch.float32, (shape3[0],), device)
+        if self.prefix_lens is not None:
+            _need(where, "prefix_lens", self.prefix_lens, torch.int32, (n_seqs,), device)
+
+
+def hyp_op_attn_mod_scratch_bytes(shape3, n_seqs: int, max_pages_per_seq: int) -> int:
+    return lib().hyp_op_attn_mod_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, max_pages_per_seq)
+
+
+def hyp_op_attn_decode_mod(shape3, mod: AttnMod, q, kv_pages, block_table, ctx_lens, scratch, out, stream=None):
+    import torch
+    where, n = "hyp_op_attn_decode_mod", q.shape[0]
+    _need_query(where, shape3, q, out, kv_pages)
+    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
+    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
+    mod.check(where, shape3, n, q.device)
+    sp, sb = _scratch_args(where, scratch, q.device)
+    _call_on(q.device, lib().hyp_op_attn_decode_mod, where,
+             (C.byref(hyp_attn_shape(*shape3)), C.byref(mod.struct), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(),
+              block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), sp, sb, out.data_ptr()), stream)
+
+
+def hyp_op_attn_prefill_mod(shape3, mod: AttnMod, q, kv_pages, block_table, cu_q, ctx_lens, out, stream=None):
+    import torch
+    where, n = "hyp_op_attn_prefill_mod", ctx_lens.shape[0]
+    _need_query(where, shape3, q, out, kv_pages)
+    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
+    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
+    _need(where, "cu_q", cu_q, torch.int32, (n + 1,), q.device)
+    mod.check(where, shape3, n, q.device)
+    _call_on(q.device, lib().hyp_op_attn_prefill_mod, where,
+             (C.byref(hyp_attn_shape(*shape3)), C.byref(mod.struct), n, q.shape[0], q.data_ptr(), _query_stride(q, shape3),
+              kv_pages.data_ptr(), block_table.data_ptr(), block_table.shape[1], cu_q.data_ptr(), ctx_lens.data_ptr(),
+              out.data_ptr()), stream)
+
+
+def hyp_op_attn_scored_scratch_bytes(shape3, n_seqs: int, max_pages_per_seq: int) -> int:
+    return lib().hyp_op_attn_scored_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, max_pages_per_seq)
+
+
+def hyp_op_attn_decode_scored(shape3, q, kv_pages, block_table, ctx_lens, decay: float, weights_in, weights_out, scratch, out,
+                              stream=None):
+    """weights_in: fp32 [n_seqs, n_kv_heads, width] or None; weights_out the same shape, may be weights_in."""
+    import torch
+    where, n = "hyp_op_attn_decode_scored", q.shape[0]
+    _need_query(where, shape3, q, out, kv_pages)
+    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
+    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
+    _need(where, "weights_out", weights_out, torch.float32, (n, shape3[1], None), q.device)
+    if weights_in is not None:
+        _need(where, "weights_in", weights_in, torch.float32, tuple(weights_out.shape), q.device)
+    sp, sb = _scratch_args(where, scratch, q.device)
+    _call_on(q.device, lib().hyp_op_attn_decode_scored, where,
+             (C.byref(hyp_attn_shape(*shape3)), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(),
+              block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), decay,
+              None if weights_in is None else weights_in.data_ptr(), weights_out.data_ptr(), weights_out.shape[2], sp, sb,
+              out.data_ptr()), stream)
+
+
+def hyp_op_kv_evict(shape3, kv_pages, block_table, n_cached, weights_in, n_keep: int, n_sink: int, n_recent: int, dst_pages,
+                    dst_table, kept, new_lens, weights_out, stream=None):
+    """dst_pages, dst_table: kv_pages and block_table themselves (in place), or pages that are not among the source's."""
+    import torch
+    where, n, dev = "hyp_op_kv_evict", n_cached.shape[0], kv_pages.device
+    hq, hkv, d = shape3
+    if not kv_pages.is_cuda:
+        _refuse(where, "kv_pages must be a CUDA tensor")
+    _need(where, "kv_pages", kv_pages, torch.float16, (None, 2, hkv, 16, d), dev)
+    _need(where, "dst_pages", dst_pages, torch.float16, (None, 2, hkv, 16, d), dev)
+    _need(where, "block_table", block_table, torch.int32, (n, None), dev)
+    _need(where, "dst_table", dst_table, torch.int32, (n, None), dev)
+    _need(where, "n_cached", n_cached, torch.int32, (n,), dev)
+    _need(where, "new_lens", new_lens, torch.int32, (n,), dev)
+    _need(where, "kept", kept, torch.int32, (n, hkv, n_keep), dev)
+    _need(where, "weights_in", weights_in, torch.float32, (n, hkv, None), dev)
+    _need(where, "weights_out", weights_out, torch.float32, (n, hkv, None), dev)
+    _call_on(dev, lib().hyp_op_kv_evict, where,
+             (C.byref(hyp_attn_shape(*shape3)), n, kv_pages.data_ptr(), block_table.data_ptr(), block_table.shape[1],
+              n_cached.data_ptr(), weights_in.data_ptr(), weights_in.shape[2], n_keep, n_sink, n_recent, dst_pages.data_ptr(),
+              dst_table.data_ptr(), dst_table.shape[1], kept.data_ptr(), new_lens.data_ptr(), weights_out.data_ptr(),
+              weights_out.shape[2]), stream)
+
+
+def hyp_op_attn_shared_scratch_bytes(shape3, n_seqs: int, n_groups: int, max_prefix_pages: int, max_pages_per_seq: int) -> int:
+    return lib().hyp_op_attn_shared_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, n_groups, max_prefix_pages,
+                                                  max_pages_per_seq)
+
+
+def hyp_op_attn_decode_shared(shape3, q, kv_pages, cu_group, prefix_table, prefix_lens, block_table, ctx_lens, scratch, out,
+                              stream=None):
+    import torch
+    where, n, ng = "hyp_op_attn_decode_shared", q.shape[0], prefix_lens.shape[0]
+    _need_query(where, shape3, q, out, kv_pages)
+    _need(where, "cu_group", cu_group, torch.int32, (ng + 1,), q.device)
+    _need(where, "prefix_table", prefix_table, torch.int32, (ng, None), q.device)
+    _need(where, "prefix_lens", prefix_lens, torch.int32, (ng,), q.device)
+    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
+    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
+    sp, sb = _scratch_args(where, scratch, q.device)
+    _call_on(q.device, lib().hyp_op_attn_decode_shared, where,
+             (C.byref(hyp_attn_shape(*shape3)), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(), ng,
+              cu_group.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[1], prefix_lens.data_ptr(), block_table.data_ptr(),
+              block_table.shape[1], ctx_lens.data_ptr(), sp, sb, out.data_ptr()), stream)
 
 
 # --------------------------------------------------------------------------------------------
