@@ -415,50 +415,92 @@ def hyp_op_attn_prefill(shape3, q, kv_pages, block_table, cu_q, ctx_lens, out, s
 # operators over the paged cache (hyperion_ops.h).  These check their tensors: type, device, shape, strides; a call that
 # does not fit raises HYP_EINVAL before anything is launched, and a call on tensors of another device than the current one
 # runs there (on that device's current stream unless one is given).
+# A small call runs for a few microseconds on the device, so the checks are written to cost little: one comparison a
+# property, the message is only formed where one fails, and the ctypes shape of a head layout is made once.
 # --------------------------------------------------------------------------------------------
+_F16 = _F32 = _I32 = _raw_stream = _current_device = None
+_SHAPES = {}
+
+
+def _bind_torch():
+    global _F16, _F32, _I32, _raw_stream, _current_device
+    import torch
+    _F16, _F32, _I32, _current_device = torch.float16, torch.float32, torch.int32, torch.cuda.current_device
+    # the stream's address without making a Stream object of it, where this torch has the call
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _refuse(where: str, why: str):
     err = HyperionError(HYP_EINVAL, where)
     err.args = (f"{where}: {why} ({HYP_EINVAL})",)
     raise err
 
 
-def _need(where, name, t, dtype, shape, device):
-    """A dense tensor of this type and shape (None in the shape: any size) on this device."""
-    if t.dtype != dtype or t.device != device or t.dim() != len(shape) or not t.is_contiguous():
-        _refuse(where, f"{name} must be a contiguous {dtype} tensor of {len(shape)} dimensions on {device}")
-    for have, want in zip(t.shape, shape):
-        if want is not None and have != want:
-            _refuse(where, f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
+def _shape(shape3):
+    s = _SHAPES.get(shape3)
+    if s is None:
+        if _F16 is None:
+            _bind_torch()
+        s = _SHAPES[tuple(shape3)] = C.byref(hyp_attn_shape(*shape3))
+    return s
 
 
-def _need_query(where, shape3, q, out, kv_pages):
-    import torch
-    hq, hkv, d = shape3
-    if q.dtype != torch.float16 or not q.is_cuda or q.dim() != 2 or q.shape[1] < hq * d or q.stride(1) != 1:
-        _refuse(where, "q must be a CUDA fp16 matrix [rows, >= n_q_heads * head_dim] with dense rows")
-    if q.shape[0] > 1 and q.stride(0) < q.shape[1]:
-        _refuse(where, "the rows of q overlap")
-    _need(where, "out", out, torch.float16, (q.shape[0], hq * d), q.device)
-    _need(where, "kv_pages", kv_pages, torch.float16, (None, 2, hkv, 16, d), q.device)
+def _dense(where, name, t, dtype, dev, shape):
+    """The address of a contiguous tensor of this type and shape on device `dev`."""
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.shape != shape:
+        _refuse(where, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, not {t.dtype} "
+                       f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _query_stride(q, shape3):
-    return q.stride(0) if q.shape[0] > 1 else (shape3[0] * shape3[2] + 7) // 8 * 8
+def _rows(where, name, t, dtype, dev, lead):
+    """(address, size of the last dimension) of a contiguous tensor whose other dimensions are `lead`."""
+    s = t.shape
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or s[:-1] != lead:
+        _refuse(where, f"{name} must be a contiguous {dtype} tensor of shape {(*lead, '*')} on device {dev}, not {t.dtype} "
+                       f"{tuple(s)} on {t.device}")
+    return t.data_ptr(), s[-1]
 
 
-def _scratch_args(where, scratch, device):
-    if scratch.device != device or not scratch.is_contiguous():
-        _refuse(where, f"scratch must be a contiguous tensor on {device}")
-    return scratch.data_ptr(), scratch.numel() * scratch.element_size()
+def _pool(where, name, t, dev, shape3):
+    s = t.shape
+    if t.dtype is not _F16 or t.get_device() != dev or not t.is_contiguous() or s[1:] != (2, shape3[1], 16, shape3[2]):
+        _refuse(where, f"{name} must be a contiguous fp16 page pool [pages, 2, {shape3[1]}, 16, {shape3[2]}] on device {dev}, not {t.dtype} "
+                       f"{tuple(s)} on {t.device}")
+    return t.data_ptr()
 
 
-def _call_on(device, fn, where, args, stream):
-    import torch
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream_handle(stream)), where)
+def _query(where, q, shape3):
+    """(device, rows, address, row stride) of the query matrix: dense rows, which may lie in a wider buffer."""
+    width = shape3[0] * shape3[2]
+    dev, s = q.get_device(), q.shape
+    if q.dtype is not _F16 or dev < 0 or len(s) != 2 or s[1] < width:
+        _refuse(where, f"q must be a CUDA fp16 matrix [rows, >= {width}], not {q.dtype} {tuple(s)} on {q.device}")
+    stride, one = q.stride()
+    if one != 1 or (stride < s[1] and s[0] > 1):
+        _refuse(where, f"q must have dense rows that do not overlap, not strides {q.stride()}")
+    return dev, s[0], q.data_ptr(), stride if s[0] > 1 else (width + 7) // 8 * 8
+
+
+def _scratch(where, t, dev):
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(where, f"scratch must be a contiguous tensor on device {dev}")
+    return t.data_ptr(), t.nbytes
+
+
+def _launch(where, fn, dev, stream, *args):
+    if stream is None:
+        st = _raw_stream(dev)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, _stream_handle(stream)), where)
+        st = stream if isinstance(stream, int) else stream.cuda_stream
+    if dev == _current_device():
+        code = fn(*args, st)
+    else:
+        import torch
+        with torch.cuda.device(dev):
+            code = fn(*args, st)
+    if code != HYP_OK:
+        raise HyperionError(code, where)
 
 
 class AttnMod:
@@ -469,113 +511,106 @@ class AttnMod:
         self.slopes, self.prefix_lens = slopes, prefix_lens
         self.struct = hyp_attn_mod(softcap, window, None if slopes is None else slopes.data_ptr(),
                                    None if prefix_lens is None else prefix_lens.data_ptr())
+        self.ref = C.byref(self.struct)
 
-    def check(self, where, shape3, n_seqs, device):
-        import torch
+    def check(self, where, shape3, n_seqs, dev):
+        """The struct for a call with this head layout and batch; the tensors still have to be where they were."""
         if self.slopes is not None:
-            _need(where, "slopes", self.slopes, torch.float32, (shape3[0],), device)
+            self.struct.slopes = _dense(where, "slopes", self.slopes, _F32, dev, (shape3[0],))
         if self.prefix_lens is not None:
-            _need(where, "prefix_lens", self.prefix_lens, torch.int32, (n_seqs,), device)
+            self.struct.prefix_lens = _dense(where, "prefix_lens", self.prefix_lens, _I32, dev, (n_seqs,))
+        return self.ref
 
 
 def hyp_op_attn_mod_scratch_bytes(shape3, n_seqs: int, max_pages_per_seq: int) -> int:
-    return lib().hyp_op_attn_mod_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, max_pages_per_seq)
+    return lib().hyp_op_attn_mod_scratch_bytes(_shape(shape3), n_seqs, max_pages_per_seq)
 
 
 def hyp_op_attn_decode_mod(shape3, mod: AttnMod, q, kv_pages, block_table, ctx_lens, scratch, out, stream=None):
-    import torch
-    where, n = "hyp_op_attn_decode_mod", q.shape[0]
-    _need_query(where, shape3, q, out, kv_pages)
-    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
-    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
-    mod.check(where, shape3, n, q.device)
-    sp, sb = _scratch_args(where, scratch, q.device)
-    _call_on(q.device, lib().hyp_op_attn_decode_mod, where,
-             (C.byref(hyp_attn_shape(*shape3)), C.byref(mod.struct), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(),
-              block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), sp, sb, out.data_ptr()), stream)
+    """q fp16 [n_seqs, >= n_q_heads * head_dim], kv_pages fp16 [pages, 2, n_kv_heads, 16, head_dim], block_table int32
+    [n_seqs, pages per sequence], ctx_lens int32 [n_seqs], out fp16 [n_seqs, n_q_heads * head_dim]."""
+    where, sh = "hyp_op_attn_decode_mod", _shape(shape3)
+    dev, n, qp, qs = _query(where, q, shape3)
+    pool = _pool(where, "kv_pages", kv_pages, dev, shape3)
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    ctx = _dense(where, "ctx_lens", ctx_lens, _I32, dev, (n,))
+    op = _dense(where, "out", out, _F16, dev, (n, shape3[0] * shape3[2]))
+    sp, sb = _scratch(where, scratch, dev)
+    _launch(where, lib().hyp_op_attn_decode_mod, dev, stream, sh, mod.check(where, shape3, n, dev), n, qp, qs, pool, table, width, ctx,
+            sp, sb, op)
 
 
 def hyp_op_attn_prefill_mod(shape3, mod: AttnMod, q, kv_pages, block_table, cu_q, ctx_lens, out, stream=None):
-    import torch
-    where, n = "hyp_op_attn_prefill_mod", ctx_lens.shape[0]
-    _need_query(where, shape3, q, out, kv_pages)
-    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
-    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
-    _need(where, "cu_q", cu_q, torch.int32, (n + 1,), q.device)
-    mod.check(where, shape3, n, q.device)
-    _call_on(q.device, lib().hyp_op_attn_prefill_mod, where,
-             (C.byref(hyp_attn_shape(*shape3)), C.byref(mod.struct), n, q.shape[0], q.data_ptr(), _query_stride(q, shape3),
-              kv_pages.data_ptr(), block_table.data_ptr(), block_table.shape[1], cu_q.data_ptr(), ctx_lens.data_ptr(),
-              out.data_ptr()), stream)
+    """q fp16 [rows, >= n_q_heads * head_dim], cu_q int32 [n_seqs + 1], the rest as hyp_op_attn_decode_mod."""
+    where, sh = "hyp_op_attn_prefill_mod", _shape(shape3)
+    dev, m, qp, qs = _query(where, q, shape3)
+    pool = _pool(where, "kv_pages", kv_pages, dev, shape3)
+    ctx, n = _rows(where, "ctx_lens", ctx_lens, _I32, dev, ())
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    cu = _dense(where, "cu_q", cu_q, _I32, dev, (n + 1,))
+    op = _dense(where, "out", out, _F16, dev, (m, shape3[0] * shape3[2]))
+    _launch(where, lib().hyp_op_attn_prefill_mod, dev, stream, sh, mod.check(where, shape3, n, dev), n, m, qp, qs, pool, table, width,
+            cu, ctx, op)
 
 
 def hyp_op_attn_scored_scratch_bytes(shape3, n_seqs: int, max_pages_per_seq: int) -> int:
-    return lib().hyp_op_attn_scored_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, max_pages_per_seq)
+    return lib().hyp_op_attn_scored_scratch_bytes(_shape(shape3), n_seqs, max_pages_per_seq)
 
 
 def hyp_op_attn_decode_scored(shape3, q, kv_pages, block_table, ctx_lens, decay: float, weights_in, weights_out, scratch, out,
                               stream=None):
     """weights_in: fp32 [n_seqs, n_kv_heads, width] or None; weights_out the same shape, may be weights_in."""
-    import torch
-    where, n = "hyp_op_attn_decode_scored", q.shape[0]
-    _need_query(where, shape3, q, out, kv_pages)
-    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
-    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
-    _need(where, "weights_out", weights_out, torch.float32, (n, shape3[1], None), q.device)
-    if weights_in is not None:
-        _need(where, "weights_in", weights_in, torch.float32, tuple(weights_out.shape), q.device)
-    sp, sb = _scratch_args(where, scratch, q.device)
-    _call_on(q.device, lib().hyp_op_attn_decode_scored, where,
-             (C.byref(hyp_attn_shape(*shape3)), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(),
-              block_table.data_ptr(), block_table.shape[1], ctx_lens.data_ptr(), decay,
-              None if weights_in is None else weights_in.data_ptr(), weights_out.data_ptr(), weights_out.shape[2], sp, sb,
-              out.data_ptr()), stream)
+    where, sh = "hyp_op_attn_decode_scored", _shape(shape3)
+    dev, n, qp, qs = _query(where, q, shape3)
+    pool = _pool(where, "kv_pages", kv_pages, dev, shape3)
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    ctx = _dense(where, "ctx_lens", ctx_lens, _I32, dev, (n,))
+    wo, ws = _rows(where, "weights_out", weights_out, _F32, dev, (n, shape3[1]))
+    wi = None if weights_in is None else _dense(where, "weights_in", weights_in, _F32, dev, (n, shape3[1], ws))
+    op = _dense(where, "out", out, _F16, dev, (n, shape3[0] * shape3[2]))
+    sp, sb = _scratch(where, scratch, dev)
+    _launch(where, lib().hyp_op_attn_decode_scored, dev, stream, sh, n, qp, qs, pool, table, width, ctx, decay, wi, wo, ws, sp, sb, op)
 
 
 def hyp_op_kv_evict(shape3, kv_pages, block_table, n_cached, weights_in, n_keep: int, n_sink: int, n_recent: int, dst_pages,
                     dst_table, kept, new_lens, weights_out, stream=None):
-    """dst_pages, dst_table: kv_pages and block_table themselves (in place), or pages that are not among the source's."""
-    import torch
-    where, n, dev = "hyp_op_kv_evict", n_cached.shape[0], kv_pages.device
-    hq, hkv, d = shape3
-    if not kv_pages.is_cuda:
+    """dst_pages, dst_table: kv_pages and block_table themselves (in place), or pages that are not among the source's.
+    kept int32 [n_seqs, n_kv_heads, n_keep], new_lens int32 [n_seqs], weights_* fp32 [n_seqs, n_kv_heads, *]."""
+    where, sh, hkv = "hyp_op_kv_evict", _shape(shape3), shape3[1]
+    dev = kv_pages.get_device()
+    if dev < 0:
         _refuse(where, "kv_pages must be a CUDA tensor")
-    _need(where, "kv_pages", kv_pages, torch.float16, (None, 2, hkv, 16, d), dev)
-    _need(where, "dst_pages", dst_pages, torch.float16, (None, 2, hkv, 16, d), dev)
-    _need(where, "block_table", block_table, torch.int32, (n, None), dev)
-    _need(where, "dst_table", dst_table, torch.int32, (n, None), dev)
-    _need(where, "n_cached", n_cached, torch.int32, (n,), dev)
-    _need(where, "new_lens", new_lens, torch.int32, (n,), dev)
-    _need(where, "kept", kept, torch.int32, (n, hkv, n_keep), dev)
-    _need(where, "weights_in", weights_in, torch.float32, (n, hkv, None), dev)
-    _need(where, "weights_out", weights_out, torch.float32, (n, hkv, None), dev)
-    _call_on(dev, lib().hyp_op_kv_evict, where,
-             (C.byref(hyp_attn_shape(*shape3)), n, kv_pages.data_ptr(), block_table.data_ptr(), block_table.shape[1],
-              n_cached.data_ptr(), weights_in.data_ptr(), weights_in.shape[2], n_keep, n_sink, n_recent, dst_pages.data_ptr(),
-              dst_table.data_ptr(), dst_table.shape[1], kept.data_ptr(), new_lens.data_ptr(), weights_out.data_ptr(),
-              weights_out.shape[2]), stream)
+    src, dst = _pool(where, "kv_pages", kv_pages, dev, shape3), _pool(where, "dst_pages", dst_pages, dev, shape3)
+    cached, n = _rows(where, "n_cached", n_cached, _I32, dev, ())
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    dtable, dwidth = _rows(where, "dst_table", dst_table, _I32, dev, (n,))
+    new = _dense(where, "new_lens", new_lens, _I32, dev, (n,))
+    kp = _dense(where, "kept", kept, _I32, dev, (n, hkv, n_keep))
+    wi, ws = _rows(where, "weights_in", weights_in, _F32, dev, (n, hkv))
+    wo, wos = _rows(where, "weights_out", weights_out, _F32, dev, (n, hkv))
+    _launch(where, lib().hyp_op_kv_evict, dev, stream, sh, n, src, table, width, cached, wi, ws, n_keep, n_sink, n_recent, dst, dtable,
+            dwidth, kp, new, wo, wos)
 
 
 def hyp_op_attn_shared_scratch_bytes(shape3, n_seqs: int, n_groups: int, max_prefix_pages: int, max_pages_per_seq: int) -> int:
-    return lib().hyp_op_attn_shared_scratch_bytes(C.byref(hyp_attn_shape(*shape3)), n_seqs, n_groups, max_prefix_pages,
-                                                  max_pages_per_seq)
+    return lib().hyp_op_attn_shared_scratch_bytes(_shape(shape3), n_seqs, n_groups, max_prefix_pages, max_pages_per_seq)
 
 
 def hyp_op_attn_decode_shared(shape3, q, kv_pages, cu_group, prefix_table, prefix_lens, block_table, ctx_lens, scratch, out,
                               stream=None):
-    import torch
-    where, n, ng = "hyp_op_attn_decode_shared", q.shape[0], prefix_lens.shape[0]
-    _need_query(where, shape3, q, out, kv_pages)
-    _need(where, "cu_group", cu_group, torch.int32, (ng + 1,), q.device)
-    _need(where, "prefix_table", prefix_table, torch.int32, (ng, None), q.device)
-    _need(where, "prefix_lens", prefix_lens, torch.int32, (ng,), q.device)
-    _need(where, "block_table", block_table, torch.int32, (n, None), q.device)
-    _need(where, "ctx_lens", ctx_lens, torch.int32, (n,), q.device)
-    sp, sb = _scratch_args(where, scratch, q.device)
-    _call_on(q.device, lib().hyp_op_attn_decode_shared, where,
-             (C.byref(hyp_attn_shape(*shape3)), n, q.data_ptr(), _query_stride(q, shape3), kv_pages.data_ptr(), ng,
-              cu_group.data_ptr(), prefix_table.data_ptr(), prefix_table.shape[1], prefix_lens.data_ptr(), block_table.data_ptr(),
-              block_table.shape[1], ctx_lens.data_ptr(), sp, sb, out.data_ptr()), stream)
+    """cu_group int32 [n_groups + 1], prefix_table int32 [n_groups, pages], prefix_lens int32 [n_groups]; block_table and
+    ctx_lens: what every sequence has behind its group's prefix."""
+    where, sh = "hyp_op_attn_decode_shared", _shape(shape3)
+    dev, n, qp, qs = _query(where, q, shape3)
+    pool = _pool(where, "kv_pages", kv_pages, dev, shape3)
+    pl, ng = _rows(where, "prefix_lens", prefix_lens, _I32, dev, ())
+    cu = _dense(where, "cu_group", cu_group, _I32, dev, (ng + 1,))
+    pt, pw = _rows(where, "prefix_table", prefix_table, _I32, dev, (ng,))
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    ctx = _dense(where, "ctx_lens", ctx_lens, _I32, dev, (n,))
+    op = _dense(where, "out", out, _F16, dev, (n, shape3[0] * shape3[2]))
+    sp, sb = _scratch(where, scratch, dev)
+    _launch(where, lib().hyp_op_attn_decode_shared, dev, stream, sh, n, qp, qs, pool, ng, cu, pt, pw, pl, table, width, ctx, sp, sb, op)
 
 
 # --------------------------------------------------------------------------------------------
