@@ -46,8 +46,9 @@ struct TileRow {
   int lo, hi, pre;
 };
 struct TileScore {
-  float softcap;              // CAP
-  float slope_l2;             // BIAS: this thread's slope times log2(e)
+  float scale;                // x -> exponent (base 2)
+  float to_tanh;              // CAP: raw product -> argument of the tanh
+  float ratio;                // BIAS: this thread's slope, in units of x
 };
 
 struct TileShared {
@@ -91,35 +92,111 @@ __device__ __forceinline__ uint64_t at_desc_mn(uint32_t addr) {
   return d;
 }
 
-// Softmax of one 64-key tile for one query row: see the head of the file.
+// Two fp32 values in one 64-bit register: the packed forms issue one instruction for both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pk2(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void up2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max3abs(float m, float a, float b) { return max3(m, fabsf(a), fabsf(b)); }
+
+// tanh x for |x| <= 0.75 as x times a polynomial in x^2 (five coefficients, least absolute error of tanh x over the range,
+// fitted by reweighted least squares): off by 1.9e-7 at most.  Runs on the packed FMA path; the exact form needs two
+// of the sixteen special-function lanes' operations a score, which alone would take longer than both matrix products.
+constexpr float TANH_RANGE = 0.75f;
+__device__ __forceinline__ f32x2 tanh2_small(f32x2 x) {
+  const f32x2 u = mul2(x, x);
+  f32x2 p = fma2(u, pk2(0.012318827410786189f, 0.012318827410786189f), pk2(-0.049280441976393266f, -0.049280441976393266f));
+  p = fma2(u, p, pk2(0.13226091419102248f, 0.13226091419102248f));
+  p = fma2(u, p, pk2(-0.3332307645376031f, -0.3332307645376031f));
+  p = fma2(u, p, pk2(0.9999972283092571f, 0.9999972283092571f));
+  return mul2(x, p);
+}
+__device__ __forceinline__ float tanh_exact(float x) {  // 1 - 2 / (1 + e^(2x)); see softcap_log2
+  return fmaf(-2.f, rcp_approx(1.f + ex2_approx(2.f * PG_LOG2E * x)), 1.f);
+}
+
+// Softmax of one 64-key tile for one query row: see the head of the file.  A score enters the exponent as x * scale with
+// x the raw product (scale = log2(e) / sqrt(D)) or, capped, the tanh (scale = softcap * log2(e)); the distance bias is
+// added to x as ratio * distance, ratio = slope * log2(e) / scale.  What a row may not see becomes -1e30, which the exponent
+// turns into 0 as long as the reference stays above -1e20.
 template <int D, bool CAP, bool BIAS, bool MASKED>
 __device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, const TileRow& rw,
                                            const TileScore& sc, int j, uint32_t o_prev, uint32_t o_parity,
                                            volatile int* abort_flag, float& m_ref, float& l) {
-  const float sl2 = rsqrtf((float)D) * PG_LOG2E;
-  const float sl = CAP || BIAS ? 1.f : sl2;  // what the exponent still has to be multiplied with
   uint32_t sv[AT_KEYS];
-  float mx = PG_NEG;
 #pragma unroll
   for (int c = 0; c < AT_KEYS; c += 16) tmem_ld16(tmem_sb + lane_off + c, reinterpret_cast<uint32_t(&)[16]>(sv[c]));
   tmem_ld_wait();
-  if (CAP || BIAS) {
-    const float cap_l2 = sc.softcap * PG_LOG2E, cap_y = CAP ? 2.f * sl2 / sc.softcap : 0.f;
+  float x[AT_KEYS];
 #pragma unroll
-    for (int i = 0; i < AT_KEYS; ++i) {
-      float t = __uint_as_float(sv[i]);
-      t = CAP ? softcap_log2(t * cap_y, cap_l2) : t * sl2;
-      if (BIAS) t = fmaf(-sc.slope_l2, fabsf((float)(key0 + i - pos)), t);
-      sv[i] = __float_as_uint(t);
+  for (int i = 0; i < AT_KEYS; ++i) x[i] = __uint_as_float(sv[i]);
+  if (CAP) {
+    float a4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < AT_KEYS; i += 2) a4[(i >> 1) & 3] = max3abs(a4[(i >> 1) & 3], x[i], x[i + 1]);
+    // NaN (garbage behind the end of a sequence) compares false here and takes the exact form; it is masked below
+    const bool small = max3(fmaxf(a4[0], a4[1]), a4[2], a4[3]) * sc.to_tanh <= TANH_RANGE;
+    if (__all_sync(0xffffffffu, small)) {
+      const f32x2 k = pk2(sc.to_tanh, sc.to_tanh);
+#pragma unroll
+      for (int i = 0; i < AT_KEYS; i += 2) up2(tanh2_small(mul2(pk2(x[i], x[i + 1]), k)), x[i], x[i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < AT_KEYS; ++i) x[i] = tanh_exact(x[i] * sc.to_tanh);
     }
   }
-  auto visible = [&](int key) { return !MASKED || (key >= rw.lo && key <= rw.hi) || key < rw.pre; };
-  {  // four independent chains: one or two warps per scheduler leave little else to hide the latency behind
-    float m4[4] = {PG_NEG, PG_NEG, PG_NEG, PG_NEG};
+  if (BIAS) {
+    if (MASKED) {
 #pragma unroll
-    for (int i = 0; i < AT_KEYS; ++i) m4[i & 3] = fmaxf(m4[i & 3], visible(key0 + i) ? __uint_as_float(sv[i]) : PG_NEG);
-    mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sl;  // sl > 0
+      for (int i = 0; i < AT_KEYS; ++i) x[i] = fmaf(-sc.ratio, fabsf((float)(key0 + i - pos)), x[i]);
+    } else if (key0 + AT_KEYS - 1 <= pos) {  // every key behind the query: the distance is pos - key
+      f32x2 dist = pk2((float)(key0 - pos), (float)(key0 + 1 - pos));
+      const f32x2 r2 = pk2(sc.ratio, sc.ratio), two = pk2(2.f, 2.f);
+#pragma unroll
+      for (int i = 0; i < AT_KEYS; i += 2) {
+        up2(fma2(r2, dist, pk2(x[i], x[i + 1])), x[i], x[i + 1]);
+        dist = add2(dist, two);  // whole numbers: exact
+      }
+    } else {  // inside a prefix, some keys ahead of the query
+#pragma unroll
+      for (int i = 0; i < AT_KEYS; ++i) x[i] = fmaf(-sc.ratio, fabsf((float)(key0 + i - pos)), x[i]);
+    }
   }
+  if (MASKED) {
+    // bit i: key0 + i is visible
+    auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; };
+    const unsigned long long vis = (below(rw.hi + 1 - key0) & ~below(rw.lo - key0)) | below(rw.pre - key0);
+    const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
+#pragma unroll
+    for (int i = 0; i < AT_KEYS; ++i) x[i] = ((i < 32 ? v0 : v1) & (1u << (i & 31))) ? x[i] : PG_NEG;
+  }
+  float m4[4] = {PG_NEG, PG_NEG, PG_NEG, PG_NEG};
+#pragma unroll
+  for (int i = 0; i < AT_KEYS; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], x[i], x[i + 1]);
+  const float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]) * sc.scale;  // scale > 0
   if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
     const float new_ref = fmaxf(m_ref, mx);
     if (j > 0) {
@@ -129,41 +206,37 @@ __device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
       const float corr = ex2_approx(m_ref - new_ref);
       l *= corr;
 #pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        uint32_t v[16], w[16];
+      for (int c = 0; c < D; c += 16) {
+        uint32_t v[16];
         tmem_ld16(tmem_o + lane_off + c, v);
-        tmem_ld16(tmem_o + lane_off + c + 16, w);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
-          w[i] = __float_as_uint(__uint_as_float(w[i]) * corr);
-        }
+        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
         at_tmem_st16(tmem_o + lane_off + c, v);
-        at_tmem_st16(tmem_o + lane_off + c + 16, w);
       }
     }
     m_ref = new_ref;
   }
-  const float neg_ref = -m_ref;
-  float l4[4] = {0.f, 0.f, 0.f, 0.f};
+  const float neg_ref = -fmaxf(m_ref, -1e20f);
+  const f32x2 s2 = pk2(sc.scale, sc.scale), n2 = pk2(neg_ref, neg_ref);
+  f32x2 l2[2] = {0ull, 0ull};
 #pragma unroll
   for (int c = 0; c < AT_KEYS; c += 32) {
     uint32_t pk[16];
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
-      float p0 = ex2_approx(fmaf(__uint_as_float(sv[c + i]), sl, neg_ref));
-      float p1 = ex2_approx(fmaf(__uint_as_float(sv[c + i + 1]), sl, neg_ref));
-      if (MASKED) {
-        p0 = visible(key0 + c + i) ? p0 : 0.f;
-        p1 = visible(key0 + c + i + 1) ? p1 : 0.f;
-      }
-      l4[(i >> 1) & 3] += p0 + p1;
+      float p0, p1;
+      up2(fma2(pk2(x[c + i], x[c + i + 1]), s2, n2), p0, p1);
+      p0 = ex2_approx(p0);
+      p1 = ex2_approx(p1);
+      l2[(i >> 1) & 1] = add2(l2[(i >> 1) & 1], pk2(p0, p1));
       pk[i >> 1] = pack_f16(p0, p1);
     }
     at_tmem_st16(tmem_sb + lane_off + 32 + (c >> 1), pk);  // key k of the tile: 16-bit half k & 1 of column 32 + k / 2
   }
-  l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+  float l0, l1;
+  up2(add2(l2[0], l2[1]), l0, l1);
+  l += l0 + l1;
   at_tmem_st_wait();
   return true;
 }
@@ -311,8 +384,12 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
     const bool warp_idle = (32 * q) / G >= wk.rows;  // no row of this warp exists: its weights are never used
     int pos;
     const TileRow rw = row_fn(min(t, wk.rows - 1), pos);  // rows past the end are clamped: computed, never stored
-    TileScore sc{softcap, 0.f};
-    if (BIAS) sc.slope_l2 = slopes[wk.head0 + gh] * PG_LOG2E;
+    TileScore sc{rsqrtf((float)D) * PG_LOG2E, 0.f, 0.f};
+    if (CAP) {
+      sc.to_tanh = rsqrtf((float)D) / softcap;
+      sc.scale = softcap * PG_LOG2E;
+    }
+    if (BIAS) sc.ratio = slopes[wk.head0 + gh] * PG_LOG2E / sc.scale;
     float m_ref = PG_NEG, l = 0.f;
     bool ok = true;
     for (int j = 0; j < n_tiles && ok; ++j) {
