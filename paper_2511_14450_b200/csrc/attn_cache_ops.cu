@@ -24,55 +24,73 @@ __global__ void __launch_bounds__(PD_WARPS * 32) paged_decode_kernel(PagedArgs a
 
 // Joins the partial rows of one (sequence, query head) and writes fp16.
 template <int D>
-__global__ void paged_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots, __half* __restrict__ out) {
+__global__ void __launch_bounds__(MERGE_THREADS)
+paged_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots, __half* __restrict__ out) {
+  __shared__ float sm[MERGE_THREADS / 32 * D];
   pdl_wait();
   pdl_trigger();
   const size_t row = blockIdx.x;  // b * Hq + h
-  out[row * D + threadIdx.x] = __float2half_rn(paged_merge_element<D>(acc, ml, row * n_slots, n_slots, threadIdx.x));
+  paged_merge_row<D>(acc, ml, row * n_slots, n_slots, out + row * D, sm);
 }
 
-// Second kernel of the scored operator.  grid (key chunks, Hkv, n_seqs): every CTA joins the splits' (maximum,
-// denominator) of its G query heads, turns its chunk of scores into weights and adds them to the running sums; the
-// CTA of chunk 0 also joins the value sums.
-constexpr int SC_THREADS = 256, SC_KEYS = 1024;
+// Second kernel of the scored operator.  grid (G + key chunks, Hkv, n_seqs): the first G CTAs of a (sequence, KV head) join
+// the value sums of one query head each; every other one joins the splits' (maximum, denominator) of the G heads, turns
+// its chunk of scores into weights and adds them to the running sums.
+constexpr int SC_PER = 4, SC_KEYS = MERGE_THREADS * SC_PER;
 template <int D, int G>
-__global__ void __launch_bounds__(SC_THREADS)
+__global__ void __launch_bounds__(MERGE_THREADS)
 scored_finish_kernel(PagedArgs a, float decay, const float* __restrict__ w_in, float* __restrict__ w_out, long long w_stride,
                      __half* __restrict__ out) {
-  __shared__ float s_m[G], s_inv[G];
+  __shared__ float sm[MERGE_THREADS / 32 * D];
   pdl_wait();
   pdl_trigger();
   const int kvh = blockIdx.y, b = blockIdx.z;
-  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
-  const int k_begin = blockIdx.x * SC_KEYS;
-  if (blockIdx.x > 0 && k_begin >= total) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const size_t row0 = (size_t)b * a.Hq + kvh * G;
-  if (warp < G) {
-    const float* ml = a.ml + (row0 + warp) * a.n_slots * 2;
+  if (blockIdx.x < G) {
+    const size_t row = row0 + blockIdx.x;
+    paged_merge_row<D>(a.acc, a.ml, row * a.n_slots, a.n_slots, out + row * D, sm);
+    return;
+  }
+  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
+  const int k_begin = (blockIdx.x - G) * SC_KEYS + threadIdx.x;
+  if (k_begin - (int)threadIdx.x >= total) return;
+  const float* wi = w_in ? w_in + ((long long)b * a.Hkv + kvh) * w_stride : nullptr;
+  float* wo = w_out + ((long long)b * a.Hkv + kvh) * w_stride;
+  // everything this thread needs from memory is asked for before the maxima are joined
+  float s[SC_PER][G], old[SC_PER];
+#pragma unroll
+  for (int i = 0; i < SC_PER; ++i) {
+    const int k = k_begin + i * MERGE_THREADS;
+    old[i] = wi && k < total - 1 ? wi[k] : 0.f;  // the new token's sum starts here
+#pragma unroll
+    for (int gq = 0; gq < G; ++gq) s[i][gq] = k < total ? a.scores[(row0 + gq) * a.score_stride + k] : PG_NEG;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float *s_m = sm, *s_inv = sm + G;
+  for (int gq = warp; gq < G; gq += MERGE_THREADS / 32) {
+    const float* ml = a.ml + (row0 + gq) * a.n_slots * 2;
     float mx = PG_NEG, l = 0.f;
-    for (int s = lane; s < a.n_slots; s += 32) mx = fmaxf(mx, ml[2 * s]);
-    mx = warp_max(mx);
-    for (int s = lane; s < a.n_slots; s += 32) l += ml[2 * s + 1] * ex2_approx(ml[2 * s] - mx);
-    l = warp_sum(l);
+    for (int i = lane; i < a.n_slots; i += 32) {
+      const float2 x = *reinterpret_cast<const float2*>(ml + 2 * i);
+      const float top = fmaxf(mx, x.x);
+      l = l * ex2_approx(mx - top) + x.y * ex2_approx(x.x - top);
+      mx = top;
+    }
+    const float top = warp_max(mx);
+    l = warp_sum(l * ex2_approx(mx - top));
     if (lane == 0) {
-      s_m[warp] = mx;
-      s_inv[warp] = l != 0.f ? 1.f / l : 0.f;
+      s_m[gq] = top;
+      s_inv[gq] = l != 0.f ? 1.f / l : 0.f;
     }
   }
   __syncthreads();
-  if (blockIdx.x == 0)
-    for (int e = threadIdx.x; e < G * D; e += SC_THREADS) {
-      const int gq = e / D, dd = e % D;
-      out[(row0 + gq) * D + dd] = __float2half_rn(paged_merge_element<D>(a.acc, a.ml, (row0 + gq) * a.n_slots, a.n_slots, dd));
-    }
-  const float* wi = w_in ? w_in + ((long long)b * a.Hkv + kvh) * w_stride : nullptr;
-  float* wo = w_out + ((long long)b * a.Hkv + kvh) * w_stride;
-  for (int k = k_begin + threadIdx.x; k < min(total, k_begin + SC_KEYS); k += SC_THREADS) {
+#pragma unroll
+  for (int i = 0; i < SC_PER; ++i) {
+    const int k = k_begin + i * MERGE_THREADS;
     float w = 0.f;
 #pragma unroll
-    for (int gq = 0; gq < G; ++gq) w += ex2_approx(a.scores[(row0 + gq) * a.score_stride + k] - s_m[gq]) * s_inv[gq];
-    wo[k] = (wi && k < total - 1) ? fmaf(decay, wi[k], w) : w;  // the new token's sum starts here
+    for (int gq = 0; gq < G; ++gq) w += ex2_approx(s[i][gq] - s_m[gq]) * s_inv[gq];
+    if (k < total) wo[k] = fmaf(decay, old[i], w);
   }
 }
 
@@ -256,7 +274,7 @@ int launch_paged(const PagedArgs& a, int n_splits, int n_seqs, cudaStream_t st) 
 
 template <int D>
 int launch_merge(const PagedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
-  HYP_CUDA_TRY(launch_pdl<2>(paged_merge_kernel<D>, dim3(n_seqs * a.Hq), dim3(D), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
+  HYP_CUDA_TRY(launch_pdl<2>(paged_merge_kernel<D>, dim3(n_seqs * a.Hq), dim3(MERGE_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
   return 1;
 }
 
@@ -288,7 +306,7 @@ int decode_scored_dg(const PagedArgs& a, int n_splits, int n_seqs, float decay, 
   const int rc = launch_paged<D, G, PAGED_SCORED>(a, n_splits, n_seqs, st);
   if (rc < 0) return rc;
   const int chunks = (a.table_stride * PG_PT + SC_KEYS - 1) / SC_KEYS;
-  HYP_CUDA_TRY(launch_pdl<2>(scored_finish_kernel<D, G>, dim3(chunks, a.Hkv, n_seqs), dim3(SC_THREADS), (size_t)0, st, a, decay, w_in,
+  HYP_CUDA_TRY(launch_pdl<2>(scored_finish_kernel<D, G>, dim3(G + chunks, a.Hkv, n_seqs), dim3(MERGE_THREADS), (size_t)0, st, a, decay, w_in,
                              w_out, w_stride, out));
   return rc + 1;
 }
@@ -319,11 +337,13 @@ int prefill_mod_launch(const CUtensorMap& mq, const CUtensorMap& mkv, const Pref
 }  // namespace
 
 int paged_splits(int n_seqs, int Hkv, int max_pages) {
-  // about four waves of three CTAs per SM at the longest length the table allows, so that ragged batches even out;
-  // at least two pages per warp, so that the ring has something to run ahead of
+  // Short contexts: one wave of three CTAs per SM.  Longer ones (more than 64 pages a CTA that way): about four waves, so
+  // that ragged batches even out.  At least one page per warp.
   const int groups = n_seqs * Hkv;
-  int want = (12 * sm_count() + groups - 1) / groups;
-  const int cap = (max_pages + 2 * PD_WARPS - 1) / (2 * PD_WARPS);
+  int want = 3 * sm_count() / groups;
+  if (want < 1) want = 1;
+  if (max_pages > 64 * want) want = (12 * sm_count() + groups - 1) / groups;
+  const int cap = (max_pages + PD_WARPS - 1) / PD_WARPS;
   if (want > cap) want = cap;
   if (want > 64) want = 64;
   return want < 1 ? 1 : want;
@@ -364,8 +384,10 @@ SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int n_groups, int prefix_pag
   if (p.prefix_splits > 32) p.prefix_splits = 32;
   if (p.prefix_splits < 1) p.prefix_splits = 1;
   const int groups = n_seqs * Hkv;
-  p.own_splits = (4 * slots + groups - 1) / groups;
-  const int cap = (own_pages + 2 * SH_WARPS - 1) / (2 * SH_WARPS);
+  p.own_splits = slots / groups;  // as paged_splits: one wave, or four where a CTA would have more than 64 pages
+  if (p.own_splits < 1) p.own_splits = 1;
+  if (own_pages > 64 * p.own_splits) p.own_splits = (4 * slots + groups - 1) / groups;
+  const int cap = (own_pages + SH_WARPS - 1) / SH_WARPS;
   if (p.own_splits > cap) p.own_splits = cap;
   if (p.own_splits > 32) p.own_splits = 32;
   if (p.own_splits < 1) p.own_splits = 1;

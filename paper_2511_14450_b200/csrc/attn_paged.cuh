@@ -74,6 +74,13 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   const int warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, tq = lane & 3;
 
+  const int32_t* bt = a.table + (long long)b * a.table_stride;
+  const bool early = MODE != PAGED_MOD || (a.window == 0 && a.prefix == nullptr);
+  int32_t ids_cur = 0;
+  if (early) {
+    const int v = split + n_splits * (warp + WARPS * lane);
+    if (v < a.table_stride) ids_cur = bt[v];
+  }
   // visible keys: [lo, total) behind the query, and [0, pre)
   const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
   int lo = 0, pre = 0;
@@ -92,14 +99,15 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   const int first = split + n_splits * warp, stride_p = n_splits * WARPS;
   const int my_n = first < n_vis ? (n_vis - first + stride_p - 1) / stride_p : 0;
 
-  const int32_t* bt = a.table + (long long)b * a.table_stride;
   const size_t page_elems = kv_page_elems(a.Hkv, PG_PT, D);
   const size_t v_off = (size_t)a.Hkv * PG_PT * D;
   const uint32_t my_bars = smem_u32(bars) + 8u * (warp * SLOTS);
   const uint32_t my_ring = smem_u32(smem) + (uint32_t)(warp * SLOTS) * SLOT_BYTES;
-  // page ids: lane l holds the id of this warp's page base + l, for the 32 pages being issued and the 32 after them
+  // page ids: lane l holds the id of this warp's page base + l, for the 32 pages being issued and the 32 after them.  Where
+  // the walk does not depend on the length (no window, no prefix) the first ids are fetched together with it.
   auto load_ids = [&](int base) { return base + lane < my_n ? bt[page_index(base + lane)] : 0; };
-  int32_t ids_cur = load_ids(0), ids_next = load_ids(32);
+  if (!early) ids_cur = load_ids(0);
+  int32_t ids_next = load_ids(32);
   auto issue = [&](int i, int slot) {  // all lanes call, i ascending
     if (i > 0 && (i & 31) == 0) {
       ids_cur = ids_next;
@@ -276,22 +284,63 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   }
 }
 
-// Joins the n_slots partial rows of one query head.  A row whose denominator is 0 has seen nothing: its values are not
-// read.  Returns the joined value of element dd; a query with nothing to see gives 0.
+// Joins the n_slots (at most 96) partial rows that start at row0 and writes the query head's D fp16 results.  A CTA of
+// MERGE_THREADS; every warp derives the slots' weights for itself, takes every fourth slot's values, and the warps meet in
+// shared memory.  A slot whose denominator is 0 has seen nothing: its values are not read.  A query with nothing to see
+// gives zeros.
+constexpr int MERGE_THREADS = 128, MERGE_SLOTS = 96;
 template <int D>
-__device__ __forceinline__ float paged_merge_element(const float* acc, const float* ml, size_t row0, int n_slots, int dd) {
+__device__ __forceinline__ void paged_merge_row(const float* acc, const float* ml, size_t row0, int n_slots, __half* out, float* sm) {
+  constexpr int V = D / 32, WARPS = MERGE_THREADS / 32;  // values per lane
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float m[3], l[3], w[3];
   float mx = PG_NEG;
-  for (int s = 0; s < n_slots; ++s) mx = fmaxf(mx, ml[(row0 + s) * 2]);
-  float l = 0.f, v = 0.f;
-  for (int s = 0; s < n_slots; ++s) {
-    const float2 x = *reinterpret_cast<const float2*>(ml + (row0 + s) * 2);
-    if (x.y != 0.f) {  // NaN is carried on
-      const float wgt = ex2_approx(x.x - mx);
-      l += wgt * x.y;
-      v += wgt * acc[(row0 + s) * D + dd];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int s = lane + 32 * k;
+    const float2 x = s < n_slots ? *reinterpret_cast<const float2*>(ml + (row0 + s) * 2) : make_float2(PG_NEG, 0.f);
+    m[k] = x.x;
+    l[k] = x.y;
+    mx = fmaxf(mx, x.x);
+  }
+  mx = warp_max(mx);
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    w[k] = l[k] != 0.f ? ex2_approx(m[k] - mx) : 0.f;  // NaN is carried on
+    sum += l[k] != 0.f ? w[k] * l[k] : 0.f;
+  }
+  sum = warp_sum(sum);
+  float v[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = 0.f;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+#pragma unroll 4
+    for (int s = warp; s < 32; s += WARPS) {
+      if (32 * k + s >= n_slots) break;
+      const float ws = __shfl_sync(0xffffffffu, w[k], s), ls = __shfl_sync(0xffffffffu, l[k], s);
+      if (ls != 0.f) {
+        const float* src = acc + (row0 + 32 * k + s) * D + V * lane;
+        if (V == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(src);
+          v[0] += ws * x.x; v[1] += ws * x.y; v[2] += ws * x.z; v[V - 1] += ws * x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(src);
+          v[0] += ws * x.x; v[1] += ws * x.y;
+        }
+      }
     }
   }
-  return l != 0.f ? v / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) sm[warp * D + V * lane + i] = v[i];
+  __syncthreads();
+  if ((int)threadIdx.x < D) {
+    float x = 0.f;
+#pragma unroll
+    for (int k = 0; k < WARPS; ++k) x += sm[k * D + threadIdx.x];
+    out[threadIdx.x] = __float2half_rn(sum != 0.f ? x / sum : 0.f);
+  }
 }
 
 }  // namespace hyp
