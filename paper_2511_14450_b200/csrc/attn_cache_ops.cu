@@ -9,6 +9,7 @@ namespace hyp {
 namespace {
 
 constexpr int PD_WARPS = 4;      // decode kernels
+constexpr double FLAT_BYTES = 8e6;
 template <int D>
 constexpr int pd_slots() { return D == 128 ? 2 : 4; }  // 64 KB of ring: three CTAs per SM
 
@@ -39,8 +40,7 @@ paged_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, 
 constexpr int SC_PER = 4, SC_KEYS = MERGE_THREADS * SC_PER;
 template <int D, int G>
 __global__ void __launch_bounds__(MERGE_THREADS)
-scored_finish_kernel(PagedArgs a, float decay, const float* __restrict__ w_in, float* __restrict__ w_out, long long w_stride,
-                     __half* __restrict__ out) {
+scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
   __shared__ float sm[MERGE_THREADS / 32 * D];
   pdl_wait();
   pdl_trigger();
@@ -54,8 +54,8 @@ scored_finish_kernel(PagedArgs a, float decay, const float* __restrict__ w_in, f
   const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
   const int k_begin = (blockIdx.x - G) * SC_KEYS + threadIdx.x;
   if (k_begin - (int)threadIdx.x >= total) return;
-  const float* wi = w_in ? w_in + ((long long)b * a.Hkv + kvh) * w_stride : nullptr;
-  float* wo = w_out + ((long long)b * a.Hkv + kvh) * w_stride;
+  const float* wi = a.w_in ? a.w_in + ((long long)b * a.Hkv + kvh) * a.w_stride : nullptr;
+  float* wo = a.w_out + ((long long)b * a.Hkv + kvh) * a.w_stride;
   // everything this thread needs from memory is asked for before the maxima are joined
   float s[SC_PER][G], old[SC_PER];
 #pragma unroll
@@ -90,13 +90,12 @@ scored_finish_kernel(PagedArgs a, float decay, const float* __restrict__ w_in, f
     float w = 0.f;
 #pragma unroll
     for (int gq = 0; gq < G; ++gq) w += ex2_approx(s[i][gq] - s_m[gq]) * s_inv[gq];
-    if (k < total) wo[k] = fmaf(decay, old[i], w);
+    if (k < total) wo[k] = fmaf(a.decay, old[i], w);
   }
 }
 
 // ---------------------------------------------------------------------------------------------
-// shared prefix: one launch holds the CTAs of both parts, so that the tensor-core work on the prefixes runs beside the
-// streaming of the sequences' own pages; a second one joins the partial rows.
+// shared prefix: the prefixes on the row-tile body, the sequences' own pages on the streaming kernel, a join.
 // ---------------------------------------------------------------------------------------------
 struct SharedArgs {
   PagedArgs own;              // slots prefix_splits ..
@@ -104,31 +103,17 @@ struct SharedArgs {
   const int32_t* prefix_table;
   int prefix_stride;
   const int32_t* prefix_lens;
-  int n_groups, prefix_splits, own_splits, prefix_ctas;
+  int n_groups, prefix_splits, own_splits, row_tiles;
 };
-constexpr int SH_WARPS = AT_THREADS / 32;
-template <int D>
-constexpr int sh_slots() { return D == 128 ? 2 : 4; }
-template <int D>
-constexpr int sh_smem() {
-  return AtGeom<D>::SMEM > paged_smem_bytes<D, SH_WARPS>(sh_slots<D>()) ? AtGeom<D>::SMEM : paged_smem_bytes<D, SH_WARPS>(sh_slots<D>());
-}
 
+// grid (prefix_splits * Hkv * row tiles)
 template <int D, int G>
 __global__ void __launch_bounds__(AT_THREADS, 2)
-shared_decode_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
+shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
   extern __shared__ __align__(128) uint8_t sh_smem_raw[];
   __shared__ TileShared ts;
-  __shared__ uint64_t bars[SH_WARPS * sh_slots<D>()];
   pdl_wait();
   pdl_trigger();
-  if ((int)blockIdx.x >= a.prefix_ctas) {
-    const int i = blockIdx.x - a.prefix_ctas;
-    paged_body<D, G, PAGED_PLAIN, SH_WARPS, sh_slots<D>()>(a.own, sh_smem_raw, bars, i % a.own_splits, a.own_splits,
-                                                          (i / a.own_splits) % a.own.Hkv, i / (a.own_splits * a.own.Hkv),
-                                                          threadIdx.x, [] { __syncthreads(); });
-    return;
-  }
   constexpr int T = AT_ROWS / G;
   const int split = blockIdx.x % a.prefix_splits, kvh = (blockIdx.x / a.prefix_splits) % a.own.Hkv;
   const int tile = blockIdx.x / (a.prefix_splits * a.own.Hkv);
@@ -292,34 +277,36 @@ int launch_merge(const PagedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
     return HYP_EINVAL;                                                                \
   } while (0)
 
-template <int D, int G>
-int decode_mod_dg(const PagedArgs& a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
-  const int rc = launch_paged<D, G, PAGED_MOD>(a, n_splits, n_seqs, st);
-  if (rc < 0) return rc;
+template <int D, int G, int MODE>
+int decode_joined_dg(PagedArgs a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
+  if (n_splits == 1) a.out = out;
+  const int rc = launch_paged<D, G, MODE>(a, n_splits, n_seqs, st);
+  if (rc < 0 || n_splits == 1) return rc;
   const int rc2 = launch_merge<D>(a, n_seqs, out, st);
   return rc2 < 0 ? rc2 : rc + rc2;
 }
 
 template <int D, int G>
-int decode_scored_dg(const PagedArgs& a, int n_splits, int n_seqs, float decay, const float* w_in, float* w_out, long long w_stride,
-                     __half* out, cudaStream_t st) {
+int decode_scored_dg(PagedArgs a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
+  if (n_splits == 1) a.out = out;
   const int rc = launch_paged<D, G, PAGED_SCORED>(a, n_splits, n_seqs, st);
-  if (rc < 0) return rc;
+  if (rc < 0 || n_splits == 1) return rc;
   const int chunks = (a.table_stride * PG_PT + SC_KEYS - 1) / SC_KEYS;
-  HYP_CUDA_TRY(launch_pdl<2>(scored_finish_kernel<D, G>, dim3(G + chunks, a.Hkv, n_seqs), dim3(MERGE_THREADS), (size_t)0, st, a, decay, w_in,
-                             w_out, w_stride, out));
+  HYP_CUDA_TRY(launch_pdl<2>(scored_finish_kernel<D, G>, dim3(G + chunks, a.Hkv, n_seqs), dim3(MERGE_THREADS), (size_t)0, st, a, out));
   return rc + 1;
 }
 
 template <int D, int G>
 int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
-  constexpr int smem = sh_smem<D>();
-  const int rc = allow_smem<shared_decode_kernel<D, G>>(smem);
+  constexpr int smem = AtGeom<D>::SMEM;
+  int rc = allow_smem<shared_prefix_kernel<D, G>>(smem);
   if (rc) return rc;
-  const unsigned grid = (unsigned)(a.prefix_ctas + a.own_splits * a.own.Hkv * n_seqs);
-  HYP_CUDA_TRY(launch_pdl<2>(shared_decode_kernel<D, G>, dim3(grid), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
-  const int rc2 = launch_merge<D>(a.own, n_seqs, out, st);
-  return rc2 < 0 ? rc2 : 1 + rc2;
+  HYP_CUDA_TRY(launch_pdl<2>(shared_prefix_kernel<D, G>, dim3((unsigned)(a.prefix_splits * a.own.Hkv * a.row_tiles)), dim3(AT_THREADS),
+                             (size_t)smem, st, mq, mkv, a));
+  rc = launch_paged<D, G, PAGED_PLAIN>(a.own, a.own_splits, n_seqs, st);
+  if (rc < 0) return rc;
+  rc = launch_merge<D>(a.own, n_seqs, out, st);
+  return rc < 0 ? rc : 3;
 }
 
 template <int D, bool CAP, bool BIAS>
@@ -337,16 +324,17 @@ int prefill_mod_launch(const CUtensorMap& mq, const CUtensorMap& mkv, const Pref
 }  // namespace
 
 int paged_splits(int n_seqs, int Hkv, int max_pages) {
-  // Short contexts: one wave of three CTAs per SM.  Longer ones (more than 64 pages a CTA that way): about four waves, so
-  // that ragged batches even out.  At least one page per warp.
+  // Up to 16 pages (four per warp): one CTA per sequence and KV head, which then writes the result itself (the join is a
+  // launch of its own, ~2.5 us).  Short contexts: one wave of three CTAs per SM.  Longer ones (more than 64 pages a CTA
+  // that way): about four waves, so that ragged batches even out.  At least one page per warp.
   const int groups = n_seqs * Hkv;
+  if (max_pages <= 4 * PD_WARPS) return 1;
   int want = 3 * sm_count() / groups;
   if (want < 1) want = 1;
   if (max_pages > 64 * want) want = (12 * sm_count() + groups - 1) / groups;
   const int cap = (max_pages + PD_WARPS - 1) / PD_WARPS;
   if (want > cap) want = cap;
-  if (want > 64) want = 64;
-  return want < 1 ? 1 : want;
+  return want > 64 ? 64 : want;
 }
 
 size_t paged_scratch_floats(int n_seqs, int Hq, int D, int n_slots) { return (size_t)n_seqs * Hq * n_slots * (D + 2); }
@@ -356,7 +344,7 @@ int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half*
   const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride);
   PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
   a.softcap = mod.softcap; a.window = mod.window; a.slopes = mod.slopes; a.prefix = mod.prefix_lens;
-#define HYP_F(DD, GG) decode_mod_dg<DD, GG>(a, ns, c.n_seqs, out, st)
+#define HYP_F(DD, GG) decode_joined_dg<DD, GG, PAGED_MOD>(a, ns, c.n_seqs, out, st)
   HYP_DG_DISPATCH(HYP_F);
 #undef HYP_F
 }
@@ -367,42 +355,53 @@ int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride
   PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
   a.score_stride = c.table_stride * PG_PT;
   a.scores = scratch + paged_scratch_floats(c.n_seqs, c.Hq, c.D, ns);
-#define HYP_F(DD, GG) decode_scored_dg<DD, GG>(a, ns, c.n_seqs, decay, w_in, w_out, w_stride, out, st)
+  a.decay = decay; a.w_in = w_in; a.w_out = w_out; a.w_stride = w_stride;
+#define HYP_F(DD, GG) decode_scored_dg<DD, GG>(a, ns, c.n_seqs, out, st)
   HYP_DG_DISPATCH(HYP_F);
 #undef HYP_F
 }
 
-SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int n_groups, int prefix_pages, int own_pages) {
+SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int prefix_pages, int own_pages) {
   SharedPlan p;
   const int T = AT_ROWS / (Hq / Hkv);
   p.row_tiles = n_seqs / T + n_groups;  // every group adds at most one ragged tile
+  // Where the prefixes are short or the batch is small, every sequence walks its prefix for itself: what it reads again
+  // comes from the L2, and a whole launch and the row tiles' set-up fall away.
+  const double again = (double)n_seqs * Hkv * prefix_pages * (2 * PG_PT * 2) * D;
+  p.flat = again <= FLAT_BYTES;
+  if (p.flat) {
+    p.prefix_splits = 0;
+    p.own_splits = paged_splits(n_seqs, Hkv, prefix_pages + own_pages);
+    return p;
+  }
   const int slots = 2 * sm_count();     // resident CTAs
   const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
   p.prefix_splits = slots / (full * Hkv);
   const int most = (prefix_pages * PG_PT + 2 * AT_KEYS - 1) / (2 * AT_KEYS);  // at least two key tiles each
   if (p.prefix_splits > most) p.prefix_splits = most;
-  if (p.prefix_splits > 32) p.prefix_splits = 32;
+  if (p.prefix_splits > MERGE_SLOTS - 64) p.prefix_splits = MERGE_SLOTS - 64;
   if (p.prefix_splits < 1) p.prefix_splits = 1;
-  const int groups = n_seqs * Hkv;
-  p.own_splits = slots / groups;  // as paged_splits: one wave, or four where a CTA would have more than 64 pages
-  if (p.own_splits < 1) p.own_splits = 1;
-  if (own_pages > 64 * p.own_splits) p.own_splits = (4 * slots + groups - 1) / groups;
-  const int cap = (own_pages + SH_WARPS - 1) / SH_WARPS;
-  if (p.own_splits > cap) p.own_splits = cap;
-  if (p.own_splits > 32) p.own_splits = 32;
-  if (p.own_splits < 1) p.own_splits = 1;
+  p.own_splits = paged_splits(n_seqs, Hkv, own_pages);
   return p;
 }
 
 int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride, int n_groups, const int32_t* cu_group,
                          const int32_t* prefix_table, int prefix_stride, const int32_t* prefix_lens, float* scratch,
                          __half* out, int* err, cudaStream_t st) {
-  const SharedPlan p = shared_plan(c.n_seqs, c.Hq, c.Hkv, n_groups, prefix_stride, c.table_stride);
+  const SharedPlan p = shared_plan(c.n_seqs, c.Hq, c.Hkv, c.D, n_groups, prefix_stride, c.table_stride);
   SharedArgs a{};
   a.own = paged_args(c, q, q_stride, scratch, p.prefix_splits + p.own_splits, p.prefix_splits, err);
   a.cu_group = cu_group; a.prefix_table = prefix_table; a.prefix_stride = prefix_stride; a.prefix_lens = prefix_lens;
   a.n_groups = n_groups; a.prefix_splits = p.prefix_splits; a.own_splits = p.own_splits;
-  a.prefix_ctas = p.prefix_splits * c.Hkv * p.row_tiles;
+  a.row_tiles = p.row_tiles;
+  if (p.flat) {
+    PagedArgs f = a.own;
+    f.cu_group = cu_group; f.prefix_table = prefix_table; f.prefix_lens = prefix_lens;
+    f.prefix_stride = prefix_stride; f.n_groups = n_groups;
+#define HYP_F(DD, GG) decode_joined_dg<DD, GG, PAGED_FLAT>(f, p.own_splits, c.n_seqs, out, st)
+    HYP_DG_DISPATCH(HYP_F);
+#undef HYP_F
+  }
   CUtensorMap mq, mkv;
   int rc = tc_make_q_map(&mq, q, c.n_seqs, q_stride, c.Hq, c.Hq / c.Hkv, c.D);
   if (!rc) rc = tc_make_pool_map(&mkv, c.pool, c.D);

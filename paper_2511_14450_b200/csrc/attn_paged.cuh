@@ -19,7 +19,8 @@ constexpr int PG_PT = 16;           // tokens per page
 constexpr float PG_NEG = -1e30f;    // "no key seen yet": below every score that finite fp16 operands can form
 constexpr float PG_LOG2E = 1.4426950408889634f;
 
-enum PagedMode : int { PAGED_PLAIN = 0, PAGED_SCORED = 1, PAGED_MOD = 2 };
+// PAGED_FLAT: the sequence's own pages behind those of its group's prefix
+enum PagedMode : int { PAGED_PLAIN = 0, PAGED_SCORED = 1, PAGED_MOD = 2, PAGED_FLAT = 3 };
 
 struct PagedArgs {
   const __half* q;            // row b at q + b * q_stride, head h at + h * D
@@ -39,6 +40,16 @@ struct PagedArgs {
   int window;                 // PAGED_MOD: 0 = none
   const float* slopes;        // PAGED_MOD: [Hq] or null
   const int32_t* prefix;      // PAGED_MOD: [n_seqs] or null
+  const int32_t* cu_group;    // PAGED_FLAT: groups of sequences, their prefixes' pages and lengths
+  const int32_t* prefix_table;
+  const int32_t* prefix_lens;
+  int prefix_stride, n_groups;
+  // one split: the CTA's result is the operator's (out non-null); PAGED_SCORED then finishes the running sums as well
+  __half* out;                // [n_seqs, Hq * D]
+  float decay;
+  const float* w_in;
+  float* w_out;
+  long long w_stride;
 };
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -70,31 +81,41 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   constexpr int PAGE_BYTES = PG_PT * D * 2;
   constexpr int SLOT_BYTES = 2 * PAGE_BYTES;  // keys, then values
   constexpr int THREADS = WARPS * 32;
-  static_assert(paged_smem_bytes<D, WARPS>(SLOTS) >= (2 * WARPS * 8 + WARPS * G * D) * 4, "the combine buffers reuse the ring");
+  static_assert(paged_smem_bytes<D, WARPS>(SLOTS) >= (2 * WARPS * 8 + WARPS * G * D + 16) * 4, "the combine buffers reuse the ring");
   const int warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, tq = lane & 3;
 
   const int32_t* bt = a.table + (long long)b * a.table_stride;
-  const bool early = MODE != PAGED_MOD || (a.window == 0 && a.prefix == nullptr);
+  const bool early = MODE == PAGED_PLAIN || MODE == PAGED_SCORED || (MODE == PAGED_MOD && a.window == 0 && a.prefix == nullptr);
   int32_t ids_cur = 0;
   if (early) {
     const int v = split + n_splits * (warp + WARPS * lane);
     if (v < a.table_stride) ids_cur = bt[v];
   }
-  // visible keys: [lo, total) behind the query, and [0, pre)
+  // Visible keys: [lo, total) behind the query, and [0, pre).  PAGED_FLAT: [0, pre) is the prefix, in pages of its own, and
+  // its keys are numbered from -16 * (its pages) on.
   const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
   int lo = 0, pre = 0;
+  const int32_t* pt = nullptr;
   if (MODE == PAGED_MOD) {
     if (a.window > 0) lo = max(total - a.window, 0);
     if (a.prefix) pre = min(max(a.prefix[b], 0), total);
   }
+  if (MODE == PAGED_FLAT) {
+    int g = 0;  // groups that end at or before b
+    for (int i0 = 0; i0 < a.n_groups; i0 += 32) g += __popc(__ballot_sync(0xffffffffu, i0 + lane < a.n_groups && a.cu_group[i0 + lane + 1] <= b));
+    if (g < a.n_groups) {
+      pre = min(max(a.prefix_lens[g], 0), a.prefix_stride * PG_PT);
+      pt = a.prefix_table + (long long)g * a.prefix_stride;
+    }
+  }
   const int n_pages = (total + PG_PT - 1) / PG_PT;
-  const int n_pre = MODE == PAGED_MOD ? (pre + PG_PT - 1) / PG_PT : 0;
+  const int n_pre = MODE == PAGED_MOD || MODE == PAGED_FLAT ? (pre + PG_PT - 1) / PG_PT : 0;
   const int p_lo = MODE == PAGED_MOD ? max(lo / PG_PT, n_pre) : 0;
   const int n_vis = n_pre + max(n_pages - p_lo, 0);
   auto page_index = [&](int i) {  // this warp's i-th page
     const int v = split + n_splits * (warp + WARPS * i);
-    return MODE == PAGED_MOD ? (v < n_pre ? v : v - n_pre + p_lo) : v;
+    return MODE == PAGED_MOD ? (v < n_pre ? v : v - n_pre + p_lo) : MODE == PAGED_FLAT ? v - n_pre : v;
   };
   const int first = split + n_splits * warp, stride_p = n_splits * WARPS;
   const int my_n = first < n_vis ? (n_vis - first + stride_p - 1) / stride_p : 0;
@@ -105,7 +126,11 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   const uint32_t my_ring = smem_u32(smem) + (uint32_t)(warp * SLOTS) * SLOT_BYTES;
   // page ids: lane l holds the id of this warp's page base + l, for the 32 pages being issued and the 32 after them.  Where
   // the walk does not depend on the length (no window, no prefix) the first ids are fetched together with it.
-  auto load_ids = [&](int base) { return base + lane < my_n ? bt[page_index(base + lane)] : 0; };
+  auto load_ids = [&](int base) {
+    if (base + lane >= my_n) return 0;
+    const int p = page_index(base + lane);
+    return MODE == PAGED_FLAT && p < 0 ? pt[p + n_pre] : bt[p];
+  };
   if (!early) ids_cur = load_ids(0);
   int32_t ids_next = load_ids(32);
   auto issue = [&](int i, int slot) {  // all lanes call, i ascending
@@ -162,9 +187,14 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
     if (!mbar_wait(my_bars + 8u * slot, phase, nullptr)) { ok = false; break; }
     const uint32_t kt = my_ring + slot * SLOT_BYTES, vt = kt + PAGE_BYTES;
     const int k0 = page_index(i) * PG_PT;
-    auto visible = [&](int key) { return MODE == PAGED_MOD ? key < total && (key >= lo || key < pre) : key < total; };
+    auto visible = [&](int key) {
+      if (MODE == PAGED_MOD) return key < total && (key >= lo || key < pre);
+      if (MODE == PAGED_FLAT) return key < 0 ? key + n_pre * PG_PT < pre : key < total;
+      return key < total;
+    };
     // slots that nobody may see can hold anything: their values are zeroed (a weight of 0 times infinity is not 0)
-    const bool partial = k0 + PG_PT > total || (MODE == PAGED_MOD && k0 < lo && k0 + PG_PT > pre);
+    const bool partial = MODE == PAGED_FLAT && k0 < 0 ? k0 + PG_PT == 0 && (pre & (PG_PT - 1)) != 0
+                                                      : k0 + PG_PT > total || (MODE == PAGED_MOD && k0 < lo && k0 + PG_PT > pre);
     if (partial) {
       for (int e = lane; e < PG_PT * CPR; e += 32)
         if (!visible(k0 + e / CPR))
@@ -256,6 +286,7 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   float* sm_m = reinterpret_cast<float*>(smem);  // [WARPS][8]
   float* sm_l = sm_m + WARPS * 8;                // [WARPS][8]
   float* sm_o = sm_l + WARPS * 8;                // [WARPS][G][D]
+  float *fin_m = sm_o + WARPS * G * D, *fin_inv = fin_m + 8;  // one split: the heads' maxima, reciprocal denominators
   if (g < G) {
     if (tq == 0) {
       sm_m[warp * 8 + g] = m_run;
@@ -278,9 +309,28 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
       l += wgt * sm_l[w * 8 + gq];
       acc += wgt * sm_o[(w * G + gq) * D + dd];
     }
-    const size_t row = ((size_t)b * a.Hq + kvh * G + gq) * a.n_slots + a.slot0 + split;
-    a.acc[row * D + dd] = acc;
-    if (dd == 0) *reinterpret_cast<float2*>(a.ml + row * 2) = make_float2(mx, l);
+    if (a.out) {
+      a.out[((size_t)b * a.Hq + kvh * G + gq) * D + dd] = __float2half_rn(l != 0.f ? acc / l : 0.f);
+      if (MODE == PAGED_SCORED && dd == 0) {
+        fin_m[gq] = mx;
+        fin_inv[gq] = l != 0.f ? 1.f / l : 0.f;
+      }
+    } else {
+      const size_t row = ((size_t)b * a.Hq + kvh * G + gq) * a.n_slots + a.slot0 + split;
+      a.acc[row * D + dd] = acc;
+      if (dd == 0) *reinterpret_cast<float2*>(a.ml + row * 2) = make_float2(mx, l);
+    }
+  }
+  if (MODE == PAGED_SCORED && a.out) {
+    bar_sync();  // the scores in global memory are this CTA's own
+    const float* sc = a.scores + ((size_t)b * a.Hq + kvh * G) * a.score_stride;
+    const long long wrow = ((long long)b * a.Hkv + kvh) * a.w_stride;
+    for (int k = tid; k < total; k += THREADS) {
+      float w = 0.f;
+#pragma unroll
+      for (int gq = 0; gq < G; ++gq) w += ex2_approx(sc[(size_t)gq * a.score_stride + k] - fin_m[gq]) * fin_inv[gq];
+      a.w_out[wrow + k] = a.w_in && k < total - 1 ? fmaf(a.decay, a.w_in[wrow + k], w) : w;  // the new token's sum starts here
+    }
   }
 }
 

@@ -35,9 +35,10 @@ int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half*
 int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride, float decay, const float* w_in, float* w_out,
                          long long w_stride, float* scratch, __half* out, int* err, cudaStream_t st);
 struct SharedPlan {
+  bool flat;  // no row tiles: every sequence walks its prefix itself
   int prefix_splits, own_splits, row_tiles;
 };
-SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int n_groups, int prefix_pages, int own_pages);
+SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int prefix_pages, int own_pages);
 int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride, int n_groups, const int32_t* cu_group,
                          const int32_t* prefix_table, int prefix_stride, const int32_t* prefix_lens, float* scratch,
                          __half* out, int* err, cudaStream_t st);

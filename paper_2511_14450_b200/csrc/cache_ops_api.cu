@@ -120,7 +120,7 @@ extern "C" int hyp_op_kv_evict(const hyp_attn_shape* shape, int32_t n_seqs, cons
 extern "C" size_t hyp_op_attn_shared_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t n_groups,
                                                    int32_t max_prefix_pages, int32_t max_pages_per_seq) {
   if (!shape_ok(shape) || n_seqs < 1 || n_groups < 1 || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return 0;
-  const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, n_groups, max_prefix_pages, max_pages_per_seq);
+  const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, n_groups, max_prefix_pages, max_pages_per_seq);
   return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim, p.prefix_splits + p.own_splits);
 }
 
@@ -134,7 +134,7 @@ extern "C" int hyp_op_attn_decode_shared(const hyp_attn_shape* shape, int32_t n_
   if (n_seqs < 1 || n_seqs > 65535 || n_groups < 1 || n_groups > 65535 || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
   if (!aligned(kv_pages, 16) || !aligned(scratch, 16)) return HYP_EINVAL;
   if (scratch_bytes < hyp_op_attn_shared_scratch_bytes(shape, n_seqs, n_groups, max_prefix_pages, max_pages_per_seq)) return HYP_ECAPACITY;
-  const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, n_groups, max_prefix_pages, max_pages_per_seq);
+  const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, n_groups, max_prefix_pages, max_pages_per_seq);
   if ((double)shape->n_kv_heads * ((double)p.prefix_splits * p.row_tiles + (double)p.own_splits * n_seqs) > 2147483647.0) return HYP_ECAPACITY;
   const int rc = tc_prepare();
   if (rc) return rc;
