@@ -145,21 +145,19 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         pos = plen - 1;
         return TileRow{0, plen - 1, 0};
       },
-      [&](int t, int gh, bool valid, float m_ref, float l, auto load) {
+      [&](int t, int gh, bool valid, float m_ref, float l, uint32_t stage, auto load) {
         const size_t row = slot_of(t, gh);
-        float* dst = a.own.acc + row * D;
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
           uint32_t v[16], w[16];
           load(c, v, w);
-          if (valid) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-              reinterpret_cast<uint4*>(dst + c)[4 + i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-            }
+          for (int i = 0; i < 4; ++i) {
+            at_stage16(stage + 4 * c + 16 * i, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            at_stage16(stage + 4 * c + 64 + 16 * i, w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
           }
         }
+        at_send_row(a.own.acc + row * D, stage, D * 4, valid);
         if (valid) *reinterpret_cast<float2*>(a.own.ml + row * 2) = make_float2(m_ref, l);
       });
 }
@@ -214,25 +212,23 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         pos = ctx + q0 + t;
         return TileRow{max(pos - window + 1, 0), min(pos, have - 1), pre};
       },
-      [&](int t, int gh, bool valid, float, float l, auto load) {
+      [&](int t, int gh, bool valid, float, float l, uint32_t stage, auto load) {
         const float inv = l != 0.f ? 1.f / l : 0.f;
         __half* orow = a.out + ((size_t)(wk.row0 + t) * a.Hq + wk.head0 + gh) * D;
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
           uint32_t v[16], w[16];
           load(c, v, w);
-          if (valid) {
-            uint32_t pk[16];
+          uint32_t pk[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              pk[i] = pack_f16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
-              pk[8 + i] = pack_f16(__uint_as_float(w[2 * i]) * inv, __uint_as_float(w[2 * i + 1]) * inv);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              reinterpret_cast<uint4*>(orow + c)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+          for (int i = 0; i < 8; ++i) {
+            pk[i] = pack_f16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+            pk[8 + i] = pack_f16(__uint_as_float(w[2 * i]) * inv, __uint_as_float(w[2 * i + 1]) * inv);
           }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) at_stage16(stage + 2 * c + 16 * i, pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
         }
+        at_send_row(orow, stage, D * 2, valid);
       });
 }
 
