@@ -103,10 +103,68 @@ struct SharedArgs {
   const int32_t* prefix_table;
   int prefix_stride;
   const int32_t* prefix_lens;
-  int n_groups, prefix_splits, own_splits, row_tiles;
+  int n_groups, prefix_splits, own_splits;
+  bool even;                  // see prefix_cut_even
 };
 
-// grid (prefix_splits * Hkv * row tiles)
+// How the prefixes are cut: every (row tile, KV head) of group g is shared by `splits` CTAs of `per` key tiles each.
+struct PrefixCut {
+  int group, first, q0, len, plen, split, splits, per, kvh;
+};
+// Up to 32 groups, one lane each: the CTAs of the grid (two per SM) are handed out so that all get about the same number of
+// key tiles, whatever the lengths of the prefixes and the sizes of the groups.  (A fixed number of splits made 1.3
+// waves of unequal CTAs of five prefixes of 4096 to 8192 tokens: 53 us.)
+__device__ __forceinline__ bool prefix_cut_even(const SharedArgs& a, int T, PrefixCut& c) {
+  const int lane = threadIdx.x & 31;
+  const bool in = lane < a.n_groups;
+  const int c0 = in ? a.cu_group[lane] : 0, c1 = in ? a.cu_group[lane + 1] : 0;
+  const int plen = in ? min(max(a.prefix_lens[lane], 0), a.prefix_stride * PG_PT) : 0;
+  const int units = (max(c1 - c0, 0) + T - 1) / T * a.own.Hkv, tiles = (plen + AT_KEYS - 1) / AT_KEYS;
+  // lane i tries `per` = low + i * step: low is what an even share without rounding would be
+  const int all = __reduce_add_sync(0xffffffffu, units * tiles), most = max(__reduce_max_sync(0xffffffffu, tiles), 1);
+  int low = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+  low = max(low, (most + a.prefix_splits - 1) / a.prefix_splits);  // no prefix in more shares than there are slots
+  const int step = max(low / 16, 1), mine = min(low + lane * step, most);
+  int total = 0;
+  for (int g = 0; g < a.n_groups; ++g) {
+    const int ug = __shfl_sync(0xffffffffu, units, g), tg = __shfl_sync(0xffffffffu, tiles, g);
+    total += ug * max((tg + mine - 1) / mine, 1);
+  }
+  const uint32_t fits = __ballot_sync(0xffffffffu, total <= (int)gridDim.x);
+  c.per = fits ? __shfl_sync(0xffffffffu, mine, __ffs(fits) - 1) : most;  // one share each always fits
+  const int splits = max((tiles + c.per - 1) / c.per, 1), count = units * splits;
+  int incl = count;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  const uint32_t hit = __ballot_sync(0xffffffffu, (int)blockIdx.x < incl);
+  if (!hit) return false;
+  const int src = __ffs(hit) - 1;
+  const int i = (int)blockIdx.x - __shfl_sync(0xffffffffu, incl - count, src);
+  c.group = src;
+  c.first = __shfl_sync(0xffffffffu, c0, src);
+  c.len = __shfl_sync(0xffffffffu, c1, src) - c.first;
+  c.plen = __shfl_sync(0xffffffffu, plen, src);
+  c.splits = __shfl_sync(0xffffffffu, splits, src);
+  c.split = i % c.splits;
+  c.kvh = i / c.splits % a.own.Hkv;
+  c.q0 = i / (c.splits * a.own.Hkv) * T;
+  return true;
+}
+// More groups, or more row tiles than CTAs fit at once: prefix_splits shares for every (row tile, KV head).
+__device__ __forceinline__ bool prefix_cut_fixed(const SharedArgs& a, int T, PrefixCut& c) {
+  c.splits = a.prefix_splits;
+  c.split = blockIdx.x % c.splits;
+  c.kvh = blockIdx.x / c.splits % a.own.Hkv;
+  at_locate(a.cu_group, a.n_groups, T, blockIdx.x / (c.splits * a.own.Hkv), c.group, c.first, c.q0, c.len);
+  if (c.group < 0) return false;
+  c.plen = min(max(a.prefix_lens[c.group], 0), a.prefix_stride * PG_PT);
+  c.per = ((c.plen + AT_KEYS - 1) / AT_KEYS + c.splits - 1) / c.splits;
+  return true;
+}
+
 template <int D, int G>
 __global__ void __launch_bounds__(AT_THREADS, 2)
 shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
@@ -115,30 +173,27 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
   pdl_wait();
   pdl_trigger();
   constexpr int T = AT_ROWS / G;
-  const int split = blockIdx.x % a.prefix_splits, kvh = (blockIdx.x / a.prefix_splits) % a.own.Hkv;
-  const int tile = blockIdx.x / (a.prefix_splits * a.own.Hkv);
-  int group, first, q0, len;
-  at_locate(a.cu_group, a.n_groups, T, tile, group, first, q0, len);
-  if (group < 0) return;
-  const int plen = min(max(a.prefix_lens[group], 0), a.prefix_stride * PG_PT);
+  PrefixCut cut;
+  if (!(a.even ? prefix_cut_even(a, T, cut) : prefix_cut_fixed(a, T, cut))) return;
+  const int kvh = cut.kvh, split = cut.split, plen = cut.plen;
   const int all_tiles = (plen + AT_KEYS - 1) / AT_KEYS;
-  const int per = (all_tiles + a.prefix_splits - 1) / a.prefix_splits;
   TileWork wk;
   wk.head0 = kvh * G;
   wk.kvh = kvh;
-  wk.row0 = first + q0;
-  wk.rows = min(T, len - q0);
-  wk.table = a.prefix_table + (long long)group * a.prefix_stride;
+  wk.row0 = cut.first + cut.q0;
+  wk.rows = min(T, cut.len - cut.q0);
+  wk.table = a.prefix_table + (long long)cut.group * a.prefix_stride;
   wk.key_end = plen;
   wk.n_first = 0;
-  wk.second = split * per;
-  wk.n_tiles = max(0, min(per, all_tiles - split * per));
+  wk.second = split * cut.per;
+  wk.n_tiles = max(0, min(cut.per, all_tiles - split * cut.per));
   auto slot_of = [&](int t, int gh) { return ((size_t)(wk.row0 + t) * a.own.Hq + wk.head0 + gh) * a.own.n_slots + split; };
-  if (wk.n_tiles == 0) {  // the whole CTA: an empty share still has to say so
+  // shares that are empty, or that this group does not have, still have to say so
+  for (int s = split + (wk.n_tiles > 0); s < (split == cut.splits - 1 ? a.prefix_splits : split + 1); ++s) {
     const int t = threadIdx.x / G, gh = threadIdx.x % G;
-    if (threadIdx.x < AT_ROWS && t < wk.rows) *reinterpret_cast<float2*>(a.own.ml + slot_of(t, gh) * 2) = make_float2(PG_NEG, 0.f);
-    return;
+    if (threadIdx.x < AT_ROWS && t < wk.rows) *reinterpret_cast<float2*>(a.own.ml + (slot_of(t, gh) + s - split) * 2) = make_float2(PG_NEG, 0.f);
   }
+  if (wk.n_tiles == 0) return;  // the whole CTA
   tile_body<D, false, false>(
       &tm_q, &tm_kv, sh_smem_raw, ts, wk, G, a.own.Hkv, 0.f, nullptr, a.own.err,
       [&](int, int& pos) {
@@ -293,11 +348,12 @@ int decode_scored_dg(PagedArgs a, int n_splits, int n_seqs, __half* out, cudaStr
 }
 
 template <int D, int G>
-int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
+int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int prefix_ctas, int n_seqs, __half* out,
+                     cudaStream_t st) {
   constexpr int smem = AtGeom<D>::SMEM;
   int rc = allow_smem<shared_prefix_kernel<D, G>>(smem);
   if (rc) return rc;
-  HYP_CUDA_TRY(launch_pdl<2>(shared_prefix_kernel<D, G>, dim3((unsigned)(a.prefix_splits * a.own.Hkv * a.row_tiles)), dim3(AT_THREADS),
+  HYP_CUDA_TRY(launch_pdl<2>(shared_prefix_kernel<D, G>, dim3((unsigned)prefix_ctas), dim3(AT_THREADS),
                              (size_t)smem, st, mq, mkv, a));
   rc = launch_paged<D, G, PAGED_PLAIN>(a.own, a.own_splits, n_seqs, st);
   if (rc < 0) return rc;
@@ -371,12 +427,19 @@ SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int pre
     return p;
   }
   const int slots = 2 * sm_count();     // resident CTAs
-  const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
-  p.prefix_splits = slots / (full * Hkv);
   const int most = (prefix_pages * PG_PT + 2 * AT_KEYS - 1) / (2 * AT_KEYS);  // at least two key tiles each
-  if (p.prefix_splits > most) p.prefix_splits = most;
-  if (p.prefix_splits > MERGE_SLOTS - 64) p.prefix_splits = MERGE_SLOTS - 64;
-  if (p.prefix_splits < 1) p.prefix_splits = 1;
+  p.even = n_groups <= 32 && p.row_tiles * Hkv <= slots;
+  if (p.even) {
+    p.prefix_splits = most < 16 ? most : 16;
+    p.prefix_ctas = slots;
+  } else {
+    const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
+    p.prefix_splits = slots / (full * Hkv);
+    if (p.prefix_splits > most) p.prefix_splits = most;
+    if (p.prefix_splits > MERGE_SLOTS - 64) p.prefix_splits = MERGE_SLOTS - 64;
+    if (p.prefix_splits < 1) p.prefix_splits = 1;
+    p.prefix_ctas = p.prefix_splits * Hkv * p.row_tiles;
+  }
   p.own_splits = paged_splits(n_seqs, Hkv, own_pages);
   return p;
 }
@@ -389,7 +452,7 @@ int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride
   a.own = paged_args(c, q, q_stride, scratch, p.prefix_splits + p.own_splits, p.prefix_splits, err);
   a.cu_group = cu_group; a.prefix_table = prefix_table; a.prefix_stride = prefix_stride; a.prefix_lens = prefix_lens;
   a.n_groups = n_groups; a.prefix_splits = p.prefix_splits; a.own_splits = p.own_splits;
-  a.row_tiles = p.row_tiles;
+  a.even = p.even;
   if (p.flat) {
     PagedArgs f = a.own;
     f.cu_group = cu_group; f.prefix_table = prefix_table; f.prefix_lens = prefix_lens;
@@ -402,7 +465,7 @@ int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride
   int rc = tc_make_q_map(&mq, q, c.n_seqs, q_stride, c.Hq, c.Hq / c.Hkv, c.D);
   if (!rc) rc = tc_make_pool_map(&mkv, c.pool, c.D);
   if (rc) return rc;
-#define HYP_F(DD, GG) decode_shared_dg<DD, GG>(mq, mkv, a, c.n_seqs, out, st)
+#define HYP_F(DD, GG) decode_shared_dg<DD, GG>(mq, mkv, a, p.prefix_ctas, c.n_seqs, out, st)
   HYP_DG_DISPATCH(HYP_F);
 #undef HYP_F
 }

@@ -36,7 +36,8 @@ int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride
                          long long w_stride, float* scratch, __half* out, int* err, cudaStream_t st);
 struct SharedPlan {
   bool flat;  // no row tiles: every sequence walks its prefix itself
-  int prefix_splits, own_splits, row_tiles;
+  bool even;  // the prefix kernel hands its CTAs out by the lengths it finds
+  int prefix_splits, own_splits, row_tiles, prefix_ctas;
 };
 SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int prefix_pages, int own_pages);
 int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride, int n_groups, const int32_t* cu_group,
