@@ -9,11 +9,11 @@
 //            128-byte-swizzled operand.
 //   warp 1   issues tcgen05.mma: S_b = Q K^T (128 x 64) into one of two score buffers in tensor memory and, once the
 //            softmax warps have written the weights, O += P V (P from tensor memory).  The scores of tile j + 2 are
-//            issued right behind the value product of tile j, so the tensor core works ahead of the softmax.  In the
-//            tile that holds the end of the sequence it first zeroes the values behind the end (0 times garbage
-//            infinity is not 0).
+//            issued right behind the value product of tile j, so the tensor core works ahead of the softmax.  One lane
+//            waits and issues: with the whole warp waiting, a tile spent 600 of 1850 cycles between its products.
 //   warps 2-5  softmax, one thread per query row (tensor-memory lane); the reference maximum is moved, and O rescaled,
-//            only when a row of the warp has outgrown it by 2^8.
+//            only when a row of the warp has outgrown it by 2^8.  In the tile that holds the end of the sequence they also
+//            zero the values behind the end (0 times garbage infinity is not 0).
 // Every barrier exists once per buffer (phase = tile / 2), every wait is bounded, failure unwinds through a shared flag.
 #pragma once
 #include "attn_paged.cuh"
@@ -332,15 +332,14 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
         mbar_wait(full + 8 * (uint32_t)(i & 1), (uint32_t)((i >> 1) & 1), nullptr);
     }
   } else if (warp == 1) {
-    // ---------------- MMA issuer: the warp waits together, lane 0 issues ----------------
-    bool ok = mbar_wait(q_full, 0, abort_flag);
-    const uint64_t dq = smem_desc(sQ), dk = smem_desc(sK), dv = at_desc_mn(sV);
-    auto scores = [&](int j) -> bool {
-      const uint32_t b = (uint32_t)(j & 1);
-      const bool got = mbar_wait(k_full + 8 * b, (uint32_t)((j >> 1) & 1), abort_flag);
-      if (!__all_sync(0xffffffffu, got)) return false;
-      tc_fence_after();
-      if (lane == 0) {
+    // ---------------- MMA issuer: one lane ----------------
+    if (lane == 0) {
+      const uint64_t dq = smem_desc(sQ), dk = smem_desc(sK), dv = at_desc_mn(sV);
+      bool ok = mbar_wait(q_full, 0, abort_flag);
+      auto scores = [&](int j) -> bool {
+        const uint32_t b = (uint32_t)(j & 1);
+        if (!mbar_wait(k_full + 8 * b, (uint32_t)((j >> 1) & 1), abort_flag)) return false;
+        tc_fence_after();
         const uint64_t dkb = dk + (uint64_t)(b * (Geo::STAGE >> 4));
 #pragma unroll
         for (int kb = 0; kb < Geo::HALVES; ++kb)
@@ -349,29 +348,14 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
             tc_mma(tmem_s + 64u * b, dq + (uint64_t)(kb * ((128 * 64 * 2) >> 4) + ks * 2),
                    dkb + (uint64_t)(kb * ((AT_KEYS * 128) >> 4) + ks * 2), IDESC_S, (kb | ks) ? 1u : 0u);
         tc_commit(s_full + 8 * b);  // also frees the key stage
-      }
-      __syncwarp();
-      return true;
-    };
-    ok = __all_sync(0xffffffffu, ok);
-    ok = ok && scores(0);
-    if (ok && n_tiles > 1) ok = scores(1);
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const uint32_t b = (uint32_t)(j & 1), ph = (uint32_t)((j >> 1) & 1);
-      const bool got = mbar_wait(p_full + 8 * b, ph, abort_flag) && mbar_wait(v_full + 8 * b, ph, abort_flag);
-      if (!__all_sync(0xffffffffu, got)) { ok = false; break; }
-      const int left = wk.key_end - key_tile(j) * AT_KEYS;
-      if (left < AT_KEYS) {  // the end of the sequence lies in this tile
-        for (int e = lane; e < Geo::HALVES * (AT_KEYS - left) * 8; e += 32) {
-          const int h = e / ((AT_KEYS - left) * 8), r = left + (e % ((AT_KEYS - left) * 8)) / 8, c = e & 7;
-          const uint32_t dst = sV + b * Geo::STAGE + (uint32_t)(h * AT_KEYS + r) * 128u + (uint32_t)c * 16u;
-          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(dst), "r"(0u) : "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      }
-      tc_fence_after();
-      if (lane == 0) {
+        return true;
+      };
+      ok = ok && scores(0);
+      if (ok && n_tiles > 1) ok = scores(1);
+      for (int j = 0; j < n_tiles && ok; ++j) {
+        const uint32_t b = (uint32_t)(j & 1), ph = (uint32_t)((j >> 1) & 1);
+        if (!mbar_wait(v_full + 8 * b, ph, abort_flag) || !mbar_wait(p_full + 8 * b, ph, abort_flag)) { ok = false; break; }
+        tc_fence_after();
         // O += P V: 4 pages of 16 keys; P sits in tensor memory (8 columns per page)
         const uint64_t dvb = dv + (uint64_t)(b * (Geo::STAGE >> 4));
 #pragma unroll
@@ -379,14 +363,13 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
           at_mma_ta(tmem_o, tmem_s + 64u * b + 32u + (uint32_t)(8 * p), dvb + (uint64_t)(p * (2048 >> 4)), IDESC_PV,
                     (j > 0 || p > 0) ? 1u : 0u);
         tc_commit(o_done + 8 * b);  // also frees the value stage
+        // the scores of tile j + 2 reuse this tile's buffer: issued behind its value product
+        if (j + 2 < n_tiles) ok = scores(j + 2);
       }
-      __syncwarp();
-      // the scores of tile j + 2 reuse this tile's buffer: issued behind its value product
-      if (j + 2 < n_tiles) ok = scores(j + 2);
-    }
-    if (!ok && lane == 0) {
-      *abort_flag = 1;
-      atomicCAS(err, 0, 23);
+      if (!ok) {
+        *abort_flag = 1;
+        atomicCAS(err, 0, 23);
+      }
     }
   } else {
     // ---------------- softmax / epilogue: thread = query row = tensor-memory lane ----------------
@@ -421,6 +404,16 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
         else
           ok = at_softmax<D, CAP, BIAS, false>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, m_ref, l);
         if (!ok) break;
+      }
+      const int left = wk.key_end - key_tile(j) * AT_KEYS;
+      if (left < AT_KEYS) {  // the end of the sequence lies in this tile
+        ok = __all_sync(0xffffffffu, mbar_wait(v_full + 8 * b, (uint32_t)((j >> 1) & 1), abort_flag));
+        if (!ok) break;
+        for (int e = 32 * q + lane; e < Geo::HALVES * (AT_KEYS - left) * 8; e += 128) {
+          const int h = e / ((AT_KEYS - left) * 8), zr = left + (e % ((AT_KEYS - left) * 8)) / 8, c = e & 7;
+          at_stage16(sV + b * Geo::STAGE + (uint32_t)(h * AT_KEYS + zr) * 128u + (uint32_t)c * 16u, 0u, 0u, 0u, 0u);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       tc_fence_before();
       mbar_arrive(p_full + 8 * b);
