@@ -2,12 +2,13 @@
 // last n_recent tokens and the heaviest of the others stay, in their order, n_keep in all.
 //
 //   select kernel: grid (Hkv, n_seqs), 1024 threads.  The weights between the protected ends stand for order-preserving
-//   32-bit keys, held in registers (up to 32 per thread, read again from L2 for longer contexts).  The threshold, the m-th
+//   32-bit keys, held in shared memory (up to 32768, read again from L2 for longer contexts).  The threshold, the m-th
 //   largest key, is found digit by digit (11, 11 and 10 bits): a histogram in shared memory of the keys that agree with the
 //   digits found so far, scanned from the top.  Counts do not depend on the order of the additions, so the result is the
 //   same on every run.  The kept indexes and weights are then written at the places that a scan over (stripe, warp)
-//   counts gives; among keys equal to the threshold the lowest indexes win.  (Searching bit pairs with block-wide counts
-//   instead: 21 us for 40 heads of 4096 tokens.)
+//   counts gives; among keys equal to the threshold the lowest indexes win.  (40 heads of 4096
+//   tokens: 21 us searching bit pairs with block-wide counts, 16 us with the weights in registers - every CTA then runs
+//   straight through 32-fold unrolled code once, and waits for its instructions.)
 //   move kernel: copies the kept rows, 16-byte chunks, re-permuted for their new slot.  Other pages: every row at its
 //   own pace.  In place a row moves down or stays, so one CTA per (sequence, KV head, keys or values) goes up the rows and
 //   reads each batch completely before it writes it: a batch writes at or below its own sources, never at a later one's.
@@ -19,7 +20,7 @@ namespace hyp {
 
 namespace {
 
-constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_NPT = 32;
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_STRIPES = 32;  // stripes of EV_THREADS candidates in shared memory
 
 // Keys ascend with the weight; -0 equals +0, NaN counts as -infinity.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -56,9 +57,10 @@ __device__ __forceinline__ void count_bin(uint32_t* hist, bool valid, uint32_t b
   }
 }
 
-// IN_REGS: the candidates fit the threads' registers (chosen by what the table's row can name).
-template <bool IN_REGS>
+// STAGED: the candidates fit shared memory (chosen by what the table's row can name).
+template <bool STAGED>
 __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
+  extern __shared__ float sw[];  // STAGED: the candidates' weights
   __shared__ uint32_t hist[EV_BINS];
   __shared__ uint32_t tmp[EV_WARPS];
   __shared__ uint32_t found[3];  // bin, keys above it, keys in it
@@ -81,14 +83,9 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   }
   const int r0 = a.n_sink, n = t - a.n_sink - a.n_recent;  // candidates w[r0 .. r0 + n), of which m stay; n > m
   const int m = a.n_keep - a.n_sink - a.n_recent;
-  float v[IN_REGS ? EV_NPT : 1];
-  if (IN_REGS) {
-#pragma unroll
-    for (int i = 0; i < EV_NPT; ++i) {
-      const int k = i * EV_THREADS + tid;
-      v[IN_REGS ? i : 0] = k < n ? w[r0 + k] : 0.f;
-    }
-  }
+  if (STAGED)  // every thread reads back its own, so nothing has to be waited for yet
+    for (int k = tid; k < n; k += EV_THREADS) sw[k] = w[r0 + k];
+  auto weight = [&](int k) { return STAGED ? sw[k] : w[r0 + k]; };
   // threshold: the m-th largest key.  need: how many of the keys that agree with the digits found so far stay.
   uint32_t thr = 0, known = 0;
   int need = m;
@@ -101,13 +98,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
       const uint32_t key = weight_key(x);
       count_bin(hist, k < n && (key & known) == thr, (key >> shift) & digit);
     };
-    if (IN_REGS) {
-#pragma unroll
-      for (int i = 0; i < EV_NPT; ++i)
-        if (i * EV_THREADS < n) add(i * EV_THREADS + tid, v[IN_REGS ? i : 0]);
-    } else {
-      for (int s = 0; s < n; s += EV_THREADS) add(s + tid, s + tid < n ? w[r0 + s + tid] : 0.f);
-    }
+    for (int s = 0; s < n; s += EV_THREADS) add(s + tid, s + tid < n ? weight(s + tid) : 0.f);
     __syncthreads();
     // thread i has bins 2047 - 2i and 2046 - 2i: keys in the bins above a bin, from the top
     const uint32_t hi = hist[EV_BINS - 1 - 2 * tid], lo = hist[EV_BINS - 2 - 2 * tid];
@@ -131,42 +122,36 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   // A key stays if the digits found are above the threshold's, or equal to them and it is among the first `need` of those.
   const int limit = all ? (m == 0 ? 0 : n) : need;
 
-  if (IN_REGS) {
+  if (STAGED) {
     // (stripe, warp) counts, greater in the low half, equal in the high half: at most 32768 each
     uint32_t* cnt = hist;
-#pragma unroll
-    for (int i = 0; i < EV_NPT; ++i) {
-      if (i * EV_THREADS < n) {
-        const uint32_t key = weight_key(v[IN_REGS ? i : 0]) & known;
-        const bool in = i * EV_THREADS + tid < n && m > 0;
-        const uint32_t mg = __ballot_sync(0xffffffffu, in && key > thr), me = __ballot_sync(0xffffffffu, in && key == thr);
-        if (lane == 0) cnt[i * EV_WARPS + warp] = __popc(mg) | (__popc(me) << 16);
-      } else if (lane == 0) {
-        cnt[i * EV_WARPS + warp] = 0;
+    for (int i = 0; i < EV_STRIPES; ++i) {
+      uint32_t c = 0;
+      if (i * EV_THREADS < n && m > 0) {
+        const int k = i * EV_THREADS + tid;
+        const uint32_t key = k < n ? weight_key(sw[k]) & known : 0u;
+        c = __popc(__ballot_sync(0xffffffffu, k < n && key > thr)) | (__popc(__ballot_sync(0xffffffffu, k < n && key == thr)) << 16);
       }
+      if (lane == 0) cnt[i * EV_WARPS + warp] = c;
     }
-    __syncthreads();  // all weights are in registers: from here on they may be overwritten
+    __syncthreads();  // all weights have been read: from here on they may be overwritten
     const uint32_t mine = cnt[tid];
     const uint32_t upto = block_scan(mine, tmp);
     cnt[tid] = upto - mine;
     __syncthreads();
-    if (m > 0) {
-#pragma unroll
-      for (int i = 0; i < EV_NPT; ++i)
-        if (i * EV_THREADS < n) {
-          const int k = i * EV_THREADS + tid;
-          const float x = v[IN_REGS ? i : 0];
-          const uint32_t key = weight_key(x) & known;
-          const bool gt = k < n && key > thr, eq = k < n && key == thr;
-          const uint32_t below = (1u << lane) - 1u, base = cnt[i * EV_WARPS + warp];
-          const int e_before = (int)(base >> 16) + __popc(__ballot_sync(0xffffffffu, eq) & below);
-          const int g_before = (int)(base & 0xffffu) + __popc(__ballot_sync(0xffffffffu, gt) & below);
-          if (gt || (eq && e_before < limit)) {
-            const int pos = r0 + g_before + min(e_before, limit);
-            kept[pos] = r0 + k;
-            wo[pos] = x;
-          }
-        }
+    for (int i = 0; i * EV_THREADS < n && m > 0; ++i) {
+      const int k = i * EV_THREADS + tid;
+      const float x = k < n ? sw[k] : 0.f;
+      const uint32_t key = weight_key(x) & known;
+      const bool gt = k < n && key > thr, eq = k < n && key == thr;
+      const uint32_t below = (1u << lane) - 1u, base = cnt[i * EV_WARPS + warp];
+      const int e_before = (int)(base >> 16) + __popc(__ballot_sync(0xffffffffu, eq) & below);
+      const int g_before = (int)(base & 0xffffu) + __popc(__ballot_sync(0xffffffffu, gt) & below);
+      if (gt || (eq && e_before < limit)) {
+        const int pos = r0 + g_before + min(e_before, limit);
+        kept[pos] = r0 + k;
+        wo[pos] = x;
+      }
     }
   } else {
     // stripes of 1024 candidates, each read before any of it is written
@@ -211,53 +196,90 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   }
 }
 
-// grid (segments, 2 * Hkv, n_seqs)
-constexpr int MV_THREADS = 512, MV_UNROLL = 4;
-template <int D, bool IN_PLACE>
-__global__ void __launch_bounds__(MV_THREADS) evict_move_kernel(EvictArgs a, int rows_per_cta) {
-  constexpr int CPR = D / 8, STEP = MV_THREADS / CPR;  // 16-byte chunks per row, rows per pass
+// Rows to other pages: grid (segments, 2 * Hkv, n_seqs).  A warp takes 32 kept rows: each lane looks up one row's source and
+// destination (the chain kept index -> page -> row is walked once for 32 rows), then the warp copies the rows, eight
+// 512-byte pieces in flight at a time.  (With every thread walking the chain for its own chunks: 19.7 us for 84 MB.)
+constexpr int MV_THREADS = 256, MV_ROWS = MV_THREADS;
+template <int D>
+__global__ void __launch_bounds__(MV_THREADS) evict_move_kernel(EvictArgs a) {
+  constexpr int CPR = D / 8, RPI = 32 / CPR, UNROLL = 8;  // 16-byte chunks per row, rows per warp-wide access
   pdl_wait();
   pdl_trigger();
   const int kind = blockIdx.y & 1, kvh = blockIdx.y >> 1, b = blockIdx.z;
+  const int lane = threadIdx.x & 31;
   const int len = min(min(max(a.cached[b], 0), a.table_stride * 16), a.n_keep);
-  const int begin = blockIdx.x * rows_per_cta, end = min(len, begin + rows_per_cta);
-  const int32_t* kept = a.kept + ((long long)b * a.Hkv + kvh) * a.n_keep;
-  const int32_t* bt = a.table + (long long)b * a.table_stride;
-  const int32_t* dt = a.dst_table + (long long)b * a.dst_stride;
-  const int c = threadIdx.x % CPR, r = threadIdx.x / CPR;
-  auto row_at = [&](int32_t page, int slot) {
-    return ((((size_t)page * 2 + kind) * a.Hkv + kvh) * 16 + slot) * D;
-  };
-  for (int i0 = begin; i0 < end; i0 += STEP * MV_UNROLL) {
-    uint4 v[MV_UNROLL];
-    int src[MV_UNROLL];
+  const int i = blockIdx.x * MV_ROWS + (threadIdx.x & ~31) + lane;
+  const int rows = min(32, len - (i - lane));
+  if (rows <= 0) return;
+  // rows are numbered through the pool: 2^32 of them are more than any pool has
+  uint32_t from = 0, to = 0;
+  if (i < len) {
+    const int s = a.kept[((long long)b * a.Hkv + kvh) * a.n_keep + i];
+    const int32_t src_page = a.table[(long long)b * a.table_stride + (s >> 4)], dst_page = a.dst_table[(long long)b * a.dst_stride + (i >> 4)];
+    from = (((uint32_t)src_page * 2 + kind) * a.Hkv + kvh) * 16 + (s & 15);
+    to = (((uint32_t)dst_page * 2 + kind) * a.Hkv + kvh) * 16 + (i & 15);
+  }
+  const int c = lane % CPR, sub = lane / CPR;
+#pragma unroll 1
+  for (int it = 0; it < 32; it += UNROLL * RPI) {
+    if (it >= rows) return;
+    uint4 v[UNROLL];
 #pragma unroll
-    for (int u = 0; u < MV_UNROLL; ++u) {
-      const int i = i0 + u * STEP + r;
-      src[u] = i < end ? kept[i] : -1;
+    for (int u = 0; u < UNROLL; ++u) {
+      const int r = it + u * RPI + sub;
+      const uint32_t row = __shfl_sync(0xffffffffu, from, r);
+      if (r < rows) v[u] = __ldcs(reinterpret_cast<const uint4*>(a.pool + (size_t)row * D + ((c ^ (row & 7)) << 3)));
     }
 #pragma unroll
-    for (int u = 0; u < MV_UNROLL; ++u)
-      if (src[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(a.pool + row_at(bt[src[u] >> 4], src[u] & 15) + ((c ^ (src[u] & 7)) << 3));
-    if (IN_PLACE) __syncthreads();  // the whole batch is read before any of it is written
+    for (int u = 0; u < UNROLL; ++u) {
+      const int r = it + u * RPI + sub;
+      const uint32_t row = __shfl_sync(0xffffffffu, to, r);
+      if (r < rows) *reinterpret_cast<uint4*>(a.dst + (size_t)row * D + ((c ^ (row & 7)) << 3)) = v[u];
+    }
+  }
+}
+
+// In place: grid (2 * Hkv, n_seqs); the CTA goes up the rows and reads each batch completely before it writes it.
+constexpr int MI_THREADS = 512, MI_UNROLL = 4;
+template <int D>
+__global__ void __launch_bounds__(MI_THREADS) evict_move_in_place_kernel(EvictArgs a) {
+  constexpr int CPR = D / 8, STEP = MI_THREADS / CPR;  // 16-byte chunks per row, rows per pass
+  pdl_wait();
+  pdl_trigger();
+  const int kind = blockIdx.x & 1, kvh = blockIdx.x >> 1, b = blockIdx.y;
+  const int len = min(min(max(a.cached[b], 0), a.table_stride * 16), a.n_keep);
+  const int32_t* kept = a.kept + ((long long)b * a.Hkv + kvh) * a.n_keep;
+  const int32_t* bt = a.table + (long long)b * a.table_stride;
+  const int c = threadIdx.x % CPR, r = threadIdx.x / CPR;
+  auto row_at = [&](int32_t page, int slot) { return ((((size_t)page * 2 + kind) * a.Hkv + kvh) * 16 + slot) * D; };
+  for (int i0 = 0; i0 < len; i0 += STEP * MI_UNROLL) {
+    uint4 v[MI_UNROLL];
+    int src[MI_UNROLL];
 #pragma unroll
-    for (int u = 0; u < MV_UNROLL; ++u) {
+    for (int u = 0; u < MI_UNROLL; ++u) {
       const int i = i0 + u * STEP + r;
-      if (src[u] >= 0 && !(IN_PLACE && src[u] == i))
-        *reinterpret_cast<uint4*>(a.dst + row_at(dt[i >> 4], i & 15) + ((c ^ (i & 7)) << 3)) = v[u];
+      src[u] = i < len ? kept[i] : -1;
+      if (src[u] == i) src[u] = -1;  // the row stays where it is
+    }
+#pragma unroll
+    for (int u = 0; u < MI_UNROLL; ++u)
+      if (src[u] >= 0) v[u] = *reinterpret_cast<const uint4*>(a.pool + row_at(bt[src[u] >> 4], src[u] & 15) + ((c ^ (src[u] & 7)) << 3));
+    __syncthreads();  // the whole batch is read before any of it is written
+#pragma unroll
+    for (int u = 0; u < MI_UNROLL; ++u) {
+      const int i = i0 + u * STEP + r;
+      if (src[u] >= 0) *reinterpret_cast<uint4*>(a.dst + row_at(bt[i >> 4], i & 15) + ((c ^ (i & 7)) << 3)) = v[u];
     }
   }
 }
 
 template <int D>
 int launch_move(const EvictArgs& a, cudaStream_t st) {
-  constexpr int BATCH = MV_THREADS / (D / 8) * MV_UNROLL;
-  if (a.in_place) {
-    HYP_CUDA_TRY(launch_pdl<2>(evict_move_kernel<D, true>, dim3(1, 2 * a.Hkv, a.n_seqs), dim3(MV_THREADS), (size_t)0, st, a, a.n_keep));
-  } else {
-    HYP_CUDA_TRY(launch_pdl<2>(evict_move_kernel<D, false>, dim3((a.n_keep + BATCH - 1) / BATCH, 2 * a.Hkv, a.n_seqs),
-                               dim3(MV_THREADS), (size_t)0, st, a, BATCH));
-  }
+  if (a.in_place)
+    HYP_CUDA_TRY(launch_pdl<2>(evict_move_in_place_kernel<D>, dim3(2 * a.Hkv, a.n_seqs), dim3(MI_THREADS), (size_t)0, st, a));
+  else
+    HYP_CUDA_TRY(launch_pdl<2>(evict_move_kernel<D>, dim3((a.n_keep + MV_ROWS - 1) / MV_ROWS, 2 * a.Hkv, a.n_seqs), dim3(MV_THREADS),
+                               (size_t)0, st, a));
   return 1;
 }
 
@@ -265,10 +287,15 @@ int launch_move(const EvictArgs& a, cudaStream_t st) {
 
 int launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
   if (a.D != 64 && a.D != 128) return HYP_EINVAL;
-  if (a.table_stride * 16 - a.n_sink - a.n_recent <= EV_NPT * EV_THREADS)
-    HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<true>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), (size_t)0, st, a));
-  else
+  const long long most = (long long)a.table_stride * 16 - a.n_sink - a.n_recent;  // candidates a sequence can have
+  if (most <= EV_STRIPES * EV_THREADS) {
+    const size_t smem = most > 0 ? (size_t)most * sizeof(float) : 0;
+    const int rc = allow_smem<evict_select_kernel<true>>(EV_STRIPES * EV_THREADS * (int)sizeof(float));
+    if (rc) return rc;
+    HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<true>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), smem, st, a));
+  } else {
     HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<false>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), (size_t)0, st, a));
+  }
   const int rc = a.D == 128 ? launch_move<128>(a, st) : launch_move<64>(a, st);
   return rc < 0 ? rc : 1 + rc;
 }
