@@ -46,12 +46,10 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* tmp) {
 
 // One key into the histogram.  All lanes call; where the whole warp has the same bin, one lane adds for all.
 __device__ __forceinline__ void count_bin(uint32_t* hist, bool valid, uint32_t bin) {
-  const uint32_t mask = __ballot_sync(0xffffffffu, valid);
-  if (!mask) return;
-  const int leader = __ffs(mask) - 1;
-  const uint32_t first = __shfl_sync(0xffffffffu, bin, leader);
-  if (__ballot_sync(0xffffffffu, valid && bin == first) == mask) {
-    if ((int)(threadIdx.x & 31) == leader) atomicAdd(hist + first, __popc(mask));
+  if (!valid) bin = ~0u;
+  const uint32_t first = __shfl_sync(0xffffffffu, bin, 0);
+  if (__all_sync(0xffffffffu, bin == first)) {
+    if (valid && (threadIdx.x & 31) == 0) atomicAdd(hist + first, 32u);
   } else if (valid) {
     atomicAdd(hist + bin, 1u);
   }
@@ -125,21 +123,19 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   if (STAGED) {
     // (stripe, warp) counts, greater in the low half, equal in the high half: at most 32768 each
     uint32_t* cnt = hist;
-    for (int i = 0; i < EV_STRIPES; ++i) {
-      uint32_t c = 0;
-      if (i * EV_THREADS < n && m > 0) {
-        const int k = i * EV_THREADS + tid;
-        const uint32_t key = k < n ? weight_key(sw[k]) & known : 0u;
-        c = __popc(__ballot_sync(0xffffffffu, k < n && key > thr)) | (__popc(__ballot_sync(0xffffffffu, k < n && key == thr)) << 16);
-      }
-      if (lane == 0) cnt[i * EV_WARPS + warp] = c;
+    const int stripes = m > 0 ? (n + EV_THREADS - 1) / EV_THREADS : 0;
+    for (int i = 0; i < stripes; ++i) {
+      const int k = i * EV_THREADS + tid;
+      const uint32_t key = k < n ? weight_key(sw[k]) & known : 0u;
+      const uint32_t mg = __ballot_sync(0xffffffffu, k < n && key > thr), me = __ballot_sync(0xffffffffu, k < n && key == thr);
+      if (lane == 0) cnt[i * EV_WARPS + warp] = __popc(mg) | (__popc(me) << 16);
     }
     __syncthreads();  // all weights have been read: from here on they may be overwritten
-    const uint32_t mine = cnt[tid];
+    const uint32_t mine = tid < stripes * EV_WARPS ? cnt[tid] : 0u;
     const uint32_t upto = block_scan(mine, tmp);
     cnt[tid] = upto - mine;
     __syncthreads();
-    for (int i = 0; i * EV_THREADS < n && m > 0; ++i) {
+    for (int i = 0; i < stripes; ++i) {
       const int k = i * EV_THREADS + tid;
       const float x = k < n ? sw[k] : 0.f;
       const uint32_t key = weight_key(x) & known;
