@@ -274,7 +274,7 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
   const int n_tiles = wk.n_tiles;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 16; ++i) mbar_init(bar0 + 8u * i, (i == 12 || i == 13) ? 128u : 1u);  // p_full: every softmax thread
+    for (int i = 0; i < 16; ++i) mbar_init(bar0 + 8u * i, (i == 12 || i == 13) ? 4u : 1u);  // p_full: every softmax warp
     sh.abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -416,7 +416,8 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       tc_fence_before();
-      mbar_arrive(p_full + 8 * b);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 8 * b);  // one arrival a warp: 128 on one word take their time
     }
     // the last value product (a commit follows every earlier one too)
     if (ok && !mbar_wait(o_done + 8 * ((n_tiles - 1) & 1), (uint32_t)(((n_tiles - 1) >> 1) & 1), abort_flag)) ok = false;
