@@ -158,9 +158,10 @@ __device__ __forceinline__ bool prefix_cut_fixed(const SharedArgs& a, int T, Pre
   c.splits = a.prefix_splits;
   c.split = blockIdx.x % c.splits;
   c.kvh = blockIdx.x / c.splits % a.own.Hkv;
-  at_locate(a.cu_group, a.n_groups, T, blockIdx.x / (c.splits * a.own.Hkv), c.group, c.first, c.q0, c.len);
+  int plen, none;
+  at_locate(a.cu_group, a.prefix_lens, nullptr, a.n_groups, T, blockIdx.x / (c.splits * a.own.Hkv), c.group, c.first, c.q0, c.len, plen, none);
   if (c.group < 0) return false;
-  c.plen = min(max(a.prefix_lens[c.group], 0), a.prefix_stride * PG_PT);
+  c.plen = min(max(plen, 0), a.prefix_stride * PG_PT);
   c.per = ((c.plen + AT_KEYS - 1) / AT_KEYS + c.splits - 1) / c.splits;
   return true;
 }
@@ -171,10 +172,14 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
   extern __shared__ __align__(128) uint8_t sh_smem_raw[];
   __shared__ TileShared ts;
   pdl_wait();
-  pdl_trigger();
+  tile_setup(ts);
+  pdl_trigger();  // only now: a kernel that starts early must not find tensor memory free that this CTA still has to take
   constexpr int T = AT_ROWS / G;
   PrefixCut cut;
-  if (!(a.even ? prefix_cut_even(a, T, cut) : prefix_cut_fixed(a, T, cut))) return;
+  if (!(a.even ? prefix_cut_even(a, T, cut) : prefix_cut_fixed(a, T, cut))) {
+    tile_release(ts);
+    return;
+  }
   const int kvh = cut.kvh, split = cut.split, plen = cut.plen;
   const int all_tiles = (plen + AT_KEYS - 1) / AT_KEYS;
   TileWork wk;
@@ -193,7 +198,10 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     const int t = threadIdx.x / G, gh = threadIdx.x % G;
     if (threadIdx.x < AT_ROWS && t < wk.rows) *reinterpret_cast<float2*>(a.own.ml + (slot_of(t, gh) + s - split) * 2) = make_float2(PG_NEG, 0.f);
   }
-  if (wk.n_tiles == 0) return;  // the whole CTA
+  if (wk.n_tiles == 0) {  // the whole CTA
+    tile_release(ts);
+    return;
+  }
   tile_body<D, false, false>(
       &tm_q, &tm_kv, sh_smem_raw, ts, wk, G, a.own.Hkv, 0.f, nullptr, a.own.err,
       [&](int, int& pos) {
@@ -215,6 +223,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         at_send_row(a.own.acc + row * D, stage, D * 4, valid);
         if (valid) *reinterpret_cast<float2*>(a.own.ml + row * 2) = make_float2(m_ref, l);
       });
+  tile_release(ts);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -239,16 +248,20 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   extern __shared__ __align__(128) uint8_t pm_smem[];
   __shared__ TileShared ts;
   pdl_wait();
-  pdl_trigger();
+  tile_setup(ts);
+  pdl_trigger();  // only now: a kernel that starts early must not find tensor memory free that this CTA still has to take
   const int T = AT_ROWS / a.G;
   const int kvh = blockIdx.x;  // heads vary fastest: every head's heaviest tile is scheduled before any lighter one
-  int seq, first, q0, len;
+  int seq, first, q0, len, ctx, pre;
   // the last tiles of a sequence see the most keys: they go first
-  at_locate(a.cu_q, a.n_seqs, T, (int)gridDim.y - 1 - (int)blockIdx.y, seq, first, q0, len);
-  if (seq < 0) return;
-  const int ctx = max(a.ctx[seq], 0);
+  at_locate(a.cu_q, a.ctx, a.prefix, a.n_seqs, T, (int)gridDim.y - 1 - (int)blockIdx.y, seq, first, q0, len, ctx, pre);
+  if (seq < 0) {
+    tile_release(ts);
+    return;
+  }
+  ctx = max(ctx, 0);
   const int have = min(ctx + len, a.table_stride * PG_PT);  // tokens in the cache, the new rows included
-  const int pre = a.prefix ? min(max(a.prefix[seq], 0), have) : 0;
+  pre = min(max(pre, 0), have);
   const int window = a.window > 0 ? a.window : 0x40000000;
   TileWork wk;
   wk.head0 = kvh * a.G;
@@ -261,6 +274,10 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   wk.n_first = (pre + AT_KEYS - 1) / AT_KEYS;
   wk.second = max(lo / AT_KEYS, wk.n_first);
   wk.n_tiles = wk.n_first + max((hi + AT_KEYS - 1) / AT_KEYS - wk.second, 0);
+  if (wk.n_tiles == 0) {  // only where the table is too short for the lengths it comes with
+    tile_release(ts);
+    return;
+  }
   tile_body<D, CAP, BIAS>(
       &tm_q, &tm_kv, pm_smem, ts, wk, a.G, a.Hkv, a.softcap, a.slopes, a.err,
       [&](int t, int& pos) {
@@ -285,6 +302,7 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
         at_send_row(orow, stage, D * 2, valid);
       });
+  tile_release(ts);
 }
 
 PagedArgs paged_args(const CacheView& c, const __half* q, long long q_stride, float* scratch, int n_slots, int slot0, int* err) {

@@ -148,7 +148,7 @@ __device__ __forceinline__ void at_send_row(void* dst, uint32_t src, uint32_t by
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (valid) asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the row has left shared memory
 }
 
 // Softmax of one 64-key tile for one query row: see the head of the file.  A score enters the exponent as x * scale with
@@ -254,7 +254,34 @@ __device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
   return true;
 }
 
-// The whole CTA (192 threads) calls this.  `store(row, head_in_group, valid, m_ref, l, stage, load)` is called by the
+// Barriers and tensor memory; the whole CTA, behind its wait for the preceding kernel (tensor memory taken before it could be
+// what a CTA of that kernel is waiting for).
+__device__ __forceinline__ void tile_setup(TileShared& sh) {
+  if (threadIdx.x == 0) {
+    // p_full (12, 13): every softmax warp
+    for (int i = 0; i < 16; ++i) mbar_init(smem_u32(sh.bars) + 8u * i, (i == 12 || i == 13) ? 4u : 1u);
+    sh.abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x >> 5 == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_slot)), "r"(256));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+}
+// The whole CTA, last.
+__device__ __forceinline__ void tile_release(TileShared& sh) {
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x >> 5 == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem_slot), "r"(256));
+  }
+}
+
+// The whole CTA (192 threads) calls this between the two.  `store(row, head_in_group, valid, m_ref, l, stage, load)` is called by the
 // softmax threads at the end: load(c, v, w) reads columns c .. c + 31 of the thread's O row from tensor memory (all lanes call
 // it), stage is the thread's row of D floats in shared memory.
 template <int D, bool CAP, bool BIAS, typename RowFn, typename StoreFn>
@@ -272,19 +299,6 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
   volatile int* abort_flag = &sh.abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n_tiles = wk.n_tiles;
-
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < 16; ++i) mbar_init(bar0 + 8u * i, (i == 12 || i == 13) ? 4u : 1u);  // p_full: every softmax warp
-    sh.abort_word = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_slot)), "r"(256));
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
   // columns 0-63 / 64-127: the two score buffers (P over the upper half of each); from 128: O
   const uint32_t tmem_s = sh.tmem_slot, tmem_o = sh.tmem_slot + 128u;
   auto key_tile = [&](int j) { return j < wk.n_first ? j : j - wk.n_first + wk.second; };
@@ -435,27 +449,23 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
       atomicCAS(err, 0, 24);
     }
   }
-
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 1) {
-    tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem_slot), "r"(256));
-  }
 }
 
 static_assert(AT_ROWS * (128 * 4 + 16) <= AtGeom<128>::SMEM - 1024 && AT_ROWS * (64 * 4 + 16) <= AtGeom<64>::SMEM - 1024, "rows to be stored");
 
 // Which row tile of `tile_rows` rows is tile t?  Sets run from cu[i] to cu[i + 1] and are cut into tiles one by one.
-// Every warp finds it for itself, 32 sets at a time; set = -1: no such tile.
-__device__ __forceinline__ void at_locate(const int32_t* cu, int n_sets, int tile_rows, int t, int& set, int& first, int& q0, int& len) {
+// Every warp finds it for itself, 32 sets at a time; set = -1: no such tile.  a[set] and b[set] (b may be null: 0) are fetched
+// beside the bounds, not behind them.
+__device__ __forceinline__ void at_locate(const int32_t* cu, const int32_t* a, const int32_t* b, int n_sets, int tile_rows, int t, int& set,
+                                          int& first, int& q0, int& len, int& a_set, int& b_set) {
   const int lane = threadIdx.x & 31;
   set = -1;
-  first = q0 = len = 0;
+  first = q0 = len = a_set = b_set = 0;
   int before = 0;
   for (int i0 = 0; i0 < n_sets; i0 += 32) {
     const int i = i0 + lane;
     const int c0 = i < n_sets ? cu[i] : 0;
+    const int a0 = i < n_sets ? a[i] : 0, b0 = b && i < n_sets ? b[i] : 0;
     const int my_len = i < n_sets ? max(cu[i + 1] - c0, 0) : 0;
     const int nt = (my_len + tile_rows - 1) / tile_rows;
     int incl = nt;
@@ -469,6 +479,8 @@ __device__ __forceinline__ void at_locate(const int32_t* cu, int n_sets, int til
       const int src = __ffs(hit) - 1;
       set = i0 + src;
       first = __shfl_sync(0xffffffffu, c0, src);
+      a_set = __shfl_sync(0xffffffffu, a0, src);
+      b_set = __shfl_sync(0xffffffffu, b0, src);
       len = __shfl_sync(0xffffffffu, my_len, src);
       q0 = (t - before - __shfl_sync(0xffffffffu, incl - nt, src)) * tile_rows;
       return;
