@@ -31,7 +31,7 @@ struct AtGeom {
   static constexpr int SMEM = Q_BYTES + 4 * STAGE + 1024;        // queries, keys[2], values[2], alignment
 };
 
-// What one CTA works on.  Key tile j of the walk is tile j of the sequence for j < n_first, else j - n_first + second.
+// What one CTA works on: key tiles 0 .. n_first - 1 of the sequence, then n_tiles - n_first from `second` on.
 struct TileWork {
   int head0;                  // first query head of the group: kvh * G
   int kvh;
@@ -48,6 +48,7 @@ struct TileRow {
 struct TileScore {
   float scale;                // x -> exponent (base 2)
   float to_tanh;              // CAP: raw product -> argument of the tanh
+  float tanh_c[4];            // CAP: see tanh2_small
   float ratio;                // BIAS: this thread's slope, in units of x
 };
 
@@ -122,18 +123,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ float max3abs(float m, float a, float b) { return max3(m, fabsf(a), fabsf(b)); }
 
-// tanh x for |x| <= 0.75 as x times a polynomial in x^2 (five coefficients, least absolute error of tanh x over the range,
-// fitted by reweighted least squares): off by 1.9e-7 at most.  Runs on the packed FMA path; the exact form needs two
-// of the sixteen special-function lanes' operations a score, which alone would take longer than both matrix products.
-constexpr float TANH_RANGE = 0.75f;
-__device__ __forceinline__ f32x2 tanh2_small(f32x2 x) {
-  const f32x2 u = mul2(x, x);
-  f32x2 p = fma2(u, pk2(0.012318827410786189f, 0.012318827410786189f), pk2(-0.049280441976393266f, -0.049280441976393266f));
-  p = fma2(u, p, pk2(0.13226091419102248f, 0.13226091419102248f));
-  p = fma2(u, p, pk2(-0.3332307645376031f, -0.3332307645376031f));
-  p = fma2(u, p, pk2(0.9999972283092571f, 0.9999972283092571f));
-  return mul2(x, p);
+// tanh x for |x| <= 0.5 as x times a polynomial in x^2 (four coefficients, least absolute error of tanh x over the range,
+// fitted by reweighted least squares): off by 1.3e-7 at most.  The argument's factor (raw product -> x) is multiplied into
+// the coefficients: c[i] = TANH_Ci * factor^(2 i + 1).  Runs on the packed FMA path; the exact form needs two of the
+// sixteen special-function lanes' operations a score, which alone would take longer than both matrix products.
+constexpr float TANH_RANGE = 0.5f;
+constexpr float TANH_C0 = 0.9999976761797865f, TANH_C1 = -0.33320655167817165f, TANH_C2 = 0.13145145181299145f, TANH_C3 = -0.04337247117084689f;
+__device__ __forceinline__ f32x2 tanh2_small(f32x2 raw, const float (&c)[4]) {
+  const f32x2 u = mul2(raw, raw);
+  f32x2 p = fma2(u, pk2(c[3], c[3]), pk2(c[2], c[2]));
+  p = fma2(u, p, pk2(c[1], c[1]));
+  p = fma2(u, p, pk2(c[0], c[0]));
+  return mul2(raw, p);
 }
+__device__ __forceinline__ f32x2 abs2(f32x2 v) { return v & 0x7fffffff7fffffffull; }
 __device__ __forceinline__ float tanh_exact(float x) {  // 1 - 2 / (1 + e^(2x)); see softcap_log2
   return fmaf(-2.f, rcp_approx(1.f + ex2_approx(2.f * PG_LOG2E * x)), 1.f);
 }
@@ -151,14 +154,73 @@ __device__ __forceinline__ void at_send_row(void* dst, uint32_t src, uint32_t by
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the row has left shared memory
 }
 
+// The rare paths - moving the reference maximum, and capped scores beyond the polynomial's range - are functions of their
+// own: inlined, the second one alone cost the tiles that never take it 20 % (77 against 64 us, 2048 tokens).
+
+// Rescales the warp's rows of O by corr (one factor a lane) once every earlier value product has drained.
+template <int D>
+__device__ __noinline__ bool at_rescale(uint32_t tmem_o_row, float corr, uint32_t o_prev, uint32_t o_parity, volatile int* abort_flag) {
+  if (!__all_sync(0xffffffffu, mbar_wait(o_prev, o_parity, abort_flag))) return false;
+  tc_fence_after();
+#pragma unroll 2
+  for (int c = 0; c < D; c += 16) {
+    uint32_t v[16];
+    tmem_ld16(tmem_o_row + c, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
+    at_tmem_st16(tmem_o_row + c, v);
+  }
+  return true;
+}
+
+// Bit i of the 64: key0 + i is visible to the row.
+struct TileMask {
+  uint32_t lo, hi;
+};
+__device__ __forceinline__ TileMask tile_mask(const TileRow& rw, int key0) {
+  auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; };
+  const unsigned long long vis = (below(rw.hi + 1 - key0) & ~below(rw.lo - key0)) | below(rw.pre - key0);
+  return TileMask{(uint32_t)vis, (uint32_t)(vis >> 32)};
+}
+
+// The largest score (in log2 units) that a row sees in a tile with a distance bias.
+template <int D, bool CAP>
+__device__ __noinline__ float at_true_max(uint32_t tmem_row, int key0, int pos, TileMask mask, TileScore sc) {
+  float mx = PG_NEG;
+#pragma unroll 1
+  for (int c = 0; c < AT_KEYS; c += 16) {
+    uint32_t v[16];
+    tmem_ld16(tmem_row + c, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x = __uint_as_float(v[i]);
+      if (CAP) x = tanh_exact(x * sc.to_tanh);
+      x = fmaf(-sc.ratio, fabsf((float)(key0 + c + i - pos)), x);
+      mx = (c < 32 ? mask.lo : mask.hi) >> ((c + i) & 31) & 1u ? fmaxf(mx, x) : mx;
+    }
+  }
+  return mx * sc.scale;
+}
+
+struct SoftmaxState {
+  float m_ref, l;
+  bool ok;
+};
+template <int D, bool BIAS>
+__device__ __noinline__ SoftmaxState at_softmax_exact(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, TileRow rw,
+                                                      TileScore sc, int j, uint32_t o_prev, uint32_t o_parity,
+                                                      volatile int* abort_flag, SoftmaxState st);
+
 // Softmax of one 64-key tile for one query row: see the head of the file.  A score enters the exponent as x * scale with
 // x the raw product (scale = log2(e) / sqrt(D)) or, capped, the tanh (scale = softcap * log2(e)); the distance bias is
 // added to x as ratio * distance, ratio = slope * log2(e) / scale.  What a row may not see becomes -1e30, which the exponent
 // turns into 0 as long as the reference stays above -1e20.
-template <int D, bool CAP, bool BIAS, bool MASKED>
-__device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, const TileRow& rw,
-                                           const TileScore& sc, int j, uint32_t o_prev, uint32_t o_parity,
-                                           volatile int* abort_flag, float& m_ref, float& l) {
+template <int D, bool CAP, bool BIAS, bool MASKED, bool EXACT>
+__device__ __forceinline__ void at_softmax(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, const TileRow& rw,
+                                           const TileScore& sc, int j, uint32_t o_prev, uint32_t o_parity, volatile int* abort_flag,
+                                           SoftmaxState& st) {
   uint32_t sv[AT_KEYS];
 #pragma unroll
   for (int c = 0; c < AT_KEYS; c += 16) tmem_ld16(tmem_sb + lane_off + c, reinterpret_cast<uint32_t(&)[16]>(sv[c]));
@@ -166,71 +228,74 @@ __device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
   float x[AT_KEYS];
 #pragma unroll
   for (int i = 0; i < AT_KEYS; ++i) x[i] = __uint_as_float(sv[i]);
+  const TileMask mask = MASKED ? tile_mask(rw, key0) : TileMask{~0u, ~0u};
+  auto seen = [&](int i, float v) { return !MASKED || ((i < 32 ? mask.lo : mask.hi) & (1u << (i & 31))) ? v : PG_NEG; };
+  // The largest product bounds the largest score: the cap keeps the order, and the bias of the tile is at most that of its
+  // nearest (slope < 0: farthest) key.  So the cap, the bias and the second mask run beside the exponentials, which set the
+  // pace, and not in front of them.  One vote asks for everything that is rare: a bound that is too high for the
+  // reference, or a product beyond the polynomial's range.
+  float m4[4] = {PG_NEG, PG_NEG, PG_NEG, PG_NEG}, a4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < AT_KEYS; i += 2) {
+    m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], seen(i, x[i]), seen(i + 1, x[i + 1]));
+    if (CAP && !EXACT) a4[(i >> 1) & 3] = max3abs(a4[(i >> 1) & 3], x[i], x[i + 1]);
+  }
+  float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
+  bool wide = false;
+  if (CAP && !EXACT) {
+    // NaN (garbage behind the end of a sequence) compares false here and takes the exact form; it is masked there
+    wide = !(max3(fmaxf(a4[0], a4[1]), a4[2], a4[3]) * sc.to_tanh <= TANH_RANGE);
+    float top, same;
+    up2(tanh2_small(pk2(mx, mx), sc.tanh_c), top, same);
+    mx = mx > PG_NEG ? top : mx;
+  }
+  if (CAP && EXACT) mx = mx > PG_NEG ? tanh_exact(mx * sc.to_tanh) : mx;
+  if (BIAS) {
+    const int near = max(max(key0 - pos, pos - (key0 + AT_KEYS - 1)), 0), far = max(abs(key0 - pos), abs(key0 + AT_KEYS - 1 - pos));
+    mx += fmaxf(-sc.ratio * (float)near, -sc.ratio * (float)far);
+  }
+  mx *= sc.scale;  // scale > 0
+  if (__any_sync(0xffffffffu, mx > st.m_ref + 8.f || wide)) {
+    if (CAP && !EXACT && __any_sync(0xffffffffu, wide)) {
+      st = at_softmax_exact<D, BIAS>(tmem_sb, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, st);
+      return;
+    }
+    if (BIAS) mx = at_true_max<D, CAP>(tmem_sb + lane_off, key0, pos, MASKED ? mask : TileMask{~0u, ~0u}, sc);
+    if (!BIAS || __any_sync(0xffffffffu, mx > st.m_ref + 8.f)) {
+      const float new_ref = fmaxf(st.m_ref, mx), corr = ex2_approx(st.m_ref - new_ref);
+      if (j > 0) {
+        st.ok = at_rescale<D>(tmem_o + lane_off, corr, o_prev, o_parity, abort_flag);
+        if (!st.ok) return;
+        st.l *= corr;
+      }
+      st.m_ref = new_ref;
+    }
+  }
   if (CAP) {
-    float a4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < AT_KEYS; i += 2) a4[(i >> 1) & 3] = max3abs(a4[(i >> 1) & 3], x[i], x[i + 1]);
-    // NaN (garbage behind the end of a sequence) compares false here and takes the exact form; it is masked below
-    const bool small = max3(fmaxf(a4[0], a4[1]), a4[2], a4[3]) * sc.to_tanh <= TANH_RANGE;
-    if (__all_sync(0xffffffffu, small)) {
-      const f32x2 k = pk2(sc.to_tanh, sc.to_tanh);
-#pragma unroll
-      for (int i = 0; i < AT_KEYS; i += 2) up2(tanh2_small(mul2(pk2(x[i], x[i + 1]), k)), x[i], x[i + 1]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < AT_KEYS; ++i) x[i] = tanh_exact(x[i] * sc.to_tanh);
+    for (int i = 0; i < AT_KEYS; i += 2) {
+      if (EXACT) {
+        x[i] = tanh_exact(x[i] * sc.to_tanh);
+        x[i + 1] = tanh_exact(x[i + 1] * sc.to_tanh);
+      } else {
+        up2(tanh2_small(pk2(x[i], x[i + 1]), sc.tanh_c), x[i], x[i + 1]);
+      }
     }
   }
   if (BIAS) {
-    if (MASKED) {
+    f32x2 dist = pk2((float)(key0 - pos), (float)(key0 + 1 - pos));
+    const f32x2 r2 = pk2(-sc.ratio, -sc.ratio), two = pk2(2.f, 2.f);
 #pragma unroll
-      for (int i = 0; i < AT_KEYS; ++i) x[i] = fmaf(-sc.ratio, fabsf((float)(key0 + i - pos)), x[i]);
-    } else if (key0 + AT_KEYS - 1 <= pos) {  // every key behind the query: the distance is pos - key
-      f32x2 dist = pk2((float)(key0 - pos), (float)(key0 + 1 - pos));
-      const f32x2 r2 = pk2(sc.ratio, sc.ratio), two = pk2(2.f, 2.f);
-#pragma unroll
-      for (int i = 0; i < AT_KEYS; i += 2) {
-        up2(fma2(r2, dist, pk2(x[i], x[i + 1])), x[i], x[i + 1]);
-        dist = add2(dist, two);  // whole numbers: exact
-      }
-    } else {  // inside a prefix, some keys ahead of the query
-#pragma unroll
-      for (int i = 0; i < AT_KEYS; ++i) x[i] = fmaf(-sc.ratio, fabsf((float)(key0 + i - pos)), x[i]);
+    for (int i = 0; i < AT_KEYS; i += 2) {
+      up2(fma2(r2, abs2(dist), pk2(x[i], x[i + 1])), x[i], x[i + 1]);
+      dist = add2(dist, two);  // whole numbers: exact
     }
   }
   if (MASKED) {
-    // bit i: key0 + i is visible
-    auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; };
-    const unsigned long long vis = (below(rw.hi + 1 - key0) & ~below(rw.lo - key0)) | below(rw.pre - key0);
-    const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
 #pragma unroll
-    for (int i = 0; i < AT_KEYS; ++i) x[i] = ((i < 32 ? v0 : v1) & (1u << (i & 31))) ? x[i] : PG_NEG;
+    for (int i = 0; i < AT_KEYS; ++i) x[i] = seen(i, x[i]);
   }
-  float m4[4] = {PG_NEG, PG_NEG, PG_NEG, PG_NEG};
-#pragma unroll
-  for (int i = 0; i < AT_KEYS; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], x[i], x[i + 1]);
-  const float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]) * sc.scale;  // scale > 0
-  if (__any_sync(0xffffffffu, mx > m_ref + 8.f)) {
-    const float new_ref = fmaxf(m_ref, mx);
-    if (j > 0) {
-      // O must hold every earlier tile before it is scaled
-      if (!__all_sync(0xffffffffu, mbar_wait(o_prev, o_parity, abort_flag))) return false;
-      tc_fence_after();
-      const float corr = ex2_approx(m_ref - new_ref);
-      l *= corr;
-#pragma unroll
-      for (int c = 0; c < D; c += 16) {
-        uint32_t v[16];
-        tmem_ld16(tmem_o + lane_off + c, v);
-        tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
-        at_tmem_st16(tmem_o + lane_off + c, v);
-      }
-    }
-    m_ref = new_ref;
-  }
-  const float neg_ref = -fmaxf(m_ref, -1e20f);
+  const float neg_ref = -fmaxf(st.m_ref, -1e20f);
   const f32x2 s2 = pk2(sc.scale, sc.scale), n2 = pk2(neg_ref, neg_ref);
   f32x2 l2[2] = {0ull, 0ull};
 #pragma unroll
@@ -249,9 +314,15 @@ __device__ __forceinline__ bool at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
   }
   float l0, l1;
   up2(add2(l2[0], l2[1]), l0, l1);
-  l += l0 + l1;
+  st.l += l0 + l1;
   at_tmem_st_wait();
-  return true;
+}
+template <int D, bool BIAS>
+__device__ __noinline__ SoftmaxState at_softmax_exact(uint32_t tmem_sb, uint32_t tmem_o, uint32_t lane_off, int key0, int pos, TileRow rw,
+                                                      TileScore sc, int j, uint32_t o_prev, uint32_t o_parity,
+                                                      volatile int* abort_flag, SoftmaxState st) {
+  at_softmax<D, true, BIAS, true, true>(tmem_sb, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, st);
+  return st;
 }
 
 // Barriers and tensor memory; the whole CTA, behind its wait for the preceding kernel (tensor memory taken before it could be
@@ -301,7 +372,12 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
   const int n_tiles = wk.n_tiles;
   // columns 0-63 / 64-127: the two score buffers (P over the upper half of each); from 128: O
   const uint32_t tmem_s = sh.tmem_slot, tmem_o = sh.tmem_slot + 128u;
-  auto key_tile = [&](int j) { return j < wk.n_first ? j : j - wk.n_first + wk.second; };
+  // The walk goes from the last tile to the first: with a distance bias the near keys set the reference maximum at once (the
+  // other way round it moved in nearly every tile).
+  auto key_tile = [&](int j) {
+    const int i = n_tiles - 1 - j;
+    return i < wk.n_first ? i : i - wk.n_first + wk.second;
+  };
 
   if (warp == 0) {
     // ---------------- TMA producer: one box per lane and tile ----------------
@@ -395,13 +471,18 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
     const bool warp_idle = (32 * q) / G >= wk.rows;  // no row of this warp exists: its weights are never used
     int pos;
     const TileRow rw = row_fn(min(t, wk.rows - 1), pos);  // rows past the end are clamped: computed, never stored
-    TileScore sc{rsqrtf((float)D) * PG_LOG2E, 0.f, 0.f};
+    TileScore sc{rsqrtf((float)D) * PG_LOG2E, 0.f, {0.f, 0.f, 0.f, 0.f}, 0.f};
     if (CAP) {
       sc.to_tanh = rsqrtf((float)D) / softcap;
+      const float f = sc.to_tanh, f2 = f * f;
+      sc.tanh_c[0] = TANH_C0 * f;
+      sc.tanh_c[1] = TANH_C1 * f * f2;
+      sc.tanh_c[2] = TANH_C2 * f * f2 * f2;
+      sc.tanh_c[3] = TANH_C3 * f * f2 * f2 * f2;
       sc.scale = softcap * PG_LOG2E;
     }
     if (BIAS) sc.ratio = slopes[wk.head0 + gh] * PG_LOG2E / sc.scale;
-    float m_ref = PG_NEG, l = 0.f;
+    SoftmaxState st{PG_NEG, 0.f, true};
     bool ok = true;
     for (int j = 0; j < n_tiles && ok; ++j) {
       const uint32_t b = (uint32_t)(j & 1);
@@ -414,9 +495,10 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
         const uint32_t o_prev = o_done + 8 * (b ^ 1), o_parity = (uint32_t)(((j - 1) >> 1) & 1);
         const bool whole = (key0 >= rw.lo && key0 + AT_KEYS - 1 <= rw.hi) || key0 + AT_KEYS <= rw.pre;
         if (__any_sync(0xffffffffu, !whole))
-          ok = at_softmax<D, CAP, BIAS, true>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, m_ref, l);
+          at_softmax<D, CAP, BIAS, true, false>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, st);
         else
-          ok = at_softmax<D, CAP, BIAS, false>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, m_ref, l);
+          at_softmax<D, CAP, BIAS, false, false>(tmem_s + 64u * b, tmem_o, lane_off, key0, pos, rw, sc, j, o_prev, o_parity, abort_flag, st);
+        ok = st.ok;
         if (!ok) break;
       }
       const int left = wk.key_end - key_tile(j) * AT_KEYS;
@@ -439,7 +521,7 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
     tc_fence_after();
     if (ok && !warp_idle)
       // every product has drained: the operands' space is free
-      store(min(t, wk.rows - 1), gh, valid, m_ref, l, base + (uint32_t)r * (D * 4 + 16), [&](int c, uint32_t (&v)[16], uint32_t (&w)[16]) {
+      store(min(t, wk.rows - 1), gh, valid, st.m_ref, st.l, base + (uint32_t)r * (D * 4 + 16), [&](int c, uint32_t (&v)[16], uint32_t (&w)[16]) {
         tmem_ld16(tmem_o + lane_off + c, v);
         tmem_ld16(tmem_o + lane_off + c + 16, w);
         tmem_ld_wait();
