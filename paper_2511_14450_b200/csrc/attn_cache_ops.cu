@@ -95,7 +95,9 @@ scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// shared prefix: the prefixes on the row-tile body, the sequences' own pages on the streaming kernel, a join.
+// shared prefix: one launch holds the CTAs of both parts, a second one joins the partial rows.  The prefixes' row tiles go
+// first, the sequences' own pages stream through the CTA slots that they leave.  (As two launches, one after the other: 23.7
+// instead of 20.2 us for 32 sequences behind 2048 tokens, the same for 128 behind five prefixes to 8192.)
 // ---------------------------------------------------------------------------------------------
 struct SharedArgs {
   PagedArgs own;              // slots prefix_splits ..
@@ -103,7 +105,7 @@ struct SharedArgs {
   const int32_t* prefix_table;
   int prefix_stride;
   const int32_t* prefix_lens;
-  int n_groups, prefix_splits, own_splits;
+  int n_groups, prefix_splits, own_splits, prefix_ctas;
   bool even;                  // see prefix_cut_even
 };
 
@@ -111,7 +113,7 @@ struct SharedArgs {
 struct PrefixCut {
   int group, first, q0, len, plen, split, splits, per, kvh;
 };
-// Up to 32 groups, one lane each: the CTAs of the grid (two per SM) are handed out so that all get about the same number of
+// Up to 32 groups, one lane each: the prefix CTAs (at most two per SM) are handed out so that all get about the same number of
 // key tiles, whatever the lengths of the prefixes and the sizes of the groups.  (A fixed number of splits made 1.3
 // waves of unequal CTAs of five prefixes of 4096 to 8192 tokens: 53 us.)
 __device__ __forceinline__ bool prefix_cut_even(const SharedArgs& a, int T, PrefixCut& c) {
@@ -122,7 +124,7 @@ __device__ __forceinline__ bool prefix_cut_even(const SharedArgs& a, int T, Pref
   const int units = (max(c1 - c0, 0) + T - 1) / T * a.own.Hkv, tiles = (plen + AT_KEYS - 1) / AT_KEYS;
   // lane i tries `per` = low + i * step: low is what an even share without rounding would be
   const int all = __reduce_add_sync(0xffffffffu, units * tiles), most = max(__reduce_max_sync(0xffffffffu, tiles), 1);
-  int low = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+  int low = max((all + a.prefix_ctas - 1) / a.prefix_ctas, 1);
   low = max(low, (most + a.prefix_splits - 1) / a.prefix_splits);  // no prefix in more shares than there are slots
   const int step = max(low / 16, 1), mine = min(low + lane * step, most);
   int total = 0;
@@ -130,7 +132,7 @@ __device__ __forceinline__ bool prefix_cut_even(const SharedArgs& a, int T, Pref
     const int ug = __shfl_sync(0xffffffffu, units, g), tg = __shfl_sync(0xffffffffu, tiles, g);
     total += ug * max((tg + mine - 1) / mine, 1);
   }
-  const uint32_t fits = __ballot_sync(0xffffffffu, total <= (int)gridDim.x);
+  const uint32_t fits = __ballot_sync(0xffffffffu, total <= a.prefix_ctas);
   c.per = fits ? __shfl_sync(0xffffffffu, mine, __ffs(fits) - 1) : most;  // one share each always fits
   const int splits = max((tiles + c.per - 1) / c.per, 1), count = units * splits;
   int incl = count;
@@ -166,12 +168,29 @@ __device__ __forceinline__ bool prefix_cut_fixed(const SharedArgs& a, int T, Pre
   return true;
 }
 
+constexpr int SH_WARPS = AT_THREADS / 32;
+template <int D>
+constexpr int sh_slots() { return D == 128 ? 2 : 4; }
+template <int D>
+constexpr int sh_smem() {
+  return AtGeom<D>::SMEM > paged_smem_bytes<D, SH_WARPS>(sh_slots<D>()) ? AtGeom<D>::SMEM : paged_smem_bytes<D, SH_WARPS>(sh_slots<D>());
+}
+
 template <int D, int G>
 __global__ void __launch_bounds__(AT_THREADS, 2)
-shared_prefix_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
+shared_decode_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, SharedArgs a) {
   extern __shared__ __align__(128) uint8_t sh_smem_raw[];
   __shared__ TileShared ts;
+  __shared__ uint64_t bars[SH_WARPS * sh_slots<D>()];
   pdl_wait();
+  if ((int)blockIdx.x >= a.prefix_ctas) {
+    pdl_trigger();
+    const int i = blockIdx.x - a.prefix_ctas;
+    paged_body<D, G, PAGED_PLAIN, SH_WARPS, sh_slots<D>()>(a.own, sh_smem_raw, bars, i % a.own_splits, a.own_splits,
+                                                          (i / a.own_splits) % a.own.Hkv, i / (a.own_splits * a.own.Hkv),
+                                                          threadIdx.x, [] { __syncthreads(); });
+    return;
+  }
   tile_setup(ts);
   pdl_trigger();  // only now: a kernel that starts early must not find tensor memory free that this CTA still has to take
   constexpr int T = AT_ROWS / G;
@@ -366,17 +385,14 @@ int decode_scored_dg(PagedArgs a, int n_splits, int n_seqs, __half* out, cudaStr
 }
 
 template <int D, int G>
-int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int prefix_ctas, int n_seqs, __half* out,
-                     cudaStream_t st) {
-  constexpr int smem = AtGeom<D>::SMEM;
-  int rc = allow_smem<shared_prefix_kernel<D, G>>(smem);
+int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const SharedArgs& a, int n_seqs, __half* out, cudaStream_t st) {
+  constexpr int smem = sh_smem<D>();
+  int rc = allow_smem<shared_decode_kernel<D, G>>(smem);
   if (rc) return rc;
-  HYP_CUDA_TRY(launch_pdl<2>(shared_prefix_kernel<D, G>, dim3((unsigned)prefix_ctas), dim3(AT_THREADS),
-                             (size_t)smem, st, mq, mkv, a));
-  rc = launch_paged<D, G, PAGED_PLAIN>(a.own, a.own_splits, n_seqs, st);
-  if (rc < 0) return rc;
+  const unsigned grid = (unsigned)(a.prefix_ctas + a.own_splits * a.own.Hkv * n_seqs);
+  HYP_CUDA_TRY(launch_pdl<2>(shared_decode_kernel<D, G>, dim3(grid), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
   rc = launch_merge<D>(a.own, n_seqs, out, st);
-  return rc < 0 ? rc : 3;
+  return rc < 0 ? rc : 2;
 }
 
 template <int D, bool CAP, bool BIAS>
@@ -444,12 +460,14 @@ SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int pre
     p.own_splits = paged_splits(n_seqs, Hkv, prefix_pages + own_pages);
     return p;
   }
-  const int slots = 2 * sm_count();     // resident CTAs
-  const int most = (prefix_pages * PG_PT + 2 * AT_KEYS - 1) / (2 * AT_KEYS);  // at least two key tiles each
+  const int slots = 2 * sm_count();  // resident CTAs (half of them: 107 instead of 96 us for 128 sequences behind five prefixes)
+  // at least four key tiles each (two: 24.8 instead of 23.7 us for 32 sequences behind 2048 tokens, and twice the partial rows)
+  const int most = (prefix_pages * PG_PT + 4 * AT_KEYS - 1) / (4 * AT_KEYS);
   p.even = n_groups <= 32 && p.row_tiles * Hkv <= slots;
   if (p.even) {
     p.prefix_splits = most < 16 ? most : 16;
-    p.prefix_ctas = slots;
+    const int need = p.row_tiles * Hkv * p.prefix_splits;
+    p.prefix_ctas = need < slots ? need : slots;
   } else {
     const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
     p.prefix_splits = slots / (full * Hkv);
@@ -470,7 +488,7 @@ int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride
   a.own = paged_args(c, q, q_stride, scratch, p.prefix_splits + p.own_splits, p.prefix_splits, err);
   a.cu_group = cu_group; a.prefix_table = prefix_table; a.prefix_stride = prefix_stride; a.prefix_lens = prefix_lens;
   a.n_groups = n_groups; a.prefix_splits = p.prefix_splits; a.own_splits = p.own_splits;
-  a.even = p.even;
+  a.even = p.even; a.prefix_ctas = p.prefix_ctas;
   if (p.flat) {
     PagedArgs f = a.own;
     f.cu_group = cu_group; f.prefix_table = prefix_table; f.prefix_lens = prefix_lens;
@@ -483,7 +501,7 @@ int launch_decode_shared(const CacheView& c, const __half* q, long long q_stride
   int rc = tc_make_q_map(&mq, q, c.n_seqs, q_stride, c.Hq, c.Hq / c.Hkv, c.D);
   if (!rc) rc = tc_make_pool_map(&mkv, c.pool, c.D);
   if (rc) return rc;
-#define HYP_F(DD, GG) decode_shared_dg<DD, GG>(mq, mkv, a, p.prefix_ctas, c.n_seqs, out, st)
+#define HYP_F(DD, GG) decode_shared_dg<DD, GG>(mq, mkv, a, c.n_seqs, out, st)
   HYP_DG_DISPATCH(HYP_F);
 #undef HYP_F
 }

@@ -69,6 +69,15 @@ __device__ __forceinline__ float softcap_log2(float y, float cap_l2) {
   return fmaf(-2.f * cap_l2, rcp_approx(1.f + ex2_approx(y)), cap_l2);
 }
 
+// Contiguous bulk copy of data that is not read again soon: first to leave the L2.
+__device__ __forceinline__ void bulk_load_once(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy)
+               : "memory");
+}
+
 template <int D, int WARPS>
 constexpr int paged_smem_bytes(int slots) { return WARPS * slots * 2 * PG_PT * D * 2; }
 
@@ -143,8 +152,13 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
       const __half* src = a.pool + (size_t)page * page_elems + (size_t)kvh * PG_PT * D;
       const uint32_t dst = my_ring + slot * SLOT_BYTES, bar = my_bars + 8u * slot;
       mbar_expect_tx(bar, SLOT_BYTES);
-      bulk_load(dst, src, PAGE_BYTES, bar);
-      bulk_load(dst + PAGE_BYTES, src + v_off, PAGE_BYTES, bar);
+      if (MODE == PAGED_SCORED) {  // the pages pass through; the scores, written now and read by the next kernel, should stay in the L2
+        bulk_load_once(dst, src, PAGE_BYTES, bar);
+        bulk_load_once(dst + PAGE_BYTES, src + v_off, PAGE_BYTES, bar);
+      } else {
+        bulk_load(dst, src, PAGE_BYTES, bar);
+        bulk_load(dst + PAGE_BYTES, src + v_off, PAGE_BYTES, bar);
+      }
     }
   };
   if (lane == 0) {
