@@ -44,7 +44,8 @@ struct PagedArgs {
   const int32_t* prefix_table;
   const int32_t* prefix_lens;
   int prefix_stride, n_groups;
-  // one split: the CTA's result is the operator's (out non-null); PAGED_SCORED then finishes the running sums as well
+  // one split, or a cluster: the result is the operator's (out non-null); PAGED_SCORED (one split) then finishes the running
+  // sums as well
   __half* out;                // [n_seqs, Hq * D]
   float decay;
   const float* w_in;
@@ -83,14 +84,16 @@ constexpr int paged_smem_bytes(int slots) { return WARPS * slots * 2 * PG_PT * D
 
 // `smem`: 128-byte aligned shared memory, paged_smem_bytes<D, WARPS>(SLOTS) bytes; `bars`: WARPS * SLOTS mbarriers.
 // WARPS warps of the CTA call this (warp = 0 .. WARPS - 1); `bar_sync` joins exactly those warps.
-template <int D, int G, int MODE, int WARPS, int SLOTS, typename Sync>
+// CLUSTER: the n_splits (2 .. 8) CTAs of a (sequence, KV head) are a thread-block cluster and join their results through
+// distributed shared memory; every one of them must call this.
+template <int D, int G, int MODE, int WARPS, int SLOTS, bool CLUSTER, typename Sync>
 __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, uint64_t* bars, int split, int n_splits, int kvh,
                                            int b, int tid, Sync bar_sync) {
   constexpr int KS = D / 16, DN = D / 8, CPR = D / 8;
   constexpr int PAGE_BYTES = PG_PT * D * 2;
   constexpr int SLOT_BYTES = 2 * PAGE_BYTES;  // keys, then values
   constexpr int THREADS = WARPS * 32;
-  static_assert(paged_smem_bytes<D, WARPS>(SLOTS) >= (2 * WARPS * 8 + WARPS * G * D + 16) * 4, "the combine buffers reuse the ring");
+  static_assert(paged_smem_bytes<D, WARPS>(SLOTS) >= (2 * WARPS * 8 + WARPS * G * D + 16 + 16 + G * D + 128) * 4, "the combine buffers reuse the ring");
   const int warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, tq = lane & 3;
 
@@ -300,7 +303,9 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   float* sm_m = reinterpret_cast<float*>(smem);  // [WARPS][8]
   float* sm_l = sm_m + WARPS * 8;                // [WARPS][8]
   float* sm_o = sm_l + WARPS * 8;                // [WARPS][G][D]
-  float *fin_m = sm_o + WARPS * G * D, *fin_inv = fin_m + 8;  // one split: the heads' maxima, reciprocal denominators
+  float *fin_m = sm_o + WARPS * G * D, *fin_inv = fin_m + 8;  // PAGED_SCORED, one split: the heads' maxima, reciprocal denominators
+  float *ex_m = fin_inv + 8, *ex_l = ex_m + 8, *ex_o = ex_l + 8;  // CLUSTER: this CTA's result, read by its peers
+  float *all_m = ex_o + G * D, *all_l = all_m + 64;               // CLUSTER: every CTA's maxima and denominators, [head][split]
   if (g < G) {
     if (tq == 0) {
       sm_m[warp * 8 + g] = m_run;
@@ -323,7 +328,13 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
       l += wgt * sm_l[w * 8 + gq];
       acc += wgt * sm_o[(w * G + gq) * D + dd];
     }
-    if (a.out) {
+    if (CLUSTER) {
+      ex_o[e] = acc;
+      if (dd == 0) {
+        ex_m[gq] = mx;
+        ex_l[gq] = l;
+      }
+    } else if (a.out) {
       a.out[((size_t)b * a.Hq + kvh * G + gq) * D + dd] = __float2half_rn(l != 0.f ? acc / l : 0.f);
       if (MODE == PAGED_SCORED && dd == 0) {
         fin_m[gq] = mx;
@@ -335,17 +346,52 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
       if (dd == 0) *reinterpret_cast<float2*>(a.ml + row * 2) = make_float2(mx, l);
     }
   }
+  if (CLUSTER) {
+    bar_sync();
+    cluster_barrier();
+    // loads from a peer have a long latency: every thread asks for all of its own at once
+    if (tid < G * n_splits) {
+      const int gq = tid / n_splits, sp = tid % n_splits;
+      const float mv = ld_cluster_f32(smem_u32(ex_m + gq), sp), lv = ld_cluster_f32(smem_u32(ex_l + gq), sp);
+      all_m[gq * 8 + sp] = mv;
+      all_l[gq * 8 + sp] = lv;
+    }
+    bar_sync();
+    const int per = (G * D + n_splits - 1) / n_splits, e1 = min(G * D, (split + 1) * per);
+    for (int e = split * per + tid; e < e1; e += THREADS) {
+      const int gq = e / D;
+      float ov[8];
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp) ov[sp] = sp < n_splits ? ld_cluster_f32(smem_u32(ex_o + e), sp) : 0.f;
+      float mx = PG_NEG, l = 0.f, acc = 0.f;
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp)
+        if (sp < n_splits) mx = fmaxf(mx, all_m[gq * 8 + sp]);
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp)
+        if (sp < n_splits) {
+          const float wgt = ex2_approx(all_m[gq * 8 + sp] - mx);
+          l += wgt * all_l[gq * 8 + sp];
+          acc += wgt * ov[sp];
+        }
+      a.out[((size_t)b * a.Hq + kvh * G) * D + e] = __float2half_rn(l != 0.f ? acc / l : 0.f);
+    }
+  }
   if (MODE == PAGED_SCORED && a.out) {
     bar_sync();  // the scores in global memory are this CTA's own
     const float* sc = a.scores + ((size_t)b * a.Hq + kvh * G) * a.score_stride;
     const long long wrow = ((long long)b * a.Hkv + kvh) * a.w_stride;
-    for (int k = tid; k < total; k += THREADS) {
-      float w = 0.f;
+    for (int i = lane >> 4; i < my_n; i += 2) {  // a warp takes two of its pages at a time
+      const int k = page_index(i) * PG_PT + (lane & 15);
+      if (k < total) {
+        float w = 0.f;
 #pragma unroll
-      for (int gq = 0; gq < G; ++gq) w += ex2_approx(sc[(size_t)gq * a.score_stride + k] - fin_m[gq]) * fin_inv[gq];
-      a.w_out[wrow + k] = a.w_in && k < total - 1 ? fmaf(a.decay, a.w_in[wrow + k], w) : w;  // the new token's sum starts here
+        for (int gq = 0; gq < G; ++gq) w += ex2_approx(sc[(size_t)gq * a.score_stride + k] - fin_m[gq]) * fin_inv[gq];
+        a.w_out[wrow + k] = a.w_in && k < total - 1 ? fmaf(a.decay, a.w_in[wrow + k], w) : w;  // the new token's sum starts here
+      }
     }
   }
+  if (CLUSTER) cluster_barrier();  // nobody leaves while a peer may still read its result
 }
 
 // Joins the n_slots (at most 96) partial rows that start at row0 and writes the query head's D fp16 results.  A CTA of
