@@ -246,7 +246,7 @@ HYP_API int hyp_op_attn_decode_mod(const hyp_attn_shape* shape, const hyp_attn_m
 
 /* hyp_op_attn_prefill with modified scores (either head size runs on the tcgen05 tensor cores).  Sequences without new
  * rows (cu_q[i] = cu_q[i + 1]) are allowed.  Rows at or behind cu_q[n_seqs] are left as they were.
- * Errors: HYP_EINVAL, HYP_ECAPACITY (more than 65535 row tiles), HYP_ECUDA. */
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (more than 2^31 CTAs), HYP_ECUDA. */
 HYP_API int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_attn_mod* mod, int32_t n_seqs, int32_t M,
                                     const void* q, int64_t q_stride, const void* kv_pages, const int32_t* block_table,
                                     int32_t max_pages_per_seq, const int32_t* cu_q, const int32_t* ctx_lens, void* out,

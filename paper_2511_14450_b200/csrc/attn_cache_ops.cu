@@ -1,5 +1,7 @@
 // Decode attention with modified scores, decode attention that sums the weights each cached position receives, and
 // shared-prefix decode attention (see attn_paged.cuh and attn_tile.cuh for the two CTA bodies).
+#include <math.h>
+
 #include "attn_tile.cuh"
 #include "cache_ops.cuh"
 #include "gemm_tc.cuh"
@@ -270,10 +272,10 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   tile_setup(ts);
   pdl_trigger();  // only now: a kernel that starts early must not find tensor memory free that this CTA still has to take
   const int T = AT_ROWS / a.G;
-  const int kvh = blockIdx.x;  // heads vary fastest: every head's heaviest tile is scheduled before any lighter one
+  const int kvh = blockIdx.x % a.Hkv;  // heads vary fastest: every head's heaviest tile is scheduled before any lighter one
   int seq, first, q0, len, ctx, pre;
   // the last tiles of a sequence see the most keys: they go first
-  at_locate(a.cu_q, a.ctx, a.prefix, a.n_seqs, T, (int)gridDim.y - 1 - (int)blockIdx.y, seq, first, q0, len, ctx, pre);
+  at_locate(a.cu_q, a.ctx, a.prefix, a.n_seqs, T, (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), seq, first, q0, len, ctx, pre);
   if (seq < 0) {
     tile_release(ts);
     return;
@@ -419,9 +421,9 @@ int prefill_mod_launch(const CUtensorMap& mq, const CUtensorMap& mkv, const Pref
   const int rc = allow_smem<prefill_mod_kernel<D, CAP, BIAS>>(smem);
   if (rc) return rc;
   const int T = AT_ROWS / a.G;
-  const int tiles = M / T + a.n_seqs;  // every sequence adds at most one ragged tile
-  if (tiles > 65535) return HYP_ECAPACITY;
-  HYP_CUDA_TRY(launch_pdl<2>(prefill_mod_kernel<D, CAP, BIAS>, dim3(a.Hkv, tiles), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
+  const long long tiles = (long long)M / T + a.n_seqs;  // every sequence adds at most one ragged tile
+  if (tiles * a.Hkv > 0x7fffffffll) return HYP_ECAPACITY;
+  HYP_CUDA_TRY(launch_pdl<2>(prefill_mod_kernel<D, CAP, BIAS>, dim3((unsigned)(tiles * a.Hkv)), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
   return 1;
 }
 
@@ -431,11 +433,11 @@ int paged_splits(int n_seqs, int Hkv, int max_pages) {
   // Up to 16 pages (four per warp): one CTA per sequence and KV head, which then writes the result itself (the join is a
   // launch of its own, ~2.5 us).  Short contexts: one wave of three CTAs per SM.  Longer ones (more than 64 pages a CTA
   // that way): about four waves, so that ragged batches even out.  At least one page per warp.
-  const int groups = n_seqs * Hkv;
+  const long long groups = (long long)n_seqs * Hkv;
   if (max_pages <= 4 * PD_WARPS) return 1;
-  int want = 3 * sm_count() / groups;
+  int want = (int)(3 * sm_count() / groups);
   if (want < 1) want = 1;
-  if (max_pages > 64 * want) want = (12 * sm_count() + groups - 1) / groups;
+  if (max_pages > 64 * want) want = (int)((12 * sm_count() + groups - 1) / groups);
   const int cap = (max_pages + PD_WARPS - 1) / PD_WARPS;
   if (want > cap) want = cap;
   return want > 64 ? 64 : want;
@@ -481,18 +483,18 @@ SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int pre
   const int slots = 2 * sm_count();  // resident CTAs (half of them: 107 instead of 96 us for 128 sequences behind five prefixes)
   // at least four key tiles each (two: 24.8 instead of 23.7 us for 32 sequences behind 2048 tokens, and twice the partial rows)
   const int most = (prefix_pages * PG_PT + 4 * AT_KEYS - 1) / (4 * AT_KEYS);
-  p.even = n_groups <= 32 && p.row_tiles * Hkv <= slots;
+  p.even = n_groups <= 32 && (long long)p.row_tiles * Hkv <= slots;
   if (p.even) {
     p.prefix_splits = most < 16 ? most : 16;
     const int need = p.row_tiles * Hkv * p.prefix_splits;
     p.prefix_ctas = need < slots ? need : slots;
   } else {
     const int full = (n_seqs + T - 1) / T > n_groups ? (n_seqs + T - 1) / T : n_groups;
-    p.prefix_splits = slots / (full * Hkv);
+    p.prefix_splits = (int)(slots / ((long long)full * Hkv));
     if (p.prefix_splits > most) p.prefix_splits = most;
     if (p.prefix_splits > MERGE_SLOTS - 64) p.prefix_splits = MERGE_SLOTS - 64;
     if (p.prefix_splits < 1) p.prefix_splits = 1;
-    p.prefix_ctas = p.prefix_splits * Hkv * p.row_tiles;
+    p.prefix_ctas = (int)fmin((double)p.prefix_splits * Hkv * p.row_tiles, 2147483647.0);  // too many are refused by the caller
   }
   p.own_splits = paged_splits(n_seqs, Hkv, own_pages);
   return p;

@@ -366,7 +366,7 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
   const uint32_t sQ = base, sK = base + Geo::Q_BYTES, sV = sK + 2 * Geo::STAGE;
   // barriers: one per buffer b = tile & 1 (add 8 * b); phase of tile j = j / 2
   const uint32_t bar0 = smem_u32(sh.bars);
-  const uint32_t q_full = bar0, k_full = bar0 + 16, v_full = bar0 + 32, s_full = bar0 + 80, p_full = bar0 + 96, o_done = bar0 + 112;
+  const uint32_t q_full = bar0, drained = bar0 + 8, k_full = bar0 + 16, v_full = bar0 + 32, s_full = bar0 + 80, p_full = bar0 + 96, o_done = bar0 + 112;
   volatile int* abort_flag = &sh.abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n_tiles = wk.n_tiles;
@@ -418,6 +418,7 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
         atomicCAS(err, 0, 22);
       }
       // no copy may be in flight when the CTA leaves: at the end of a clean run these have long completed
+      if (lane == 0) mbar_wait(q_full, 0, nullptr);
       for (int i = max(0, j - 2); i < j && (lane & 7) == 0; ++i)
         mbar_wait(full + 8 * (uint32_t)(i & 1), (uint32_t)((i >> 1) & 1), nullptr);
     }
@@ -459,6 +460,9 @@ __device__ __forceinline__ void tile_body(const CUtensorMap* tm_q, const CUtenso
       if (!ok) {
         *abort_flag = 1;
         atomicCAS(err, 0, 23);
+        // products that are under way still read shared memory and write tensor memory
+        tc_commit(drained);
+        mbar_wait(drained, 0, nullptr);
       }
     }
   } else {

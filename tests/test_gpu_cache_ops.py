@@ -152,6 +152,27 @@ def test_decode_mod(heads, m):
     assert (out[-1] == 0).all()
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("m", [dict(cap=30.0), dict(slopes=True, window=700, prefix=33), dict(window=16)])
+@pytest.mark.parametrize("lens", [[900, 257, 1000], [7000, 3, 0, 2049], [300 + 7 * i for i in range(60)]])
+def test_decode_mod_longer_contexts(heads, m, lens):
+    """Splits that join in a cluster, and splits that a second launch joins."""
+    hq, hkv, d = heads
+    c = Cache([max(l, 1) for l in lens], hkv, d, seed=17)
+    q = queries(len(lens), hq, d, seed=18)
+    ctx = torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda")
+    mod, slopes, pre = make_mod(m, hq, len(lens))
+    out = run_decode_mod(c, heads, q, ctx, mod)
+    for i, l in enumerate(lens):
+        if l == 0:
+            assert (out[i] == 0).all()
+            continue
+        mask, bias = mask_and_bias(torch.tensor([l - 1], device="cuda"), l, m, int(pre[i]) if pre is not None else 0, slopes)
+        want, _, bound, _ = reference(q[i:i + 1].reshape(1, hq, d), c.k[i], c.v[i], mask, m.get("cap", 0.0), bias)
+        close(out[i].view(1, hq, d), want, bound, (i, l))
+    assert hyp.hyp_device_wait_status() == 0
+
+
 @pytest.mark.parametrize("heads", HEADS)
 @pytest.mark.parametrize("m", MODS)
 @pytest.mark.parametrize("lens,new", [([37, 5, 64], [37, 2, 20]), ([300, 129, 1, 64], [300, 65, 1, 0]), ([70, 257, 128], [1, 130, 128])])
@@ -396,40 +417,48 @@ def test_large_scores_and_long_tails():
     close(out.view(1, 8, 128), want, bound, "shared")
 
 
-def calls(seed):
-    """(name, state, call, outputs) of every operator on a small batch, for the tests of streams, graphs and repeats."""
+def calls(seed, n=3, longest=200):
+    """(name, input, call, outputs) of every operator on a batch, for the tests of streams, graphs and repeats: short contexts
+    (one launch each), longer ones (splits that join in a cluster), many or long ones (a second launch joins; shared
+    prefixes on row tiles)."""
     heads = (8, 2, 128)
-    lens = [200, 33, 90]
+    lens = [longest] + [1 + (37 * (i + 1)) % longest for i in range(n - 1)]
     c = Cache(lens, 2, 128, seed=seed)
-    q = queries(3, 8, 128, seed=seed + 1)
+    q = queries(n, 8, 128, seed=seed + 1)
     ctx = torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda")
     width = 16 * c.table.shape[1]
-    w = torch.rand(3, 2, width, generator=gen(seed + 2), device="cuda")
+    w = torch.rand(n, 2, width, generator=gen(seed + 2), device="cuda")
     wo = torch.zeros_like(w)
-    outs = [torch.zeros(3, 8 * 128, dtype=torch.float16, device="cuda") for _ in range(4)]
+    outs = [torch.zeros(n, 8 * 128, dtype=torch.float16, device="cuda") for _ in range(4)]
     mod = hyp.AttnMod(softcap=20.0, window=70)
-    s1 = bytes_of(hyp.hyp_op_attn_mod_scratch_bytes(heads, 3, c.table.shape[1]))
-    s2 = bytes_of(hyp.hyp_op_attn_scored_scratch_bytes(heads, 3, c.table.shape[1]))
-    s3 = bytes_of(hyp.hyp_op_attn_shared_scratch_bytes(heads, 3, 1, c.table.shape[1], c.table.shape[1]))
-    cu1, cu3 = torch.tensor([0, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
-    pl, pt = torch.tensor([200], dtype=torch.int32, device="cuda"), c.table[:1].contiguous()
-    kept = torch.zeros(3, 2, 32, dtype=torch.int32, device="cuda")
-    nl = torch.zeros(3, dtype=torch.int32, device="cuda")
+    pages = c.table.shape[1]
+    s1 = bytes_of(hyp.hyp_op_attn_mod_scratch_bytes(heads, n, pages))
+    s2 = bytes_of(hyp.hyp_op_attn_scored_scratch_bytes(heads, n, pages))
+    s3 = bytes_of(hyp.hyp_op_attn_shared_scratch_bytes(heads, n, 1, pages, pages))
+    cu1 = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    cun = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    pl, pt = torch.tensor([longest], dtype=torch.int32, device="cuda"), c.table[:1].contiguous()
+    kept = torch.zeros(n, 2, 32, dtype=torch.int32, device="cuda")
+    nl = torch.zeros(n, dtype=torch.int32, device="cuda")
     cached = torch.tensor(lens, dtype=torch.int32, device="cuda")
-    dst = torch.zeros(6, 2, 2, 16, 128, dtype=torch.float16, device="cuda")
-    dt = torch.arange(6, dtype=torch.int32, device="cuda").view(3, 2)
-    we = torch.zeros(3, 2, 32, device="cuda")
+    dst = torch.zeros(2 * n, 2, 2, 16, 128, dtype=torch.float16, device="cuda")
+    dt = torch.arange(2 * n, dtype=torch.int32, device="cuda").view(n, 2)
+    we = torch.zeros(n, 2, 32, device="cuda")
     return [
         ("decode_mod", q, lambda st=None: hyp.hyp_op_attn_decode_mod(heads, mod, q, c.pool, c.table, ctx, s1, outs[0], st), [outs[0]]),
-        ("prefill_mod", q, lambda st=None: hyp.hyp_op_attn_prefill_mod(heads, mod, q, c.pool, c.table, cu3, ctx, outs[1], st), [outs[1]]),
+        ("prefill_mod", q, lambda st=None: hyp.hyp_op_attn_prefill_mod(heads, mod, q, c.pool, c.table, cun, ctx, outs[1], st), [outs[1]]),
         ("scored", q, lambda st=None: hyp.hyp_op_attn_decode_scored(heads, q, c.pool, c.table, ctx, 1.0, w, wo, s2, outs[2], st), [outs[2], wo]),
         ("shared", q, lambda st=None: hyp.hyp_op_attn_decode_shared(heads, q, c.pool, cu1, pt, pl, c.table, ctx, s3, outs[3], st), [outs[3]]),
         ("evict", w, lambda st=None: hyp.hyp_op_kv_evict(heads, c.pool, c.table, cached, w, 32, 2, 5, dst, dt, kept, nl, we, st), [kept, nl, we, dst]),
     ]
 
 
-def test_graph_replay_takes_new_inputs_and_results_repeat_bit_for_bit():
-    for i, (name, inp, call, outs) in enumerate(calls(31)):
+BATCHES = [(3, 200), (5, 900), (40, 1500), (2, 9000)]
+
+
+@pytest.mark.parametrize("n,longest", BATCHES)
+def test_graph_replay_takes_new_inputs_and_results_repeat_bit_for_bit(n, longest):
+    for i, (name, inp, call, outs) in enumerate(calls(31, n, longest)):
         call()
         torch.cuda.synchronize()
         first = [o.clone() for o in outs]
@@ -453,9 +482,10 @@ def test_graph_replay_takes_new_inputs_and_results_repeat_bit_for_bit():
         assert not all(torch.equal(a, b) for a, b in zip(first, outs)), name
 
 
-def test_calls_follow_their_stream():
+@pytest.mark.parametrize("n,longest", BATCHES)
+def test_calls_follow_their_stream(n, longest):
     """The inputs are written late on a side stream; the call on that stream has to see them."""
-    for i, (name, inp, call, outs) in enumerate(calls(47)):
+    for i, (name, inp, call, outs) in enumerate(calls(47, n, longest)):
         fresh = torch.rand(inp.shape, generator=gen(200 + i), device="cuda").to(inp.dtype)
         st = torch.cuda.Stream()
         st.wait_stream(torch.cuda.current_stream())
@@ -586,3 +616,61 @@ def test_a_long_cache_far_into_a_large_pool():
     torch.cuda.synchronize()
     for h in range(8):
         assert torch.equal(get(pool, table[0], 0, 32)[:, h], c.k[0][kept[0, h].long(), h])
+
+
+def test_steep_and_negative_distance_slopes_on_long_prompts():
+    """Slopes that move the reference maximum from tile to tile in either direction, with and without a cap."""
+    heads, l = (4, 2, 128), 1500
+    c = Cache([l], 2, 128, seed=21)
+    q = queries(300, 4, 128, seed=22)
+    cu = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    ctx = torch.tensor([l - 300], dtype=torch.int32, device="cuda")
+    pos = torch.arange(l - 300, l, device="cuda")
+    for cap in (0.0, 4.0):
+        slopes = torch.tensor([3.0, 0.01, -0.02, 0.0], device="cuda")
+        mask, bias = mask_and_bias(pos, l, dict(prefix=200), 200, slopes)
+        mod = hyp.AttnMod(softcap=cap, slopes=slopes, prefix_lens=torch.tensor([200], dtype=torch.int32, device="cuda"))
+        out = torch.empty(300, 512, dtype=torch.float16, device="cuda")
+        hyp.hyp_op_attn_prefill_mod(heads, mod, q, c.pool, c.table, cu, ctx, out)
+        torch.cuda.synchronize()
+        want, _, bound, _ = reference(q.reshape(300, 4, 128), c.k[0], c.v[0], mask, cap, bias)
+        close(out.view(300, 4, 128), want, bound, cap)
+
+
+def test_scores_beyond_the_caps_polynomial():
+    """Scores from far below to far above the cap in one row."""
+    heads, l = (4, 2, 128), 400
+    c = Cache([l], 2, 128, seed=23)
+    q = queries(l, 4, 128, seed=24, std=15.0)
+    out = torch.empty(l, 512, dtype=torch.float16, device="cuda")
+    cu = torch.tensor([0, l], dtype=torch.int32, device="cuda")
+    hyp.hyp_op_attn_prefill_mod(heads, hyp.AttnMod(softcap=10.0), q, c.pool, c.table, cu, torch.zeros(1, dtype=torch.int32, device="cuda"), out)
+    torch.cuda.synchronize()
+    mask = torch.tril(torch.ones(l, l, dtype=torch.bool, device="cuda"))
+    want, _, bound, _ = reference(q.reshape(l, 4, 128), c.k[0], c.v[0], mask, 10.0)
+    close(out.view(l, 4, 128), want, bound, "cap")
+
+
+@pytest.mark.parametrize("n,ng", [(70, 40), (256, 3), (9, 9)])
+def test_many_groups_and_large_groups(n, ng):
+    """More groups than a warp has lanes (a fixed number of shares each), more row tiles than fit at once."""
+    heads = (40, 10, 128)
+    rng = np.random.default_rng(n)
+    prefix = [int(x) for x in rng.integers(0, 700, ng)]
+    cuts = np.sort(rng.integers(0, n + 1, ng - 1)).tolist()
+    cu = [0] + cuts + [n]
+    own = [int(x) for x in rng.integers(0, 40, n)]
+    c = Cache(prefix + own, 10, 128, seed=n)
+    pt, ot = c.table[:ng].contiguous(), c.table[ng:, :4].contiguous()
+    q = queries(n, 40, 128, seed=25)
+    out = run_shared(heads, q, c, torch.tensor(cu, dtype=torch.int32, device="cuda"), pt, torch.tensor(prefix, dtype=torch.int32, device="cuda"), ot,
+                     torch.tensor([o - 1 for o in own], dtype=torch.int32, device="cuda"))
+    for i in range(n):
+        g = sum(1 for x in cu[1:] if x <= i)
+        k, v = torch.cat([c.k[g], c.k[ng + i]]), torch.cat([c.v[g], c.v[ng + i]])
+        if k.shape[0] == 0:
+            assert (out[i] == 0).all()
+            continue
+        want, _, bound, _ = reference(q[i:i + 1].reshape(1, 40, 128), k, v, torch.ones(1, k.shape[0], dtype=torch.bool, device="cuda"))
+        close(out[i].view(1, 40, 128), want, bound, (i, g))
+    assert hyp.hyp_device_wait_status() == 0
