@@ -3,6 +3,11 @@
     python -m paper_2511_14450_b200.opbench gemm --M 8 --N 17920 --K 5120 --epi swiglu
     python -m paper_2511_14450_b200.opbench attn_decode --batch 8 --ctx 1024
     python -m paper_2511_14450_b200.opbench attn_prefill --batch 1 --ctx 512
+    python -m paper_2511_14450_b200.opbench attn_decode_mod --batch 8 --ctx 1024 --cap 30
+    python -m paper_2511_14450_b200.opbench attn_prefill_mod --batch 1 --ctx 2048 --window 1024
+    python -m paper_2511_14450_b200.opbench attn_scored --batch 4 --ctx 32768
+    python -m paper_2511_14450_b200.opbench attn_shared --batch 32 --ctx 256 --prefix 2048
+    python -m paper_2511_14450_b200.opbench kv_evict --batch 4 --ctx 4096 --keep 2048
     python -m paper_2511_14450_b200.opbench layer_gemms --M 512
     python -m paper_2511_14450_b200.opbench decode_stage --layers 2 --batch 8 --ctx 1024
     python -m paper_2511_14450_b200.opbench decode_stage --shape llama3 --layers 11 --batch 8 --ctx 1024
@@ -81,6 +86,82 @@ def attn_prefill(batch, ctx, Hq=40, Hkv=10, D=128, iters=10):
             "tflops_causal": 4.0 * batch * (ctx * (ctx + 1) / 2) * Hq * D / ms / 1e9}
 
 
+def _cache(batch, ctx, Hkv, D, n=4):
+    """n pools of random pages, a shuffled block table for `batch` sequences of `ctx` tokens."""
+    mpps = (ctx + 15) // 16
+    pools = [torch.randn(batch * mpps, 2, Hkv, 16, D, device="cuda").half() for _ in range(n)]
+    return pools, torch.randperm(batch * mpps, device="cuda").to(torch.int32).view(batch, mpps)
+
+
+def attn_decode_mod(batch, ctx, cap=0.0, window=0, Hq=40, Hkv=10, D=128, iters=20):
+    pools, table = _cache(batch, ctx, Hkv, D)
+    q = torch.randn(batch, Hq * D, device="cuda").half()
+    cl = torch.full((batch,), ctx - 1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(hyp.hyp_op_attn_mod_scratch_bytes((Hq, Hkv, D), batch, table.shape[1]), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    mod = hyp.AttnMod(softcap=cap, window=window)
+    ms = _time(lambda i: hyp.hyp_op_attn_decode_mod((Hq, Hkv, D), mod, q, pools[i % 4], table, cl, scratch, out), iters)
+    seen = min(ctx, window) if window else ctx
+    return {"op": "attn_decode_mod", "batch": batch, "ctx": ctx, "cap": cap, "window": window, "us": ms * 1e3,
+            "kv_gbs": batch * seen * 4 * Hkv * D / ms / 1e6}
+
+
+def attn_prefill_mod(batch, ctx, cap=0.0, window=0, Hq=40, Hkv=10, D=128, iters=10):
+    pools, table = _cache(batch, ctx, Hkv, D, 2)
+    q = torch.randn(batch * ctx, Hq * D, device="cuda").half()
+    cu = torch.arange(0, batch * ctx + 1, ctx, dtype=torch.int32, device="cuda")
+    c0 = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    mod = hyp.AttnMod(softcap=cap, window=window)
+    ms = _time(lambda i: hyp.hyp_op_attn_prefill_mod((Hq, Hkv, D), mod, q, pools[i % 2], table, cu, c0, out), iters)
+    w = min(window, ctx) if window else ctx
+    pairs = batch * (w * (w + 1) / 2 + (ctx - w) * w)
+    return {"op": "attn_prefill_mod", "batch": batch, "ctx": ctx, "cap": cap, "window": window, "us": ms * 1e3,
+            "tflops": 4.0 * pairs * Hq * D / ms / 1e9}
+
+
+def attn_scored(batch, ctx, Hq=40, Hkv=10, D=128, iters=20):
+    pools, table = _cache(batch, ctx, Hkv, D, 2)
+    q = torch.randn(batch, Hq * D, device="cuda").half()
+    cl = torch.full((batch,), ctx - 1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(hyp.hyp_op_attn_scored_scratch_bytes((Hq, Hkv, D), batch, table.shape[1]), dtype=torch.uint8, device="cuda")
+    w = torch.zeros(batch, Hkv, 16 * table.shape[1], device="cuda")
+    out = torch.empty_like(q)
+    ms = _time(lambda i: hyp.hyp_op_attn_decode_scored((Hq, Hkv, D), q, pools[i % 2], table, cl, 1.0, w, w, scratch, out), iters)
+    return {"op": "attn_scored", "batch": batch, "ctx": ctx, "us": ms * 1e3, "gbs": batch * ctx * Hkv * (4 * D + 8) / ms / 1e6}
+
+
+def attn_shared(batch, ctx, prefix, Hq=40, Hkv=10, D=128, iters=20):
+    """One group of `batch` sequences behind a prefix, `ctx` tokens of their own each."""
+    pools, table = _cache(batch + 1, max(ctx, prefix), Hkv, D)
+    own, pt = table[1:, :(ctx + 15) // 16].contiguous(), table[:1, :(prefix + 15) // 16].contiguous()
+    q = torch.randn(batch, Hq * D, device="cuda").half()
+    cl = torch.full((batch,), ctx - 1, dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, batch], dtype=torch.int32, device="cuda")
+    pl = torch.tensor([prefix], dtype=torch.int32, device="cuda")
+    scratch = torch.empty(hyp.hyp_op_attn_shared_scratch_bytes((Hq, Hkv, D), batch, 1, pt.shape[1], own.shape[1]), dtype=torch.uint8,
+                          device="cuda")
+    out = torch.empty_like(q)
+    ms = _time(lambda i: hyp.hyp_op_attn_decode_shared((Hq, Hkv, D), q, pools[i % 4], cu, pt, pl, own, cl, scratch, out), iters)
+    return {"op": "attn_shared", "batch": batch, "ctx": ctx, "prefix": prefix, "us": ms * 1e3,
+            "kv_gbs": (batch * ctx + prefix) * 4 * Hkv * D / ms / 1e6}
+
+
+def kv_evict(batch, ctx, keep, Hq=40, Hkv=10, D=128, iters=20):
+    pools, table = _cache(batch, ctx, Hkv, D, 2)
+    kw = (keep + 15) // 16
+    dst = torch.empty(batch * kw, 2, Hkv, 16, D, dtype=torch.float16, device="cuda")
+    dt = torch.randperm(batch * kw, device="cuda").to(torch.int32).view(batch, kw)
+    cached = torch.full((batch,), ctx, dtype=torch.int32, device="cuda")
+    w = torch.rand(batch, Hkv, 16 * table.shape[1], device="cuda")
+    wo, kept = torch.empty(batch, Hkv, keep, device="cuda"), torch.empty(batch, Hkv, keep, dtype=torch.int32, device="cuda")
+    nl = torch.empty(batch, dtype=torch.int32, device="cuda")
+    ms = _time(lambda i: hyp.hyp_op_kv_evict((Hq, Hkv, D), pools[i % 2], table, cached, w, keep, min(4, keep // 4), keep // 8, dst, dt, kept,
+                                             nl, wo), iters)
+    return {"op": "kv_evict", "batch": batch, "ctx": ctx, "keep": keep, "us": ms * 1e3,
+            "gbs": 2 * batch * min(ctx, keep) * 4 * Hkv * D / ms / 1e6}
+
+
 def _shape(name):
     from paper_2511_14450_b200 import inputs
     return inputs.llama3_8b_shape() if name == "llama3" else inputs.phi3_medium_shape()
@@ -136,7 +217,8 @@ def decode_stage(layers, batch, ctx, iters=20, shape="phi3"):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["gemm", "attn_decode", "attn_prefill", "layer_gemms", "decode_stage"])
+    ap.add_argument("op", choices=["gemm", "attn_decode", "attn_prefill", "attn_decode_mod", "attn_prefill_mod", "attn_scored", "attn_shared",
+                                   "kv_evict", "layer_gemms", "decode_stage"])
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--shape", default="phi3", choices=["phi3", "llama3"], help="model shape of layer_gemms / decode_stage")
     ap.add_argument("--M", type=int, default=8)
@@ -147,6 +229,10 @@ def main():
     ap.add_argument("--ctx", type=int, default=1024)
     ap.add_argument("--iters", type=int, default=20)
     ap.add_argument("--splits", type=int, default=0, help="attn_decode: context splits (0 = the library's choice)")
+    ap.add_argument("--cap", type=float, default=0.0, help="attn_*_mod: tanh cap of the scores (0 = none)")
+    ap.add_argument("--window", type=int, default=0, help="attn_*_mod: visible tokens behind the query (0 = all)")
+    ap.add_argument("--prefix", type=int, default=2048, help="attn_shared: tokens of the shared prefix")
+    ap.add_argument("--keep", type=int, default=512, help="kv_evict: tokens that stay")
     a = ap.parse_args()
     if a.op == "gemm":
         out = [gemm(a.M, a.N, a.K, a.epi, a.iters)]
@@ -154,6 +240,16 @@ def main():
         out = [attn_decode(a.batch, a.ctx, iters=a.iters, splits=a.splits)]
     elif a.op == "attn_prefill":
         out = [attn_prefill(a.batch, a.ctx, iters=a.iters)]
+    elif a.op == "attn_decode_mod":
+        out = [attn_decode_mod(a.batch, a.ctx, a.cap, a.window, iters=a.iters)]
+    elif a.op == "attn_prefill_mod":
+        out = [attn_prefill_mod(a.batch, a.ctx, a.cap, a.window, iters=a.iters)]
+    elif a.op == "attn_scored":
+        out = [attn_scored(a.batch, a.ctx, iters=a.iters)]
+    elif a.op == "attn_shared":
+        out = [attn_shared(a.batch, a.ctx, a.prefix, iters=a.iters)]
+    elif a.op == "kv_evict":
+        out = [kv_evict(a.batch, a.ctx, a.keep, iters=a.iters)]
     elif a.op == "decode_stage":
         out = [decode_stage(a.layers, a.batch, a.ctx, iters=a.iters, shape=a.shape)]
     else:
