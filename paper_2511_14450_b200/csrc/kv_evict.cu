@@ -193,12 +193,13 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
 }
 
 // Rows to other pages: grid (segments, 2 * Hkv, n_seqs).  A warp takes 32 kept rows: each lane looks up one row's source and
-// destination (the chain kept index -> page -> row is walked once for 32 rows), then the warp copies the rows, eight
-// 512-byte pieces in flight at a time.  (With every thread walking the chain for its own chunks: 19.7 us for 84 MB.)
+// destination (the chain kept index -> page -> row is walked once for 32 rows), then the warp copies the rows, four
+// 512-byte pieces in flight at a time and six CTAs to an SM.  (With every thread walking the chain for its own chunks: 40 us
+// for 4 x 4096 -> 2048 with the selection; eight pieces in flight and three CTAs, one and a half waves: 31.2; this: 26.5.)
 constexpr int MV_THREADS = 256, MV_ROWS = MV_THREADS;
 template <int D>
-__global__ void __launch_bounds__(MV_THREADS) evict_move_kernel(EvictArgs a) {
-  constexpr int CPR = D / 8, RPI = 32 / CPR, UNROLL = 8;  // 16-byte chunks per row, rows per warp-wide access
+__global__ void __launch_bounds__(MV_THREADS, 6) evict_move_kernel(EvictArgs a) {
+  constexpr int CPR = D / 8, RPI = 32 / CPR, UNROLL = 4;  // 16-byte chunks per row, rows per warp-wide access
   pdl_wait();
   pdl_trigger();
   const int kind = blockIdx.y & 1, kvh = blockIdx.y >> 1, b = blockIdx.z;
