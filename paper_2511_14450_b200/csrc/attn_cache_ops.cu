@@ -97,9 +97,10 @@ scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// shared prefix: one launch holds the CTAs of both parts, a second one joins the partial rows.  The prefixes' row tiles go
-// first, the sequences' own pages stream through the CTA slots that they leave.  (As two launches, one after the other: 23.7
-// instead of 20.2 us for 32 sequences behind 2048 tokens, the same for 128 behind five prefixes to 8192.)
+// shared prefix: the prefixes' row tiles and the sequences' own pages, then a join of the partial rows.  Where both parts fit
+// two waves of CTAs, one launch holds them: the own pages stream through the slots that the row tiles leave (20.2 instead of
+// 23.7 us for 32 sequences behind 2048 tokens).  Larger batches stream their own pages in a launch of their own, with three
+// smaller CTAs to an SM.
 // ---------------------------------------------------------------------------------------------
 struct SharedArgs {
   PagedArgs own;              // slots prefix_splits ..
@@ -409,10 +410,16 @@ int decode_shared_dg(const CUtensorMap& mq, const CUtensorMap& mkv, const Shared
   constexpr int smem = sh_smem<D>();
   int rc = allow_smem<shared_decode_kernel<D, G>>(smem);
   if (rc) return rc;
-  const unsigned grid = (unsigned)(a.prefix_ctas + a.own_splits * a.own.Hkv * n_seqs);
-  HYP_CUDA_TRY(launch_pdl<2>(shared_decode_kernel<D, G>, dim3(grid), dim3(AT_THREADS), (size_t)smem, st, mq, mkv, a));
+  const long long own_ctas = (long long)a.own_splits * a.own.Hkv * n_seqs;
+  const bool together = a.prefix_ctas + own_ctas <= 4ll * sm_count();
+  HYP_CUDA_TRY(launch_pdl<2>(shared_decode_kernel<D, G>, dim3((unsigned)(a.prefix_ctas + (together ? own_ctas : 0))), dim3(AT_THREADS),
+                             (size_t)smem, st, mq, mkv, a));
+  if (!together) {
+    rc = launch_paged<D, G, PAGED_PLAIN, false>(a.own, a.own_splits, n_seqs, st);
+    if (rc < 0) return rc;
+  }
   rc = launch_merge<D>(a.own, n_seqs, out, st);
-  return rc < 0 ? rc : 2;
+  return rc < 0 ? rc : together ? 2 : 3;
 }
 
 template <int D, bool CAP, bool BIAS>
