@@ -229,7 +229,7 @@ HYP_API int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int
  *   visible keys     j <= i and (window == 0 or i - j < window), or j < prefix_lens[b]
  * The prefix is visible to every row, those before its end included (as far as it is in the cache). */
 typedef struct {
-  float softcap;              /* 0 = none                                                              */
+  float softcap;              /* 0 = none, else 2^-10 .. 2^20                                          */
   int32_t window;             /* 0 = none                                                              */
   const float* slopes;        /* DEVICE fp32 [n_q_heads] or NULL                                       */
   const int32_t* prefix_lens; /* DEVICE int32 [n_seqs] or NULL                                         */

@@ -123,12 +123,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ float max3abs(float m, float a, float b) { return max3(m, fabsf(a), fabsf(b)); }
 
-// tanh x for |x| <= 0.5 as x times a polynomial in x^2 (four coefficients, least absolute error of tanh x over the range,
-// fitted by reweighted least squares): off by 1.3e-7 at most.  The argument's factor (raw product -> x) is multiplied into
-// the coefficients: c[i] = TANH_Ci * factor^(2 i + 1).  Runs on the packed FMA path; the exact form needs two of the
-// sixteen special-function lanes' operations a score, which alone would take longer than both matrix products.
-constexpr float TANH_RANGE = 0.5f;
-constexpr float TANH_C0 = 0.9999976761797865f, TANH_C1 = -0.33320655167817165f, TANH_C2 = 0.13145145181299145f, TANH_C3 = -0.04337247117084689f;
+// tanh x of two raw products within TANH_RANGE (see tanh_any); the argument's factor (raw product -> x) is multiplied into
+// the coefficients: c[i] = TANH_Ci * factor^(2 i + 1).  Runs on the packed FMA path; the form for the whole range needs two
+// of the sixteen special-function lanes' operations a score, which alone would take longer than both matrix products.
 __device__ __forceinline__ f32x2 tanh2_small(f32x2 raw, const float (&c)[4]) {
   const f32x2 u = mul2(raw, raw);
   f32x2 p = fma2(u, pk2(c[3], c[3]), pk2(c[2], c[2]));
@@ -137,10 +134,6 @@ __device__ __forceinline__ f32x2 tanh2_small(f32x2 raw, const float (&c)[4]) {
   return mul2(raw, p);
 }
 __device__ __forceinline__ f32x2 abs2(f32x2 v) { return v & 0x7fffffff7fffffffull; }
-__device__ __forceinline__ float tanh_exact(float x) {  // 1 - 2 / (1 + e^(2x)); see softcap_log2
-  return fmaf(-2.f, rcp_approx(1.f + ex2_approx(2.f * PG_LOG2E * x)), 1.f);
-}
-
 // A finished row leaves through shared memory: the thread that owns it writes it there (rows 16 bytes apart from a
 // multiple of 128, so that a quarter warp's 16-byte stores meet no bank twice) and sends it off as one bulk copy.  Direct
 // stores, 32 rows at a time and 16 bytes of each, cost 4600 cycles for 128 rows of 512 bytes.
@@ -196,7 +189,7 @@ __device__ __noinline__ float at_true_max(uint32_t tmem_row, int key0, int pos, 
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float x = __uint_as_float(v[i]);
-      if (CAP) x = tanh_exact(x * sc.to_tanh);
+      if (CAP) x = tanh_any(x * sc.to_tanh);
       x = fmaf(-sc.ratio, fabsf((float)(key0 + c + i - pos)), x);
       mx = (c < 32 ? mask.lo : mask.hi) >> ((c + i) & 31) & 1u ? fmaxf(mx, x) : mx;
     }
@@ -249,7 +242,7 @@ __device__ __forceinline__ void at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
     up2(tanh2_small(pk2(mx, mx), sc.tanh_c), top, same);
     mx = mx > PG_NEG ? top : mx;
   }
-  if (CAP && EXACT) mx = mx > PG_NEG ? tanh_exact(mx * sc.to_tanh) : mx;
+  if (CAP && EXACT) mx = mx > PG_NEG ? tanh_any(mx * sc.to_tanh) : mx;
   if (BIAS) {
     const int near = max(max(key0 - pos, pos - (key0 + AT_KEYS - 1)), 0), far = max(abs(key0 - pos), abs(key0 + AT_KEYS - 1 - pos));
     mx += fmaxf(-sc.ratio * (float)near, -sc.ratio * (float)far);
@@ -275,8 +268,8 @@ __device__ __forceinline__ void at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
 #pragma unroll
     for (int i = 0; i < AT_KEYS; i += 2) {
       if (EXACT) {
-        x[i] = tanh_exact(x[i] * sc.to_tanh);
-        x[i + 1] = tanh_exact(x[i + 1] * sc.to_tanh);
+        x[i] = tanh_any(x[i] * sc.to_tanh);
+        x[i + 1] = tanh_any(x[i + 1] * sc.to_tanh);
       } else {
         up2(tanh2_small(pk2(x[i], x[i + 1]), sc.tanh_c), x[i], x[i + 1]);
       }

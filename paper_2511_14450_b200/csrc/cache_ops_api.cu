@@ -18,7 +18,9 @@ bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0;
 // Pages of a table row: token positions stay below 2^30, so that a position plus a tile never leaves 32 bits.
 bool pages_ok(int32_t n) { return n >= 1 && n <= (1 << 26); }
 bool mod_ok(const hyp_attn_mod* m) {
-  return m && isfinite(m->softcap) && m->softcap >= 0.f && m->window >= 0 && aligned(m->slopes, 4) && aligned(m->prefix_lens, 4);
+  // the cap's powers stay within fp32 and its rounding below that of the scores
+  if (!m || !(m->softcap == 0.f || (m->softcap >= 0x1p-10f && m->softcap <= 0x1p20f))) return false;
+  return m->window >= 0 && aligned(m->slopes, 4) && aligned(m->prefix_lens, 4);
 }
 bool query_ok(const hyp_attn_shape* s, const void* q, int64_t q_stride, const void* out) {
   return q && out && q_stride >= (int64_t)s->n_q_heads * s->head_dim && q_stride % 8 == 0 && aligned(q, 16) && aligned(out, 16);

@@ -437,7 +437,7 @@ def _refuse(where: str, why: str):
 
 
 def _shape(shape3):
-    s = _SHAPES.get(shape3)
+    s = _SHAPES.get(shape3 if type(shape3) is tuple else tuple(shape3))
     if s is None:
         if _F16 is None:
             _bind_torch()
@@ -504,7 +504,7 @@ def _launch(where, fn, dev, stream, *args):
 
 
 class AttnMod:
-    """hyp_attn_mod with its device tensors: softcap (0 = none), window (0 = none), slopes fp32 [n_q_heads] or None,
+    """hyp_attn_mod with its device tensors: softcap (0 = none, else 2^-10 .. 2^20), window (0 = none), slopes fp32 [n_q_heads] or None,
     prefix_lens int32 [n_seqs] or None.  Keeps the tensors alive; make it once and use it in every call."""
 
     def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_lens=None):

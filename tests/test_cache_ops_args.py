@@ -85,7 +85,7 @@ def test_query_layout(name):
 
 
 def test_modifications():
-    for cap, window in ((-1.0, 0), (math.nan, 0), (math.inf, 0), (0.0, -1)):
+    for cap, window in ((-1.0, 0), (math.nan, 0), (math.inf, 0), (0.0, -1), (2.0 ** -11, 0), (2.0 ** 20 * 1.01, 0)):
         m = C.byref(hyp.hyp_attn_mod(cap, window, None, None))
         assert hyp.lib().hyp_op_attn_decode_mod(*mod_args(mod=m)) == hyp.HYP_EINVAL
         assert hyp.lib().hyp_op_attn_prefill_mod(*prefill_args(mod=m)) == hyp.HYP_EINVAL

@@ -674,3 +674,48 @@ def test_many_groups_and_large_groups(n, ng):
         want, _, bound, _ = reference(q[i:i + 1].reshape(1, 40, 128), k, v, torch.ones(1, k.shape[0], dtype=torch.bool, device="cuda"))
         close(out[i].view(1, 40, 128), want, bound, (i, g))
     assert hyp.hyp_device_wait_status() == 0
+
+
+@pytest.mark.parametrize("cap", [2.0 ** -10, 0.3, 300.0, 2.0 ** 20])
+def test_caps_from_the_smallest_to_the_largest(cap):
+    """A cap far above the scores leaves them as they are (to fp32 rounding, not to the cap's), a tiny one flattens them."""
+    heads, l = (4, 2, 128), 130
+    c = Cache([l], 2, 128, seed=26)
+    q = queries(l, 4, 128, seed=27)
+    mask = torch.tril(torch.ones(l, l, dtype=torch.bool, device="cuda"))
+    qq = q.reshape(l, 4, 128)
+    want, _, bound, _ = reference(qq, c.k[0], c.v[0], mask, cap)
+    if cap > 300.0:
+        # the cap's own rounding (2^-20 of it) would hide everything: the bound of the scores as they are, and 2.4e-6 of the
+        # largest score |q| |k| / sqrt(D) for the polynomial
+        top = qq.double().norm(dim=-1).amax() * c.k[0].double().norm(dim=-1).amax() / math.sqrt(128)
+        _, _, bound, _ = reference(qq, c.k[0], c.v[0], mask)
+        bound = bound + 2 * 2.4e-6 * top * c.v[0].double().abs().amax()
+    mod = hyp.AttnMod(softcap=cap)
+    out = torch.empty(l, 512, dtype=torch.float16, device="cuda")
+    cu = torch.tensor([0, l], dtype=torch.int32, device="cuda")
+    hyp.hyp_op_attn_prefill_mod(list(heads), mod, q, c.pool, c.table, cu, torch.zeros(1, dtype=torch.int32, device="cuda"), out)
+    torch.cuda.synchronize()
+    close(out.view(l, 4, 128), want, bound, "prefill")
+    one = run_decode_mod(c, heads, q[-1:], torch.tensor([l - 1], dtype=torch.int32, device="cuda"), mod)
+    close(one.view(1, 4, 128), want[-1:], bound[-1:], "decode")
+
+
+def test_two_streams_with_a_scratch_each():
+    """Calls that may overlap on the GPU, on one cache, each with its own scratch and outputs."""
+    a, b = calls(61, 40, 1500), calls(61, 40, 1500)
+    alone = []
+    for name, inp, call, outs in a:
+        call()
+        torch.cuda.synchronize()
+        alone.append([o.clone() for o in outs])
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for rep in range(5):
+        for (_, _, c1, _), (_, _, c2, _) in zip(a, reversed(b)):
+            c1(s1)
+            c2(s2)
+    torch.cuda.synchronize()
+    for i in range(len(a)):
+        assert all(torch.equal(x, y) for x, y in zip(alone[i], a[i][3])), a[i][0]
+        assert all(torch.equal(x, y) for x, y in zip(alone[i], b[i][3])), b[i][0]
