@@ -54,19 +54,18 @@ scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
     return;
   }
   const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
-  const int k_begin = (blockIdx.x - G) * SC_KEYS + threadIdx.x;
-  if (k_begin - (int)threadIdx.x >= total) return;
+  const int k0 = (blockIdx.x - G) * SC_KEYS + SC_PER * threadIdx.x;  // this thread's four keys
+  if (k0 - SC_PER * (int)threadIdx.x >= total) return;
   const float* wi = a.w_in ? a.w_in + ((long long)b * a.Hkv + kvh) * a.w_stride : nullptr;
   float* wo = a.w_out + ((long long)b * a.Hkv + kvh) * a.w_stride;
   // everything this thread needs from memory is asked for before the maxima are joined
-  float s[SC_PER][G], old[SC_PER];
+  float4 s[G];
+  float old[SC_PER];
 #pragma unroll
-  for (int i = 0; i < SC_PER; ++i) {
-    const int k = k_begin + i * MERGE_THREADS;
-    old[i] = wi && k < total - 1 ? wi[k] : 0.f;  // the new token's sum starts here
+  for (int gq = 0; gq < G; ++gq)
+    s[gq] = k0 < total ? *reinterpret_cast<const float4*>(a.scores + (row0 + gq) * a.score_stride + k0) : make_float4(PG_NEG, PG_NEG, PG_NEG, PG_NEG);
 #pragma unroll
-    for (int gq = 0; gq < G; ++gq) s[i][gq] = k < total ? a.scores[(row0 + gq) * a.score_stride + k] : PG_NEG;
-  }
+  for (int i = 0; i < SC_PER; ++i) old[i] = wi && k0 + i < total - 1 ? wi[k0 + i] : 0.f;  // the new token's sum starts here
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float *s_m = sm, *s_inv = sm + G;
   for (int gq = warp; gq < G; gq += MERGE_THREADS / 32) {
@@ -86,14 +85,17 @@ scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
     }
   }
   __syncthreads();
+  float w[SC_PER] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < SC_PER; ++i) {
-    const int k = k_begin + i * MERGE_THREADS;
-    float w = 0.f;
-#pragma unroll
-    for (int gq = 0; gq < G; ++gq) w += ex2_approx(s[i][gq] - s_m[gq]) * s_inv[gq];
-    if (k < total) wo[k] = fmaf(a.decay, old[i], w);
+  for (int gq = 0; gq < G; ++gq) {
+    w[0] += ex2_approx(s[gq].x - s_m[gq]) * s_inv[gq];
+    w[1] += ex2_approx(s[gq].y - s_m[gq]) * s_inv[gq];
+    w[2] += ex2_approx(s[gq].z - s_m[gq]) * s_inv[gq];
+    w[3] += ex2_approx(s[gq].w - s_m[gq]) * s_inv[gq];
   }
+#pragma unroll
+  for (int i = 0; i < SC_PER; ++i)
+    if (k0 + i < total) wo[k0 + i] = fmaf(a.decay, old[i], w[i]);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -454,7 +456,11 @@ size_t paged_scratch_floats(int n_seqs, int Hq, int D, int n_slots) { return (si
 
 int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half* q, long long q_stride, float* scratch,
                       __half* out, int* err, cudaStream_t st) {
-  const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride);
+  // a window bounds what is read, whatever the table could hold (a prefix is taken to be short); fewer pages never mean more
+  // splits, so the scratch for the whole table suffices
+  int pages = c.table_stride;
+  if (mod.window > 0) pages = (int)fmin((double)pages, mod.window / 16.0 + 2.0 + (mod.prefix_lens ? 16.0 : 0.0));
+  const int ns = paged_splits(c.n_seqs, c.Hkv, pages);
   PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
   a.softcap = mod.softcap; a.window = mod.window; a.slopes = mod.slopes; a.prefix = mod.prefix_lens;
 #define HYP_F(DD, GG) decode_joined_dg<DD, GG, PAGED_MOD>(a, ns, c.n_seqs, out, st)
