@@ -329,6 +329,11 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   tile_release(ts);
 }
 
+int wave_splits(int n_seqs, int Hkv) {  // three CTAs per SM
+  const int want = (int)(3 * sm_count() / ((long long)n_seqs * Hkv));
+  return want < 1 ? 1 : want;
+}
+
 PagedArgs paged_args(const CacheView& c, const __half* q, long long q_stride, float* scratch, int n_slots, int slot0, int* err) {
   PagedArgs a{};
   a.q = q; a.q_stride = q_stride;
@@ -337,6 +342,7 @@ PagedArgs paged_args(const CacheView& c, const __half* q, long long q_stride, fl
   a.acc = scratch;
   a.ml = scratch + (size_t)c.n_seqs * c.Hq * n_slots * c.D;
   a.n_slots = n_slots; a.slot0 = slot0;
+  a.wave_splits = wave_splits(c.n_seqs, c.Hkv);
   a.err = err;
   return a;
 }
@@ -444,8 +450,7 @@ int paged_splits(int n_seqs, int Hkv, int max_pages) {
   // that way): about four waves, so that ragged batches even out.  At least one page per warp.
   const long long groups = (long long)n_seqs * Hkv;
   if (max_pages <= 4 * PD_WARPS) return 1;
-  int want = (int)(3 * sm_count() / groups);
-  if (want < 1) want = 1;
+  int want = wave_splits(n_seqs, Hkv);
   if (max_pages > 64 * want) want = (int)((12 * sm_count() + groups - 1) / groups);
   const int cap = (max_pages + PD_WARPS - 1) / PD_WARPS;
   if (want > cap) want = cap;

@@ -33,6 +33,7 @@ struct PagedArgs {
   float* acc;                 // partial rows: ((b * Hq + h) * n_slots + slot0 + split) * D
   float* ml;                  // the same rows' (maximum, denominator)
   int n_slots, slot0;
+  int wave_splits;            // splits of a (sequence, KV head) that make one wave of the batch
   int* err;
   float* scores;              // PAGED_SCORED: [n_seqs * Hq][score_stride] scores in log2 units
   int score_stride;
@@ -131,25 +132,33 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   const int n_pre = MODE == PAGED_MOD || MODE == PAGED_FLAT ? (pre + PG_PT - 1) / PG_PT : 0;
   const int p_lo = MODE == PAGED_MOD ? max(lo / PG_PT, n_pre) : 0;
   const int n_vis = n_pre + max(n_pages - p_lo, 0);
+  // The splits were planned for the length that the table could hold; a shorter sequence uses no more of them than the same
+  // rule gives for its own length (see paged_splits), and the CTAs left over say that they have seen nothing.
+  const int fair = max(a.wave_splits, (n_vis + 15) / 16);  // a large batch still evens out over CTAs of 16 pages
+  const int used = n_vis > 64 * a.wave_splits ? n_splits : max(min(min(n_splits, fair), (n_vis + WARPS - 1) / WARPS), 1);
+  if (!CLUSTER && split >= used) {  // the whole CTA
+    if (tid < G) *reinterpret_cast<float2*>(a.ml + (((size_t)b * a.Hq + kvh * G + tid) * a.n_slots + a.slot0 + split) * 2) = make_float2(PG_NEG, 0.f);
+    return;
+  }
   auto page_index = [&](int i) {  // this warp's i-th page
-    const int v = split + n_splits * (warp + WARPS * i);
+    const int v = split + used * (warp + WARPS * i);
     return MODE == PAGED_MOD ? (v < n_pre ? v : v - n_pre + p_lo) : MODE == PAGED_FLAT ? v - n_pre : v;
   };
-  const int first = split + n_splits * warp, stride_p = n_splits * WARPS;
-  const int my_n = first < n_vis ? (n_vis - first + stride_p - 1) / stride_p : 0;
+  const int first = split + used * warp, stride_p = used * WARPS;
+  const int my_n = split < used && first < n_vis ? (n_vis - first + stride_p - 1) / stride_p : 0;
 
   const size_t page_elems = kv_page_elems(a.Hkv, PG_PT, D);
   const size_t v_off = (size_t)a.Hkv * PG_PT * D;
   const uint32_t my_bars = smem_u32(bars) + 8u * (warp * SLOTS);
   const uint32_t my_ring = smem_u32(smem) + (uint32_t)(warp * SLOTS) * SLOT_BYTES;
   // page ids: lane l holds the id of this warp's page base + l, for the 32 pages being issued and the 32 after them.  Where
-  // the walk does not depend on the length (no window, no prefix) the first ids are fetched together with it.
+  // the walk does not depend on the length (no window, no prefix, all splits used) the first ids are fetched together with it.
   auto load_ids = [&](int base) {
     if (base + lane >= my_n) return 0;
     const int p = page_index(base + lane);
     return MODE == PAGED_FLAT && p < 0 ? pt[p + n_pre] : bt[p];
   };
-  if (!early) ids_cur = load_ids(0);
+  if (!early || used != n_splits) ids_cur = load_ids(0);
   int32_t ids_next = load_ids(32);
   auto issue = [&](int i, int slot) {  // all lanes call, i ascending
     if (i > 0 && (i & 31) == 0) {

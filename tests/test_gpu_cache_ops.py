@@ -719,3 +719,29 @@ def test_two_streams_with_a_scratch_each():
     for i in range(len(a)):
         assert all(torch.equal(x, y) for x, y in zip(alone[i], a[i][3])), a[i][0]
         assert all(torch.equal(x, y) for x, y in zip(alone[i], b[i][3])), b[i][0]
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (40, 10, 128)])
+@pytest.mark.parametrize("lens", [[1, 300, 17, 0, 80], [5000, 40, 333], [64] * 50])
+def test_tables_much_wider_than_the_sequences(heads, lens):
+    """Rows of a table made for long contexts (splits are planned by its width), sequences of any length in it."""
+    hq, hkv, d = heads
+    c = Cache([max(l, 1) for l in lens], hkv, d, seed=31, extra=700)
+    n = len(lens)
+    q = queries(n, hq, d, seed=32)
+    ctx = torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda")
+    w = torch.zeros(n, hkv, 16 * c.table.shape[1], device="cuda")
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    a = run_decode_mod(c, heads, q, ctx, hyp.AttnMod())
+    b = run_scored(c, heads, q, ctx, 1.0, None, w)
+    s = run_shared(heads, q, c, cu, c.table[:1].contiguous(), torch.zeros(1, dtype=torch.int32, device="cuda"), c.table, ctx)
+    for i, l in enumerate(lens):
+        if l == 0:
+            assert (a[i] == 0).all() and (b[i] == 0).all() and (s[i] == 0).all()
+            continue
+        want, p, bound, serr = reference(q[i:i + 1].reshape(1, hq, d), c.k[i], c.v[i], torch.ones(1, l, dtype=torch.bool, device="cuda"))
+        for o in (a, b, s):
+            close(o[i].view(1, hq, d), want, bound, (i, l))
+        got = p[:, 0].view(hkv, hq // hkv, l).sum(1)
+        assert ((w[i, :, :l].double() - got).abs() <= (2 * serr + 2.0 ** -20) * got).all(), (i, l)
+    assert hyp.hyp_device_wait_status() == 0
