@@ -9,9 +9,10 @@
 //   counts gives; among keys equal to the threshold the lowest indexes win.  (40 heads of 4096
 //   tokens: 21 us searching bit pairs with block-wide counts, 16 us with the weights in registers - every CTA then runs
 //   straight through 32-fold unrolled code once, and waits for its instructions.)
-//   move kernel: copies the kept rows, 16-byte chunks, re-permuted for their new slot.  Other pages: every row at its
-//   own pace.  In place a row moves down or stays, so one CTA per (sequence, KV head, keys or values) goes up the rows and
-//   reads each batch completely before it writes it: a batch writes at or below its own sources, never at a later one's.
+//   Then the kept rows move, re-permuted for their new slots.  To other pages: a warp for 32 rows.  In place a row moves down
+//   or stays, so one CTA per (sequence, KV head, keys or values) goes up the rows and reads each batch completely before it
+//   writes it: a batch writes at or below its own sources, never at a later one's.  A few rows of a few heads are moved by
+//   the selecting CTA.
 // The move is bound by HBM (every kept row read and written once), the selection by its block-wide steps.
 #include "cache_ops.cuh"
 #include "hyperion.h"
@@ -55,8 +56,36 @@ __device__ __forceinline__ void count_bin(uint32_t* hist, bool valid, uint32_t b
   }
 }
 
+// Few rows and at most one CTA per SM (MOVES): the selecting CTA moves them itself, keys and values, all read before any is written - in place or
+// not - and a launch falls away (13.0 -> 10.8 us for 4 x 1000 -> 200; 320 CTAs, two to an SM without this, 31.8 -> 40).
+constexpr int MH_UNROLL = 8;
+__host__ __device__ constexpr int move_here_rows(int D) { return MH_UNROLL * EV_THREADS / (2 * (D / 8)); }
+__device__ __forceinline__ void move_rows(const EvictArgs& a, int kvh, int b, int len, const int32_t* kept) {
+  const int lg = a.D == 128 ? 4 : 3;  // 16-byte chunks of a row: 1 << lg
+  const int32_t* bt = a.table + (long long)b * a.table_stride;
+  const int32_t* dt = a.dst_table + (long long)b * a.dst_stride;
+  auto at = [&](int32_t page, int kind, int slot, int c) {
+    return ((((size_t)page * 2 + kind) * a.Hkv + kvh) * 16 + slot) * a.D + ((c ^ (slot & 7)) << 3);
+  };
+  uint4 v[MH_UNROLL];
+#pragma unroll
+  for (int u = 0; u < MH_UNROLL; ++u) {
+    const int e = u * EV_THREADS + threadIdx.x, i = e >> (lg + 1);
+    if (i < len) {
+      const int s = kept[i];
+      v[u] = *reinterpret_cast<const uint4*>(a.pool + at(bt[s >> 4], (e >> lg) & 1, s & 15, e & ((1 << lg) - 1)));
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < MH_UNROLL; ++u) {
+    const int e = u * EV_THREADS + threadIdx.x, i = e >> (lg + 1);
+    if (i < len) *reinterpret_cast<uint4*>(a.dst + at(dt[i >> 4], (e >> lg) & 1, i & 15, e & ((1 << lg) - 1))) = v[u];
+  }
+}
+
 // STAGED: the candidates fit shared memory (chosen by what the table's row can name).
-template <bool STAGED>
+template <bool STAGED, bool MOVES>
 __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   extern __shared__ float sw[];  // STAGED: the candidates' weights
   __shared__ uint32_t hist[EV_BINS];
@@ -76,6 +105,10 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
     for (int i = tid; i < a.n_keep; i += EV_THREADS) {
       kept[i] = i < t ? i : -1;
       if (i < t) wo[i] = w[i];
+    }
+    if (MOVES) {
+      __syncthreads();  // the kept slots are this CTA's own
+      move_rows(a, kvh, b, t, kept);
     }
     return;
   }
@@ -190,6 +223,10 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
       wo[a.n_keep - a.n_recent + i] = x;
     }
   }
+  if (MOVES) {
+    __syncthreads();
+    move_rows(a, kvh, b, a.n_keep, kept);
+  }
 }
 
 // Rows to other pages: grid (segments, 2 * Hkv, n_seqs).  A warp takes 32 kept rows: each lane looks up one row's source and
@@ -287,11 +324,15 @@ int launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
   const long long most = (long long)a.table_stride * 16 - a.n_sink - a.n_recent;  // candidates a sequence can have
   if (most <= EV_STRIPES * EV_THREADS) {
     const size_t smem = most > 0 ? (size_t)most * sizeof(float) : 0;
-    const int rc = allow_smem<evict_select_kernel<true>>(EV_STRIPES * EV_THREADS * (int)sizeof(float));
+    constexpr int most_smem = EV_STRIPES * EV_THREADS * (int)sizeof(float);
+    const bool moves = a.n_keep <= move_here_rows(a.D) && (long long)a.n_seqs * a.Hkv <= sm_count();
+    const int rc = moves ? allow_smem<evict_select_kernel<true, true>>(most_smem) : allow_smem<evict_select_kernel<true, false>>(most_smem);
     if (rc) return rc;
-    HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<true>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), smem, st, a));
+    HYP_CUDA_TRY(launch_pdl<2>(moves ? evict_select_kernel<true, true> : evict_select_kernel<true, false>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS),
+                               smem, st, a));
+    if (moves) return 1;
   } else {
-    HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<false>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), (size_t)0, st, a));
+    HYP_CUDA_TRY(launch_pdl<2>(evict_select_kernel<false, false>, dim3(a.Hkv, a.n_seqs), dim3(EV_THREADS), (size_t)0, st, a));
   }
   const int rc = a.D == 128 ? launch_move<128>(a, st) : launch_move<64>(a, st);
   return rc < 0 ? rc : 1 + rc;
