@@ -11,7 +11,11 @@ namespace hyp {
 namespace {
 
 constexpr int PD_WARPS = 4;      // decode kernels
-constexpr double FLAT_BYTES = 8e6;
+// Bytes of prefix that the sequences of a batch may read again, each for itself, and prefix pages below which they always
+// do; measured on 2 to 128 sequences of three head layouts: at 21 MB 9.9-12.5 us against 12.4 with row tiles, at 42 MB equal,
+// at 84 MB 14.1-17.2 against 12.3-16.1; behind 128 tokens 10.4-19.1 against 12.5-27.8 whatever the batch.
+constexpr double FLAT_BYTES = 32e6;
+constexpr int FLAT_PAGES = 8;
 template <int D>
 constexpr int pd_slots() { return D == 128 ? 2 : 4; }  // 64 KB of ring: three CTAs per SM
 
@@ -492,7 +496,7 @@ SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int pre
   // Where the prefixes are short or the batch is small, every sequence walks its prefix for itself: what it reads again
   // comes from the L2, and a whole launch and the row tiles' set-up fall away.
   const double again = (double)n_seqs * Hkv * prefix_pages * (2 * PG_PT * 2) * D;
-  p.flat = again <= FLAT_BYTES;
+  p.flat = again <= FLAT_BYTES || prefix_pages <= FLAT_PAGES;
   if (p.flat) {
     p.prefix_splits = 0;
     p.own_splits = paged_splits(n_seqs, Hkv, prefix_pages + own_pages);
