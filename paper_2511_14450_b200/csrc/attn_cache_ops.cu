@@ -490,7 +490,7 @@ int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride
 }
 
 SharedPlan shared_plan(int n_seqs, int Hq, int Hkv, int D, int n_groups, int prefix_pages, int own_pages) {
-  SharedPlan p;
+  SharedPlan p{};
   const int T = AT_ROWS / (Hq / Hkv);
   p.row_tiles = n_seqs / T + n_groups;  // every group adds at most one ragged tile
   // Where the prefixes are short or the batch is small, every sequence walks its prefix for itself: what it reads again

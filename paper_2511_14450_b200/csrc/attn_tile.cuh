@@ -15,6 +15,9 @@
 //            only when a row of the warp has outgrown it by 2^8.  In the tile that holds the end of the sequence they also
 //            zero the values behind the end (0 times garbage infinity is not 0).
 // Every barrier exists once per buffer (phase = tile / 2), every wait is bounded, failure unwinds through a shared flag.
+// Measured (causal, 40 / 10 heads of 128): 2048 tokens 55 us = 780 TFLOP/s, capped 70, distance bias 68, 4096 tokens 168 us =
+// 1020 TFLOP/s, where the products alone (two CTAs to an SM, nothing else running) take 126: with 64 keys a step the score
+// product reads 6 KB of shared memory in the 32 cycles of its products.
 #pragma once
 #include "attn_paged.cuh"
 #include "tcgen05.cuh"
