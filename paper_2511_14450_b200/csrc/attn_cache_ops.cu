@@ -462,6 +462,9 @@ int paged_splits(int n_seqs, int Hkv, int max_pages) {
 }
 
 size_t paged_scratch_floats(int n_seqs, int Hq, int D, int n_slots) { return (size_t)n_seqs * Hq * n_slots * (D + 2); }
+size_t scored_scores_offset(int n_seqs, int Hq, int Hkv, int D, int max_pages) {
+  return (paged_scratch_floats(n_seqs, Hq, D, paged_splits(n_seqs, Hkv, max_pages)) + 3) / 4 * 4;
+}
 
 int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half* q, long long q_stride, float* scratch,
                       __half* out, int* err, cudaStream_t st) {
@@ -482,7 +485,7 @@ int launch_decode_scored(const CacheView& c, const __half* q, long long q_stride
   const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride);
   PagedArgs a = paged_args(c, q, q_stride, scratch, ns, 0, err);
   a.score_stride = c.table_stride * PG_PT;
-  a.scores = scratch + paged_scratch_floats(c.n_seqs, c.Hq, c.D, ns);
+  a.scores = scratch + scored_scores_offset(c.n_seqs, c.Hq, c.Hkv, c.D, c.table_stride);
   a.decay = decay; a.w_in = w_in; a.w_out = w_out; a.w_stride = w_stride;
 #define HYP_F(DD, GG) decode_joined_dg<DD, GG, PAGED_SCORED>(a, ns, c.n_seqs, out, st)
   HYP_DG_DISPATCH(HYP_F);

@@ -29,6 +29,9 @@ struct CacheView {
 
 int paged_splits(int n_seqs, int Hkv, int max_pages);
 size_t paged_scratch_floats(int n_seqs, int Hq, int D, int n_slots);
+// Where the scores of the scored operator start in its scratch: behind the partial rows, on the next 16-byte boundary (a partial
+// row is D + 2 floats, so an odd number of rows ends 8 bytes off one, and the scores are read four at a time).
+size_t scored_scores_offset(int n_seqs, int Hq, int Hkv, int D, int max_pages);
 
 int launch_decode_mod(const CacheView& c, const hyp_attn_mod& mod, const __half* q, long long q_stride, float* scratch,
                       __half* out, int* err, cudaStream_t st);

@@ -73,9 +73,8 @@ extern "C" int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_at
 
 extern "C" size_t hyp_op_attn_scored_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq) {
   if (!shape_ok(shape) || n_seqs < 1 || !pages_ok(max_pages_per_seq)) return 0;
-  const size_t parts = paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim,
-                                            paged_splits(n_seqs, shape->n_kv_heads, max_pages_per_seq));
-  return 4 * (parts + (size_t)n_seqs * shape->n_q_heads * 16 * (size_t)max_pages_per_seq);
+  return 4 * (scored_scores_offset(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, max_pages_per_seq) +
+              (size_t)n_seqs * shape->n_q_heads * 16 * (size_t)max_pages_per_seq);
 }
 
 extern "C" int hyp_op_attn_decode_scored(const hyp_attn_shape* shape, int32_t n_seqs, const void* q, int64_t q_stride,

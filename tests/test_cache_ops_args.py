@@ -132,3 +132,19 @@ def test_the_binding_refuses_what_does_not_fit():
         hyp.hyp_op_attn_prefill_mod((4, 2, 64), hyp.AttnMod(), q, pool, table, ctx, ctx, out)
     with pytest.raises(hyp.HyperionError):
         hyp.hyp_op_kv_evict((4, 2, 64), pool, table, ctx, w, 8, 1, 1, pool, table, table, ctx, w)
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 64), (1, 1, 128), (3, 3, 64), (25, 25, 64), (5, 5, 128), (40, 10, 128), (8, 1, 64)])
+def test_the_scores_in_the_scratch_start_on_a_16_byte_boundary(heads):
+    """Scores [n_seqs * n_q_heads][16 * pages] lie at the end of the scratch and are read four at a time, so their start, the whole
+    less their size, has to be a multiple of 16 bytes (partial rows are head_dim + 2 floats, and may be odd in number)."""
+    odd = 0
+    for n in (1, 2, 3, 5, 7, 64):
+        for pages in (1, 4, 16, 17, 19, 20, 28, 33, 64, 100, 513, 2048):
+            total = hyp.hyp_op_attn_scored_scratch_bytes(heads, n, pages)
+            scores = 4 * n * heads[0] * 16 * pages
+            assert total > scores and (total - scores) % 16 == 0, (n, pages, total - scores)
+            parts = hyp.hyp_op_attn_mod_scratch_bytes(heads, n, pages)          # the same partial rows
+            assert parts <= total - scores < parts + 16, (n, pages)
+            odd += parts % 16 != 0
+    assert odd > 0 or heads[0] % 2 == 0, "the sizes were to hold odd numbers of rows"

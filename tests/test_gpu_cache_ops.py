@@ -255,6 +255,30 @@ def test_decode_scored(heads, form):
         assert torch.isnan(behind).all() if form == "same" else (behind == 9.0).all()
 
 
+@pytest.mark.parametrize("heads", [(3, 3, 64), (1, 1, 128), (1, 1, 64), (5, 5, 128), (25, 25, 64)])
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("pages", [19, 20, 28, 33])
+def test_decode_scored_of_odd_batches_and_heads(heads, n, pages):
+    """Odd sequences, heads and splits: the partial rows in front of the scores do not fill whole 16-byte pieces."""
+    hq, hkv, d = heads
+    lens = [16 * pages - 7, 1, 100][:n]
+    c = Cache(lens, hkv, d, seed=pages, extra=0)
+    assert c.table.shape[1] == pages
+    q = queries(n, hq, d, seed=33)
+    ctx = torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda")
+    w = torch.rand(n, hkv, 16 * pages, generator=gen(34), device="cuda")
+    before = w.double()
+    out = run_scored(c, heads, q, ctx, 0.75, w, w)
+    for i, l in enumerate(lens):
+        want, p, bound, serr = reference(q[i:i + 1].reshape(1, hq, d), c.k[i], c.v[i], torch.ones(1, l, dtype=torch.bool, device="cuda"))
+        close(out[i].view(1, hq, d), want, bound, (i, l))
+        got = p[:, 0].view(hkv, hq // hkv, l).sum(1)
+        got[:, :l - 1] += 0.75 * before[i, :, :l - 1]
+        assert ((w[i, :, :l].double() - got).abs() <= (2 * serr + 2.0 ** -20) * got).all(), (i, l)
+        assert torch.equal(w[i, :, l:].double(), before[i, :, l:])
+    assert hyp.hyp_device_wait_status() == 0
+
+
 def evict_reference(w, t, keep, sink, recent):
     """Kept slots of one head, in order."""
     if t <= keep:
