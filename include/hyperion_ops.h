@@ -86,7 +86,8 @@ HYP_API int hyp_device_wait_status(int32_t* code_out, int32_t clear);
 /* Process-wide tuning switches (measurement aids; the defaults are the measured best).
  *   HYP_TUNE_PDL           which kernels are launched with programmatic dependent launch, so that their
  *                          prologue and weight prefetch may overlap the predecessor's tail: 0 none, 1 the
- *                          weight-streaming projections, 2 also the norms between them, 3 every kernel
+ *                          weight-streaming projections, 2 also the norms between them, 3 every kernel but that of
+ *                          hyp_op_attn_decode_step (it reads lengths, table and pages ahead of its wait)
  *   HYP_TUNE_STREAM_SLOTS  ring slots per warp of the weight-streaming kernel, 1..8 (0 = built-in choice)
  *   HYP_TUNE_ATTN_SPLITS   context splits (cluster size) of the stage's decode attention, 1..8 (0 = built-in)
  *   HYP_TUNE_ATTN_SLOTS    ring slots per warp of that kernel, 2..4 (0 = built-in)

@@ -435,7 +435,7 @@ attn_decode_fused_kernel(AttnFusedArgs a, BatchMeta bm, ModelDims d) {
 }
 
 template <int D, int G, bool SPLIT, bool GLOBAL>
-int launch_dg(const AttnFusedArgs& a_in, int n_splits, const BatchMeta& bm, const ModelDims& d, cudaStream_t st) {
+int launch_dg(const AttnFusedArgs& a_in, int n_splits, const BatchMeta& bm, const ModelDims& d, cudaStream_t st, bool early) {
   static bool configured = false;
   constexpr int SLOT_BYTES = (SPLIT ? 3 : 2) * AF_PT * D * 2;
   constexpr int COMBINE_BYTES = (2 * AF_WARPS * 8 + AF_WARPS * G * D) * 4;
@@ -460,7 +460,7 @@ int launch_dg(const AttnFusedArgs& a_in, int n_splits, const BatchMeta& bm, cons
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = pdl_level() >= 2 ? 1 : 0;
+    cfg.numAttrs = early && pdl_level() >= 2 ? 1 : 0;
   } else {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = n_splits;
@@ -469,7 +469,7 @@ int launch_dg(const AttnFusedArgs& a_in, int n_splits, const BatchMeta& bm, cons
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = pdl_level() >= 3 ? 2 : 1;  // measured: launching the cluster variant early costs 2 %
+    cfg.numAttrs = early && pdl_level() >= 3 ? 2 : 1;  // measured: launching the cluster variant early costs 2 %
   }
   HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, attn_decode_fused_kernel<D, G, SPLIT, GLOBAL>, a, bm, d));
   return 1;
@@ -508,7 +508,7 @@ int attn_decode_fused_splits(int n_seqs, int Hkv, int max_ctx) {
 
 int launch_attn_decode_fused(const float* qkv32, int stride, __half* kv_layer, const float2* rope_table, __half* attn_out,
                              int n_splits, int slots, int* err, const BatchMeta& bm, const ModelDims& d, cudaStream_t st,
-                             const float* row_scale, __half* klo_layer, float* scratch, int* tickets) {
+                             const float* row_scale, __half* klo_layer, float* scratch, int* tickets, bool may_start_early) {
   if (n_splits < 1 || n_splits > 8 || !err || (row_scale != nullptr) != (klo_layer != nullptr)) return HYP_EINVAL;
   if ((scratch != nullptr) != (tickets != nullptr)) return HYP_EINVAL;
   AttnFusedArgs a;
@@ -518,10 +518,10 @@ int launch_attn_decode_fused(const float* qkv32, int stride, __half* kv_layer, c
   const int G = d.Hq / d.Hkv;
 #define HYP_AF_CASE(DD, GG)                                                \
   if (d.D == DD && G == GG)                                                \
-    return scratch ? (row_scale ? launch_dg<DD, GG, true, true>(a, n_splits, bm, d, st)                            \
-                                : launch_dg<DD, GG, false, true>(a, n_splits, bm, d, st))                          \
-                   : (row_scale ? launch_dg<DD, GG, true, false>(a, n_splits, bm, d, st)                           \
-                                : launch_dg<DD, GG, false, false>(a, n_splits, bm, d, st));
+    return scratch ? (row_scale ? launch_dg<DD, GG, true, true>(a, n_splits, bm, d, st, may_start_early)                            \
+                                : launch_dg<DD, GG, false, true>(a, n_splits, bm, d, st, may_start_early))                          \
+                   : (row_scale ? launch_dg<DD, GG, true, false>(a, n_splits, bm, d, st, may_start_early)                           \
+                                : launch_dg<DD, GG, false, false>(a, n_splits, bm, d, st, may_start_early));
   HYP_AF_CASE(128, 1) HYP_AF_CASE(128, 2) HYP_AF_CASE(128, 4) HYP_AF_CASE(128, 8)
   HYP_AF_CASE(64, 1) HYP_AF_CASE(64, 2) HYP_AF_CASE(64, 4) HYP_AF_CASE(64, 8)
 #undef HYP_AF_CASE

@@ -196,7 +196,9 @@ int& attn_fused_slots_override();   // 0 = built-in choice
 int launch_attn_decode_fused(const float* qkv32, int stride, __half* kv_layer, const float2* rope_table, __half* attn_out,
                              int n_splits, int slots, int* err, const BatchMeta& bm, const ModelDims& d, cudaStream_t st,
                              const float* row_scale = nullptr, __half* klo_layer = nullptr,
-                             float* scratch = nullptr, int* tickets = nullptr);
+                             float* scratch = nullptr, int* tickets = nullptr, bool may_start_early = true);
+// may_start_early: lengths, block table and cache pages do not come from a kernel that may still be running when this one is let
+// in (they are read before its wait); true in the stage, whose own kernels are the only ones that write them.
 // scratch / tickets (both or neither): the splits meet in global memory instead of a cluster (see the kernel);
 // scratch holds n_seqs * Hkv * n_splits rows of attn_fused_scratch_row(G, D) floats, tickets n_seqs * Hkv zeroed ints
 inline size_t attn_fused_scratch_row(int G, int D) { return (size_t)G * D + 16; }

@@ -211,8 +211,9 @@ extern "C" int hyp_op_attn_decode_step(const hyp_attn_shape* shape, int32_t n_se
   bm.block_table = block_table;
   const ModelDims d = attn_dims(shape, stride);
   if (n_splits == 0) n_splits = attn_decode_fused_splits(n_seqs, shape->n_kv_heads, 16 * max_pages_per_seq);
+  // never early: the call before may have written the lengths or moved rows of these pages (hyp_op_kv_evict, another step)
   return finish(launch_attn_decode_fused(qkv, stride, (__half*)kv_pages, (const float2*)rope_table, (__half*)out, n_splits,
-                                         2, tc_err_flag_ptr(), bm, d, (cudaStream_t)stream));
+                                         2, tc_err_flag_ptr(), bm, d, (cudaStream_t)stream, nullptr, nullptr, nullptr, nullptr, false));
 }
 
 extern "C" int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int32_t M, const void* q,

@@ -376,6 +376,46 @@ def test_kv_evict_beyond_the_register_range(place):
         assert torch.equal(get(dst, dtab[0], kind, keep), x[idx])
 
 
+@pytest.mark.parametrize("keep", [40, 700])
+@pytest.mark.parametrize("between", [False, True])
+def test_a_decode_step_behind_an_eviction_at_every_overlap_level(keep, between):
+    """The step takes its lengths from the eviction before it and appends to the rows that this one moved, also where kernels may be
+    launched early and a projection stands in between."""
+    heads, n, longest = (8, 2, 128), 24, 1600
+    hq, hkv, d = heads
+    lens = [longest - 13 * i for i in range(n)]
+    c = Cache(lens, hkv, d, seed=41)
+    w0 = torch.rand(n, hkv, 16 * c.table.shape[1], generator=gen(42), device="cuda")
+    cached = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qkv = torch.randn(n, (hq + 2 * hkv) * d, generator=gen(43), device="cuda")
+    angle = torch.arange(longest + 1, device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(d // 2, device="cuda") * 2 / d)
+    rope = torch.stack([angle.cos(), angle.sin()], -1).float().contiguous()
+    a, wt = torch.randn(4, 512, generator=gen(44), device="cuda").half(), torch.randn(1024, 512, generator=gen(45), device="cuda").bfloat16()
+    packed, prod = hyp.hyp_op_pack_weight(wt, 1024, False, f16=True), torch.empty(4, 1024, device="cuda")
+    pool0 = c.pool.clone()
+    results = []
+    for level in (0, 2, 3, 3, 3):
+        c.pool.copy_(pool0)
+        w, kept = w0.clone(), torch.empty(n, hkv, keep, dtype=torch.int32, device="cuda")
+        new_lens = torch.full((n,), 5, dtype=torch.int32, device="cuda")
+        out = torch.empty(n, hq * d, dtype=torch.float16, device="cuda")
+        torch.cuda.synchronize()
+        hyp.hyp_tune(hyp.HYP_TUNE_PDL, level)
+        try:
+            hyp.hyp_op_kv_evict(heads, c.pool, c.table, cached, w, keep, 4, 16, c.pool, c.table, kept, new_lens, w)
+            if between:
+                hyp.hyp_op_gemm_f16(a, packed, 1024, hyp.HYP_EPI_STORE_F32, prod)
+            hyp.hyp_op_attn_decode_step(heads, qkv, c.pool, c.table, new_lens, rope, 0, out)
+        finally:
+            hyp.hyp_tune(hyp.HYP_TUNE_PDL, 2)
+        torch.cuda.synchronize()
+        assert torch.isfinite(out.float()).all()
+        results.append((out, torch.nan_to_num(c.pool, nan=123.0), new_lens))
+    for r in results[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(results[0], r))
+    assert results[0][2].tolist() == [keep] * n
+
+
 def run_shared(heads, q, c, cu, ptable, plens, own_table, ctx):
     out = torch.full((q.shape[0], heads[0] * heads[2]), 7.0, dtype=torch.float16, device="cuda")
     scratch = bytes_of(hyp.hyp_op_attn_shared_scratch_bytes(heads, q.shape[0], plens.shape[0], ptable.shape[1], own_table.shape[1]))
