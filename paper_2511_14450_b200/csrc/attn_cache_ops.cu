@@ -302,7 +302,10 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   wk.n_first = (pre + AT_KEYS - 1) / AT_KEYS;
   wk.second = max(lo / AT_KEYS, wk.n_first);
   wk.n_tiles = wk.n_first + max((hi + AT_KEYS - 1) / AT_KEYS - wk.second, 0);
-  if (wk.n_tiles == 0) {  // only where the table is too short for the lengths it comes with
+  if (wk.n_tiles == 0) {  // a window that lies wholly behind what the table can name: rows that see nothing
+    const int per = a.G * D / 8;  // 16-byte pieces of a token's G heads
+    for (int e = threadIdx.x; e < wk.rows * per; e += AT_THREADS)
+      *reinterpret_cast<uint4*>(a.out + ((size_t)(wk.row0 + e / per) * a.Hq + wk.head0) * D + (size_t)(e % per) * 8) = make_uint4(0u, 0u, 0u, 0u);
     tile_release(ts);
     return;
   }

@@ -200,6 +200,28 @@ def test_prefill_mod(heads, m, lens, new):
     assert hyp.hyp_device_wait_status() == 0
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (40, 10, 128)])
+@pytest.mark.parametrize("m", [dict(window=16), dict(window=16, prefix=3), dict(window=70, cap=9.0, slopes=True), dict()])
+@pytest.mark.parametrize("ctx", [100, 40, 3000])
+def test_prefill_mod_where_the_table_is_too_short(heads, m, ctx):
+    """Rows whose positions lie behind the last key that the table can name: those that see some of it get what they see, those
+    that see nothing zeros."""
+    hq, hkv, d = heads
+    have, rows = 64, 200
+    c = Cache([have], hkv, d, seed=51, extra=0)
+    q = queries(rows, hq, d, seed=52)
+    mod, slopes, pre = make_mod(m, hq, 1)
+    out = torch.full((rows, hq * d), 7.0, dtype=torch.float16, device="cuda")
+    hyp.hyp_op_attn_prefill_mod(heads, mod, q, c.pool, c.table, torch.tensor([0, rows], dtype=torch.int32, device="cuda"),
+                                torch.tensor([ctx], dtype=torch.int32, device="cuda"), out)
+    torch.cuda.synchronize()
+    mask, bias = mask_and_bias(torch.arange(ctx, ctx + rows, device="cuda"), have, m, int(pre[0]) if pre is not None else 0, slopes)
+    want, _, bound, _ = reference(q.reshape(rows, hq, d), c.k[0], c.v[0], mask, m.get("cap", 0.0), bias)
+    close(out.view(rows, hq, d), want, bound, ctx)
+    assert (out[~mask.any(1)] == 0).all()
+    assert hyp.hyp_device_wait_status() == 0
+
+
 def test_prefill_mod_without_modification_agrees_with_plain_prefill():
     heads, lens, new = (40, 10, 128), [700, 128, 257], [700, 128, 130]
     c = Cache(lens, 10, 128, seed=3)
