@@ -217,7 +217,9 @@ HYP_API int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int
  * Decode calls take ctx_lens as hyp_op_attn_decode does: the new token sits at position ctx_lens[b] and its key and value
  * are already in the cache.  ctx_lens[b] = -1 marks a row that has nothing of its own to see (padding of a batch);
  * a row that sees nothing at all gives zeros.  Cache slots behind a sequence's end may hold anything.  Lengths are read
- * on the device and clamped to what the table's row can name; table entries behind a sequence's end are not read.
+ * on the device and clamped to what the table's row can name (any value may stand there); in a prompt a row keeps its position
+ * (up to 2^30) and sees those of its keys that the table names.  Table entries behind a sequence's end may hold anything:
+ * they may be fetched, they are not followed.
  * All lengths and tables may change between replays of a captured graph; the shapes and sizes passed by value may not.
  * Scratch is caller-owned, 16-byte aligned, needs no initialisation and keeps nothing between calls; two calls whose
  * kernels can overlap need a scratch each.  Pointers belong to the current device.  The first attention call on a process

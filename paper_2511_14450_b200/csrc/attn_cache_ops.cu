@@ -57,7 +57,7 @@ scored_finish_kernel(PagedArgs a, __half* __restrict__ out) {
     paged_merge_row<D>(a.acc, a.ml, row * a.n_slots, a.n_slots, out + row * D, sm);
     return;
   }
-  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
+  const int total = paged_total(a.ctx[b], a.table_stride);
   const int k0 = (blockIdx.x - G) * SC_KEYS + SC_PER * threadIdx.x;  // this thread's four keys
   if (k0 - SC_PER * (int)threadIdx.x >= total) return;
   const float* wi = a.w_in ? a.w_in + ((long long)b * a.Hkv + kvh) * a.w_stride : nullptr;
@@ -287,10 +287,10 @@ prefill_mod_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     tile_release(ts);
     return;
   }
-  ctx = max(ctx, 0);
+  ctx = min(max(ctx, 0), 1 << 30);  // no table names more; a position, and a position plus a tile, stay within 32 bits
   const int have = min(ctx + len, a.table_stride * PG_PT);  // tokens in the cache, the new rows included
   pre = min(max(pre, 0), have);
-  const int window = a.window > 0 ? a.window : 0x40000000;
+  const int window = a.window > 0 ? a.window : 0x7fffffff;
   TileWork wk;
   wk.head0 = kvh * a.G;
   wk.kvh = kvh;

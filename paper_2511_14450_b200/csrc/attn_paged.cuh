@@ -56,6 +56,10 @@ struct PagedArgs {
   long long w_stride;
 };
 
+// Tokens of a sequence, the new one at position ctx included, as far as its table row can name them; any ctx (the row holds at
+// most 2^30 tokens, and the clamp comes before the sum).
+__device__ __forceinline__ int paged_total(int ctx, int table_stride) { return min(max(ctx, -1), table_stride * PG_PT - 1) + 1; }
+
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -115,7 +119,7 @@ __device__ __forceinline__ void paged_body(const PagedArgs& a, uint8_t* smem, ui
   }
   // Visible keys: [lo, total) behind the query, and [0, pre).  PAGED_FLAT: [0, pre) is the prefix, in pages of its own, and
   // its keys are numbered from -16 * (its pages) on.
-  const int total = min(max(a.ctx[b] + 1, 0), a.table_stride * PG_PT);
+  const int total = paged_total(a.ctx[b], a.table_stride);
   int lo = 0, pre = 0;
   const int32_t* pt = nullptr;
   if (MODE == PAGED_MOD) {

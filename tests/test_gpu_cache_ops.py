@@ -222,6 +222,46 @@ def test_prefill_mod_where_the_table_is_too_short(heads, m, ctx):
     assert hyp.hyp_device_wait_status() == 0
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (3, 3, 64)])
+@pytest.mark.parametrize("far", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30, 4000])
+def test_lengths_far_beyond_the_table(heads, far):
+    """A length that the table cannot hold counts as the table's own, up to the largest 32-bit one."""
+    hq, hkv, d = heads
+    have = 80
+    c = Cache([have, have], hkv, d, seed=53, extra=0)
+    q = queries(2, hq, d, seed=54)
+    far_ctx, ctx = (torch.full((2,), x, dtype=torch.int32, device="cuda") for x in (far, have - 1))
+    one = torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    mod = hyp.AttnMod(softcap=20.0, window=33, prefix_lens=far_ctx)
+    assert torch.equal(run_decode_mod(c, heads, q, far_ctx, hyp.AttnMod()), run_decode_mod(c, heads, q, ctx, hyp.AttnMod()))
+    assert torch.equal(run_decode_mod(c, heads, q, far_ctx, mod), run_decode_mod(c, heads, q, ctx, mod))
+    w1, w2 = torch.zeros(2, hkv, have, device="cuda"), torch.zeros(2, hkv, have, device="cuda")
+    assert torch.equal(run_scored(c, heads, q, far_ctx, 1.0, None, w1), run_scored(c, heads, q, ctx, 1.0, None, w2)) and torch.equal(w1, w2)
+    pt = c.table[:1].contiguous()
+    assert torch.equal(run_shared(heads, q, c, one, pt, far_ctx[:1], c.table, far_ctx), run_shared(heads, q, c, one, pt, ctx[:1] + 1, c.table, ctx))
+    kept, new_lens = torch.empty(2, hkv, 20, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    w1.copy_(torch.rand(w1.shape, generator=gen(55), device="cuda"))
+    dst, dtab = torch.zeros(4, 2, hkv, 16, d, dtype=torch.float16, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    hyp.hyp_op_kv_evict(heads, c.pool, c.table, far_ctx, w1, 20, 2, 3, dst, dtab, kept, new_lens, w2)
+    assert new_lens.tolist() == [20, 20]
+    for b in range(2):
+        for h in range(hkv):
+            assert kept[b, h].tolist() == evict_reference(w1[b, h].tolist(), have, 20, 2, 3)
+    # a prompt's rows behind everything: all keys, or none with a window
+    rows = queries(40, hq, d, seed=56)
+    cu = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    want, _, bound, _ = reference(rows.reshape(40, hq, d), c.k[0], c.v[0], torch.ones(40, have, dtype=torch.bool, device="cuda"))
+    for window in (0, 50):
+        out = torch.full((40, hq * d), 7.0, dtype=torch.float16, device="cuda")
+        hyp.hyp_op_attn_prefill_mod(heads, hyp.AttnMod(window=window), rows, c.pool, pt, cu, far_ctx[:1], out)
+        torch.cuda.synchronize()
+        if window:
+            assert (out == 0).all()
+        else:
+            close(out.view(40, hq, d), want, bound, far)
+    assert hyp.hyp_device_wait_status() == 0
+
+
 def test_prefill_mod_without_modification_agrees_with_plain_prefill():
     heads, lens, new = (40, 10, 128), [700, 128, 257], [700, 128, 130]
     c = Cache(lens, 10, 128, seed=3)
