@@ -63,7 +63,7 @@ HYP_API int hyp_op_pack_weight(const void* w, int32_t N, int32_t K, int32_t swig
  * swiglu = (epilogue == HYP_EPI_SWIGLU_BF16); K multiple of 8, N and ldo multiples of 16 and 8 unless M <= 8.
  * M <= 8 runs the weight-streaming kernel, larger M the tcgen05 kernels (for 9-128 rows the plain-store
  * epilogues of narrow matrices take the variant with the operands swapped and K split over a cluster).
- * The first call on a process allocates one device word for error reporting. */
+ * The first call on a device allocates one word there for error reporting. */
 HYP_API int hyp_op_gemm(const void* a, const void* w_packed, int32_t M, int32_t N, int32_t K, int32_t epilogue,
                         void* out, int32_t ldo, void* stream);
 
@@ -77,9 +77,9 @@ HYP_API int hyp_op_gemm_f16(const void* a, const void* w_packed, int32_t M, int3
                             void* out, int32_t ldo, void* stream);
 
 /* Device-side wait status.  Every wait inside the library's kernels (on a copy's completion, on tensor memory, on a
- * peer CTA) is bounded; a kernel whose wait runs out records a small non-zero code in one device word, unwinds and
+ * peer CTA) is bounded; a kernel whose wait runs out records a small non-zero code in one word of its device, unwinds and
  * returns by itself (its results are invalid).  The calls that synchronise report that word as HYP_ETIMEOUT; this
- * call reads it for the others: it synchronises the device, writes the code to *code_out (HOST; 0 = no wait ever
+ * call reads it for the others: it synchronises the current device, writes the code to *code_out (HOST; 0 = no wait ever
  * expired) and, if clear != 0, resets the word.  Errors: HYP_EINVAL, HYP_ECUDA. */
 HYP_API int hyp_device_wait_status(int32_t* code_out, int32_t clear);
 
@@ -164,7 +164,7 @@ HYP_API int hyp_op_attn_decode(const hyp_attn_shape* shape, int32_t n_seqs, cons
  *              ctx_lens[b] (not checked: the lengths live on the device)
  *   n_splits   1 .. 8 context splits, 0 = the library's choice
  *   out        fp16 [n_seqs, n_q_heads * head_dim]
- * The first call on a process allocates one device word for error reporting (bounded waits). */
+ * The first call on a device allocates one word there for error reporting (bounded waits). */
 HYP_API int hyp_op_attn_decode_step(const hyp_attn_shape* shape, int32_t n_seqs, const float* qkv, int32_t stride,
                                     void* kv_pages, const int32_t* block_table, int32_t max_pages_per_seq,
                                     const int32_t* ctx_lens, const float* rope_table, int32_t n_splits, void* out,
@@ -222,8 +222,8 @@ HYP_API int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int
  * they may be fetched, they are not followed.
  * All lengths and tables may change between replays of a captured graph; the shapes and sizes passed by value may not.
  * Scratch is caller-owned, 16-byte aligned, needs no initialisation and keeps nothing between calls; two calls whose
- * kernels can overlap need a scratch each.  Pointers belong to the current device.  The first attention call on a process
- * allocates one device word for error reporting (bounded waits): make it before capturing a graph.
+ * kernels can overlap need a scratch each.  Pointers belong to the current device.  The first attention call on a device
+ * allocates one word there for error reporting (bounded waits): make it before capturing a graph.
  * --------------------------------------------------------------------------------------------- */
 
 /* Modification of the scores s = q . k / sqrt(D) of query position i and key position j, in this order:

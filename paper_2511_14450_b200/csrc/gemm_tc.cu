@@ -645,7 +645,13 @@ int encode_out_map(CUtensorMap* map, void* out, int ldo, int M, int N, int epi, 
   return HYP_OK;
 }
 
-int* g_err_flag = nullptr;  // one device word per process: first non-zero code wins
+// One word on every device that is used (first non-zero code wins): a kernel reports on the device that it runs on.
+constexpr int MAX_DEVICES = 64;
+int** err_flag_slot() {  // of the current device; null: no device
+  static int* words[MAX_DEVICES] = {};
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < MAX_DEVICES ? &words[dev] : nullptr;
+}
 
 template <int EPI, int BNT>
 int launch_pair_bn(const TcAct& act, const TcWeight& w, int M, int N, int K, void* out, int ldo, cudaStream_t st,
@@ -661,10 +667,10 @@ int launch_pair_bn(const TcAct& act, const TcWeight& w, int M, int N, int K, voi
   const CUtensorMap& tm_b = BNT == 256 ? w.map : w.map7;
   if (early)
     HYP_CUDA_TRY(launch_pdl<1>(gemm_tc2_kernel<EPI, BNT>, dim3((unsigned)(2 * pairs)), dim3(TC_THREADS), (size_t)SMEM2_BYTES, st,
-                               act.map, tm_b, tm_out, M, N, K, w.N16p, team, idesc2(act.f16, BNT), g_err_flag));
+                               act.map, tm_b, tm_out, M, N, K, w.N16p, team, idesc2(act.f16, BNT), tc_err_flag_ptr()));
   else
     HYP_CUDA_TRY(launch_pdl(gemm_tc2_kernel<EPI, BNT>, dim3((unsigned)(2 * pairs)), dim3(TC_THREADS), (size_t)SMEM2_BYTES, st,
-                            act.map, tm_b, tm_out, M, N, K, w.N16p, team, idesc2(act.f16, BNT), g_err_flag));
+                            act.map, tm_b, tm_out, M, N, K, w.N16p, team, idesc2(act.f16, BNT), tc_err_flag_ptr()));
   return 1;
 }
 
@@ -750,10 +756,10 @@ int launch_epi(const TcAct& act, const TcWeight& w, int M, int N, int K, void* o
   if (mrc) return mrc;
   if (early)
     HYP_CUDA_TRY(launch_pdl<1>(gemm_tc_kernel<EPI>, dim3(grid), dim3(TC_THREADS), (size_t)SMEM_BYTES, st, act.map, w.map,
-                               tm_out, M, N, K, w.N16p, team, act.f16 ? IDESC_F16 : IDESC_BF16, g_err_flag));
+                               tm_out, M, N, K, w.N16p, team, act.f16 ? IDESC_F16 : IDESC_BF16, tc_err_flag_ptr()));
   else
     HYP_CUDA_TRY(launch_pdl(gemm_tc_kernel<EPI>, dim3(grid), dim3(TC_THREADS), (size_t)SMEM_BYTES, st, act.map, w.map,
-                            tm_out, M, N, K, w.N16p, team, act.f16 ? IDESC_F16 : IDESC_BF16, g_err_flag));
+                            tm_out, M, N, K, w.N16p, team, act.f16 ? IDESC_F16 : IDESC_BF16, tc_err_flag_ptr()));
   return 1;
 }
 
@@ -905,32 +911,36 @@ int tc_make_act(TcAct* a, const void* ptr, int rows, int K, bool f16) {
   return rc;
 }
 
-int* tc_err_flag_ptr() { return g_err_flag; }
+int* tc_err_flag_ptr() {
+  int** word = err_flag_slot();
+  return word ? *word : nullptr;
+}
 
 int tc_prepare() {
-  if (!g_err_flag) {
-    HYP_CUDA_TRY(cudaMalloc((void**)&g_err_flag, sizeof(int)));
-    HYP_CUDA_TRY(cudaMemset(g_err_flag, 0, sizeof(int)));
+  int** word = err_flag_slot();
+  if (!word) return HYP_ECUDA;
+  if (!*word) {
+    HYP_CUDA_TRY(cudaMalloc((void**)word, sizeof(int)));
+    HYP_CUDA_TRY(cudaMemset(*word, 0, sizeof(int)));
   }
   return HYP_OK;
 }
 
 int tc_error_flag(int* value_out) {
   *value_out = 0;
-  if (!g_err_flag) return HYP_OK;
-  HYP_CUDA_TRY(cudaMemcpy(value_out, g_err_flag, sizeof(int), cudaMemcpyDeviceToHost));
+  if (int* word = tc_err_flag_ptr()) HYP_CUDA_TRY(cudaMemcpy(value_out, word, sizeof(int), cudaMemcpyDeviceToHost));
   return HYP_OK;
 }
 
 int tc_error_flag_take(int* value_out, bool clear) {
   const int rc = tc_error_flag(value_out);
-  if (rc == HYP_OK && clear && g_err_flag && *value_out) HYP_CUDA_TRY(cudaMemset(g_err_flag, 0, sizeof(int)));
+  if (rc == HYP_OK && clear && *value_out) HYP_CUDA_TRY(cudaMemset(tc_err_flag_ptr(), 0, sizeof(int)));
   return rc;
 }
 
 int launch_gemm_tc(const TcAct& act, const TcWeight& w, int M, int N, int K, int epi, void* out, int ldo,
                    cudaStream_t st, bool early) {
-  if (M < 1 || N < 1 || K < 8 || act.K != K || w.K != K || M > act.rows || !g_err_flag) return HYP_EINVAL;
+  if (M < 1 || N < 1 || K < 8 || act.K != K || w.K != K || M > act.rows || !tc_err_flag_ptr()) return HYP_EINVAL;
   if (w.rows != N || w.halves != (epi == EPI_SWIGLU_BF16 ? 2 : 1)) return HYP_EINVAL;
   if (act.f16 != w.f16) return HYP_EINVAL;  // one instruction takes both operands in the same 16-bit type
   // the epilogues write 16 bytes per lane at out + row * ldo + col (col a multiple of 16)

@@ -61,12 +61,12 @@ int launch_attn_prefill_tc(const CUtensorMap& q_map, const CUtensorMap& kv_map, 
 // 1 (default): the two-CTA tile kernel may take 224-column tiles where they fill the last wave better.
 int& tile_width_224_enabled();
 
-// One-time set-up of the device-side error word (allocates; call from stage creation, not from the hot path).
+// One-time set-up of the current device's error word (allocates; call from stage creation, not from the hot path).
 int tc_prepare();
-// Reads the error word (synchronises the device): 0 = no kernel gave up on a wait.
+// Reads the current device's error word (synchronises it): 0 = no kernel gave up on a wait there.
 int tc_error_flag(int* value_out);
 
-// Device word that kernels set when a bounded wait expires (null before tc_prepare).
+// Word of the current device that kernels set when a bounded wait expires (null before tc_prepare on that device).
 int* tc_err_flag_ptr();
 
 // Ring depth override of the weight-streaming kernel (0 = the built-in choice).

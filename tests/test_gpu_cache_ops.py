@@ -871,3 +871,22 @@ def test_tables_much_wider_than_the_sequences(heads, lens):
         got = p[:, 0].view(hkv, hq // hkv, l).sum(1)
         assert ((w[i, :, :l].double() - got).abs() <= (2 * serr + 2.0 ** -20) * got).all(), (i, l)
     assert hyp.hyp_device_wait_status() == 0
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_tensors_of_another_device_than_the_current_one():
+    """The call runs where its tensors are, and reports a wait that ran out to that device's own word."""
+    heads, lens = (8, 2, 128), [700, 33]
+    c = Cache(lens, 2, 128, seed=71)
+    q = queries(2, 8, 128, seed=72)
+    ctx = torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda")
+    here = run_decode_mod(c, heads, q, ctx, hyp.AttnMod(softcap=20.0))
+    other = torch.device("cuda", (torch.cuda.current_device() + 1) % torch.cuda.device_count())
+    c.pool, c.table = c.pool.to(other), c.table.to(other)
+    out = torch.empty(2, 1024, dtype=torch.float16, device=other)
+    scratch = bytes_of(hyp.hyp_op_attn_mod_scratch_bytes(heads, 2, c.table.shape[1])).to(other)
+    hyp.hyp_op_attn_decode_mod(heads, hyp.AttnMod(softcap=20.0), q.to(other), c.pool, c.table, ctx.to(other), scratch, out)
+    torch.cuda.synchronize(other)
+    assert torch.equal(out.cpu(), here.cpu())
+    with torch.cuda.device(other):
+        assert hyp.hyp_device_wait_status() == 0
