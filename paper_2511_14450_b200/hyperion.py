@@ -456,7 +456,7 @@ def _dense(where, name, t, dtype, dev, shape):
 def _rows(where, name, t, dtype, dev, lead):
     """(address, size of the last dimension) of a contiguous tensor whose other dimensions are `lead`."""
     s = t.shape
-    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or s[:-1] != lead:
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or not s or s[:-1] != lead:
         _refuse(where, f"{name} must be a contiguous {dtype} tensor of shape {(*lead, '*')} on device {dev}, not {t.dtype} "
                        f"{tuple(s)} on {t.device}")
     return t.data_ptr(), s[-1]

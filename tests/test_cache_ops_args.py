@@ -148,3 +148,11 @@ def test_the_scores_in_the_scratch_start_on_a_16_byte_boundary(heads):
             assert parts <= total - scores < parts + 16, (n, pages)
             odd += parts % 16 != 0
     assert odd > 0 or heads[0] % 2 == 0, "the sizes were to hold odd numbers of rows"
+
+
+def test_a_tensor_without_dimensions_is_refused_like_any_other_that_does_not_fit():
+    scalar = torch.tensor(3, dtype=torch.int32)
+    with pytest.raises(hyp.HyperionError) as e:
+        hyp._rows("hyp_op_attn_prefill_mod", "ctx_lens", scalar, torch.int32, scalar.get_device(), ())
+    assert e.value.code == hyp.HYP_EINVAL and "ctx_lens" in str(e.value)
+    assert hyp._rows("hyp_op_attn_prefill_mod", "ctx_lens", scalar[None], torch.int32, scalar.get_device(), ())[1] == 1
