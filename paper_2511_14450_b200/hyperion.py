@@ -515,10 +515,8 @@ class AttnMod:
 
     def check(self, where, shape3, n_seqs, dev):
         """The struct for a call with this head layout and batch; the tensors still have to be where they were."""
-        if self.slopes is not None:
-            self.struct.slopes = _dense(where, "slopes", self.slopes, _F32, dev, (shape3[0],))
-        if self.prefix_lens is not None:
-            self.struct.prefix_lens = _dense(where, "prefix_lens", self.prefix_lens, _I32, dev, (n_seqs,))
+        self.struct.slopes = None if self.slopes is None else _dense(where, "slopes", self.slopes, _F32, dev, (shape3[0],))
+        self.struct.prefix_lens = None if self.prefix_lens is None else _dense(where, "prefix_lens", self.prefix_lens, _I32, dev, (n_seqs,))
         return self.ref
 
 

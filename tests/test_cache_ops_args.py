@@ -156,3 +156,18 @@ def test_a_tensor_without_dimensions_is_refused_like_any_other_that_does_not_fit
         hyp._rows("hyp_op_attn_prefill_mod", "ctx_lens", scalar, torch.int32, scalar.get_device(), ())
     assert e.value.code == hyp.HYP_EINVAL and "ctx_lens" in str(e.value)
     assert hyp._rows("hyp_op_attn_prefill_mod", "ctx_lens", scalar[None], torch.int32, scalar.get_device(), ())[1] == 1
+
+
+def test_a_modification_follows_its_tensors():
+    """Slopes or prefixes that are taken out of a modification after it was made are not used any more (their memory may be gone)."""
+    hyp._shape((4, 2, 64))
+    slopes, prefix = torch.ones(4), torch.zeros(2, dtype=torch.int32)
+    mod = hyp.AttnMod(slopes=slopes, prefix_lens=prefix)
+    mod.check("hyp_op_attn_decode_mod", (4, 2, 64), 2, -1)
+    assert mod.struct.slopes == slopes.data_ptr() and mod.struct.prefix_lens == prefix.data_ptr()
+    mod.slopes = mod.prefix_lens = None
+    mod.check("hyp_op_attn_decode_mod", (4, 2, 64), 2, -1)
+    assert mod.struct.slopes is None and mod.struct.prefix_lens is None
+    mod.slopes = torch.ones(5)
+    with pytest.raises(hyp.HyperionError):
+        mod.check("hyp_op_attn_decode_mod", (4, 2, 64), 2, -1)
