@@ -873,6 +873,92 @@ def test_tables_much_wider_than_the_sequences(heads, lens):
     assert hyp.hyp_device_wait_status() == 0
 
 
+def partial_rows(heads, n, ng, prefix_pages, own_pages):
+    """Partial rows per (sequence, query head) that the scratch of a shared call is made for."""
+    return hyp.hyp_op_attn_shared_scratch_bytes(heads, n, ng, prefix_pages, own_pages) // (4 * n * heads[0] * (heads[2] + 2))
+
+
+def rereads(heads, n, prefix_pages):
+    """Bytes of prefix that every sequence would read for itself; row tiles take over above 32 MB (and 8 pages)."""
+    return n * heads[1] * prefix_pages * 64 * heads[2]
+
+
+def check_shared(heads, prefix, sizes, own, c, q, ot):
+    n, ng = len(own), len(prefix)
+    hq, hkv, d = heads
+    cu = torch.tensor([sum(sizes[:i]) for i in range(ng + 1)], dtype=torch.int32, device="cuda")
+    ctx = torch.tensor([o - 1 for o in own], dtype=torch.int32, device="cuda")
+    out = run_shared(heads, q, c, cu, c.table[:ng].contiguous(), torch.tensor(prefix, dtype=torch.int32, device="cuda"), ot, ctx)
+    group = [g for g, size in enumerate(sizes) for _ in range(size)]
+    for i in range(n):
+        k, v = torch.cat([c.k[group[i]], c.k[ng + i]]), torch.cat([c.v[group[i]], c.v[ng + i]])
+        if k.shape[0] == 0:
+            assert (out[i] == 0).all()
+            continue
+        want, _, bound, _ = reference(q[i:i + 1].reshape(1, hq, d), k, v, torch.ones(1, k.shape[0], dtype=torch.bool, device="cuda"))
+        close(out[i].view(1, hq, d), want, bound, (i, group[i], own[i]))
+    assert hyp.hyp_device_wait_status() == 0
+
+
+@pytest.mark.parametrize("order", ["growing", "falling", "spread"])
+def test_large_scores_through_the_row_tiles_and_their_join(order):
+    """Scores far apart, a maximum that moves along the prefix in either direction, shares whose maxima differ by far: enough
+    sequences that the prefix goes through row tiles."""
+    heads, n, l = (8, 2, 128), 64, 700
+    own = [[0, 1, 20, 40][i % 4] for i in range(n)]
+    c = Cache([l] + own, 2, 128, seed=61)
+    pages, ot = c.table.shape[1], c.table[1:, :4].contiguous()
+    assert rereads(heads, n, pages) > 32e6 and partial_rows(heads, n, 1, pages, 4) == 3 + 1      # three shares of the prefix, one own
+    scale = {"growing": torch.linspace(0.02, 1.0, l), "falling": torch.linspace(1.0, 0.02, l), "spread": torch.rand(l)}[order]
+    c.k[0] = (c.k[0] * scale.cuda().half()[:, None, None]).contiguous()
+    for p in range((l + 15) // 16):
+        put(c.pool, int(c.table[0, p]), 0, c.k[0][16 * p:16 * p + 16])
+    check_shared(heads, [l], [n], own, c, queries(n, 8, 128, seed=62, std=12.0), ot)
+
+
+@pytest.mark.parametrize("n,ng", [(70, 30), (1000, 2)])
+def test_more_row_tiles_than_fit_at_once(n, ng):
+    """At most 32 groups, but more (row tile, KV head) pairs than CTAs fit: a fixed number of shares."""
+    heads = (40, 10, 128)
+    rng = np.random.default_rng(n + ng)
+    prefix = [699] + [int(x) for x in rng.integers(0, 700, ng - 1)]
+    cuts = [0] + np.sort(rng.integers(0, n + 1, ng - 1)).tolist() + [n]
+    sizes = [b - a for a, b in zip(cuts, cuts[1:])]
+    own = [int(x) for x in rng.integers(0, 40, n)]
+    c = Cache(prefix + own, 10, 128, seed=n)
+    pages = c.table.shape[1]
+    # even shares would be three of the prefix; every sequence for itself would be one row
+    assert (n // 32 + ng) * 10 > 2 * 148 and rereads(heads, n, pages) > 32e6 and partial_rows(heads, n, ng, pages, 4) == 1 + 1
+    check_shared(heads, prefix, sizes, own, c, queries(n, 40, 128, seed=63), c.table[ng:, :4].contiguous())
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (40, 10, 128), (3, 3, 64)])
+@pytest.mark.parametrize("m", [dict(window=128, prefix=2000), dict(window=1, prefix=900, cap=20.0), dict(window=300, prefix=2500, slopes=True)])
+def test_a_long_visible_prefix_beside_a_window(heads, m):
+    """Decode and prompts whose window stands behind, in, or around the end of a long prefix."""
+    hq, hkv, d = heads
+    lens, new = [2600, 950, 2003, 120], [150, 33, 20, 120]
+    c = Cache(lens, hkv, d, seed=64)
+    mod, slopes, pre = make_mod(m, hq, len(lens))
+    q = queries(len(lens), hq, d, seed=65)
+    out = run_decode_mod(c, heads, q, torch.tensor([l - 1 for l in lens], dtype=torch.int32, device="cuda"), mod)
+    rows = queries(sum(new), hq, d, seed=66)
+    cu = torch.tensor([sum(new[:i]) for i in range(len(new) + 1)], dtype=torch.int32, device="cuda")
+    pout = torch.full((sum(new), hq * d), 7.0, dtype=torch.float16, device="cuda")
+    hyp.hyp_op_attn_prefill_mod(heads, mod, rows, c.pool, c.table, cu, torch.tensor([l - r for l, r in zip(lens, new)], dtype=torch.int32, device="cuda"),
+                                pout)
+    torch.cuda.synchronize()
+    for i, (l, r) in enumerate(zip(lens, new)):
+        mask, bias = mask_and_bias(torch.tensor([l - 1], device="cuda"), l, m, int(pre[i]), slopes)
+        want, _, bound, _ = reference(q[i:i + 1].reshape(1, hq, d), c.k[i], c.v[i], mask, m.get("cap", 0.0), bias)
+        close(out[i].view(1, hq, d), want, bound, (i, l))
+        a, b = int(cu[i]), int(cu[i + 1])
+        mask, bias = mask_and_bias(torch.arange(l - r, l, device="cuda"), l, m, int(pre[i]), slopes)
+        want, _, bound, _ = reference(rows[a:b].reshape(r, hq, d), c.k[i], c.v[i], mask, m.get("cap", 0.0), bias)
+        close(pout[a:b].view(r, hq, d), want, bound, (i, l, r))
+    assert hyp.hyp_device_wait_status() == 0
+
+
 @pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
 def test_tensors_of_another_device_than_the_current_one():
     """The call runs where its tensors are, and reports a wait that ran out to that device's own word."""
