@@ -17,6 +17,8 @@ bool shape_ok(const hyp_attn_shape* s) {
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 // Pages of a table row: token positions stay below 2^30, so that a position plus a tile never leaves 32 bits.
 bool pages_ok(int32_t n) { return n >= 1 && n <= (1 << 26); }
+// Sequences and groups: a dimension of the grid.
+bool count_ok(int32_t n) { return n >= 1 && n <= 65535; }
 bool mod_ok(const hyp_attn_mod* m) {
   // the cap's powers stay within fp32 and its rounding below that of the scores
   if (!m || !(m->softcap == 0.f || (m->softcap >= 0x1p-10f && m->softcap <= 0x1p20f))) return false;
@@ -41,7 +43,7 @@ int finish(int rc) {
 }  // namespace
 
 extern "C" size_t hyp_op_attn_mod_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq) {
-  if (!shape_ok(shape) || n_seqs < 1 || !pages_ok(max_pages_per_seq)) return 0;
+  if (!shape_ok(shape) || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return 0;
   return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim,
                                   paged_splits(n_seqs, shape->n_kv_heads, max_pages_per_seq));
 }
@@ -50,7 +52,7 @@ extern "C" int hyp_op_attn_decode_mod(const hyp_attn_shape* shape, const hyp_att
                                       int64_t q_stride, const void* kv_pages, const int32_t* block_table, int32_t max_pages_per_seq,
                                       const int32_t* ctx_lens, void* scratch, size_t scratch_bytes, void* out, void* stream) {
   if (!shape_ok(shape) || !mod_ok(mod) || !query_ok(shape, q, q_stride, out)) return HYP_EINVAL;
-  if (!kv_pages || !block_table || !ctx_lens || !scratch || n_seqs < 1 || n_seqs > 65535 || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
+  if (!kv_pages || !block_table || !ctx_lens || !scratch || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
   if (!aligned(kv_pages, 16) || !aligned(scratch, 16)) return HYP_EINVAL;
   if (scratch_bytes < hyp_op_attn_mod_scratch_bytes(shape, n_seqs, max_pages_per_seq)) return HYP_ECAPACITY;
   const int rc = tc_prepare();
@@ -72,7 +74,7 @@ extern "C" int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_at
 }
 
 extern "C" size_t hyp_op_attn_scored_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq) {
-  if (!shape_ok(shape) || n_seqs < 1 || !pages_ok(max_pages_per_seq)) return 0;
+  if (!shape_ok(shape) || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return 0;
   return 4 * (scored_scores_offset(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, max_pages_per_seq) +
               (size_t)n_seqs * shape->n_q_heads * 16 * (size_t)max_pages_per_seq);
 }
@@ -82,7 +84,7 @@ extern "C" int hyp_op_attn_decode_scored(const hyp_attn_shape* shape, int32_t n_
                                          const int32_t* ctx_lens, float decay, const float* weights_in, float* weights_out,
                                          int64_t weights_stride, void* scratch, size_t scratch_bytes, void* out, void* stream) {
   if (!shape_ok(shape) || !query_ok(shape, q, q_stride, out)) return HYP_EINVAL;
-  if (!kv_pages || !block_table || !ctx_lens || !weights_out || !scratch || n_seqs < 1 || n_seqs > 65535 || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
+  if (!kv_pages || !block_table || !ctx_lens || !weights_out || !scratch || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
   if (!aligned(kv_pages, 16) || !aligned(scratch, 16) || !aligned(weights_in, 4) || !aligned(weights_out, 4)) return HYP_EINVAL;
   if (!isfinite(decay) || weights_stride < 16 * (int64_t)max_pages_per_seq) return HYP_EINVAL;
   if (scratch_bytes < hyp_op_attn_scored_scratch_bytes(shape, n_seqs, max_pages_per_seq)) return HYP_ECAPACITY;
@@ -100,7 +102,7 @@ extern "C" int hyp_op_kv_evict(const hyp_attn_shape* shape, int32_t n_seqs, cons
                                int64_t weights_out_stride, void* stream) {
   if (!shape_ok(shape) || !kv_pages || !block_table || !n_cached || !weights_in || !dst_pages || !dst_table || !kept || !new_lens || !weights_out)
     return HYP_EINVAL;
-  if (n_seqs < 1 || n_seqs > 65535 || shape->n_kv_heads > 32767 || !pages_ok(max_pages_per_seq) || !pages_ok(dst_pages_per_seq)) return HYP_EINVAL;
+  if (!count_ok(n_seqs) || shape->n_kv_heads > 32767 || !pages_ok(max_pages_per_seq) || !pages_ok(dst_pages_per_seq)) return HYP_EINVAL;
   if (n_keep < 1 || n_sink < 0 || n_recent < 0 || n_sink > n_keep || n_recent > n_keep - n_sink) return HYP_EINVAL;
   if (16 * (int64_t)dst_pages_per_seq < n_keep || weights_stride < 16 * (int64_t)max_pages_per_seq || weights_out_stride < n_keep) return HYP_EINVAL;
   if (!aligned(kv_pages, 16) || !aligned(dst_pages, 16) || !aligned(weights_in, 4) || !aligned(weights_out, 4)) return HYP_EINVAL;
@@ -120,7 +122,7 @@ extern "C" int hyp_op_kv_evict(const hyp_attn_shape* shape, int32_t n_seqs, cons
 
 extern "C" size_t hyp_op_attn_shared_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t n_groups,
                                                    int32_t max_prefix_pages, int32_t max_pages_per_seq) {
-  if (!shape_ok(shape) || n_seqs < 1 || n_groups < 1 || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return 0;
+  if (!shape_ok(shape) || !count_ok(n_seqs) || !count_ok(n_groups) || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return 0;
   const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, n_groups, max_prefix_pages, max_pages_per_seq);
   return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim, p.prefix_splits + p.own_splits);
 }
@@ -132,7 +134,7 @@ extern "C" int hyp_op_attn_decode_shared(const hyp_attn_shape* shape, int32_t n_
                                          void* out, void* stream) {
   if (!shape_ok(shape) || !query_ok(shape, q, q_stride, out)) return HYP_EINVAL;
   if (!kv_pages || !cu_group || !prefix_table || !prefix_lens || !block_table || !ctx_lens || !scratch) return HYP_EINVAL;
-  if (n_seqs < 1 || n_seqs > 65535 || n_groups < 1 || n_groups > 65535 || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
+  if (!count_ok(n_seqs) || !count_ok(n_groups) || !pages_ok(max_prefix_pages) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
   if (!aligned(kv_pages, 16) || !aligned(scratch, 16)) return HYP_EINVAL;
   if (scratch_bytes < hyp_op_attn_shared_scratch_bytes(shape, n_seqs, n_groups, max_prefix_pages, max_pages_per_seq)) return HYP_ECAPACITY;
   const SharedPlan p = shared_plan(n_seqs, shape->n_q_heads, shape->n_kv_heads, shape->head_dim, n_groups, max_prefix_pages, max_pages_per_seq);

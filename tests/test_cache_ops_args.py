@@ -171,3 +171,13 @@ def test_a_modification_follows_its_tensors():
     mod.slopes = torch.ones(5)
     with pytest.raises(hyp.HyperionError):
         mod.check("hyp_op_attn_decode_mod", (4, 2, 64), 2, -1)
+
+
+def test_the_size_calls_refuse_the_counts_that_the_calls_refuse():
+    sh = (8, 2, 128)
+    for n in (65536, 2 ** 31 - 1, 0, -1):
+        assert hyp.hyp_op_attn_mod_scratch_bytes(sh, n, 4) == 0
+        assert hyp.hyp_op_attn_scored_scratch_bytes(sh, n, 4) == 0
+        assert hyp.hyp_op_attn_shared_scratch_bytes(sh, n, 1, 4, 4) == 0
+        assert hyp.hyp_op_attn_shared_scratch_bytes(sh, 3, n, 4, 4) == 0
+    assert hyp.hyp_op_attn_shared_scratch_bytes(sh, 65535, 65535, 4, 4) > 0
