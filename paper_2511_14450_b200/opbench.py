@@ -147,18 +147,19 @@ def attn_shared(batch, ctx, prefix, Hq=40, Hkv=10, D=128, iters=20):
             "kv_gbs": (batch * ctx + prefix) * 4 * Hkv * D / ms / 1e6}
 
 
-def kv_evict(batch, ctx, keep, Hq=40, Hkv=10, D=128, iters=20):
+def kv_evict(batch, ctx, keep, in_place=False, Hq=40, Hkv=10, D=128, iters=20):
+    """in_place: the rows move inside their own pages; the weights go elsewhere, so that every call moves the same rows."""
     pools, table = _cache(batch, ctx, Hkv, D, 2)
     kw = (keep + 15) // 16
     dst = torch.empty(batch * kw, 2, Hkv, 16, D, dtype=torch.float16, device="cuda")
-    dt = torch.randperm(batch * kw, device="cuda").to(torch.int32).view(batch, kw)
+    dt = table if in_place else torch.randperm(batch * kw, device="cuda").to(torch.int32).view(batch, kw)
     cached = torch.full((batch,), ctx, dtype=torch.int32, device="cuda")
     w = torch.rand(batch, Hkv, 16 * table.shape[1], device="cuda")
     wo, kept = torch.empty(batch, Hkv, keep, device="cuda"), torch.empty(batch, Hkv, keep, dtype=torch.int32, device="cuda")
     nl = torch.empty(batch, dtype=torch.int32, device="cuda")
-    ms = _time(lambda i: hyp.hyp_op_kv_evict((Hq, Hkv, D), pools[i % 2], table, cached, w, keep, min(4, keep // 4), keep // 8, dst, dt, kept,
-                                             nl, wo), iters)
-    return {"op": "kv_evict", "batch": batch, "ctx": ctx, "keep": keep, "us": ms * 1e3,
+    ms = _time(lambda i: hyp.hyp_op_kv_evict((Hq, Hkv, D), pools[i % 2], table, cached, w, keep, min(4, keep // 4), keep // 8,
+                                             pools[i % 2] if in_place else dst, dt, kept, nl, wo), iters)
+    return {"op": "kv_evict", "batch": batch, "ctx": ctx, "keep": keep, "in_place": in_place, "us": ms * 1e3,
             "gbs": 2 * batch * min(ctx, keep) * 4 * Hkv * D / ms / 1e6}
 
 
@@ -233,6 +234,7 @@ def main():
     ap.add_argument("--window", type=int, default=0, help="attn_*_mod: visible tokens behind the query (0 = all)")
     ap.add_argument("--prefix", type=int, default=2048, help="attn_shared: tokens of the shared prefix")
     ap.add_argument("--keep", type=int, default=512, help="kv_evict: tokens that stay")
+    ap.add_argument("--in-place", action="store_true", help="kv_evict: the kept rows stay in their own pages")
     a = ap.parse_args()
     if a.op == "gemm":
         out = [gemm(a.M, a.N, a.K, a.epi, a.iters)]
@@ -249,7 +251,7 @@ def main():
     elif a.op == "attn_shared":
         out = [attn_shared(a.batch, a.ctx, a.prefix, iters=a.iters)]
     elif a.op == "kv_evict":
-        out = [kv_evict(a.batch, a.ctx, a.keep, iters=a.iters)]
+        out = [kv_evict(a.batch, a.ctx, a.keep, a.in_place, iters=a.iters)]
     elif a.op == "decode_stage":
         out = [decode_stage(a.layers, a.batch, a.ctx, iters=a.iters, shape=a.shape)]
     else:
