@@ -216,8 +216,8 @@ HYP_API int hyp_op_attn_prefill(const hyp_attn_shape* shape, int32_t n_seqs, int
  * product as fp16 relative to a running maximum.
  * Decode calls take ctx_lens as hyp_op_attn_decode does: the new token sits at position ctx_lens[b] and its key and value
  * are already in the cache.  ctx_lens[b] = -1 marks a row that has nothing of its own to see (padding of a batch);
- * a row that sees nothing at all gives zeros.  Cache slots behind a sequence's end may hold anything.  Lengths are read
- * on the device and clamped to what the table's row can name (any value may stand there); in a prompt a row keeps its position
+ * a row that sees nothing at all gives zeros.  Cache slots behind a sequence's end may hold anything.  Lengths (ctx_lens, n_cached,
+ * prefix_lens) are read on the device and clamped to what the table's row can name, any value may stand there; in a prompt a row keeps its position
  * (up to 2^30) and sees those of its keys that the table names.  Table entries behind a sequence's end may hold anything:
  * they may be fetched, they are not followed.
  * All lengths and tables may change between replays of a captured graph; the shapes and sizes passed by value may not.
@@ -238,7 +238,8 @@ typedef struct {
   const int32_t* prefix_lens; /* DEVICE int32 [n_seqs] or NULL                                         */
 } hyp_attn_mod;
 
-/* hyp_op_attn_decode with modified scores; only the pages that hold visible keys are read.
+/* hyp_op_attn_decode with modified scores; only the pages that hold visible keys are read.  Beside a window the context is split
+ * for the window and a visible prefix of up to 256 tokens: few sequences behind a prefix of many thousands run below speed.
  * scratch: hyp_op_attn_mod_scratch_bytes(...) bytes (0 on bad arguments).
  * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
 HYP_API size_t hyp_op_attn_mod_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
@@ -248,7 +249,9 @@ HYP_API int hyp_op_attn_decode_mod(const hyp_attn_shape* shape, const hyp_attn_m
                                    void* out, void* stream);
 
 /* hyp_op_attn_prefill with modified scores (either head size runs on the tcgen05 tensor cores).  Sequences without new
- * rows (cu_q[i] = cu_q[i + 1]) are allowed.  Rows at or behind cu_q[n_seqs] are left as they were.
+ * rows (cu_q[i] = cu_q[i + 1]) are allowed.  Rows at or behind cu_q[n_seqs] are left as they were (cu_q[n_seqs] <= M).  Keys go by in
+ * steps of 64: pages beside the visible ones are read too, so a sequence's table has to name pages of finite values up to its
+ * end, also in front of a window.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (more than 2^31 CTAs), HYP_ECUDA. */
 HYP_API int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_attn_mod* mod, int32_t n_seqs, int32_t M,
                                     const void* q, int64_t q_stride, const void* kv_pages, const int32_t* block_table,
@@ -262,6 +265,8 @@ HYP_API int hyp_op_attn_prefill_mod(const hyp_attn_shape* shape, const hyp_attn_
  *   weights_in  DEVICE fp32 [n_seqs, n_kv_heads, weights_stride], or NULL (all zero)
  *   weights_out the same shape; may be weights_in itself, must not overlap it otherwise
  *   weights_stride >= 16 * max_pages_per_seq
+ * The scratch holds a score for every query head and key that the tables could name, and the sums are formed in as many pieces: for short
+ * sequences pass a narrow table.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
 HYP_API size_t hyp_op_attn_scored_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
 HYP_API int hyp_op_attn_decode_scored(const hyp_attn_shape* shape, int32_t n_seqs, const void* q, int64_t q_stride,
@@ -273,11 +278,12 @@ HYP_API int hyp_op_attn_decode_scored(const hyp_attn_shape* shape, int32_t n_seq
  * n_sink, the last n_recent and, of the others, those of the largest weight (ties: the lowest position; NaN counts as
  * -infinity); a sequence with n_cached[b] <= n_keep keeps all.  The kept tokens' keys, values and weights move, in their
  * order, to slots 0, 1, ... of the destination.  (Keys keep the rotation of their original position: the caller goes on
- * counting positions from there when it rotates the next query and key.)
+ * counting positions from there when it rotates the next query and key.  hyp_op_attn_decode_step takes a token's slot for its
+ * position, so it does not fit a cache that has been cut.)
  *   n_cached   DEVICE int32 [n_seqs]: tokens in the cache
  *   weights_in DEVICE fp32 [n_seqs, n_kv_heads, weights_stride], weights_stride >= 16 * max_pages_per_seq
  *   dst_pages, dst_table [n_seqs, dst_pages_per_seq]: where the kept rows go.  Either kv_pages and block_table themselves
- *              (in place: the pages behind the new length become free), or pages that are not among the source pages
+ *              (in place: the pages behind the new length become free; no page in two rows), or pages that are not among the source pages
  *              (of the same pool or of another one); 16 * dst_pages_per_seq >= n_keep
  *   kept       DEVICE int32 [n_seqs, n_kv_heads, n_keep]: the old slot of every kept token, -1 behind the new length
  *   new_lens   DEVICE int32 [n_seqs]: min(n_cached, n_keep); not n_cached itself

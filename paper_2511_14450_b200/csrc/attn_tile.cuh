@@ -239,7 +239,7 @@ __device__ __forceinline__ void at_softmax(uint32_t tmem_sb, uint32_t tmem_o, ui
   float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
   bool wide = false;
   if (CAP && !EXACT) {
-    // NaN (garbage behind the end of a sequence) compares false here and takes the exact form; it is masked there
+    // NaN (garbage behind the end of a sequence) is dropped by the maxima and removed by the mask below
     wide = !(max3(fmaxf(a4[0], a4[1]), a4[2], a4[3]) * sc.to_tanh <= TANH_RANGE);
     float top, same;
     up2(tanh2_small(pk2(mx, mx), sc.tanh_c), top, same);
