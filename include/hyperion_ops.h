@@ -311,6 +311,53 @@ HYP_API int hyp_op_attn_decode_shared(const hyp_attn_shape* shape, int32_t n_seq
                                       const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* ctx_lens,
                                       void* scratch, size_t scratch_bytes, void* out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * A decode step in few bits: weights in 4 bits, the cache in 8 (neither has a counterpart in the paper).
+ * --------------------------------------------------------------------------------------------- */
+enum { HYP_TYPE_F32 = 0, HYP_TYPE_F16 = 1, HYP_TYPE_BF16 = 2 };
+
+/* Microscaled 4-bit floating point.  Blocks of 32 values along a row (the last one may be shorter) share a power of two 2^(s - 127),
+ * one byte s; the values are E2M1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6, with a sign in the code's highest bit), two to a byte, the even
+ * column in the low half.
+ *   quantize    s - 127 = floor(log2 amax) - 2, at least -127 (amax = the block's largest magnitude); every value times 2^(127 - s) is
+ *               rounded to the nearest E2M1 number, ties to the even code, and saturates at 6.  A block of zeros gets s = 0, a block that holds
+ *               an infinity or NaN gets s = 255 and codes of 0: it reads back as NaN.
+ *   dequantize  the product, rounded once (fp16: values beyond +-65504 saturate; E2M1 times any power of two is exact in fp32 down to
+ *               2^-149, in bf16 down to 2^-133).
+ *   x, out  [N, K] of `type` (HYP_TYPE_*), rows x_stride / out_stride elements apart, 16-byte aligned; strides multiples of 8 (fp32: 4)
+ *   codes   uint8 [N, K / 2], 16-byte aligned;  scales uint8 [N, ceil(K / 32)]
+ * K a multiple of 8, N >= 1.  Errors: HYP_EINVAL, HYP_ECAPACITY (more than 2^31 CTAs), HYP_ECUDA. */
+HYP_API int hyp_op_mx4_quantize(const void* x, int32_t type, int32_t N, int32_t K, int64_t x_stride, void* codes, void* scales,
+                                void* stream);
+HYP_API int hyp_op_mx4_dequantize(const void* codes, const void* scales, int32_t N, int32_t K, int32_t type, void* out,
+                                  int64_t out_stride, void* stream);
+
+/* The copy of such a matrix that hyp_op_gemm_mx4 reads, made once: blocks of 128 rows x 128 k (8 KB of codes, 512 bytes of scales), zero
+ * padding to whole blocks.  swiglu != 0: codes and scales hold 2N rows, N gate rows then N up rows.
+ *   packed  at least hyp_op_mx4_packed_bytes(N, K, swiglu) bytes (0 on bad arguments), 128-byte aligned
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (packed_bytes too small, matrix too large), HYP_ECUDA. */
+HYP_API size_t hyp_op_mx4_packed_bytes(int32_t N, int32_t K, int32_t swiglu);
+HYP_API int hyp_op_mx4_pack(const void* codes, const void* scales, int32_t N, int32_t K, int32_t swiglu, void* packed,
+                            size_t packed_bytes, void* stream);
+
+/* Projection with 4-bit weights: acc[m, n] = sum_k a[m, k] * w[n, k], fp32 accumulation, then `epilogue` (HYP_EPI_*, 16-bit results in
+ * a's type; fp16 results saturate at +-65504).  The tensor cores take every activation as the sum of `terms` E4M3 numbers, each under a
+ * power of two of its own per row and block of 32 k: term 1 is a rounded to 4 significant bits, the next ones what is left.  terms = 3 holds
+ * fp16 values, terms = 2 bf16 values (up to 2^-17, for three terms 2^-25, of their block's largest magnitude); terms = 1 is an 8-bit
+ * product, off by up to 2^-4 of every activation.  The term's power of two is the least p with amax <= 448 p.
+ *   a         HYP_TYPE_F16 or HYP_TYPE_BF16 [M, K], rows a_stride elements apart (a multiple of 8), 16-byte aligned
+ *   w_packed  from hyp_op_mx4_pack for the same N, K and swiglu = (epilogue == HYP_EPI_SWIGLU_BF16)
+ *   out       [M, ldo], ldo >= N; HYP_EPI_RESID_F32 adds to it
+ *   scratch   at least hyp_op_gemm_mx4_scratch_bytes(M, K, terms) bytes (0 on bad arguments), 128-byte aligned; needs no initialisation;
+ *             calls whose kernels can overlap need one each
+ * M, N >= 1, K a multiple of 8, terms 1 .. 3.  An activation row that holds an infinity or NaN gives NaN, as does a weight row with a scale
+ * of 255.  The first call on a device allocates one word there for error reporting: make it before capturing a graph.  The weights are
+ * read ahead of the kernel launched before: w_packed is not to be written by that kernel (hyp_op_mx4_pack itself may come before).
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, matrix too large), HYP_ECUDA. */
+HYP_API size_t hyp_op_gemm_mx4_scratch_bytes(int32_t M, int32_t K, int32_t terms);
+HYP_API int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, const void* w_packed, int32_t M, int32_t N, int32_t K,
+                            int32_t terms, int32_t epilogue, void* out, int32_t ldo, void* scratch, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -891,6 +891,25 @@ int tc_make_pool_map(CUtensorMap* map, const void* pool, int D) {
   return HYP_OK;
 }
 
+// Lines of 128 four-bit codes.  The copy puts 16 codes (8 bytes) to every 16 bytes of shared memory, the form in which the 8-bit
+// tensor-core kinds take a four-bit operand; the box's inner extent is the 128 codes that this element type asks for.
+int tc_make_mx4_map(CUtensorMap* map, const void* packed, long long lines) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return HYP_ECUDA;
+  if (lines < 1 || lines > 0x7fffffffll || ((uintptr_t)packed & 127) != 0) return HYP_EINVAL;
+  const cuuint64_t dims[2] = {128, (cuuint64_t)lines};
+  const cuuint64_t strides[1] = {64};
+  const cuuint32_t box[2] = {128u, 128u};
+  const cuuint32_t estr[2] = {1u, 1u};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 2, (void*)packed, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_last_cuda_error((int)r);
+    return HYP_ECUDA;
+  }
+  return HYP_OK;
+}
+
 // Activations: 128-row boxes for the tile kernels, 16/32/64-row boxes for the swapped-operand kernel.
 int tc_make_act(TcAct* a, const void* ptr, int rows, int K, bool f16) {
   a->ptr = ptr; a->rows = rows; a->K = K; a->f16 = f16;

@@ -53,6 +53,8 @@ int tc_make_kv_map(CUtensorMap* map, const void* kv_layer, size_t n_pages, int H
 // Tensor maps of the row-tile attention: query rows by heads, and a page pool of either head size.
 int tc_make_q_map(CUtensorMap* map, const void* q, int rows, long long stride, int Hq, int G, int D);
 int tc_make_pool_map(CUtensorMap* map, const void* pool, int D);
+// Packed 4-bit weights as lines of 64 bytes: boxes of 128 lines, spread to one byte a code (128-byte swizzle) on their way.
+int tc_make_mx4_map(CUtensorMap* map, const void* packed, long long lines);
 // Prefill attention on tcgen05 (head_dim 128); q_map = TcAct::map of the rotated-query buffer.
 int& attn_prefill_tc_enabled();
 int launch_attn_prefill_tc(const CUtensorMap& q_map, const CUtensorMap& kv_map, __half* attn_out, const BatchMeta& bm,

@@ -107,6 +107,13 @@ SIGNATURES = {
     "hyp_op_attn_prefill": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                                       C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                       C.c_void_p]),
+    "hyp_op_mx4_quantize": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hyp_op_mx4_dequantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
+    "hyp_op_mx4_packed_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "hyp_op_mx4_pack": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hyp_op_gemm_mx4_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "hyp_op_gemm_mx4": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                  C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hyp_op_attn_mod_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32]),
     "hyp_op_attn_decode_mod": (C.c_int, [C.POINTER(hyp_attn_shape), C.POINTER(hyp_attn_mod), C.c_int32, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p,
@@ -609,6 +616,99 @@ def hyp_op_attn_decode_shared(shape3, q, kv_pages, cu_group, prefix_table, prefi
     op = _dense(where, "out", out, _F16, dev, (n, shape3[0] * shape3[2]))
     sp, sb = _scratch(where, scratch, dev)
     _launch(where, lib().hyp_op_attn_decode_shared, dev, stream, sh, n, qp, qs, pool, ng, cu, pt, pw, pl, table, width, ctx, sp, sb, op)
+
+
+# --------------------------------------------------------------------------------------------
+# operators in few bits (hyperion_ops.h): 4-bit weights.  Tensors are checked as those of the operators over the paged cache.
+# --------------------------------------------------------------------------------------------
+HYP_TYPE_F32, HYP_TYPE_F16, HYP_TYPE_BF16 = range(3)
+_U8 = None
+_TYPES = {}
+
+
+def _types():
+    """torch dtype -> HYP_TYPE_*"""
+    global _U8
+    if not _TYPES:
+        import torch
+        if _F16 is None:
+            _bind_torch()
+        _U8 = torch.uint8
+        _TYPES.update({torch.float32: HYP_TYPE_F32, torch.float16: HYP_TYPE_F16, torch.bfloat16: HYP_TYPE_BF16})
+    return _TYPES
+
+
+def _matrix(where, name, t):
+    """(device, type, rows, columns, address, row stride) of a matrix with dense rows, which may lie in a wider buffer."""
+    code = _types().get(t.dtype)
+    dev, s = t.get_device(), t.shape
+    if code is None or dev < 0 or len(s) != 2:
+        _refuse(where, f"{name} must be a CUDA matrix of fp32, fp16 or bf16, not {t.dtype} {tuple(s)} on {t.device}")
+    stride, one = t.stride()
+    if (one != 1 and s[1] > 1) or (stride < s[1] and s[0] > 1):
+        _refuse(where, f"{name} must have dense rows that do not overlap, not strides {t.stride()}")
+    return dev, code, s[0], s[1], t.data_ptr(), stride if s[0] > 1 else (s[1] + 7) // 8 * 8
+
+
+def hyp_op_mx4_quantize(x, codes, scales, stream=None):
+    """x [N, K] fp32, fp16 or bf16 -> codes uint8 [N, K / 2], scales uint8 [N, ceil(K / 32)]."""
+    where = "hyp_op_mx4_quantize"
+    dev, code, n, k, xp, xs = _matrix(where, "x", x)
+    cp = _dense(where, "codes", codes, _U8, dev, (n, k // 2))
+    sp = _dense(where, "scales", scales, _U8, dev, (n, (k + 31) // 32))
+    _launch(where, lib().hyp_op_mx4_quantize, dev, stream, xp, code, n, k, xs, cp, sp)
+
+
+def hyp_op_mx4_dequantize(codes, scales, out, stream=None):
+    """codes uint8 [N, K / 2], scales uint8 [N, ceil(K / 32)] -> out [N, K] fp32, fp16 or bf16."""
+    where = "hyp_op_mx4_dequantize"
+    dev, code, n, k, op, os_ = _matrix(where, "out", out)
+    cp = _dense(where, "codes", codes, _U8, dev, (n, k // 2))
+    sp = _dense(where, "scales", scales, _U8, dev, (n, (k + 31) // 32))
+    _launch(where, lib().hyp_op_mx4_dequantize, dev, stream, cp, sp, n, k, code, op, os_)
+
+
+def hyp_op_mx4_packed_bytes(N: int, K: int, swiglu: bool) -> int:
+    return lib().hyp_op_mx4_packed_bytes(N, K, int(swiglu))
+
+
+def hyp_op_mx4_pack(codes, scales, swiglu: bool = False, stream=None):
+    """The packed copy (a uint8 tensor) of codes [N, K / 2] and scales [N, ceil(K / 32)], for hyp_op_gemm_mx4; SwiGLU: 2N rows of
+    each, gate rows then up rows."""
+    import torch
+    where = "hyp_op_mx4_pack"
+    _types()
+    dev, s = codes.get_device(), codes.shape
+    if dev < 0 or len(s) != 2 or (swiglu and s[0] % 2):
+        _refuse(where, f"codes must be a CUDA matrix{' of an even number of rows' if swiglu else ''}, not {tuple(s)} on {codes.device}")
+    n, k = s[0] // 2 if swiglu else s[0], 2 * s[1]
+    cp = _dense(where, "codes", codes, _U8, dev, s)
+    sp = _dense(where, "scales", scales, _U8, dev, (s[0], (k + 31) // 32))
+    nbytes = hyp_op_mx4_packed_bytes(n, k, swiglu)
+    if not nbytes:
+        _refuse(where, f"no matrix of {n} rows and {k} columns")
+    packed = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    _launch(where, lib().hyp_op_mx4_pack, dev, stream, cp, sp, n, k, int(swiglu), packed.data_ptr(), nbytes)
+    return packed
+
+
+def hyp_op_gemm_mx4_scratch_bytes(M: int, K: int, terms: int) -> int:
+    return lib().hyp_op_gemm_mx4_scratch_bytes(M, K, terms)
+
+
+def hyp_op_gemm_mx4(a, w_packed, N: int, terms: int, epilogue: int, out, scratch, stream=None):
+    """a [M, K] fp16 or bf16, w_packed from hyp_op_mx4_pack, out [M, >= N] (fp32, or a's type for the 16-bit epilogues)."""
+    where = "hyp_op_gemm_mx4"
+    dev, code, m, k, ap, as_ = _matrix(where, "a", a)
+    odev, ocode, om, on, op, os_ = _matrix(where, "out", out)
+    swiglu = epilogue == HYP_EPI_SWIGLU_BF16
+    if odev != dev or om != m or on < N or ocode != (code if swiglu or epilogue == HYP_EPI_STORE_BF16 else HYP_TYPE_F32):
+        _refuse(where, f"out {out.dtype} {tuple(out.shape)} on {out.device} does not fit {m} rows of {N} results of epilogue {epilogue}")
+    nbytes = hyp_op_mx4_packed_bytes(N, k, swiglu)
+    if w_packed.dtype is not _U8 or w_packed.get_device() != dev or not w_packed.is_contiguous() or w_packed.nbytes < max(nbytes, 1):
+        _refuse(where, f"w_packed must be the uint8 tensor that hyp_op_mx4_pack gives for {N} x {k} on device {dev}")
+    sp, sb = _scratch(where, scratch, dev)
+    _launch(where, lib().hyp_op_gemm_mx4, dev, stream, ap, code, as_, w_packed.data_ptr(), m, N, k, terms, epilogue, op, max(os_, on), sp, sb)
 
 
 # --------------------------------------------------------------------------------------------
