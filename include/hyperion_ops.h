@@ -358,6 +358,52 @@ HYP_API size_t hyp_op_gemm_mx4_scratch_bytes(int32_t M, int32_t K, int32_t terms
 HYP_API int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, const void* w_packed, int32_t M, int32_t N, int32_t K,
                             int32_t terms, int32_t epilogue, void* out, int32_t ldo, void* scratch, size_t scratch_bytes, void* stream);
 
+/* The paged cache in 8 bits.  Pool uint8 [n_pages][2 (K then V)][n_kv_heads][16 * head_dim + 64], 16-byte aligned: a half page of a head
+ * is 16 token rows of head_dim one-byte codes, then the 16 tokens' scales (fp32).  At head_dim 128 the 16-byte chunk c of slot t's row
+ * sits at chunk position c ^ (4 * (t & 1)).
+ *   HYP_KV8_INT8  value = (code - 128) * scale; scale = amax / 127 rounded to fp32 (amax = the row's largest magnitude), code - 128 the
+ *                 integer nearest to value / scale, ties to even
+ *   HYP_KV8_E4M3  value = code * scale; scale = the least power of two p with amax <= 448 p, code the E4M3 number nearest to value / scale,
+ *                 ties to even
+ * A row with amax < 2^-118 is zeros under a scale of 0; one that holds an infinity or NaN gets a NaN scale: it reads back as NaN.
+ * Lengths, tables and streams as for the operators over the fp16 cache above. */
+enum { HYP_KV8_INT8 = 0, HYP_KV8_E4M3 = 1 };
+
+/* Appends M new rows, packed sequence by sequence as hyp_op_attn_prefill takes them (a decode step: one row each): sequence i owns rows
+ * cu_q[i] .. cu_q[i+1]-1 at positions ctx_lens[i], ctx_lens[i] + 1, ...; keys and values are quantised and written, queries go to q_out.
+ *   qkv         [M, stride] of `type` (HYP_TYPE_*): [Q heads | K heads | V heads], stride >= (n_q_heads + 2 n_kv_heads) * head_dim, a
+ *               multiple of 8, 16-byte aligned
+ *   rope_table  fp32 [rope_positions, head_dim / 2, 2] (cos, sin), 16-byte aligned: queries and keys are rotated (pairs i, i + head_dim / 2)
+ *               first, the keys with one rounding to 53 bits, so that a code is that of the exact rotation; NULL: they are rotated already
+ *               (rope_positions is ignored).  A position at or behind rope_positions takes the last row's angles, a negative one the first's.
+ *   q_out       fp16 [M, n_q_heads * head_dim], 16-byte aligned, values beyond +-65504 saturate; NULL: the queries are not read
+ * A row whose position is negative or behind what the table's row can name writes no key and value (ctx_lens = -1: padding of a decode
+ * batch); rows at or behind cu_q[n_seqs] (<= M) are not touched.  The pages of the new positions must be listed in the table.
+ * n_seqs <= 65535, n_kv_heads <= 32767.  Errors: HYP_EINVAL, HYP_ECUDA. */
+HYP_API int hyp_op_kv8_write(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, int32_t M, const void* qkv, int32_t type,
+                             int64_t stride, const float* rope_table, int32_t rope_positions, void* kv8_pages,
+                             const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* cu_q, const int32_t* ctx_lens,
+                             void* q_out, void* stream);
+
+/* Tokens first[i] .. lens[i] - 1 of every sequence to the same slots of fp16 pages (the layout at the top of this file), for prefill attention
+ * and the other operators over the fp16 cache.  Values are code times scale rounded once; beyond +-65504 they saturate.
+ *   first  DEVICE int32 [n_seqs] or NULL (0);  lens DEVICE int32 [n_seqs]; both clamped to what both tables' rows can name
+ *   dst_pages fp16 pool, 16-byte aligned;  dst_table int32 [n_seqs, dst_pages_per_seq].  Other slots are left as they were.
+ * Errors: HYP_EINVAL, HYP_ECUDA. */
+HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* kv8_pages, const int32_t* block_table,
+                            int32_t max_pages_per_seq, const int32_t* first, const int32_t* lens, void* dst_pages,
+                            const int32_t* dst_table, int32_t dst_pages_per_seq, void* stream);
+
+/* hyp_op_attn_decode over the 8-bit cache (keys and values 0 .. ctx_lens[b], the new token's included; -1: nothing, the row is zeros).
+ * The softmax weights, times their values' scales, enter the value product as fp16 relative to (2^-8 of) the largest so far; results beyond
+ * fp16 are infinities.  A key or value row with a NaN scale makes its sequence's results NaN, unless its weight is 0 in fp32.
+ * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
+HYP_API size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
+HYP_API int hyp_op_attn_decode_kv8(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* q, int64_t q_stride,
+                                   const void* kv8_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                                   const int32_t* ctx_lens, void* scratch, size_t scratch_bytes, void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,411 @@
+// Decode attention of one new token per sequence over the 8-bit paged cache.
+//
+// A CTA takes one (split, KV head, sequence); the pages go round-robin over the splits and, inside the CTA, over the warps.  Every warp
+// streams its pages through a ring of bulk copies (a half page of one head is one run: codes and scales) and forms, with no CTA-wide
+// step, S^T = K Q^T and O^T += V^T P^T on mma.sync.m16n8k16: the page's 16 keys, or 16 of the head's dimensions, are the operand of 16
+// rows and the (up to eight) query heads of the KV head that of eight columns, so that no row of an instruction is idle.
+//   Codes become fp16 on their way to the operand registers: offset codes by a byte permute that puts them below the exponent of
+//   1024 and one packed subtraction, E4M3 by the hardware conversion; both exact.  The order of the dimensions inside a product is that
+//   in which a lane reads 16 bytes of a key's row; the queries are fetched in the same order.
+//   A key's scale multiplies its score in fp32.  A value's scale goes into its weight: w = p * scale * 2^(m - m2), with references m for
+//   the scores and m2 for score + log2(scale), so that the fp16 weights are relative to the largest one, whatever the scales are.
+//   Both references move only when a weight outgrows 2^8 (one vote a page instead of shuffles and a rescaled O).
+// Weights are rounded to fp16 (2^-11 of each); sums, references and O are fp32.  Bound by HBM.
+#include "attn_paged.cuh"
+#include "cache_ops.cuh"
+#include "kv8.cuh"
+#include "mx4.cuh"
+
+namespace hyp {
+
+namespace {
+
+constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32, K8_SLOTS = 4;
+constexpr float K8_GROWN = 256.f;
+
+struct Kv8Args {
+  const __half* q;  // row b at q + b * q_stride
+  long long q_stride;
+  const uint8_t* pool;
+  const int32_t* table;
+  int table_stride;
+  const int32_t* ctx;
+  int Hq, Hkv;
+  float* acc;  // partial rows ((b * Hq + h) * n_slots + split) * D, their (maximum, denominator) in ml
+  float* ml;
+  int n_slots, wave_splits;
+  __half* out;  // one split, or a cluster: the result itself
+  int* err;
+};
+
+template <int D>
+constexpr int kv8_smem() { return K8_WARPS * K8_SLOTS * 2 * kv8_half_page(D); }
+
+// Four codes of one row to two operand registers: (0, 1) and (2, 3).
+template <int FMT>
+__device__ __forceinline__ void key_pair(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (FMT == HYP_KV8_INT8) {
+    const __half2 bias = __half2half2(__ushort_as_half(0x6480));  // 1152
+    uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  } else {
+    lo = e4m3x2_to_half2(w & 0xffffu);
+    hi = e4m3x2_to_half2(w >> 16);
+  }
+}
+// Two dimensions of two tokens, bytes (t0 d0, t0 d1, t1 d0, t1 d1), to the token pairs of d0 and of d1.
+template <int FMT>
+__device__ __forceinline__ void value_pair(uint32_t w, uint32_t& d0, uint32_t& d1) {
+  if (FMT == HYP_KV8_INT8) {
+    const __half2 bias = __half2half2(__ushort_as_half(0x6480));
+    uint32_t a = __byte_perm(w, 0x64646464u, 0x4240), b = __byte_perm(w, 0x64646464u, 0x4341);
+    const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), bias), y = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+    d0 = *reinterpret_cast<const uint32_t*>(&x);
+    d1 = *reinterpret_cast<const uint32_t*>(&y);
+  } else {
+    const uint32_t t = __byte_perm(w, 0u, 0x3120);
+    d0 = e4m3x2_to_half2(t & 0xffffu);
+    d1 = e4m3x2_to_half2(t >> 16);
+  }
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ float lds32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+  return v;
+}
+
+template <int D, int G, int FMT, bool CLUSTER>
+__global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
+  constexpr int KS = D / 16, HALF = kv8_half_page(D), SLOT = 2 * HALF;
+  extern __shared__ __align__(128) uint8_t k8_smem[];
+  __shared__ uint64_t bars[K8_WARPS * K8_SLOTS];
+  static_assert(kv8_smem<D>() >= (2 * K8_WARPS * 8 + K8_WARPS * G * D + 16 + G * D + 128) * 4, "the combine buffers reuse the ring");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, tq = lane & 3;
+  const int split = blockIdx.x, n_splits = gridDim.x, kvh = blockIdx.y, b = blockIdx.z;
+  pdl_wait();     // queries, lengths and cache rows may come from the kernel launched just before
+  pdl_trigger();
+
+  const int32_t* bt = a.table + (long long)b * a.table_stride;
+  int32_t ids_cur = 0;  // page ids of this warp's next 32 pages, one a lane; the first ones do not wait for the length
+  {
+    const int v = split + n_splits * (warp + K8_WARPS * lane);
+    if (v < a.table_stride) ids_cur = bt[v];
+  }
+  const int total = paged_total(a.ctx[b], a.table_stride), n_pages = (total + PG_PT - 1) / PG_PT;
+  // a shorter sequence uses no more splits than the plan's rule gives for its own length
+  const int fair = max(a.wave_splits, (n_pages + 15) / 16);
+  const int used = n_pages > 64 * a.wave_splits ? n_splits : max(min(min(n_splits, fair), (n_pages + K8_WARPS - 1) / K8_WARPS), 1);
+  if (!CLUSTER && split >= used) {
+    if (tid < G) *reinterpret_cast<float2*>(a.ml + (((size_t)b * a.Hq + kvh * G + tid) * a.n_slots + split) * 2) = make_float2(PG_NEG, 0.f);
+    return;
+  }
+  const int first = split + used * warp, stride_p = used * K8_WARPS;
+  const int my_n = split < used && first < n_pages ? (n_pages - first + stride_p - 1) / stride_p : 0;
+  auto load_ids = [&](int base) { return base + lane < my_n ? bt[first + stride_p * (base + lane)] : 0; };
+  if (used != n_splits) ids_cur = load_ids(0);
+  int32_t ids_next = load_ids(32);
+  const uint32_t my_bars = smem_u32(bars) + 8u * (warp * K8_SLOTS), my_ring = smem_u32(k8_smem) + (uint32_t)(warp * K8_SLOTS) * SLOT;
+  auto issue = [&](int i, int slot) {  // all lanes call, i ascending
+    if (i > 0 && (i & 31) == 0) {
+      ids_cur = ids_next;
+      ids_next = load_ids(i + 32);
+    }
+    const int page = __shfl_sync(0xffffffffu, ids_cur, i & 31);
+    if (lane == 0) {
+      const uint32_t dst = my_ring + slot * SLOT, bar = my_bars + 8u * slot;
+      mbar_expect_tx(bar, SLOT);
+      bulk_load(dst, a.pool + kv8_half_offset(page, 0, kvh, a.Hkv, D), HALF, bar);
+      bulk_load(dst + HALF, a.pool + kv8_half_offset(page, 1, kvh, a.Hkv, D), HALF, bar);
+    }
+  };
+  if (lane == 0) {
+    for (int s = 0; s < K8_SLOTS; ++s) mbar_init(my_bars + 8u * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  for (int s = 0; s < K8_SLOTS && s < my_n; ++s) issue(s, s);
+
+  // queries: column g of the operand, four dimensions a product in the order of the keys' bytes
+  uint32_t qf[KS][2];
+  {
+    const __half* qrow = a.q + (long long)b * a.q_stride + (size_t)(kvh * G + (g < G ? g : 0)) * D;
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      const uint2 x = *reinterpret_cast<const uint2*>(qrow + 64 * (j / 4) + 16 * tq + 4 * (j % 4));
+      qf[j][0] = g < G ? x.x : 0u;
+      qf[j][1] = g < G ? x.y : 0u;
+    }
+  }
+  const float sl2 = rsqrtf((float)D) * PG_LOG2E;
+  float o[KS][4];  // 16-byte chunk c of the head: (dims 16c + 2g, + 1) x (heads 2tq, 2tq + 1)
+#pragma unroll
+  for (int c = 0; c < KS; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
+  float m[2] = {PG_NEG, PG_NEG}, m2[2] = {PG_NEG, PG_NEG}, f[2] = {1.f, 1.f}, l[2] = {0.f, 0.f};  // of heads 2tq, 2tq + 1
+
+  bool ok = true;
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int i = 0; i < my_n; ++i) {
+    if (!mbar_wait(my_bars + 8u * slot, phase, nullptr)) { ok = false; break; }
+    const uint32_t kt = my_ring + slot * SLOT, vt = kt + HALF;
+    const int k0 = (first + stride_p * i) * PG_PT;
+    const bool partial = k0 + PG_PT > total;
+    if (FMT == HYP_KV8_E4M3 && partial) {  // a code behind the end may be a NaN, and a weight of 0 times NaN is not 0
+      for (int e = lane; e < D; e += 32)
+        if (k0 + e / (D / 16) >= total) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (uint32_t)e * 16u), "r"(0u) : "memory");
+      __syncwarp();
+    }
+    // scores of keys g and g + 8 for heads 2tq, 2tq + 1
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) {
+      const uint32_t at = kt + g * D + kv8_chunk<D>(tq + 4 * h, g);  // slots g and g + 8 have the same parity
+      const uint4 x = lds128(at), y = lds128(at + 8 * D);
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t a0, a1, a2, a3;
+        key_pair<FMT>(xw[j], a0, a2);
+        key_pair<FMT>(yw[j], a1, a3);
+        mma_f16_16816(s, a0, a1, a2, a3, qf[4 * h + j][0], qf[4 * h + j][1]);
+      }
+    }
+    const uint32_t sc = kt + 16 * D + 4 * g;
+    const float ks0 = lds32(sc) * sl2, ks1 = lds32(sc + 32) * sl2;
+    const float vs0 = lds32(sc + HALF), vs1 = lds32(sc + HALF + 32);
+    const bool see0 = !partial || k0 + g < total, see1 = !partial || k0 + g + 8 < total;
+    float v[4], p[4], w[4];  // (key g, head 2tq), (g, 2tq + 1), (g + 8, 2tq), (g + 8, 2tq + 1)
+    bool grown = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool see = e < 2 ? see0 : see1;
+      v[e] = s[e] * (e < 2 ? ks0 : ks1);
+      p[e] = see ? ex2_approx(v[e] - m[e & 1]) : 0.f;
+      w[e] = p[e] != 0.f ? p[e] * ((e < 2 ? vs0 : vs1) * f[e & 1]) : 0.f;
+      grown = grown || p[e] > K8_GROWN || w[e] > K8_GROWN;
+    }
+    if (__any_sync(0xffffffffu, grown)) {  // new references: the largest score, the largest score + log2(scale)
+      // (values whose scale is below 2^-64 are zeros in fp16)
+      const float lv0 = fmaxf(lg2_approx(vs0), -64.f), lv1 = fmaxf(lg2_approx(vs1), -64.f);
+      float corr2[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float top = fmaxf(see0 ? v[h] : PG_NEG, see1 ? v[2 + h] : PG_NEG);
+        float top2 = fmaxf(see0 ? v[h] + lv0 : PG_NEG, see1 ? v[2 + h] + lv1 : PG_NEG);
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
+        }
+        top = fmaxf(top, m[h]);
+        top2 = fmaxf(top2, m2[h]);
+        l[h] *= ex2_approx(m[h] - top);
+        corr2[h] = ex2_approx(m2[h] - top2);
+        m[h] = top;
+        m2[h] = top2;
+        f[h] = ex2_approx(top - top2);
+      }
+#pragma unroll
+      for (int c = 0; c < KS; ++c) {
+        o[c][0] *= corr2[0]; o[c][2] *= corr2[0];
+        o[c][1] *= corr2[1]; o[c][3] *= corr2[1];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool see = e < 2 ? see0 : see1;
+        p[e] = see ? ex2_approx(v[e] - m[e & 1]) : 0.f;
+        w[e] = p[e] != 0.f ? p[e] * ((e < 2 ? vs0 : vs1) * f[e & 1]) : 0.f;
+      }
+    }
+    l[0] += p[0] + p[2];
+    l[1] += p[1] + p[3];
+    const uint32_t b0 = transpose_8x8(pack_f16(w[0], w[1])), b1 = transpose_8x8(pack_f16(w[2], w[3]));
+#pragma unroll
+    for (int c2 = 0; c2 < KS / 2; ++c2) {
+      const int t = lane & 15;  // slots 0-7 and 8-15 of chunk 2 c2, then of the next one
+      uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+      ldsm_x4_t(vt + t * D + kv8_chunk<D>(2 * c2 + (lane >> 4), t), r0, r1, r2, r3);
+      value_pair<FMT>(r0, a0, a1);
+      value_pair<FMT>(r1, a2, a3);
+      mma_f16_16816(o[2 * c2], a0, a1, a2, a3, b0, b1);
+      value_pair<FMT>(r2, a0, a1);
+      value_pair<FMT>(r3, a2, a3);
+      mma_f16_16816(o[2 * c2 + 1], a0, a1, a2, a3, b0, b1);
+    }
+    __syncwarp();  // every lane's reads of the slot are done; hand it back to the copy engine
+    if (i + K8_SLOTS < my_n) issue(i + K8_SLOTS, slot);
+    if (++slot == K8_SLOTS) { slot = 0; phase ^= 1u; }
+  }
+  if (!ok) {
+    if (lane == 0) atomicCAS(a.err, 0, 34);
+    for (int s = 0; s < K8_SLOTS; ++s) mbar_wait(my_bars + 8u * s, 0, nullptr), mbar_wait(my_bars + 8u * s, 1, nullptr);
+  }
+  __syncthreads();  // every warp is done with its ring: the space is reused below
+
+  float* sm_m = reinterpret_cast<float*>(k8_smem);  // [warps][8]
+  float* sm_l = sm_m + K8_WARPS * 8;
+  float* sm_o = sm_l + K8_WARPS * 8;                // [warps][G][D]
+  float *ex_m = sm_o + K8_WARPS * G * D, *ex_l = ex_m + 8, *ex_o = ex_l + 8;  // CLUSTER: this CTA's result, read by its peers
+  float *all_m = ex_o + G * D, *all_l = all_m + 64;                           // CLUSTER: every CTA's, [head][split]
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
+    const float back = ex2_approx(m2[h] - m[h]);  // O in units of 2^m
+    const int head = 2 * tq + h;
+    if (head < G) {
+      if (g == 0) {
+        sm_m[warp * 8 + head] = m[h];
+        sm_l[warp * 8 + head] = l[h];
+      }
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        *reinterpret_cast<float2*>(sm_o + (warp * G + head) * D + 16 * c + 2 * g) = make_float2(o[c][h] * back, o[c][2 + h] * back);
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < G * D; e += K8_THREADS) {
+    const int gq = e / D, dd = e % D;
+    float mx = PG_NEG;
+#pragma unroll
+    for (int w = 0; w < K8_WARPS; ++w) mx = fmaxf(mx, sm_m[w * 8 + gq]);
+    float lsum = 0.f, acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < K8_WARPS; ++w) {
+      const float wgt = ex2_approx(sm_m[w * 8 + gq] - mx);
+      lsum += wgt * sm_l[w * 8 + gq];
+      acc += wgt * sm_o[(w * G + gq) * D + dd];
+    }
+    if (CLUSTER) {
+      ex_o[e] = acc;
+      if (dd == 0) {
+        ex_m[gq] = mx;
+        ex_l[gq] = lsum;
+      }
+    } else if (a.out) {
+      a.out[((size_t)b * a.Hq + kvh * G + gq) * D + dd] = __float2half_rn(lsum != 0.f ? acc / lsum : 0.f);
+    } else {
+      const size_t row = ((size_t)b * a.Hq + kvh * G + gq) * a.n_slots + split;
+      a.acc[row * D + dd] = acc;
+      if (dd == 0) *reinterpret_cast<float2*>(a.ml + row * 2) = make_float2(mx, lsum);
+    }
+  }
+  if (CLUSTER) {
+    __syncthreads();
+    cluster_barrier();
+    if (tid < G * n_splits) {  // loads from a peer have a long latency: every thread asks for all of its own at once
+      const int gq = tid / n_splits, sp = tid % n_splits;
+      const float mv = ld_cluster_f32(smem_u32(ex_m + gq), sp), lv = ld_cluster_f32(smem_u32(ex_l + gq), sp);
+      all_m[gq * 8 + sp] = mv;
+      all_l[gq * 8 + sp] = lv;
+    }
+    __syncthreads();
+    const int per = (G * D + n_splits - 1) / n_splits, e1 = min(G * D, (split + 1) * per);
+    for (int e = split * per + tid; e < e1; e += K8_THREADS) {
+      const int gq = e / D;
+      float ov[8];
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp) ov[sp] = sp < n_splits ? ld_cluster_f32(smem_u32(ex_o + e), sp) : 0.f;
+      float mx = PG_NEG, lsum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp)
+        if (sp < n_splits) mx = fmaxf(mx, all_m[gq * 8 + sp]);
+#pragma unroll
+      for (int sp = 0; sp < 8; ++sp)
+        if (sp < n_splits) {
+          const float wgt = ex2_approx(all_m[gq * 8 + sp] - mx);
+          lsum += wgt * all_l[gq * 8 + sp];
+          acc += wgt * ov[sp];
+        }
+      a.out[((size_t)b * a.Hq + kvh * G) * D + e] = __float2half_rn(lsum != 0.f ? acc / lsum : 0.f);
+    }
+    cluster_barrier();  // nobody leaves while a peer may still read its result
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots,
+                                                                  __half* __restrict__ out) {
+  __shared__ float sm[MERGE_THREADS / 32 * D];
+  pdl_wait();
+  pdl_trigger();
+  const size_t row = blockIdx.x;  // b * Hq + h
+  paged_merge_row<D>(acc, ml, row * n_slots, n_slots, out + row * D, sm);
+}
+
+template <int D, int G, int FMT, bool CLUSTER>
+int launch_one(const Kv8Args& a, int n_splits, int n_seqs, cudaStream_t st) {
+  constexpr int smem = kv8_smem<D>();
+  const int rc = allow_smem<attn_kv8_kernel<D, G, FMT, CLUSTER>>(smem);
+  if (rc) return rc;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n_splits, a.Hkv, n_seqs);
+  cfg.blockDim = dim3(K8_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = pdl_level() >= 2;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = n_splits;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CLUSTER ? 2 : 1;
+  HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, attn_kv8_kernel<D, G, FMT, CLUSTER>, a));
+  return 1;
+}
+
+template <int D, int G, int FMT>
+int launch_joined(Kv8Args a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
+  const bool cluster = n_splits >= 2 && n_splits <= 8 && (long long)n_splits * a.Hkv * n_seqs <= 3ll * sm_count();
+  if (n_splits == 1 || cluster) a.out = out;
+  if (cluster) return launch_one<D, G, FMT, true>(a, n_splits, n_seqs, st);
+  const int rc = launch_one<D, G, FMT, false>(a, n_splits, n_seqs, st);
+  if (rc < 0 || n_splits == 1) return rc;
+  HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_kernel<D>, dim3((unsigned)(n_seqs * a.Hq)), dim3(MERGE_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
+  return rc + 1;
+}
+
+template <int D, int G>
+int launch_fmt(const Kv8Args& a, int fmt, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
+  return fmt == HYP_KV8_INT8 ? launch_joined<D, G, HYP_KV8_INT8>(a, n_splits, n_seqs, out, st)
+                             : launch_joined<D, G, HYP_KV8_E4M3>(a, n_splits, n_seqs, out, st);
+}
+
+}  // namespace
+
+int launch_attn_kv8(const Kv8View& c, const __half* q, long long q_stride, const int32_t* ctx, float* scratch, __half* out, int* err,
+                    cudaStream_t st) {
+  const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride), G = c.Hq / c.Hkv;
+  Kv8Args a{};
+  a.q = q; a.q_stride = q_stride; a.pool = c.pool; a.table = c.table; a.table_stride = c.table_stride; a.ctx = ctx;
+  a.Hq = c.Hq; a.Hkv = c.Hkv;
+  a.acc = scratch; a.ml = scratch + (size_t)c.n_seqs * c.Hq * ns * c.D; a.n_slots = ns;
+  const int wave = (int)(3 * sm_count() / ((long long)c.n_seqs * c.Hkv));
+  a.wave_splits = wave < 1 ? 1 : wave;
+  a.err = err;
+#define HYP_F(DD, GG) if (c.D == DD && G == GG) return launch_fmt<DD, GG>(a, c.fmt, ns, c.n_seqs, out, st);
+  HYP_F(128, 1) HYP_F(128, 2) HYP_F(128, 4) HYP_F(128, 8) HYP_F(64, 1) HYP_F(64, 2) HYP_F(64, 4) HYP_F(64, 8)
+#undef HYP_F
+  return HYP_EINVAL;
+}
+
+}  // namespace hyp

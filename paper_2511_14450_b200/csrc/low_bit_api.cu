@@ -1,5 +1,7 @@
 // C entry points of the operators in few bits: argument checks, then the launchers.
+#include "cache_ops.cuh"
 #include "gemm_tc.cuh"
+#include "kv8.cuh"
 #include "mx4.cuh"
 
 using namespace hyp;
@@ -7,6 +9,17 @@ using namespace hyp;
 namespace {
 
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+bool shape_ok(const hyp_attn_shape* s, int32_t format) {
+  if (!s || s->n_kv_heads < 1 || s->n_kv_heads > 32767 || s->n_q_heads < s->n_kv_heads || s->n_q_heads % s->n_kv_heads) return false;
+  if (format != HYP_KV8_INT8 && format != HYP_KV8_E4M3) return false;
+  const int G = s->n_q_heads / s->n_kv_heads;
+  return (G == 1 || G == 2 || G == 4 || G == 8) && (s->head_dim == 64 || s->head_dim == 128);
+}
+bool pages_ok(int32_t n) { return n >= 1 && n <= (1 << 26); }
+bool count_ok(int32_t n) { return n >= 1 && n <= 65535; }
+Kv8View view(const hyp_attn_shape* s, int32_t format, int32_t n_seqs, const void* pool, const int32_t* table, int32_t table_stride) {
+  return Kv8View{(uint8_t*)pool, table, table_stride, n_seqs, s->n_q_heads, s->n_kv_heads, s->head_dim, format};
+}
 bool type_ok(int32_t t) { return t == HYP_TYPE_F32 || t == HYP_TYPE_F16 || t == HYP_TYPE_BF16; }
 bool matrix_ok(int32_t N, int32_t K) { return N >= 1 && K >= 8 && K % 8 == 0; }
 // The tensor map counts lines of 64 bytes in 31 bits.
@@ -69,4 +82,45 @@ extern "C" int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, 
   if (rc) return rc;
   return finish(launch_gemm_mx4(a, a_type, a_stride, (const uint8_t*)w_packed, M, N, K, terms, epilogue, out, ldo, (uint8_t*)scratch,
                                 (cudaStream_t)stream));
+}
+
+extern "C" int hyp_op_kv8_write(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, int32_t M, const void* qkv, int32_t type,
+                                int64_t stride, const float* rope_table, int32_t rope_positions, void* kv8_pages,
+                                const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* cu_q, const int32_t* ctx_lens,
+                                void* q_out, void* stream) {
+  if (!shape_ok(shape, format) || !qkv || !kv8_pages || !block_table || !cu_q || !ctx_lens || !type_ok(type)) return HYP_EINVAL;
+  if (!count_ok(n_seqs) || M < 1 || M > (1 << 26) || !pages_ok(max_pages_per_seq) || (rope_table && rope_positions < 1)) return HYP_EINVAL;
+  if (stride < ((int64_t)shape->n_q_heads + 2 * shape->n_kv_heads) * shape->head_dim || stride % 8) return HYP_EINVAL;
+  if (!aligned(qkv, 16) || !aligned(kv8_pages, 16) || !aligned(rope_table, 16) || !aligned(q_out, 16)) return HYP_EINVAL;
+  return finish(launch_kv8_write(view(shape, format, n_seqs, kv8_pages, block_table, max_pages_per_seq), M, qkv, type, stride, rope_table,
+                                 rope_positions, cu_q, ctx_lens, (__half*)q_out, (cudaStream_t)stream));
+}
+
+extern "C" int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* kv8_pages, const int32_t* block_table,
+                               int32_t max_pages_per_seq, const int32_t* first, const int32_t* lens, void* dst_pages,
+                               const int32_t* dst_table, int32_t dst_pages_per_seq, void* stream) {
+  if (!shape_ok(shape, format) || !kv8_pages || !block_table || !lens || !dst_pages || !dst_table) return HYP_EINVAL;
+  if (!count_ok(n_seqs) || !pages_ok(max_pages_per_seq) || !pages_ok(dst_pages_per_seq)) return HYP_EINVAL;
+  if (!aligned(kv8_pages, 16) || !aligned(dst_pages, 16)) return HYP_EINVAL;
+  return finish(launch_kv8_read(view(shape, format, n_seqs, kv8_pages, block_table, max_pages_per_seq), first, lens, (__half*)dst_pages,
+                                dst_table, dst_pages_per_seq, (cudaStream_t)stream));
+}
+
+extern "C" size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq) {
+  if (!shape_ok(shape, HYP_KV8_INT8) || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return 0;
+  return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim, paged_splits(n_seqs, shape->n_kv_heads, max_pages_per_seq));
+}
+
+extern "C" int hyp_op_attn_decode_kv8(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* q, int64_t q_stride,
+                                      const void* kv8_pages, const int32_t* block_table, int32_t max_pages_per_seq,
+                                      const int32_t* ctx_lens, void* scratch, size_t scratch_bytes, void* out, void* stream) {
+  if (!shape_ok(shape, format) || !q || !out || !kv8_pages || !block_table || !ctx_lens || !scratch) return HYP_EINVAL;
+  if (!count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return HYP_EINVAL;
+  if (q_stride < (int64_t)shape->n_q_heads * shape->head_dim || q_stride % 8) return HYP_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(kv8_pages, 16) || !aligned(scratch, 16)) return HYP_EINVAL;
+  if (scratch_bytes < hyp_op_attn_kv8_scratch_bytes(shape, n_seqs, max_pages_per_seq)) return HYP_ECAPACITY;
+  const int rc = tc_prepare();
+  if (rc) return rc;
+  return finish(launch_attn_kv8(view(shape, format, n_seqs, kv8_pages, block_table, max_pages_per_seq), (const __half*)q, q_stride, ctx_lens,
+                                (float*)scratch, (__half*)out, tc_err_flag_ptr(), (cudaStream_t)stream));
 }

@@ -114,6 +114,14 @@ SIGNATURES = {
     "hyp_op_gemm_mx4_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     "hyp_op_gemm_mx4": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hyp_op_kv8_write": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int64,
+                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_void_p]),
+    "hyp_op_kv8_read": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "hyp_op_attn_kv8_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32]),
+    "hyp_op_attn_decode_kv8": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                         C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
     "hyp_op_attn_mod_scratch_bytes": (C.c_size_t, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32]),
     "hyp_op_attn_decode_mod": (C.c_int, [C.POINTER(hyp_attn_shape), C.POINTER(hyp_attn_mod), C.c_int32, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p,
@@ -619,7 +627,7 @@ def hyp_op_attn_decode_shared(shape3, q, kv_pages, cu_group, prefix_table, prefi
 
 
 # --------------------------------------------------------------------------------------------
-# operators in few bits (hyperion_ops.h): 4-bit weights.  Tensors are checked as those of the operators over the paged cache.
+# operators in few bits (hyperion_ops.h): 4-bit weights, the 8-bit cache.  Tensors are checked as those of the operators over the paged cache.
 # --------------------------------------------------------------------------------------------
 HYP_TYPE_F32, HYP_TYPE_F16, HYP_TYPE_BF16 = range(3)
 _U8 = None
@@ -709,6 +717,73 @@ def hyp_op_gemm_mx4(a, w_packed, N: int, terms: int, epilogue: int, out, scratch
         _refuse(where, f"w_packed must be the uint8 tensor that hyp_op_mx4_pack gives for {N} x {k} on device {dev}")
     sp, sb = _scratch(where, scratch, dev)
     _launch(where, lib().hyp_op_gemm_mx4, dev, stream, ap, code, as_, w_packed.data_ptr(), m, N, k, terms, epilogue, op, max(os_, on), sp, sb)
+
+
+HYP_KV8_INT8, HYP_KV8_E4M3 = range(2)
+
+
+def hyp_kv8_half_page_bytes(head_dim: int) -> int:
+    """Bytes of 16 tokens' codes and scales of one head (keys, or values)."""
+    return 16 * head_dim + 64
+
+
+def _pool8(where, t, dev, shape3):
+    _types()
+    s = t.shape
+    if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous() or s[1:] != (2, shape3[1], 16 * shape3[2] + 64):
+        _refuse(where, f"kv8_pages must be a contiguous uint8 page pool [pages, 2, {shape3[1]}, {16 * shape3[2] + 64}] on device {dev}, not "
+                       f"{t.dtype} {tuple(s)} on {t.device}")
+    return t.data_ptr()
+
+
+def hyp_op_kv8_write(shape3, fmt: int, qkv, kv8_pages, block_table, cu_q, ctx_lens, rope_table=None, q_out=None, stream=None):
+    """qkv [rows, >= (n_q_heads + 2 n_kv_heads) * head_dim] fp32, fp16 or bf16; kv8_pages uint8 [pages, 2, n_kv_heads, 16 * head_dim + 64];
+    block_table int32 [n_seqs, pages per sequence]; cu_q int32 [n_seqs + 1]; ctx_lens int32 [n_seqs]; rope_table fp32
+    [positions, head_dim / 2, 2] or None; q_out fp16 [rows, n_q_heads * head_dim] or None."""
+    where, sh = "hyp_op_kv8_write", _shape(shape3)
+    dev, code, m, width, qp, qs = _matrix(where, "qkv", qkv)
+    if width < (shape3[0] + 2 * shape3[1]) * shape3[2]:
+        _refuse(where, f"qkv has {width} columns, the heads need {(shape3[0] + 2 * shape3[1]) * shape3[2]}")
+    pool = _pool8(where, kv8_pages, dev, shape3)
+    ctx, n = _rows(where, "ctx_lens", ctx_lens, _I32, dev, ())
+    table, pages = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    cu = _dense(where, "cu_q", cu_q, _I32, dev, (n + 1,))
+    rope = 0 if rope_table is None else rope_table.shape[0]
+    rp = None if rope_table is None else _dense(where, "rope_table", rope_table, _F32, dev, (rope, shape3[2] // 2, 2))
+    op = None if q_out is None else _dense(where, "q_out", q_out, _F16, dev, (m, shape3[0] * shape3[2]))
+    _launch(where, lib().hyp_op_kv8_write, dev, stream, sh, fmt, n, m, qp, code, qs, rp, rope, pool, table, pages, cu, ctx, op)
+
+
+def hyp_op_kv8_read(shape3, fmt: int, kv8_pages, block_table, first, lens, dst_pages, dst_table, stream=None):
+    """first int32 [n_seqs] or None, lens int32 [n_seqs]; dst_pages fp16 [pages, 2, n_kv_heads, 16, head_dim], dst_table int32
+    [n_seqs, pages per sequence]."""
+    where, sh = "hyp_op_kv8_read", _shape(shape3)
+    dev = kv8_pages.get_device()
+    if dev < 0:
+        _refuse(where, "kv8_pages must be a CUDA tensor")
+    pool = _pool8(where, kv8_pages, dev, shape3)
+    lp, n = _rows(where, "lens", lens, _I32, dev, ())
+    fp = None if first is None else _dense(where, "first", first, _I32, dev, (n,))
+    table, pages = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    dst = _pool(where, "dst_pages", dst_pages, dev, shape3)
+    dtable, dpages = _rows(where, "dst_table", dst_table, _I32, dev, (n,))
+    _launch(where, lib().hyp_op_kv8_read, dev, stream, sh, fmt, n, pool, table, pages, fp, lp, dst, dtable, dpages)
+
+
+def hyp_op_attn_kv8_scratch_bytes(shape3, n_seqs: int, max_pages_per_seq: int) -> int:
+    return lib().hyp_op_attn_kv8_scratch_bytes(_shape(shape3), n_seqs, max_pages_per_seq)
+
+
+def hyp_op_attn_decode_kv8(shape3, fmt: int, q, kv8_pages, block_table, ctx_lens, scratch, out, stream=None):
+    """hyp_op_attn_decode_mod without a modification, over the 8-bit cache."""
+    where, sh = "hyp_op_attn_decode_kv8", _shape(shape3)
+    dev, n, qp, qs = _query(where, q, shape3)
+    pool = _pool8(where, kv8_pages, dev, shape3)
+    table, width = _rows(where, "block_table", block_table, _I32, dev, (n,))
+    ctx = _dense(where, "ctx_lens", ctx_lens, _I32, dev, (n,))
+    op = _dense(where, "out", out, _F16, dev, (n, shape3[0] * shape3[2]))
+    sp, sb = _scratch(where, scratch, dev)
+    _launch(where, lib().hyp_op_attn_decode_kv8, dev, stream, sh, fmt, n, qp, qs, pool, table, width, ctx, sp, sb, op)
 
 
 # --------------------------------------------------------------------------------------------
