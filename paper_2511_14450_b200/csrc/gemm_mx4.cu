@@ -52,17 +52,16 @@ int row_cap(int epi) { return epi == EPI_SWIGLU_BF16 ? 240 : 256; }
 // activations to terms: four threads take a block of 32 k of one token, eight values each
 // ---------------------------------------------------------------------------------------------
 constexpr int TERM_THREADS = 128;
+// grid (M, segments of 128 chunks of eight values)
 template <int TYPE>
 __global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int M, int K8, int KB, int terms,
                                                                 int tt, int nb, size_t block_bytes, uint8_t* __restrict__ out) {
-  const int per_row = 16 * KB;
-  const long long i = (long long)blockIdx.x * TERM_THREADS + threadIdx.x;
-  const int m = (int)(i / per_row), c = (int)(i - (long long)m * per_row);
-  const bool row_in = m < M;
+  const int m = blockIdx.x, c = blockIdx.y * TERM_THREADS + threadIdx.x;
+  const bool row_in = c < 16 * KB;
   float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   pdl_wait();
   pdl_trigger();
-  if (row_in && c < K8) load8<TYPE>(a + (m * stride + 8 * c) * 2, v);
+  if (c < K8) load8<TYPE>(a + (m * stride + 8 * c) * 2, v);
   const int kb = c >> 4, chunk = (c & 15) >> 1;  // 16-byte chunk of the 128-byte operand row
   uint8_t* blk = out + ((size_t)(m / tt) * KB + kb) * block_bytes;
   bool bad = false;
@@ -427,10 +426,10 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(epi == EPI_SWIGLU_BF16 ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
-  const long long ctas = ((long long)M * 16 * p.KB + TERM_THREADS - 1) / TERM_THREADS;
-  if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
+  const int segments = (16 * p.KB + TERM_THREADS - 1) / TERM_THREADS;
+  if (segments > 65535) return HYP_ECAPACITY;
   auto go = [&](auto kernel) {
-    return launch_pdl<2>(kernel, dim3((unsigned)ctas), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, M, K / 8, p.KB, terms,
+    return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, M, K / 8, p.KB, terms,
                          t.tt, t.nb, t.block_bytes, scratch);
   };
   HYP_CUDA_TRY(a_type == HYP_TYPE_F16 ? go(mx_terms_kernel<HYP_TYPE_F16>) : go(mx_terms_kernel<HYP_TYPE_BF16>));

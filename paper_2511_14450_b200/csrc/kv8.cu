@@ -8,12 +8,6 @@ namespace {
 
 constexpr float KV8_LEAST = 0x1p-118f;  // rows whose largest magnitude is below this count as zeros: their scales would leave fp32's normal range
 
-__device__ __forceinline__ __half half_sat(float x) { return __float2half_rn(x != x ? x : fminf(fmaxf(x, -65504.f), 65504.f)); }
-__device__ __forceinline__ uint32_t half2_sat(float a, float b) {
-  const __half2 h = __halves2half2(half_sat(a), half_sat(b));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // Four consecutive values of a row as fp32.
 template <int TYPE>
 __device__ __forceinline__ void load4(const void* p, float (&v)[4]) {
@@ -43,49 +37,62 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int n, int row, in
   return lo;
 }
 
-// Scale of a row from its largest magnitude, in the arithmetic T of its values (fp32 as they came, fp64 where they were rotated).
-// int8: amax / 127 rounded to fp32.  e4m3: the least power of two p with amax <= 448 p.
-template <int FMT>
-__device__ __forceinline__ float row_scale(float amax) {
-  if (FMT == HYP_KV8_INT8) return __fdiv_rn(amax, 127.f);
-  return pow2(e4m3_exponent(__float_as_uint(amax)));
-}
+// Scale of a row from its largest magnitude.  int8: amax / 127 rounded to fp32 (the fp64 product with the rounded 1 / 127 is off by
+// 2^-52; a quotient of a 24-bit amax is never that near to a border).  e4m3: the least power of two p with amax <= 448 p.
 template <int FMT>
 __device__ __forceinline__ float row_scale(double amax) {
-  if (FMT == HYP_KV8_INT8) return (float)(amax / 127.0);
+  if (FMT == HYP_KV8_INT8) return (float)(amax * (1.0 / 127.0));
   const long long b = __double_as_longlong(amax);
   return pow2((int)(b >> 52) - 1023 - 8 + ((b & 0xfffffffffffffll) > 0xc000000000000ll ? 1 : 0));
 }
-
-// The integer nearest to x / s, ties to even, exactly: the estimate from the product is off by one at most next to a border, and
-// the remainder x - q s is formed without rounding (q has 8 bits, s 24; the difference is at most s).
-__device__ __forceinline__ int to_int(float x) { return __float2int_rn(x); }
-__device__ __forceinline__ int to_int(double x) { return __double2int_rn(x); }
-template <typename T>
-__device__ __forceinline__ int nearest_code(T x, float s, float inv) {
-  int q = to_int(x * (T)inv);
-  const T r = fma((T)-q, (T)s, x), twice = r < 0 ? -2 * r : 2 * r;
-  if (twice > (T)s || (twice == (T)s && (q & 1))) q += r < 0 ? -1 : 1;
-  return q;
-}
-// x times an exact power of two, to E4M3 (nearest, ties to even); fp64 goes to fp32 rounded to odd, so that it is not rounded twice.
-__device__ __forceinline__ float e4m3_input(float x, float inv) { return x * inv; }
-__device__ __forceinline__ float e4m3_input(double x, float inv) {
-  const double y = x * (double)inv;
+// x times an exact power of two, to fp32 rounded to odd, so that the rounding to E4M3 behind it is the only one.
+__device__ __forceinline__ float odd_product(double x, double inv) {
+  const double y = x * inv;
   const float f = __double2float_rz(y);
   return (double)f != y ? __uint_as_float(__float_as_uint(f) | 1u) : f;
 }
-template <int FMT, typename T>
-__device__ __forceinline__ uint32_t four_codes(const T (&x)[4], float s) {
+
+// Four codes of values x[i] (fp32, off by at most tol[i] from the value meant; 0: exact) under scale s > 0.  Returns false where some code
+// hangs on what lies within tol: next to a border between two codes.
+constexpr float ROUND_INT = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+template <int FMT>
+__device__ __forceinline__ bool fast_codes(const float (&x)[4], const float (&tol)[4], bool exact, float s, float inv, uint32_t& w) {
+  bool sure = true;
   if (FMT == HYP_KV8_INT8) {
-    const float inv = s > 0.f ? 1.f / s : 0.f;
+    const float half = 0.5f * s;
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float t = fmaf(x[i], inv, ROUND_INT + 128.f);
+      const float r = fabsf(fmaf(-(t - (ROUND_INT + 128.f)), s, x[i]));  // without rounding: the code has 8 bits, s 24, the rest is at most s
+      sure = sure && r + tol[i] < half;
+      q[i] = __float_as_uint(t);
+    }
+    w = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    return sure;
+  }
+  w = to_e4m3x2(x[0] * inv, x[1] * inv) | to_e4m3x2(x[2] * inv, x[3] * inv) << 16;
+  if (exact) return true;
+  const uint32_t lo = to_e4m3x2((x[0] - tol[0]) * inv, (x[1] - tol[1]) * inv) | to_e4m3x2((x[2] - tol[2]) * inv, (x[3] - tol[3]) * inv) << 16;
+  const uint32_t hi = to_e4m3x2((x[0] + tol[0]) * inv, (x[1] + tol[1]) * inv) | to_e4m3x2((x[2] + tol[2]) * inv, (x[3] + tol[3]) * inv) << 16;
+  return lo == hi;
+}
+// The same from fp64 values, exactly: nearest, ties to even.
+template <int FMT>
+__device__ __noinline__ uint32_t exact_codes(double x0, double x1, double x2, double x3, float s) {
+  const double x[4] = {x0, x1, x2, x3}, inv = 1.0 / (double)s;
+  if (FMT == HYP_KV8_INT8) {
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)(nearest_code(x[i], s, inv) + 128) << (8 * i);
+    for (int i = 0; i < 4; ++i) {
+      int q = __double2int_rn(x[i] * inv);
+      const double r = fma((double)-q, (double)s, x[i]), twice = 2.0 * fabs(r);
+      if (twice > (double)s || (twice == (double)s && (q & 1))) q += r < 0.0 ? -1 : 1;
+      w |= (uint32_t)(q + 128) << (8 * i);
+    }
     return w;
   }
-  const float inv = s > 0.f ? 1.f / s : 0.f;  // exact: a power of two
-  return to_e4m3x2(e4m3_input(x[0], inv), e4m3_input(x[1], inv)) | to_e4m3x2(e4m3_input(x[2], inv), e4m3_input(x[3], inv)) << 16;
+  return to_e4m3x2(odd_product(x[0], inv), odd_product(x[1], inv)) | to_e4m3x2(odd_product(x[2], inv), odd_product(x[3], inv)) << 16;
 }
 
 struct WriteArgs {
@@ -102,76 +109,106 @@ struct WriteArgs {
   int n_seqs, M, Hq, Hkv;
 };
 
-// D / 4 lanes take a head of a row, four values each.
+// grid (M, shares of the heads).  D / 4 lanes take a head of a row, four values each; a warp takes every (8 gridDim.y)-th head (pair of heads
+// at D = 64) of its row, so that the row's sequence, page and angles are found once, and has the next head's values on their way.
+//   Bound by HBM for prompts (fp32 rows: 7 bytes in for 1 out), by latency for single tokens.  Codes have to be those of the exact value, and
+// exact arithmetic on every value costs more than the memory: a first version in fp64 took 76 us for 4096 rows of 60 heads, issue slots 84 %
+// busy.  So values are rotated and rounded in fp32 with a bound on the error beside them, and only where a code would hang on
+// it (about one warp in a hundred), and for the row's largest value, is fp64 used: its products of fp32 numbers are exact.
 template <int D, int FMT, int TYPE>
 __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
   constexpr int LANES = D / 4, PER = 32 / LANES, SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LANES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LANES, sub = lane / LANES;
+  const uint32_t mine = LANES == 32 ? 0xffffffffu : 0xffffu << (16 * sub);  // the lanes of this head
   const int row = blockIdx.x;
-  const int h0 = a.q_out ? 0 : a.Hq, heads = a.Hq + 2 * a.Hkv;
-  const int head = h0 + (blockIdx.y * 8 + warp) * PER + lane / LANES;
+  const int heads = a.Hq + 2 * a.Hkv, step = 8 * gridDim.y * PER;
+  int head = (a.q_out ? 0 : a.Hq) + (blockIdx.y * 8 + warp) * PER + sub;
   pdl_wait();
   pdl_trigger();
   if (row >= a.cu[a.n_seqs]) return;
-  const bool in = head < heads;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (in) load4<TYPE>(a.qkv + ((long long)row * a.stride + (long long)head * D + 4 * l) * SIZE, v);
+  const uint8_t* src = a.qkv + ((long long)row * a.stride + 4 * l) * SIZE;
+  float next[4] = {0.f, 0.f, 0.f, 0.f};
+  if (head < heads) load4<TYPE>(src + (long long)head * (D * SIZE), next);
   const int seq = sequence_of(a.cu, a.n_seqs, row, lane);
   const long long pos = (long long)a.ctx[seq] + (row - a.cu[seq]);
-  const bool turn = a.rope && in && head < a.Hq + a.Hkv;
-  float cs[8];  // (cos, sin) of this lane's four pairs
-  if (turn) {
+  const bool kept = pos >= 0 && pos < (long long)a.table_stride * 16;
+  const int slot = (int)(pos & 15);
+  uint8_t* page = a.pool + (kept ? (size_t)a.table[(long long)seq * a.table_stride + (pos >> 4)] * 2 * a.Hkv * kv8_half_page(D) : 0);
+  float cs[8];  // (cos, sin) of this lane's four pairs, the sine with the sign of its term
+  if (a.rope) {
     const long long at = min(max(pos, 0ll), (long long)a.rope_positions - 1);
     const float4* t = reinterpret_cast<const float4*>(a.rope + (at * (D / 2) + 4 * (l % (LANES / 2))) * 2);
     const float4 t0 = t[0], t1 = t[1];
-    cs[0] = t0.x; cs[1] = t0.y; cs[2] = t0.z; cs[3] = t0.w; cs[4] = t1.x; cs[5] = t1.y; cs[6] = t1.z; cs[7] = t1.w;
+    const float sign = l < LANES / 2 ? -1.f : 1.f;
+    cs[0] = t0.x; cs[1] = t0.y * sign; cs[2] = t0.z; cs[3] = t0.w * sign; cs[4] = t1.x; cs[5] = t1.y * sign; cs[6] = t1.z; cs[7] = t1.w * sign;
   }
-  float o[4];  // the other member of each pair, D / 2 away
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = __shfl_xor_sync(0xffffffffu, v[i], LANES / 2);
-  const float sign = l < LANES / 2 ? -1.f : 1.f;
-
-  if (in && head < a.Hq) {
-    if (turn) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], cs[2 * i], sign * o[i] * cs[2 * i + 1]);
-    }
-    *reinterpret_cast<uint2*>(a.q_out + ((long long)row * a.Hq + head) * D + 4 * l) = make_uint2(half2_sat(v[0], v[1]), half2_sat(v[2], v[3]));
-  }
-  // A warp may hold heads of both kinds: everybody takes part in the reductions.  Rotated keys are formed in fp64: the two products are
-  // exact there, so a code does not depend on how a sum was rounded.
-  const bool wide = __any_sync(0xffffffffu, turn && head >= a.Hq);
-  double x[4];
-  float m = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-  bool bad = !(isfinite(v[0]) && isfinite(v[1]) && isfinite(v[2]) && isfinite(v[3]));
-  double md = 0.0;
-  if (wide) {
+  const int code_at = slot * D + kv8_chunk<D>(l >> 2, slot) + 4 * (l & 3);
+  for (int h0 = head - sub; h0 < heads; h0 += step, head += step) {  // the warp's lanes stay together
+    float x[4], o[4], tol[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[i] = turn ? fma((double)v[i], (double)cs[2 * i], (double)(sign * o[i]) * (double)cs[2 * i + 1]) : (double)v[i];
-      md = fmax(md, fabs(x[i]));
-      bad = bad || !isfinite(x[i]);
+      x[i] = next[i];
+      next[i] = 0.f;
     }
-  }
+    if (head + step < heads) load4<TYPE>(src + (long long)(head + step) * (D * SIZE), next);
+    const bool any_turn = a.rope && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
+    const float v[4] = {x[0], x[1], x[2], x[3]};
+    if (any_turn) {
 #pragma unroll
-  for (int k = LANES / 2; k > 0; k >>= 1) {
-    if (wide)
-      md = fmax(md, __shfl_xor_sync(0xffffffffu, md, k));
-    else
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-    bad = (__shfl_xor_sync(0xffffffffu, (int)bad, k) != 0) || bad;
+      for (int i = 0; i < 4; ++i) {
+        o[i] = __shfl_xor_sync(0xffffffffu, v[i], LANES / 2);  // the other member of the pair, D / 2 away
+        if (turn) {
+          const float t = o[i] * cs[2 * i + 1];
+          x[i] = fmaf(v[i], cs[2 * i], t);
+          tol[i] = (fabsf(t) + fabsf(x[i])) * 0x1p-23f;  // two roundings of half a step each
+        }
+      }
+    }
+    if (h0 + PER <= a.Hq || head < a.Hq) {
+      if (head < a.Hq) *reinterpret_cast<uint2*>(a.q_out + ((long long)row * a.Hq + head) * D + 4 * l) = make_uint2(half2_sat(x[0], x[1]), half2_sat(x[2], x[3]));
+      if (h0 + PER <= a.Hq) continue;  // the whole warp
+    }
+    uint32_t top = max(max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu),
+                       max(__float_as_uint(x[2]) & 0x7fffffffu, __float_as_uint(x[3]) & 0x7fffffffu));
+    const uint32_t own_top = top;
+#pragma unroll
+    for (int k = LANES / 2; k > 0; k >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, k));
+    const bool bad = top >= 0x7f800000u;
+    // the largest magnitude exactly: among the values whose fp32 form is within its error of the largest one
+    double amax = (double)__uint_as_float(top);
+    if (any_turn) {
+      const float close = __uint_as_float(top) * (1.f - 0x1p-19f);
+      double m = 0.0;
+      if (turn && __uint_as_float(own_top) >= close) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmax(m, fabs(fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1])));
+      }
+      const uint32_t owners = __ballot_sync(0xffffffffu, m > 0.0) & mine;
+      double best = __shfl_sync(0xffffffffu, m, owners ? __ffs(owners) - 1 : lane);  // every lane takes part, zeros among them
+      if (__any_sync(0xffffffffu, __popc(owners) > 1)) {
+        best = m;
+#pragma unroll
+        for (int k = LANES / 2; k > 0; k >>= 1) best = fmax(best, __shfl_xor_sync(0xffffffffu, best, k));
+      }
+      if (turn) amax = best;
+    }
+    const bool zero = !(amax >= (double)KV8_LEAST);
+    float s = 0.f;
+    uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
+    if (!bad && !zero) {
+      s = row_scale<FMT>(amax);
+      if (!fast_codes<FMT>(x, tol, !turn, s, __frcp_rn(s), w)) {
+        double xd[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xd[i] = turn ? fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1]) : (double)x[i];
+        w = exact_codes<FMT>(xd[0], xd[1], xd[2], xd[3], s);
+      }
+    }
+    if (head < a.Hq || head >= heads || !kept) continue;
+    uint8_t* half_page = page + (size_t)(head - a.Hq) * kv8_half_page(D);  // value heads follow the key heads
+    *reinterpret_cast<uint32_t*>(half_page + code_at) = w;
+    if (l == 0) *reinterpret_cast<float*>(half_page + 16 * D + 4 * slot) = bad ? __uint_as_float(0x7fffffffu) : s;
   }
-  if (!in || head < a.Hq || pos < 0 || pos >= (long long)a.table_stride * 16) return;
-  const int kvh = (head - a.Hq) % a.Hkv, kind = (head - a.Hq) / a.Hkv, slot = (int)(pos & 15);
-  uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
-  float s = 0.f;
-  if (!bad && (wide ? md >= (double)KV8_LEAST : m >= KV8_LEAST)) {
-    s = wide ? row_scale<FMT>(md) : row_scale<FMT>(m);
-    w = wide ? four_codes<FMT>(x, s) : four_codes<FMT>(v, s);
-  }
-  uint8_t* half_page = a.pool + kv8_half_offset(a.table[(long long)seq * a.table_stride + (pos >> 4)], kind, kvh, a.Hkv, D);
-  *reinterpret_cast<uint32_t*>(half_page + slot * D + kv8_chunk<D>(l >> 2, slot) + 4 * (l & 3)) = w;
-  if (l == 0) *reinterpret_cast<float*>(half_page + 16 * D + 4 * slot) = bad ? __uint_as_float(0x7fffffffu) : s;
 }
 
 // A warp takes half pages in turn: 16-byte chunks of codes, times their slot's scale, to two chunks of fp16.
@@ -209,9 +246,9 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         float2 lo, hi;
-        if (FMT == HYP_KV8_INT8) {
-          lo = make_float2((float)((int)(w[k] & 255u) - 128), (float)((int)(w[k] >> 8 & 255u) - 128));
-          hi = make_float2((float)((int)(w[k] >> 16 & 255u) - 128), (float)((int)(w[k] >> 24) - 128));
+        if (FMT == HYP_KV8_INT8) {  // a code below the exponent of 2^23, which then goes
+          lo = make_float2(__uint_as_float(__byte_perm(w[k], 0x4b000000u, 0x7440)) - 8388736.f, __uint_as_float(__byte_perm(w[k], 0x4b000000u, 0x7441)) - 8388736.f);
+          hi = make_float2(__uint_as_float(__byte_perm(w[k], 0x4b000000u, 0x7442)) - 8388736.f, __uint_as_float(__byte_perm(w[k], 0x4b000000u, 0x7443)) - 8388736.f);
         } else {
           lo = half2_values(e4m3x2_to_half2(w[k] & 0xffffu));
           hi = half2_values(e4m3x2_to_half2(w[k] >> 16));
@@ -228,9 +265,10 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
 
 template <int D, int FMT, int TYPE>
 int write_go(const WriteArgs& a, cudaStream_t st) {
-  const int units = (a.q_out ? a.Hq : 0) + 2 * a.Hkv, per_cta = 8 * (128 / D);
-  HYP_CUDA_TRY(launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE>, dim3((unsigned)a.M, (unsigned)((units + per_cta - 1) / per_cta)), dim3(256),
-                             (size_t)0, st, a));
+  const int heads = (a.q_out ? a.Hq : 0) + 2 * a.Hkv, most = (heads + 8 * (128 / D) - 1) / (8 * (128 / D));
+  int y = (8 * sm_count() + a.M - 1) / a.M;  // few rows: a head for every warp; many: one CTA a row
+  if (y > most) y = most;
+  HYP_CUDA_TRY(launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE>, dim3((unsigned)a.M, (unsigned)y), dim3(256), (size_t)0, st, a));
   return 1;
 }
 template <int D, int FMT>

@@ -64,6 +64,13 @@ __device__ __forceinline__ void e2m1x8_to_half2(uint32_t v, uint32_t (&h)[4]) {
 }
 __device__ __forceinline__ float2 half2_values(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
+// fp32 -> fp16 pair, saturating at +-65504; NaN stays NaN
+__device__ __forceinline__ uint32_t half2_sat(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // Eight consecutive values of a matrix row as fp32 (16-byte loads; p aligned to 16 bytes).
 template <int TYPE>
 __device__ __forceinline__ void load8(const void* p, float (&v)[8]) {

@@ -1,55 +1,82 @@
 // Microscaled 4-bit floating point: a matrix to codes and block exponents, back, and to the packed form of the product.
 //
-// Four threads take a block of 32 values, eight each: the block's largest magnitude by two shuffles, the exponent
-// floor(log2 amax) - 2 from its bits (so that amax lands in [4, 8), where 6 is the largest code: what lies above 6 saturates),
-// every value times the exact inverse power, rounded to E2M1 by the hardware conversion (nearest, ties to even).  Bound by HBM: one
-// pass, 16-byte loads.
+// A warp takes a run of a row, a lane eight values at a time, so that four lanes hold a block of 32: the block's largest magnitude by
+// two shuffles, the exponent floor(log2 amax) - 2 from its bits (amax lands in [4, 8), where 6 is the largest code: what lies above
+// saturates), every value times the exact inverse power, rounded to E2M1 by the hardware conversion (nearest, ties to even).
+// Bound by HBM (one pass, 16-byte loads, up to four in flight a lane), next by issue slots: with a division by the row length in every
+// thread and eight values to a thread the two passes over 17920 x 5120 bf16 values took 65 + 52 us.
 #include "mx4.cuh"
 
 namespace hyp {
 
 namespace {
 
-constexpr int QT = 256;
+constexpr int QT = 256, QW = QT / 32;
 
-template <int TYPE>
-__global__ void __launch_bounds__(QT) mx4_quantize_kernel(const void* __restrict__ x, int N, int K8, long long x_stride,
+// grid (rows / 8, segments of 32 U chunks); a chunk is eight values
+template <int TYPE, int U>
+__global__ void __launch_bounds__(QT) mx4_quantize_kernel(const uint8_t* __restrict__ x, int N, int K8, long long x_stride,
                                                           uint32_t* __restrict__ codes, uint8_t* __restrict__ scales, int blocks) {
   constexpr int SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
-  const int per_row = 4 * blocks;  // threads of a row; those behind K take zeros
-  const long long i = (long long)blockIdx.x * QT + threadIdx.x;
-  const long long row = i / per_row;
-  const int c = (int)(i - row * per_row);
-  const bool in = row < N && c < K8;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int lane = threadIdx.x & 31, row = blockIdx.x * QW + (threadIdx.x >> 5), c0 = blockIdx.y * (32 * U) + lane;
   pdl_wait();
-  if (in) load8<TYPE>(reinterpret_cast<const uint8_t*>(x) + (row * x_stride + 8 * c) * SIZE, v);
-  uint32_t m = absmax_bits(v);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const bool bad = m >= 0x7f800000u;
-  const int e = max((int)(m >> 23) - 127 - 2, -127);  // amax below 2^-126 included: it is far below 2^-127 * 4
-  const float inv = pow2(-e);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = bad ? 0.f : v[k] * inv;
-  if (in) codes[row * K8 + c] = to_e2m1x8(v);
-  if (row < N && (c & 3) == 0) scales[row * blocks + (c >> 2)] = bad ? 255 : (uint8_t)(m == 0u ? 0 : e + 127);
   pdl_trigger();
+  if (row >= N) return;
+  const uint8_t* src = x + (row * x_stride + 8ll * c0) * SIZE;
+  uint32_t* to = codes + (long long)row * K8 + c0;
+  uint8_t* sc = scales + (long long)row * blocks + (c0 >> 2);
+  float v[U][8];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (c0 + 32 * u < K8) {
+      load8<TYPE>(src + 32 * u * 8 * SIZE, v[u]);
+    } else {  // behind K: zeros
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[u][k] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    uint32_t m = absmax_bits(v[u]);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    const bool bad = m >= 0x7f800000u;
+    const int e = max((int)(m >> 23) - 127 - 2, -127);  // amax below 2^-126 included: it is far below 4 * 2^-127
+    const float inv = bad ? 0.f : pow2(-e);
+    float y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = v[u][k] * inv;
+    const int c = c0 + 32 * u;
+    if (c < K8) to[32 * u] = bad ? 0u : to_e2m1x8(y);
+    if (c < K8 && (c & 3) == 0) sc[8 * u] = bad ? 255 : (uint8_t)(m == 0u ? 0 : e + 127);
+  }
 }
 
-template <int TYPE>
+template <int TYPE, int U>
 __global__ void __launch_bounds__(QT) mx4_dequantize_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int N,
-                                                            int K8, int blocks, void* __restrict__ out, long long out_stride) {
+                                                            int K8, int blocks, uint8_t* __restrict__ out, long long out_stride) {
   constexpr int SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
-  const long long i = (long long)blockIdx.x * QT + threadIdx.x;
+  const int lane = threadIdx.x & 31, row = blockIdx.x * QW + (threadIdx.x >> 5), c0 = blockIdx.y * (32 * U) + lane;
   pdl_wait();
-  if (i < (long long)N * K8) {
-    const long long row = i / K8;
-    const int c = (int)(i - row * K8);
-    const int s = scales[row * blocks + (c >> 2)];
-    const float f = s == 255 ? __uint_as_float(0x7fffffffu) : pow2(s - 127);
+  pdl_trigger();
+  if (row >= N) return;
+  const uint32_t* src = codes + (long long)row * K8 + c0;
+  const uint8_t* sc = scales + (long long)row * blocks + (c0 >> 2);
+  uint8_t* to = out + (row * out_stride + 8ll * c0) * SIZE;
+  uint32_t q[U];
+  int s[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool in = c0 + 32 * u < K8;
+    q[u] = in ? src[32 * u] : 0u;
+    s[u] = in ? sc[8 * u] : 0;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (c0 + 32 * u >= K8) continue;
+    const float f = s[u] == 255 ? __uint_as_float(0x7fffffffu) : pow2(s[u] - 127);
     uint32_t h[4], w[4];
-    e2m1x8_to_half2(codes[i], h);
+    e2m1x8_to_half2(q[u], h);
     float v[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -57,20 +84,16 @@ __global__ void __launch_bounds__(QT) mx4_dequantize_kernel(const uint32_t* __re
       v[2 * k] = t.x * f;
       v[2 * k + 1] = t.y * f;
     }
-    uint8_t* o = reinterpret_cast<uint8_t*>(out) + (row * out_stride + 8 * c) * SIZE;
+    uint8_t* o = to + 32 * u * 8 * SIZE;
     if (TYPE == HYP_TYPE_F32) {
       reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
       reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        w[k] = TYPE == HYP_TYPE_BF16 ? pack_bf16(v[2 * k], v[2 * k + 1])
-               : s == 255            ? 0x7fff7fffu
-                                     : pack_f16_sat(v[2 * k], v[2 * k + 1]);
+      for (int k = 0; k < 4; ++k) w[k] = TYPE == HYP_TYPE_BF16 ? pack_bf16(v[2 * k], v[2 * k + 1]) : half2_sat(v[2 * k], v[2 * k + 1]);
       *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
-  pdl_trigger();
 }
 
 // One thread for a row's 32 k of a block: 16 bytes of codes and their scale.
@@ -99,25 +122,43 @@ __global__ void __launch_bounds__(QT) mx4_pack_kernel(const uint8_t* __restrict_
   dst[MX_CODE_BYTES + (r & 31) * 16 + (r >> 5) * 4 + j] = s;
 }
 
+// Long rows: four chunks a lane; short ones: one.
+template <template <int, int> class F, int U, typename... A>
+cudaError_t by_type(int type, A... a) {
+  return type == HYP_TYPE_F32 ? F<HYP_TYPE_F32, U>::go(a...) : type == HYP_TYPE_F16 ? F<HYP_TYPE_F16, U>::go(a...) : F<HYP_TYPE_BF16, U>::go(a...);
+}
+dim3 matrix_grid(int N, int K8, int u) { return dim3((unsigned)((N + QW - 1) / QW), (unsigned)((K8 + 32 * u - 1) / (32 * u))); }
+template <int TYPE, int U>
+struct Quantize {
+  static cudaError_t go(const void* x, int N, int K, long long stride, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
+    return launch_pdl<2>(mx4_quantize_kernel<TYPE, U>, matrix_grid(N, K / 8, U), dim3(QT), (size_t)0, st, (const uint8_t*)x, N, K / 8, stride,
+                         (uint32_t*)codes, scales, (K + MX_BLOCK - 1) / MX_BLOCK);
+  }
+};
+template <int TYPE, int U>
+struct Dequantize {
+  static cudaError_t go(const uint8_t* codes, const uint8_t* scales, int N, int K, void* out, long long stride, cudaStream_t st) {
+    return launch_pdl<2>(mx4_dequantize_kernel<TYPE, U>, matrix_grid(N, K / 8, U), dim3(QT), (size_t)0, st, (const uint32_t*)codes, scales, N,
+                         K / 8, (K + MX_BLOCK - 1) / MX_BLOCK, (uint8_t*)out, stride);
+  }
+};
+// segments of a row are the grid's second dimension
+bool wide_rows(int K) { return K > 1024; }
+bool grid_ok(int K) { return K / 8 <= 65535 * 128; }
+
 }  // namespace
 
 int launch_mx4_quantize(const void* x, int type, int N, int K, long long x_stride, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
-  const int blocks = (K + MX_BLOCK - 1) / MX_BLOCK;
-  const long long ctas = ((long long)N * 4 * blocks + QT - 1) / QT;
-  if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
-  auto go = [&](auto kernel) { return launch_pdl<2>(kernel, dim3((unsigned)ctas), dim3(QT), (size_t)0, st, x, N, K / 8, x_stride, (uint32_t*)codes, scales, blocks); };
-  HYP_CUDA_TRY(type == HYP_TYPE_F32 ? go(mx4_quantize_kernel<HYP_TYPE_F32>)
-               : type == HYP_TYPE_F16 ? go(mx4_quantize_kernel<HYP_TYPE_F16>) : go(mx4_quantize_kernel<HYP_TYPE_BF16>));
+  if (!grid_ok(K)) return HYP_ECAPACITY;
+  HYP_CUDA_TRY((wide_rows(K) ? by_type<Quantize, 4>(type, x, N, K, x_stride, codes, scales, st)
+                            : by_type<Quantize, 1>(type, x, N, K, x_stride, codes, scales, st)));
   return 1;
 }
 
 int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int N, int K, int type, void* out, long long out_stride, cudaStream_t st) {
-  const int blocks = (K + MX_BLOCK - 1) / MX_BLOCK;
-  const long long ctas = ((long long)N * (K / 8) + QT - 1) / QT;
-  if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
-  auto go = [&](auto kernel) { return launch_pdl<2>(kernel, dim3((unsigned)ctas), dim3(QT), (size_t)0, st, (const uint32_t*)codes, scales, N, K / 8, blocks, out, out_stride); };
-  HYP_CUDA_TRY(type == HYP_TYPE_F32 ? go(mx4_dequantize_kernel<HYP_TYPE_F32>)
-               : type == HYP_TYPE_F16 ? go(mx4_dequantize_kernel<HYP_TYPE_F16>) : go(mx4_dequantize_kernel<HYP_TYPE_BF16>));
+  if (!grid_ok(K)) return HYP_ECAPACITY;
+  HYP_CUDA_TRY((wide_rows(K) ? by_type<Dequantize, 4>(type, codes, scales, N, K, out, out_stride, st)
+                            : by_type<Dequantize, 1>(type, codes, scales, N, K, out, out_stride, st)));
   return 1;
 }
 
