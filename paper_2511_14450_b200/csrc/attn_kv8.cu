@@ -20,7 +20,8 @@ namespace hyp {
 
 namespace {
 
-constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32, K8_SLOTS = 4;
+constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32, K8_SLOTS = 2;
+constexpr int K8_PER_SM = 5, K8_WAVES = 2;  // resident CTAs; waves that a long context is cut for
 constexpr float K8_GROWN = 256.f;
 
 struct Kv8Args {
@@ -80,6 +81,11 @@ __device__ __forceinline__ float lg2_approx(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
@@ -92,7 +98,7 @@ __device__ __forceinline__ float lds32(uint32_t addr) {
 }
 
 template <int D, int G, int FMT, bool CLUSTER>
-__global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
+__global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const Kv8Args a) {
   constexpr int KS = D / 16, HALF = kv8_half_page(D), SLOT = 2 * HALF;
   extern __shared__ __align__(128) uint8_t k8_smem[];
   __shared__ uint64_t bars[K8_WARPS * K8_SLOTS];
@@ -122,6 +128,8 @@ __global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
   if (used != n_splits) ids_cur = load_ids(0);
   int32_t ids_next = load_ids(32);
   const uint32_t my_bars = smem_u32(bars) + 8u * (warp * K8_SLOTS), my_ring = smem_u32(k8_smem) + (uint32_t)(warp * K8_SLOTS) * SLOT;
+  const uint32_t page_bytes = 2u * a.Hkv * HALF, v_off = (uint32_t)a.Hkv * HALF;
+  const uint8_t* head_base = a.pool + (size_t)kvh * HALF;
   auto issue = [&](int i, int slot) {  // all lanes call, i ascending
     if (i > 0 && (i & 31) == 0) {
       ids_cur = ids_next;
@@ -131,8 +139,9 @@ __global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
     if (lane == 0) {
       const uint32_t dst = my_ring + slot * SLOT, bar = my_bars + 8u * slot;
       mbar_expect_tx(bar, SLOT);
-      bulk_load(dst, a.pool + kv8_half_offset(page, 0, kvh, a.Hkv, D), HALF, bar);
-      bulk_load(dst + HALF, a.pool + kv8_half_offset(page, 1, kvh, a.Hkv, D), HALF, bar);
+      const uint8_t* src = head_base + (uint64_t)(uint32_t)page * page_bytes;
+      bulk_load(dst, src, HALF, bar);
+      bulk_load(dst + HALF, src + v_off, HALF, bar);
     }
   };
   if (lane == 0) {
@@ -189,26 +198,30 @@ __global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
     }
     const uint32_t sc = kt + 16 * D + 4 * g;
     const float ks0 = lds32(sc) * sl2, ks1 = lds32(sc + 32) * sl2;
-    const float vs0 = lds32(sc + HALF), vs1 = lds32(sc + HALF + 32);
-    const bool see0 = !partial || k0 + g < total, see1 = !partial || k0 + g + 8 < total;
+    float vs0 = lds32(sc + HALF), vs1 = lds32(sc + HALF + 32);
     float v[4], p[4], w[4];  // (key g, head 2tq), (g, 2tq + 1), (g + 8, 2tq), (g + 8, 2tq + 1)
-    bool grown = false;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool see = e < 2 ? see0 : see1;
-      v[e] = s[e] * (e < 2 ? ks0 : ks1);
-      p[e] = see ? ex2_approx(v[e] - m[e & 1]) : 0.f;
-      w[e] = p[e] != 0.f ? p[e] * ((e < 2 ? vs0 : vs1) * f[e & 1]) : 0.f;
-      grown = grown || p[e] > K8_GROWN || w[e] > K8_GROWN;
+    for (int e = 0; e < 4; ++e) v[e] = s[e] * (e < 2 ? ks0 : ks1);
+    if (partial) {  // keys behind the end: no weight, whatever their slots hold
+      if (k0 + g >= total) v[0] = v[1] = -INFINITY, vs0 = 0.f;
+      if (k0 + g + 8 >= total) v[2] = v[3] = -INFINITY, vs1 = 0.f;
     }
-    if (__any_sync(0xffffffffu, grown)) {  // new references: the largest score, the largest score + log2(scale)
+    auto weigh = [&] {  // (a scale times a reference may leave fp32: 0 times infinity would be NaN)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = ex2_approx(v[e] - m[e & 1]);
+        w[e] = p[e] * min_nan((e < 2 ? vs0 : vs1) * f[e & 1], 3e38f);
+      }
+    };
+    weigh();
+    const float most = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
+    if (__any_sync(0xffffffffu, most > K8_GROWN)) {  // new references: the largest score, the largest score + log2(scale)
       // (values whose scale is below 2^-64 are zeros in fp16)
       const float lv0 = fmaxf(lg2_approx(vs0), -64.f), lv1 = fmaxf(lg2_approx(vs1), -64.f);
       float corr2[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = fmaxf(see0 ? v[h] : PG_NEG, see1 ? v[2 + h] : PG_NEG);
-        float top2 = fmaxf(see0 ? v[h] + lv0 : PG_NEG, see1 ? v[2 + h] + lv1 : PG_NEG);
+        float top = fmaxf(v[h], v[2 + h]), top2 = fmaxf(v[h] + lv0, v[2 + h] + lv1);
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) {
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -227,12 +240,7 @@ __global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
         o[c][0] *= corr2[0]; o[c][2] *= corr2[0];
         o[c][1] *= corr2[1]; o[c][3] *= corr2[1];
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool see = e < 2 ? see0 : see1;
-        p[e] = see ? ex2_approx(v[e] - m[e & 1]) : 0.f;
-        w[e] = p[e] != 0.f ? p[e] * ((e < 2 ? vs0 : vs1) * f[e & 1]) : 0.f;
-      }
+      weigh();
     }
     l[0] += p[0] + p[2];
     l[1] += p[1] + p[3];
@@ -340,14 +348,67 @@ __global__ void __launch_bounds__(K8_THREADS) attn_kv8_kernel(const Kv8Args a) {
   }
 }
 
+// Joins the partial rows of one (sequence, query head), at most 64.  Every warp derives the weights for itself and takes every fourth row,
+// eight loads on their way at a time; a row that has seen nothing (denominator 0) holds anything and counts as zeros.
 template <int D>
-__global__ void __launch_bounds__(MERGE_THREADS) kv8_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots,
-                                                                  __half* __restrict__ out) {
-  __shared__ float sm[MERGE_THREADS / 32 * D];
+__global__ void __launch_bounds__(K8_THREADS) kv8_merge_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots,
+                                                               __half* __restrict__ out) {
+  constexpr int V = D / 32, BATCH = 8;
+  __shared__ float sm[K8_WARPS * D];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const size_t row = blockIdx.x, row0 = row * n_slots;  // row = b * Hq + h
   pdl_wait();
   pdl_trigger();
-  const size_t row = blockIdx.x;  // b * Hq + h
-  paged_merge_row<D>(acc, ml, row * n_slots, n_slots, out + row * D, sm);
+  float m[2], l[2], w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = lane + 32 * k;
+    const float2 x = s < n_slots ? *reinterpret_cast<const float2*>(ml + (row0 + s) * 2) : make_float2(PG_NEG, 0.f);
+    m[k] = x.x;
+    l[k] = x.y;
+  }
+  float v[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = 0.f;
+  const float mx = warp_max(fmaxf(m[0], m[1]));
+#pragma unroll
+  for (int k = 0; k < 2; ++k) w[k] = l[k] != 0.f ? ex2_approx(m[k] - mx) : 0.f;  // NaN is carried on
+  const float sum = warp_sum((l[0] != 0.f ? w[0] * l[0] : 0.f) + (l[1] != 0.f ? w[1] * l[1] : 0.f));
+  for (int s0 = warp; s0 < n_slots; s0 += K8_WARPS * BATCH) {
+    float r[BATCH][V];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int s = s0 + K8_WARPS * i;
+      const float* src = acc + (row0 + (s < n_slots ? s : s0)) * D + V * lane;
+      if (V == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        r[i][0] = x.x; r[i][1] = x.y; r[i][2] = x.z; r[i][V - 1] = x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        r[i][0] = x.x; r[i][1] = x.y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int s = s0 + K8_WARPS * i;
+      const float w0 = __shfl_sync(0xffffffffu, w[0], s & 31), w1 = __shfl_sync(0xffffffffu, w[1], s & 31);
+      const float l0 = __shfl_sync(0xffffffffu, l[0], s & 31), l1 = __shfl_sync(0xffffffffu, l[1], s & 31);
+      const float ws = s < 32 ? w0 : w1;
+      if (s < n_slots && (s < 32 ? l0 : l1) != 0.f) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = fmaf(ws, r[i][j], v[j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) sm[warp * D + V * lane + i] = v[i];
+  __syncthreads();
+  if ((int)threadIdx.x < D) {
+    float x = 0.f;
+#pragma unroll
+    for (int k = 0; k < K8_WARPS; ++k) x += sm[k * D + threadIdx.x];
+    out[row * D + threadIdx.x] = __float2half_rn(sum != 0.f ? x / sum : 0.f);
+  }
 }
 
 template <int D, int G, int FMT, bool CLUSTER>
@@ -375,12 +436,12 @@ int launch_one(const Kv8Args& a, int n_splits, int n_seqs, cudaStream_t st) {
 
 template <int D, int G, int FMT>
 int launch_joined(Kv8Args a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
-  const bool cluster = n_splits >= 2 && n_splits <= 8 && (long long)n_splits * a.Hkv * n_seqs <= 3ll * sm_count();
+  const bool cluster = n_splits >= 2 && n_splits <= 8 && (long long)n_splits * a.Hkv * n_seqs <= (long long)K8_PER_SM * sm_count();
   if (n_splits == 1 || cluster) a.out = out;
   if (cluster) return launch_one<D, G, FMT, true>(a, n_splits, n_seqs, st);
   const int rc = launch_one<D, G, FMT, false>(a, n_splits, n_seqs, st);
   if (rc < 0 || n_splits == 1) return rc;
-  HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_kernel<D>, dim3((unsigned)(n_seqs * a.Hq)), dim3(MERGE_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
+  HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_kernel<D>, dim3((unsigned)(n_seqs * a.Hq)), dim3(K8_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
   return rc + 1;
 }
 
@@ -390,17 +451,34 @@ int launch_fmt(const Kv8Args& a, int fmt, int n_splits, int n_seqs, __half* out,
                              : launch_joined<D, G, HYP_KV8_E4M3>(a, n_splits, n_seqs, out, st);
 }
 
+int wave_splits(int n_seqs, int Hkv) {
+  const int want = (int)((long long)K8_PER_SM * sm_count() / ((long long)n_seqs * Hkv));
+  return want < 1 ? 1 : want;
+}
+
 }  // namespace
+
+int kv8_splits(int n_seqs, int Hkv, int max_pages) {
+  // Up to 16 pages: one CTA per sequence and KV head, which writes the result itself (the join is a launch of its own).  Short contexts:
+  // one wave.  Longer ones (more than 64 pages a CTA that way): about four waves, so that ragged batches even out.  At least one
+  // page per warp.
+  const long long groups = (long long)n_seqs * Hkv;
+  if (max_pages <= 4 * K8_WARPS) return 1;
+  int want = wave_splits(n_seqs, Hkv);
+  if (max_pages > 64 * want) want = (int)((K8_WAVES * K8_PER_SM * sm_count() + groups - 1) / groups);
+  const int cap = (max_pages + K8_WARPS - 1) / K8_WARPS;
+  if (want > cap) want = cap;
+  return want > 64 ? 64 : want;
+}
 
 int launch_attn_kv8(const Kv8View& c, const __half* q, long long q_stride, const int32_t* ctx, float* scratch, __half* out, int* err,
                     cudaStream_t st) {
-  const int ns = paged_splits(c.n_seqs, c.Hkv, c.table_stride), G = c.Hq / c.Hkv;
+  const int ns = kv8_splits(c.n_seqs, c.Hkv, c.table_stride), G = c.Hq / c.Hkv;
   Kv8Args a{};
   a.q = q; a.q_stride = q_stride; a.pool = c.pool; a.table = c.table; a.table_stride = c.table_stride; a.ctx = ctx;
   a.Hq = c.Hq; a.Hkv = c.Hkv;
   a.acc = scratch; a.ml = scratch + (size_t)c.n_seqs * c.Hq * ns * c.D; a.n_slots = ns;
-  const int wave = (int)(3 * sm_count() / ((long long)c.n_seqs * c.Hkv));
-  a.wave_splits = wave < 1 ? 1 : wave;
+  a.wave_splits = wave_splits(c.n_seqs, c.Hkv);
   a.err = err;
 #define HYP_F(DD, GG) if (c.D == DD && G == GG) return launch_fmt<DD, GG>(a, c.fmt, ns, c.n_seqs, out, st);
   HYP_F(128, 1) HYP_F(128, 2) HYP_F(128, 4) HYP_F(128, 8) HYP_F(64, 1) HYP_F(64, 2) HYP_F(64, 4) HYP_F(64, 8)

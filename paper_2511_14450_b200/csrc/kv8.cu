@@ -56,9 +56,11 @@ __device__ __forceinline__ float odd_product(double x, double inv) {
 // hangs on what lies within tol: next to a border between two codes.
 constexpr float ROUND_INT = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
 template <int FMT>
-__device__ __forceinline__ bool fast_codes(const float (&x)[4], const float (&tol)[4], bool exact, float s, float inv, uint32_t& w) {
+__device__ __forceinline__ bool fast_codes(const float (&x)[4], const float (&tol)[4], bool exact, float s, uint32_t& w) {
   bool sure = true;
   if (FMT == HYP_KV8_INT8) {
+    float inv;  // near enough: the rest decides
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
     const float half = 0.5f * s;
     uint32_t q[4];
 #pragma unroll
@@ -71,6 +73,7 @@ __device__ __forceinline__ bool fast_codes(const float (&x)[4], const float (&to
     w = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
     return sure;
   }
+  const float inv = __uint_as_float(0x7f000000u - __float_as_uint(s));  // 1 / s, a power of two in [2^-126, 2^121]
   w = to_e4m3x2(x[0] * inv, x[1] * inv) | to_e4m3x2(x[2] * inv, x[3] * inv) << 16;
   if (exact) return true;
   const uint32_t lo = to_e4m3x2((x[0] - tol[0]) * inv, (x[1] - tol[1]) * inv) | to_e4m3x2((x[2] - tol[2]) * inv, (x[3] - tol[3]) * inv) << 16;
@@ -144,35 +147,25 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
   }
   const int code_at = slot * D + kv8_chunk<D>(l >> 2, slot) + 4 * (l & 3);
   for (int h0 = head - sub; h0 < heads; h0 += step, head += step) {  // the warp's lanes stay together
-    float x[4], o[4], tol[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = next[i];
-      next[i] = 0.f;
-    }
+    const float v[4] = {next[0], next[1], next[2], next[3]};
     if (head + step < heads) load4<TYPE>(src + (long long)(head + step) * (D * SIZE), next);
     const bool any_turn = a.rope && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
-    const float v[4] = {x[0], x[1], x[2], x[3]};
+    float x[4] = {v[0], v[1], v[2], v[3]}, o[4], t[4] = {0.f, 0.f, 0.f, 0.f};
     if (any_turn) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         o[i] = __shfl_xor_sync(0xffffffffu, v[i], LANES / 2);  // the other member of the pair, D / 2 away
         if (turn) {
-          const float t = o[i] * cs[2 * i + 1];
-          x[i] = fmaf(v[i], cs[2 * i], t);
-          tol[i] = (fabsf(t) + fabsf(x[i])) * 0x1p-23f;  // two roundings of half a step each
+          t[i] = o[i] * cs[2 * i + 1];
+          x[i] = fmaf(v[i], cs[2 * i], t[i]);
         }
       }
     }
-    if (h0 + PER <= a.Hq || head < a.Hq) {
-      if (head < a.Hq) *reinterpret_cast<uint2*>(a.q_out + ((long long)row * a.Hq + head) * D + 4 * l) = make_uint2(half2_sat(x[0], x[1]), half2_sat(x[2], x[3]));
-      if (h0 + PER <= a.Hq) continue;  // the whole warp
-    }
-    uint32_t top = max(max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu),
-                       max(__float_as_uint(x[2]) & 0x7fffffffu, __float_as_uint(x[3]) & 0x7fffffffu));
-    const uint32_t own_top = top;
-#pragma unroll
-    for (int k = LANES / 2; k > 0; k >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, k));
+    if (head < a.Hq) *reinterpret_cast<uint2*>(a.q_out + ((long long)row * a.Hq + head) * D + 4 * l) = make_uint2(half2_sat(x[0], x[1]), half2_sat(x[2], x[3]));
+    if (h0 + PER <= a.Hq) continue;  // the whole warp holds queries
+    const uint32_t own_top = max(max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu),
+                                 max(__float_as_uint(x[2]) & 0x7fffffffu, __float_as_uint(x[3]) & 0x7fffffffu));
+    const uint32_t top = __reduce_max_sync(mine, own_top);
     const bool bad = top >= 0x7f800000u;
     // the largest magnitude exactly: among the values whose fp32 form is within its error of the largest one
     double amax = (double)__uint_as_float(top);
@@ -181,7 +174,8 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
       double m = 0.0;
       if (turn && __uint_as_float(own_top) >= close) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = fmax(m, fabs(fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1])));
+        for (int i = 0; i < 4; ++i)
+          if (fabsf(x[i]) >= close) m = fmax(m, fabs(fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1])));
       }
       const uint32_t owners = __ballot_sync(0xffffffffu, m > 0.0) & mine;
       double best = __shfl_sync(0xffffffffu, m, owners ? __ffs(owners) - 1 : lane);  // every lane takes part, zeros among them
@@ -197,7 +191,10 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
     uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
     if (!bad && !zero) {
       s = row_scale<FMT>(amax);
-      if (!fast_codes<FMT>(x, tol, !turn, s, __frcp_rn(s), w)) {
+      float tol[4];  // two roundings of half a step each
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tol[i] = turn ? (fabsf(t[i]) + fabsf(x[i])) * 0x1p-23f : 0.f;
+      if (!fast_codes<FMT>(x, tol, !turn, s, w)) {
         double xd[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) xd[i] = turn ? fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1]) : (double)x[i];

@@ -108,7 +108,7 @@ extern "C" int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int3
 
 extern "C" size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq) {
   if (!shape_ok(shape, HYP_KV8_INT8) || !count_ok(n_seqs) || !pages_ok(max_pages_per_seq)) return 0;
-  return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim, paged_splits(n_seqs, shape->n_kv_heads, max_pages_per_seq));
+  return 4 * paged_scratch_floats(n_seqs, shape->n_q_heads, shape->head_dim, kv8_splits(n_seqs, shape->n_kv_heads, max_pages_per_seq));
 }
 
 extern "C" int hyp_op_attn_decode_kv8(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* q, int64_t q_stride,
