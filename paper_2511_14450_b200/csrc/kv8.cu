@@ -1,6 +1,7 @@
 // Writing the 8-bit paged cache and reading it back.
 #include "kv8.cuh"
 #include "mx4.cuh"
+#include "sm100_common.cuh"
 
 namespace hyp {
 
@@ -52,32 +53,32 @@ __device__ __forceinline__ float odd_product(double x, double inv) {
   return (double)f != y ? __uint_as_float(__float_as_uint(f) | 1u) : f;
 }
 
-// Four codes of values x[i] (fp32, off by at most tol[i] from the value meant; 0: exact) under scale s > 0.  Returns false where some code
-// hangs on what lies within tol: next to a border between two codes.
+// Four codes of values x[i] under scale s > 0; the values are off by at most `tol` from those meant (0: exact).  Returns false where some
+// code hangs on what lies within tol: next to a border between two codes.
 constexpr float ROUND_INT = 12582912.f;  // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
 template <int FMT>
-__device__ __forceinline__ bool fast_codes(const float (&x)[4], const float (&tol)[4], bool exact, float s, uint32_t& w) {
-  bool sure = true;
+__device__ __forceinline__ bool fast_codes(const float (&x)[4], float tol, float s, uint32_t& w) {
   if (FMT == HYP_KV8_INT8) {
     float inv;  // near enough: the rest decides
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
-    const float half = 0.5f * s;
+    const float most = fmaf(0.5f, s, -tol);
     uint32_t q[4];
+    bool sure = true;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float t = fmaf(x[i], inv, ROUND_INT + 128.f);
-      const float r = fabsf(fmaf(-(t - (ROUND_INT + 128.f)), s, x[i]));  // without rounding: the code has 8 bits, s 24, the rest is at most s
-      sure = sure && r + tol[i] < half;
+      const float r = fmaf(-(t - (ROUND_INT + 128.f)), s, x[i]);  // without rounding: the code has 8 bits, s 24, the rest is at most s
+      sure = sure && fabsf(r) < most;
       q[i] = __float_as_uint(t);
     }
     w = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
     return sure;
   }
-  const float inv = __uint_as_float(0x7f000000u - __float_as_uint(s));  // 1 / s, a power of two in [2^-126, 2^121]
+  const float inv = __uint_as_float(0x7f000000u - __float_as_uint(s));  // 1 / s, a power of two in [2^-121, 2^126]
   w = to_e4m3x2(x[0] * inv, x[1] * inv) | to_e4m3x2(x[2] * inv, x[3] * inv) << 16;
-  if (exact) return true;
-  const uint32_t lo = to_e4m3x2((x[0] - tol[0]) * inv, (x[1] - tol[1]) * inv) | to_e4m3x2((x[2] - tol[2]) * inv, (x[3] - tol[3]) * inv) << 16;
-  const uint32_t hi = to_e4m3x2((x[0] + tol[0]) * inv, (x[1] + tol[1]) * inv) | to_e4m3x2((x[2] + tol[2]) * inv, (x[3] + tol[3]) * inv) << 16;
+  if (tol == 0.f) return true;
+  const uint32_t lo = to_e4m3x2((x[0] - tol) * inv, (x[1] - tol) * inv) | to_e4m3x2((x[2] - tol) * inv, (x[3] - tol) * inv) << 16;
+  const uint32_t hi = to_e4m3x2((x[0] + tol) * inv, (x[1] + tol) * inv) | to_e4m3x2((x[2] + tol) * inv, (x[3] + tol) * inv) << 16;
   return lo == hi;
 }
 // The same from fp64 values, exactly: nearest, ties to even.
@@ -110,28 +111,38 @@ struct WriteArgs {
   const int32_t* ctx;
   __half* q_out;      // or null
   int n_seqs, M, Hq, Hkv;
+  int per;            // heads of a CTA, a multiple of 128 / D
+  int* err;
 };
 
-// grid (M, shares of the heads).  D / 4 lanes take a head of a row, four values each; a warp takes every (8 gridDim.y)-th head (pair of heads
-// at D = 64) of its row, so that the row's sequence, page and angles are found once, and has the next head's values on their way.
-//   Bound by HBM for prompts (fp32 rows: 7 bytes in for 1 out), by latency for single tokens.  Codes have to be those of the exact value, and
-// exact arithmetic on every value costs more than the memory: a first version in fp64 took 76 us for 4096 rows of 60 heads, issue slots 84 %
-// busy.  So values are rotated and rounded in fp32 with a bound on the error beside them, and only where a code would hang on
-// it (about one warp in a hundred), and for the row's largest value, is fp64 used: its products of fp32 numbers are exact.
+// grid (M, shares of the heads).  One bulk copy brings a CTA's heads of a row to shared memory while the warps look up the row's sequence, page
+// and angles; then D / 4 lanes take a head, four values each.
+//   Bound by HBM for prompts (fp32 rows: 7 bytes in for 2.7 out), by latency for single tokens.  Loads by the warps themselves, one head
+// ahead, had 24 KB on their way on an SM: 3.4 TB/s.
+//   Codes have to be those of the exact value.  Exact arithmetic on every value costs more than the memory (in fp64 76 us for 4096 rows of 60
+// heads, issue slots 84 % busy), so values are rotated and rounded in fp32, and fp64, in which products of fp32 numbers are exact, is
+// used for the largest value of a row and where a code hangs on the rotation's roundings.  Those are two of half a step each, of a term and of
+// the sum; as both members of the row's pairs are kept, neither exceeds 1.42 times the row's largest magnitude: 2^-22 of it covers them.
 template <int D, int FMT, int TYPE>
 __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
   constexpr int LANES = D / 4, PER = 32 / LANES, SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
+  extern __shared__ __align__(128) uint8_t wr_smem[];
+  __shared__ uint64_t bar_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LANES, sub = lane / LANES;
   const uint32_t mine = LANES == 32 ? 0xffffffffu : 0xffffu << (16 * sub);  // the lanes of this head
-  const int row = blockIdx.x;
-  const int heads = a.Hq + 2 * a.Hkv, step = 8 * gridDim.y * PER;
-  int head = (a.q_out ? 0 : a.Hq) + (blockIdx.y * 8 + warp) * PER + sub;
+  const int row = blockIdx.x, heads = a.Hq + 2 * a.Hkv;
+  const int h_lo = (a.q_out ? 0 : a.Hq) + blockIdx.y * a.per, h_hi = min(h_lo + a.per, heads);
+  const uint32_t bar = smem_u32(&bar_word);
   pdl_wait();
   pdl_trigger();
   if (row >= a.cu[a.n_seqs]) return;
-  const uint8_t* src = a.qkv + ((long long)row * a.stride + 4 * l) * SIZE;
-  float next[4] = {0.f, 0.f, 0.f, 0.f};
-  if (head < heads) load4<TYPE>(src + (long long)head * (D * SIZE), next);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    const uint32_t bytes = (uint32_t)(h_hi - h_lo) * (D * SIZE);
+    mbar_expect_tx(bar, bytes);
+    bulk_load(smem_u32(wr_smem), a.qkv + ((long long)row * a.stride + (long long)h_lo * D) * SIZE, bytes, bar);
+  }
   const int seq = sequence_of(a.cu, a.n_seqs, row, lane);
   const long long pos = (long long)a.ctx[seq] + (row - a.cu[seq]);
   const bool kept = pos >= 0 && pos < (long long)a.table_stride * 16;
@@ -146,22 +157,30 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
     cs[0] = t0.x; cs[1] = t0.y * sign; cs[2] = t0.z; cs[3] = t0.w * sign; cs[4] = t1.x; cs[5] = t1.y * sign; cs[6] = t1.z; cs[7] = t1.w * sign;
   }
   const int code_at = slot * D + kv8_chunk<D>(l >> 2, slot) + 4 * (l & 3);
-  for (int h0 = head - sub; h0 < heads; h0 += step, head += step) {  // the warp's lanes stay together
-    const float v[4] = {next[0], next[1], next[2], next[3]};
-    if (head + step < heads) load4<TYPE>(src + (long long)(head + step) * (D * SIZE), next);
-    const bool any_turn = a.rope && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
-    float x[4] = {v[0], v[1], v[2], v[3]}, o[4], t[4] = {0.f, 0.f, 0.f, 0.f};
-    if (any_turn) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        o[i] = __shfl_xor_sync(0xffffffffu, v[i], LANES / 2);  // the other member of the pair, D / 2 away
-        if (turn) {
-          t[i] = o[i] * cs[2 * i + 1];
-          x[i] = fmaf(v[i], cs[2 * i], t[i]);
-        }
-      }
+  __syncthreads();  // the barrier is set up
+  if (!mbar_wait(bar, 0, nullptr)) {
+    if (threadIdx.x == 0) {
+      atomicCAS(a.err, 0, 35);
+      mbar_wait(bar, 0, nullptr);
     }
-    if (head < a.Hq) *reinterpret_cast<uint2*>(a.q_out + ((long long)row * a.Hq + head) * D + 4 * l) = make_uint2(half2_sat(x[0], x[1]), half2_sat(x[2], x[3]));
+    return;
+  }
+  const uint8_t* mine_at = wr_smem + 4 * l * SIZE;
+  const int other = (l < LANES / 2 ? D / 2 : -D / 2) * SIZE;
+  __half* q_to = a.q_out + (long long)row * a.Hq * D + 4 * l;
+  for (int h0 = h_lo + warp * PER; h0 < h_hi; h0 += 8 * PER) {  // the warp's lanes stay together
+    const int head = h0 + sub;
+    const bool in = head < h_hi;
+    const bool any_turn = a.rope && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};  // own values and the other members of their pairs, D / 2 away
+    if (in) load4<TYPE>(mine_at + (head - h_lo) * (D * SIZE), v);
+    if (turn && in) load4<TYPE>(mine_at + (head - h_lo) * (D * SIZE) + other, o);
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    if (turn) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = fmaf(v[i], cs[2 * i], o[i] * cs[2 * i + 1]);
+    }
+    if (head < a.Hq) *reinterpret_cast<uint2*>(q_to + (size_t)head * D) = make_uint2(half2_sat(x[0], x[1]), half2_sat(x[2], x[3]));
     if (h0 + PER <= a.Hq) continue;  // the whole warp holds queries
     const uint32_t own_top = max(max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu),
                                  max(__float_as_uint(x[2]) & 0x7fffffffu, __float_as_uint(x[3]) & 0x7fffffffu));
@@ -170,7 +189,7 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
     // the largest magnitude exactly: among the values whose fp32 form is within its error of the largest one
     double amax = (double)__uint_as_float(top);
     if (any_turn) {
-      const float close = __uint_as_float(top) * (1.f - 0x1p-19f);
+      const float close = __uint_as_float(top) * (1.f - 0x1p-20f);
       double m = 0.0;
       if (turn && __uint_as_float(own_top) >= close) {
 #pragma unroll
@@ -186,25 +205,22 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
       }
       if (turn) amax = best;
     }
-    const bool zero = !(amax >= (double)KV8_LEAST);
     float s = 0.f;
     uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
-    if (!bad && !zero) {
+    if (!bad && amax >= (double)KV8_LEAST) {
       s = row_scale<FMT>(amax);
-      float tol[4];  // two roundings of half a step each
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tol[i] = turn ? (fabsf(t[i]) + fabsf(x[i])) * 0x1p-23f : 0.f;
-      if (!fast_codes<FMT>(x, tol, !turn, s, w)) {
+      if (!fast_codes<FMT>(x, turn ? __uint_as_float(top) * 0x1p-22f : 0.f, s, w)) {
         double xd[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) xd[i] = turn ? fma((double)v[i], (double)cs[2 * i], (double)o[i] * (double)cs[2 * i + 1]) : (double)x[i];
         w = exact_codes<FMT>(xd[0], xd[1], xd[2], xd[3], s);
       }
     }
-    if (head < a.Hq || head >= heads || !kept) continue;
-    uint8_t* half_page = page + (size_t)(head - a.Hq) * kv8_half_page(D);  // value heads follow the key heads
-    *reinterpret_cast<uint32_t*>(half_page + code_at) = w;
-    if (l == 0) *reinterpret_cast<float*>(half_page + 16 * D + 4 * slot) = bad ? __uint_as_float(0x7fffffffu) : s;
+    if (head >= a.Hq && in && kept) {
+      uint8_t* half_page = page + (size_t)(head - a.Hq) * kv8_half_page(D);  // value heads follow the key heads
+      *reinterpret_cast<uint32_t*>(half_page + code_at) = w;
+      if (l == 0) *reinterpret_cast<float*>(half_page + 16 * D + 4 * slot) = bad ? __uint_as_float(0x7fffffffu) : s;
+    }
   }
 }
 
@@ -260,12 +276,19 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
   }
 }
 
+constexpr int WR_SMEM = 32 * 1024;  // of a row in a CTA
 template <int D, int FMT, int TYPE>
-int write_go(const WriteArgs& a, cudaStream_t st) {
-  const int heads = (a.q_out ? a.Hq : 0) + 2 * a.Hkv, most = (heads + 8 * (128 / D) - 1) / (8 * (128 / D));
-  int y = (8 * sm_count() + a.M - 1) / a.M;  // few rows: a head for every warp; many: one CTA a row
+int write_go(WriteArgs a, cudaStream_t st) {
+  constexpr int PER = 128 / D, HEAD = D * (TYPE == HYP_TYPE_F32 ? 4 : 2);
+  const int heads = (a.q_out ? a.Hq : 0) + 2 * a.Hkv;
+  // few rows: down to a head (a pair at D = 64) for every warp; many: as much of a row as a CTA holds
+  int y = (8 * sm_count() + a.M - 1) / a.M;
+  const int most = (heads + 8 * PER - 1) / (8 * PER), least = (heads * HEAD + WR_SMEM - 1) / WR_SMEM;
   if (y > most) y = most;
-  HYP_CUDA_TRY(launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE>, dim3((unsigned)a.M, (unsigned)y), dim3(256), (size_t)0, st, a));
+  if (y < least) y = least;
+  a.per = ((heads + y - 1) / y + PER - 1) / PER * PER;
+  y = (heads + a.per - 1) / a.per;
+  HYP_CUDA_TRY(launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE>, dim3((unsigned)a.M, (unsigned)y), dim3(256), (size_t)a.per * HEAD, st, a));
   return 1;
 }
 template <int D, int FMT>
@@ -278,8 +301,9 @@ int write_type(const WriteArgs& a, int type, cudaStream_t st) {
 }  // namespace
 
 int launch_kv8_write(const Kv8View& c, int M, const void* qkv, int type, long long stride, const float* rope, int rope_positions,
-                     const int32_t* cu_q, const int32_t* ctx, __half* q_out, cudaStream_t st) {
+                     const int32_t* cu_q, const int32_t* ctx, __half* q_out, int* err, cudaStream_t st) {
   WriteArgs a{};
+  a.err = err;
   a.qkv = (const uint8_t*)qkv; a.stride = stride; a.rope = rope; a.rope_positions = rope_positions;
   a.pool = c.pool; a.table = c.table; a.table_stride = c.table_stride; a.cu = cu_q; a.ctx = ctx; a.q_out = q_out;
   a.n_seqs = c.n_seqs; a.M = M; a.Hq = c.Hq; a.Hkv = c.Hkv;

@@ -26,7 +26,7 @@ struct Kv8View {
 };
 
 int launch_kv8_write(const Kv8View& c, int M, const void* qkv, int type, long long stride, const float* rope, int rope_positions,
-                     const int32_t* cu_q, const int32_t* ctx, __half* q_out, cudaStream_t st);
+                     const int32_t* cu_q, const int32_t* ctx, __half* q_out, int* err, cudaStream_t st);
 int launch_kv8_read(const Kv8View& c, const int32_t* first, const int32_t* lens, __half* dst, const int32_t* dst_table, int dst_stride,
                     cudaStream_t st);
 int kv8_splits(int n_seqs, int Hkv, int max_pages);

@@ -92,8 +92,10 @@ extern "C" int hyp_op_kv8_write(const hyp_attn_shape* shape, int32_t format, int
   if (!count_ok(n_seqs) || M < 1 || M > (1 << 26) || !pages_ok(max_pages_per_seq) || (rope_table && rope_positions < 1)) return HYP_EINVAL;
   if (stride < ((int64_t)shape->n_q_heads + 2 * shape->n_kv_heads) * shape->head_dim || stride % 8) return HYP_EINVAL;
   if (!aligned(qkv, 16) || !aligned(kv8_pages, 16) || !aligned(rope_table, 16) || !aligned(q_out, 16)) return HYP_EINVAL;
+  const int rc = tc_prepare();
+  if (rc) return rc;
   return finish(launch_kv8_write(view(shape, format, n_seqs, kv8_pages, block_table, max_pages_per_seq), M, qkv, type, stride, rope_table,
-                                 rope_positions, cu_q, ctx_lens, (__half*)q_out, (cudaStream_t)stream));
+                                 rope_positions, cu_q, ctx_lens, (__half*)q_out, tc_err_flag_ptr(), (cudaStream_t)stream));
 }
 
 extern "C" int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* kv8_pages, const int32_t* block_table,
