@@ -21,7 +21,7 @@ namespace hyp {
 namespace {
 
 constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32, K8_SLOTS = 2;
-constexpr int K8_PER_SM = 5, K8_WAVES = 2;  // resident CTAs; waves that a long context is cut for
+constexpr int K8_PER_SM = 5, K8_WAVES = 4;  // resident CTAs; waves that a long context is cut for
 constexpr float K8_GROWN = 256.f;
 
 struct Kv8Args {

@@ -12,9 +12,9 @@
 // N operand, terms x tokens columns, at most 256).  Where there are few such tiles K is split over a cluster of up to eight CTAs:
 // each leaves its sums in shared memory, and every one of them finishes a share of the tokens, adding the others' in rank order
 // through distributed shared memory: deterministic.
-//   warp 0     one lane fills the ring: weight codes (a TMA box), weight scales, terms with their scales (bulk copies);
+//   warp 0     one lane fills the ring with weight codes (a TMA box), one of warp 2 with weight scales, one of warp 3 with terms;
 //   warp 1     one lane copies the scales to tensor memory and issues the MMAs;
-//   warps 2-5  epilogue, lane = weight row.
+//   warps 2-9  epilogue, lane = weight row.
 // Every mbarrier wait is bounded; the cluster barriers are reached by every thread of every CTA.
 #include <cuda.h>
 
@@ -27,7 +27,7 @@ namespace hyp {
 
 namespace {
 
-constexpr int MX_THREADS = 192, MX_MAX_STAGES = 12, MX_A_BYTES = MX_ROWS * MX_BK;
+constexpr int MX_EPI_WARPS = 8, MX_THREADS = 64 + 32 * MX_EPI_WARPS, MX_MAX_STAGES = 12, MX_A_BYTES = MX_ROWS * MX_BK;
 
 // How M tokens are cut: tiles of `tt` tokens, `nb` operand rows (terms x tokens, filled up to a multiple of 16).  `cap`: most rows.
 struct TokenTiles {
@@ -49,45 +49,62 @@ TokenTiles token_tiles(int M, int terms, int cap) {
 int row_cap(int epi) { return epi == EPI_SWIGLU_BF16 ? 240 : 256; }
 
 // ---------------------------------------------------------------------------------------------
-// activations to terms: four threads take a block of 32 k of one token, eight values each
+// activations to terms: four lanes take a block of 32 k of one token, eight values each
 // ---------------------------------------------------------------------------------------------
+// U chunks at a time; calls put(chunk, term, codes, scale).  Every lane of the warp calls this.
+template <int U, typename Put>
+__device__ __forceinline__ void make_terms(float (&v)[U][8], int terms, Put put) {
+  bool bad[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) bad[j] = false;
+  for (int t = 0; t < terms; ++t) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      uint32_t top = absmax_bits(v[j]);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      bad[j] = bad[j] || top >= 0x7f800000u;
+      const int e = bad[j] ? 0 : e4m3_exponent(top);
+      const float inv = bad[j] ? 0.f : pow2(-e), scale = pow2(e);
+      uint32_t w[2] = {0u, 0u};
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t q = bad[j] ? 0u : to_e4m3x2(v[j][2 * p] * inv, v[j][2 * p + 1] * inv);
+        w[p >> 1] |= q << (16 * (p & 1));
+        if (t + 1 < terms) {
+          const float2 f = half2_values(e4m3x2_to_half2(q));
+          v[j][2 * p] = fmaf(-f.x, scale, v[j][2 * p]);  // exact: what is left has fewer bits
+          v[j][2 * p + 1] = fmaf(-f.y, scale, v[j][2 * p + 1]);
+        }
+      }
+      put(j, t, make_uint2(w[0], w[1]), bad[j] ? 255 : (uint8_t)(e + 127));
+    }
+  }
+}
+// Where chunk c (eight k) of operand row r goes in a block of terms, and the scale of its 32 k.
+__device__ __forceinline__ uint32_t term_at(int r, int c) { return (uint32_t)(r * MX_BK + (((c >> 1) ^ (r & 7)) << 4) + 8 * (c & 1)); }
+__device__ __forceinline__ uint32_t term_scale_at(int nb, int r, int c) {
+  return (uint32_t)(nb * MX_BK + (r >> 7) * MX_SF_BYTES + (r & 31) * 16 + ((r >> 5) & 3) * 4 + (c >> 2));
+}
+
 constexpr int TERM_THREADS = 128;
 // grid (M, segments of 128 chunks of eight values)
 template <int TYPE>
-__global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int M, int K8, int KB, int terms,
+__global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int K8, int KB, int terms,
                                                                 int tt, int nb, size_t block_bytes, uint8_t* __restrict__ out) {
   const int m = blockIdx.x, c = blockIdx.y * TERM_THREADS + threadIdx.x;
-  const bool row_in = c < 16 * KB;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float v[1][8] = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
   pdl_wait();
   pdl_trigger();
-  if (c < K8) load8<TYPE>(a + (m * stride + 8 * c) * 2, v);
-  const int kb = c >> 4, chunk = (c & 15) >> 1;  // 16-byte chunk of the 128-byte operand row
-  uint8_t* blk = out + ((size_t)(m / tt) * KB + kb) * block_bytes;
-  bool bad = false;
-  for (int t = 0; t < terms; ++t) {
-    uint32_t top = absmax_bits(v);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    bad = bad || top >= 0x7f800000u;
-    const int e = bad ? 0 : e4m3_exponent(top);
-    const float inv = pow2(-e), scale = pow2(e);
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const uint32_t q = bad ? 0u : to_e4m3x2(v[2 * p] * inv, v[2 * p + 1] * inv);
-      w[p >> 1] |= q << (16 * (p & 1));
-      const float2 f = half2_values(e4m3x2_to_half2(q));
-      v[2 * p] -= f.x * scale;
-      v[2 * p + 1] -= f.y * scale;
-    }
-    if (row_in) {
-      const int r = t * tt + m % tt;
-      *reinterpret_cast<uint2*>(blk + r * MX_BK + ((chunk ^ (r & 7)) << 4) + 8 * (c & 1)) = make_uint2(w[0], w[1]);
-      if ((c & 3) == 0)
-        blk[nb * MX_BK + (r >> 7) * MX_SF_BYTES + (r & 31) * 16 + ((r >> 5) & 3) * 4 + ((c >> 2) & 3)] = bad ? 255 : (uint8_t)(e + 127);
-    }
-  }
+  if (c < K8) load8<TYPE>(a + (m * stride + 8ll * c) * 2, v[0]);
+  const int tile = m / tt, row = m - tile * tt;
+  uint8_t* blk = out + ((size_t)tile * KB + (c >> 4)) * block_bytes;
+  make_terms<1>(v, terms, [&](int, int t, uint2 codes, uint8_t scale) {
+    if (c >= 16 * KB) return;
+    const int r = t * tt + row;
+    *reinterpret_cast<uint2*>(blk + term_at(r, c & 15)) = codes;
+    if ((c & 3) == 0) blk[term_scale_at(nb, r, c & 15)] = scale;
+  });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -101,50 +118,81 @@ struct MxArgs {
   int tiles, token_tiles, tt, nb, n_terms, sf_bytes;
   int stages, stage_bytes, ksplit, tmem_cols;
   uint32_t idesc;
-  bool f16;
+  bool f16, vec;          // vec: four results at a time may be stored
   void* out;
   int* err;
 };
 
-__device__ __forceinline__ void mx_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t acc) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc)
-      : "memory");
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+// The issuing threads run alone, at about five cycles an instruction: what they do for a stage is kept to additions.
+template <bool ACC>
+__device__ __forceinline__ void mx_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb) {
+  if (ACC)
+    asm volatile("tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], 1;"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb) : "memory");
+  else
+    asm volatile("tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], 0;"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb) : "memory");
 }
 // 512 bytes of scales (32 lines of 16 bytes) to four columns of tensor memory, the same in every quarter of the lanes.
-__device__ __forceinline__ void mx_copy_scales(uint32_t tmem, uint32_t smem) {
-  uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4);
-  d |= (uint64_t)1 << 16;           // not used: one 16-byte column
-  d |= (uint64_t)(128 >> 4) << 32;  // eight lines on
-  d |= (uint64_t)1 << 46;
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(d) : "memory");
+__device__ __forceinline__ void mx_copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+// Their shared-memory descriptor: eight lines are 128 bytes, no swizzle.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// without the wait: several loads share one
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
   uint32_t r[8];
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
-  tmem_ld_wait();
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t local_addr, uint32_t rank) {
+  uint32_t remote;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local_addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+  return v;
+}
+__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
+// Four results of token m, columns n .. n + 3.
 template <int EPI>
-__device__ __forceinline__ void mx_store(const MxArgs& p, int m, int n, float a, float b) {
+__device__ __forceinline__ void mx_store(const MxArgs& p, int m, int n, float4 y) {
   const size_t o = (size_t)m * p.ldo + n;
+  const float e[4] = {y.x, y.y, y.z, y.w};
   if (EPI == EPI_STORE_BF16 || EPI == EPI_SWIGLU_BF16) {
-    const float y = EPI == EPI_SWIGLU_BF16 ? a / (1.f + __expf(-a)) * b : a;
-    if (p.f16)
-      reinterpret_cast<__half*>(p.out)[o] = __float2half_rn(y != y ? y : fminf(fmaxf(y, -65504.f), 65504.f));
-    else
-      reinterpret_cast<__nv_bfloat16*>(p.out)[o] = __float2bfloat16_rn(y);
-  } else if (EPI == EPI_RESID_F32) {
-    reinterpret_cast<float*>(p.out)[o] += a;
+    uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + o;
+    const uint32_t lo = p.f16 ? half2_sat(y.x, y.y) : pack_bf16(y.x, y.y), hi = p.f16 ? half2_sat(y.z, y.w) : pack_bf16(y.z, y.w);
+    if (p.vec && n + 3 < p.N) {
+      *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+    } else {
+      const uint16_t h[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n + i < p.N) to[i] = h[i];
+    }
   } else {
-    reinterpret_cast<float*>(p.out)[o] = a;
+    float* to = reinterpret_cast<float*>(p.out) + o;
+    if (p.vec && n + 3 < p.N) {
+      if (EPI == EPI_RESID_F32) {
+        const float4 x = *reinterpret_cast<const float4*>(to);
+        y.x += x.x; y.y += x.y; y.z += x.z; y.w += x.w;
+      }
+      *reinterpret_cast<float4*>(to) = y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n + i < p.N) to[i] = EPI == EPI_RESID_F32 ? to[i] + e[i] : e[i];
+    }
   }
 }
 
@@ -158,7 +206,8 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   const uint32_t base = (smem_u32(mx_smem) + 1023u) & ~1023u;
-  float* dump = reinterpret_cast<float*>(mx_smem + (base - smem_u32(mx_smem)));  // [accumulator][token][128 rows]
+  uint8_t* ring = mx_smem + (base - smem_u32(mx_smem));
+  float* sums = reinterpret_cast<float*>(ring);  // behind the main loop: [accumulator][token][128 rows]
   const int S = p.stages;
   const uint32_t b_off = A_TILES * MX_A_BYTES, sfa_off = b_off + (uint32_t)p.block_bytes;  // terms, their scales, weight scales
   const uint32_t bar0 = smem_u32(bars);
@@ -167,7 +216,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   const uint32_t tfull_bar = bar0 + 8u * (2 * MX_MAX_STAGES);
   volatile int* abort_flag = &abort_word;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % (unsigned)p.ksplit);
   const int unit = (int)(blockIdx.x / (unsigned)p.ksplit);
   const int tile = unit / p.token_tiles, tok = unit % p.token_tiles;  // the token tiles of a weight tile run side by side
@@ -175,31 +224,58 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(full_bar(s), 1);
+      mbar_init(full_bar(s), 3);  // codes, weight scales, terms
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(tfull_bar, 1);
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const uint8_t* terms = p.terms + (size_t)tok * p.KB * p.block_bytes;
-  auto load_w = [&](int kb, int s) {
-    const uint32_t st = base + s * p.stage_bytes;
-    mbar_expect_tx(full_bar(s), (uint32_t)(A_TILES * MX_PACK_BYTES + p.block_bytes));  // the box counts by what it reads
-#pragma unroll
-    for (int h = 0; h < A_TILES; ++h) {
-      const long long blk = (long long)(h * p.tiles + tile) * p.KB + kb;
-      tma_load_2d(st + h * MX_A_BYTES, &tm_w, 0, (int)(blk * (MX_PACK_BYTES / 64)), full_bar(s));
-      bulk_load(st + sfa_off + h * MX_SF_BYTES, p.packed + blk * MX_PACK_BYTES + MX_CODE_BYTES, MX_SF_BYTES, full_bar(s));
+  const uint8_t* terms = p.terms + ((size_t)tok * p.KB + kb0) * p.block_bytes;
+  // What a producing thread adds to the ring: `src` steps by `step` from k-block to k-block, `dst` and `bar` from stage to stage.
+  const int n_kb = kb1 - kb0, n_first = min(S, n_kb);
+  const int line0 = (int)(((long long)tile * p.KB + kb0) * (MX_PACK_BYTES / 64)), up_lines = (int)((long long)p.tiles * p.KB * (MX_PACK_BYTES / 64));
+  auto load_w = [&](int line, uint32_t dst, uint32_t bar) {
+    mbar_expect_tx(bar, A_TILES * MX_CODE_BYTES);  // a box counts by what it reads
+    tma_load_2d(dst, &tm_w, 0, line, bar);
+    if (SWIGLU) tma_load_2d(dst + MX_A_BYTES, &tm_w, 0, line + up_lines, bar);
+  };
+  auto load_s = [&](const uint8_t* src, uint32_t dst, uint32_t bar) {
+    mbar_expect_tx(bar, A_TILES * MX_SF_BYTES);
+    bulk_load(dst + sfa_off, src, MX_SF_BYTES, bar);
+    if (SWIGLU) bulk_load(dst + sfa_off + MX_SF_BYTES, src + 64ll * up_lines, MX_SF_BYTES, bar);
+  };
+  const uint32_t term_bytes = (uint32_t)p.block_bytes;
+  auto load_t = [&](const uint8_t* src, uint32_t dst, uint32_t bar) {
+    mbar_expect_tx(bar, term_bytes);
+    bulk_load(dst + b_off, src, term_bytes, bar);
+  };
+  // One thread: all of the CTA's stages from `from` (at most S) on.
+  auto produce = [&](auto load, auto src, auto step, int from) {
+    src += step * from;
+    int stage = from == S ? 0 : from;
+    uint32_t phase = from == S ? 0u : 1u;  // of the "empty" phase waited for; the first pass over the ring waits for nothing
+    uint32_t dst = base + stage * p.stage_bytes;
+    for (int i = from; i < n_kb; ++i) {
+      if (i >= S && !mbar_wait(empty_bar(stage), phase, abort_flag)) {
+        *abort_flag = 1;
+        atomicCAS(p.err, 0, 31);
+        return false;
+      }
+      load(src, dst, full_bar(stage));
+      src += step;
+      dst += p.stage_bytes;
+      if (++stage == S) {
+        stage = 0;
+        phase ^= 1u;
+        dst = base;
+      }
     }
+    return true;
   };
-  auto load_t = [&](int kb, int s) {
-    bulk_load(base + s * p.stage_bytes + b_off, terms + (size_t)kb * p.block_bytes, (uint32_t)p.block_bytes, full_bar(s));
-  };
-  const int n_first = min(S, kb1 - kb0);
   __syncwarp();
   if (threadIdx.x == 0)  // weights are no kernel's output: their first boxes go out before the wait
-    for (int i = 0; i < n_first; ++i) load_w(kb0 + i, i);
+    for (int i = 0; i < n_first; ++i) load_w(line0 + i * (MX_PACK_BYTES / 64), base + i * p.stage_bytes, full_bar(i));
   __syncwarp();
   pdl_wait();
   if (warp == 1) {
@@ -212,129 +288,157 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   const uint32_t tmem_base = tmem_slot;
   pdl_trigger();
 
-  int issued = n_first;  // stages that the producer has filled
+  const int m0 = tok * p.tt, mt = min(p.tt, p.M - m0);
   if (warp == 0) {
-    if (lane == 0) {
-      for (int i = 0; i < n_first; ++i) load_t(kb0 + i, i);
-      int stage = n_first == S ? 0 : n_first;
-      uint32_t phase = n_first == S ? 1 : 0;
-      bool ok = true;
-      for (int kb = kb0 + n_first; kb < kb1; ++kb) {
-        if (!mbar_wait(empty_bar(stage), phase ^ 1, abort_flag)) { ok = false; break; }
-        load_w(kb, stage);
-        load_t(kb, stage);
-        issued = kb + 1 - kb0;
-        if (++stage == S) { stage = 0; phase ^= 1; }
-      }
-      if (!ok) {
-        *abort_flag = 1;
-        atomicCAS(p.err, 0, 31);
-      }
-    }
+    if (lane == 0) produce(load_w, line0, MX_PACK_BYTES / 64, n_first);
   } else if (warp == 1) {
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      const uint32_t t_sfa = tmem_base + (uint32_t)(A_TILES * p.nb), t_sfb = t_sfa + 4 * A_TILES;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t sa = base + stage * p.stage_bytes;
+    // The whole warp walks the loop and one lane issues: so the operands stay in uniform registers (a lane on its own moves each of them there
+    // for every instruction: 800 cycles a stage).
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0), ub = __shfl_sync(0xffffffffu, base, 0);
+    const uint32_t sfa = tm + (uint32_t)(A_TILES * p.nb), sfb = sfa + 4 * A_TILES, step = (uint32_t)p.stage_bytes >> 4;
+    const uint64_t da0 = smem_desc(ub), db0 = smem_desc(ub + b_off), dsa0 = scales_desc(ub + sfa_off), dsb0 = scales_desc(ub + b_off + p.nb * MX_BK);
+    const uint32_t id0 = p.idesc, id1 = id0 | 1u << 29 | 1u << 4, id2 = id0 | 2u << 29 | 2u << 4, id3 = id0 | 3u << 29 | 3u << 4;  // byte of a scale word
+    const uint32_t acc2 = tm + (uint32_t)p.nb;
+    const bool two_sf = p.nb > MX_ROWS;
+    int stage = 0;
+    uint32_t phase = 0, at = 0;  // at: the stage's place, in descriptor units
+    bool ok = true;
+    for (int i = 0; i < n_kb; ++i) {
+      ok = __all_sync(0xffffffffu, mbar_wait(full_bar(stage), phase, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t da = da0 + at, db = db0 + at;
+      if (elect_one()) {
         // scales of this stage: in order behind the MMAs that still read the ones before
-#pragma unroll
-        for (int h = 0; h < A_TILES; ++h) mx_copy_scales(t_sfa + 4 * h, sa + sfa_off + h * MX_SF_BYTES);
-        for (int h = 0; h < p.sf_bytes; h += MX_SF_BYTES) mx_copy_scales(t_sfb + h / (MX_SF_BYTES / 4), sa + b_off + p.nb * MX_BK + h);
-        const uint64_t da = smem_desc(sa), db = smem_desc(sa + b_off);
-#pragma unroll
-        for (int k = 0; k < MX_BK / 32; ++k) {
-          const uint32_t accum = (kb > kb0 || k > 0) ? 1u : 0u;
-          const uint32_t idesc = p.idesc | (uint32_t)k << 29 | (uint32_t)k << 4;  // which byte of a scale word
-          mx_mma(tmem_base, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, t_sfa, t_sfb, accum);
-          if (SWIGLU)
-            mx_mma(tmem_base + (uint32_t)p.nb, da + (uint64_t)(MX_A_BYTES / 16 + k * 2), db + (uint64_t)(k * 2), idesc, t_sfa + 4, t_sfb, accum);
+        mx_copy_scales(sfa, dsa0 + at);
+        if (SWIGLU) mx_copy_scales(sfa + 4, dsa0 + at + MX_SF_BYTES / 16);
+        mx_copy_scales(sfb, dsb0 + at);
+        if (two_sf) mx_copy_scales(sfb + 4, dsb0 + at + MX_SF_BYTES / 16);
+        if (i == 0) {
+          mx_mma<false>(tm, da, db, id0, sfa, sfb);
+          if (SWIGLU) mx_mma<false>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
+        } else {
+          mx_mma<true>(tm, da, db, id0, sfa, sfb);
+          if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
         }
+        mx_mma<true>(tm, da + 2, db + 2, id1, sfa, sfb);
+        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 2, db + 2, id1, sfa + 4, sfb);
+        mx_mma<true>(tm, da + 4, db + 4, id2, sfa, sfb);
+        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 4, db + 4, id2, sfa + 4, sfb);
+        mx_mma<true>(tm, da + 6, db + 6, id3, sfa, sfb);
+        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 6, db + 6, id3, sfa + 4, sfb);
         tc_commit(empty_bar(stage));
-        if (++stage == S) { stage = 0; phase ^= 1; }
+        if (i == n_kb - 1) tc_commit(tfull_bar);
       }
-      if (ok) {
-        tc_commit(tfull_bar);
-      } else {
-        *abort_flag = 1;
-        atomicCAS(p.err, 0, 32);
-      }
+      __syncwarp();
+      at += step;
+      if (++stage == S) { stage = 0; phase ^= 1u; at = 0; }
     }
-  }
-
-  // ---------------- epilogue warps ----------------
-  const int row = 32 * (warp & 3) + lane;  // the quarter of the lanes that this warp may read
-  const uint32_t t0 = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
-  const int n = tile * MX_ROWS + row, m0 = tok * p.tt, mt = min(p.tt, p.M - m0);
-  bool acc_ok = true;
-  // eight tokens' sums over the terms, `acc` = accumulator
-  auto sums = [&](int acc, int c, float (&v)[8]) {
-    tmem_ld8(t0 + acc * p.nb + c, v);
-    for (int t = 1; t < p.n_terms; ++t) {
-      float w[8];
-      tmem_ld8(t0 + acc * p.nb + t * p.tt + c, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += w[i];
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      atomicCAS(p.err, 0, 32);
     }
-  };
-  if (warp >= 2) {
-    acc_ok = mbar_wait(tfull_bar, 0, abort_flag);
+  } else {
+    bool ok = true;
+    // two of these warps issue copies first: a thread takes about 250 cycles for one, three to a stage would hold up the stream
+    if (warp == 2 && lane == 0) ok = produce(load_s, p.packed + 64ll * line0 + MX_CODE_BYTES, MX_PACK_BYTES, 0);
+    if (warp == 3 && lane == 0) ok = produce(load_t, terms, term_bytes, 0);
+    ok = __all_sync(0xffffffffu, ok);
+    // accumulators to shared memory, the terms added up (one CTA to a tile: SwiGLU applied); lane = weight row
+    const int row = 32 * (warp & 3) + lane;
+    const uint32_t t0 = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
+    ok = mbar_wait(tfull_bar, 0, abort_flag) && ok;
     tc_fence_after();
-    if (!acc_ok && lane == 0) {
+    if (!ok && lane == 0) {
       *abort_flag = 1;
       atomicCAS(p.err, 0, 33);
     }
-    if (acc_ok) {
-      for (int c = 0; c < mt; c += 8) {
-        float v[8], u[8];
-        sums(0, c, v);
-        if (SWIGLU) sums(1, c, u);
-        if (p.ksplit > 1) {
+    if (ok) {
+      constexpr int B = 2;  // groups of eight tokens in flight
+      for (int c = 8 * B * ((warp - 2) / 4); c < mt; c += 8 * B * (MX_EPI_WARPS / 4)) {  // two warps share a quarter of the lanes
+        float v[B][8], u[B][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            dump[(c + i) * MX_ROWS + row] = v[i];
-            if (SWIGLU) dump[(p.tt + c + i) * MX_ROWS + row] = u[i];
+        for (int i = 0; i < B; ++i) {
+          if (c + 8 * i < p.tt) {
+            tmem_ld8(t0 + c + 8 * i, v[i]);
+            if (SWIGLU) tmem_ld8(t0 + p.nb + c + 8 * i, u[i]);
           }
-        } else if (n < p.N) {
+        }
+        tmem_ld_wait();
+        for (int t = 1; t < p.n_terms; ++t) {
+          float w[B][8], x[B][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (c + i < mt) mx_store<EPI>(p, m0 + c + i, n, v[i], SWIGLU ? u[i] : 0.f);
+          for (int i = 0; i < B; ++i) {
+            if (c + 8 * i < p.tt) {
+              tmem_ld8(t0 + t * p.tt + c + 8 * i, w[i]);
+              if (SWIGLU) tmem_ld8(t0 + p.nb + t * p.tt + c + 8 * i, x[i]);
+            }
+          }
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[i][j] += w[i][j];
+              if (SWIGLU) u[i][j] += x[i][j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          if (c + 8 * i < p.tt) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int m = c + 8 * i + j;
+              if (SWIGLU && p.ksplit == 1) {
+                sums[m * MX_ROWS + row] = swiglu(v[i][j], u[i][j]);
+              } else {
+                sums[m * MX_ROWS + row] = v[i][j];
+                if (SWIGLU) sums[(p.tt + m) * MX_ROWS + row] = u[i][j];
+              }
+            }
+          }
         }
       }
     }
   }
-  if (p.ksplit > 1) {
-    __syncthreads();
-    cluster_barrier();
-    if (warp >= 2 && acc_ok && n < p.N) {
-      const uint32_t at = smem_u32(dump) + 4u * row;
-      for (int c = rank; c < mt; c += p.ksplit) {
-        float v[8], u[8];
+  __syncthreads();
+  if (p.ksplit > 1) cluster_barrier();
+  // every warp finishes tokens, a lane four columns: 512 bytes of a row at a time
+  if (!abort_word) {
+    const int n = tile * MX_ROWS + 4 * lane;
+    if (n < p.N) {
+      if (p.ksplit == 1) {
+        for (int m = warp; m < mt; m += MX_THREADS / 32) mx_store<EPI>(p, m0 + m, n, *reinterpret_cast<const float4*>(sums + m * MX_ROWS + 4 * lane));
+      } else {
+        const uint32_t at = smem_u32(sums) + 16u * lane;
+        for (int m = rank + p.ksplit * warp; m < mt; m += p.ksplit * (MX_THREADS / 32)) {
+          float4 v[8], u[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          v[r] = r < p.ksplit ? ld_cluster_f32(at + 4u * (c * MX_ROWS), r) : 0.f;
-          u[r] = SWIGLU && r < p.ksplit ? ld_cluster_f32(at + 4u * ((p.tt + c) * MX_ROWS), r) : 0.f;
-        }
-        float a = v[0], b = u[0];
-#pragma unroll
-        for (int r = 1; r < 8; ++r) {
-          if (r < p.ksplit) {
-            a += v[r];
-            b += u[r];
+          for (int r = 0; r < 8; ++r) {
+            v[r] = u[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < p.ksplit) {
+              v[r] = ld_cluster_v4(at + 512u * m, r);
+              if (SWIGLU) u[r] = ld_cluster_v4(at + 512u * (p.tt + m), r);
+            }
           }
+          float4 y = v[0], z = u[0];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) {
+            if (r < p.ksplit) {
+              y.x += v[r].x; y.y += v[r].y; y.z += v[r].z; y.w += v[r].w;
+              z.x += u[r].x; z.y += u[r].y; z.z += u[r].z; z.w += u[r].w;
+            }
+          }
+          if (SWIGLU) y = make_float4(swiglu(y.x, z.x), swiglu(y.y, z.y), swiglu(y.z, z.z), swiglu(y.w, z.w));
+          mx_store<EPI>(p, m0 + m, n, y);
         }
-        mx_store<EPI>(p, m0 + c, n, a, b);
       }
     }
   }
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && abort_word)  // given up: let the copies in flight land
-    for (int i = max(issued - S, 0); i < issued; ++i) mbar_wait(full_bar(i % S), (uint32_t)(i / S) & 1u, nullptr);
+    for (int s = 0; s < S; ++s) mbar_wait(full_bar(s), 0, nullptr, 50000000), mbar_wait(full_bar(s), 1, nullptr, 50000000);
   if (p.ksplit > 1) cluster_barrier();  // nobody leaves while a peer may still read its sums
   if (warp == 1) {
     tc_fence_after();
@@ -348,27 +452,27 @@ int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   constexpr int MAX_DYN = 216 * 1024;
   const int rc = allow_smem<gemm_mx4_kernel<EPI>>(MAX_DYN);
   if (rc) return rc;
-  // K shares: about 1.5 CTAs per SM in all, at least four k-blocks each
-  const int sms = sm_count();
-  const long long units = (long long)p.tiles * p.token_tiles;
-  long long ks = (3ll * sms / 2 + units / 2) / units;
-  if (ks > p.KB / 4) ks = p.KB / 4;
-  if (ks > 8) ks = 8;
-  if (ks < 1) ks = 1;
-  p.ksplit = (int)ks;
-  if (units * ks > 0x7fffffffll) return HYP_ECAPACITY;
   int cols = 32;
   while (cols < A_TILES * (p.nb + 4) + 8) cols <<= 1;
   p.tmem_cols = cols;
-  p.stage_bytes = A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (int)p.block_bytes;
-  p.stage_bytes = (p.stage_bytes + 1023) / 1024 * 1024;
-  const int dump_bytes = ks > 1 ? A_TILES * p.tt * MX_ROWS * 4 : 0;
-  // two CTAs to an SM where there are that many and tensor memory has room for both
+  p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (int)p.block_bytes + 1023) / 1024 * 1024;
+  const int sms = sm_count();
+  const long long units = (long long)p.tiles * p.token_tiles;
+  // K shares: one CTA to an SM as far as the tiles can be divided that way, at least four k-blocks each; the shares' sums have to fit
+  long long ks = sms / units;
+  if (ks > p.KB / 4) ks = p.KB / 4;
+  if (ks > 8) ks = 8;
+  while (ks > 1 && A_TILES * p.tt * MX_ROWS * 4 > MAX_DYN - 1024) --ks;
+  if (ks < 1) ks = 1;
+  p.ksplit = (int)ks;
+  if (units * ks > 0x7fffffffll) return HYP_ECAPACITY;
+  const int sum_bytes = (ks > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
+  // two CTAs to an SM where there are more than SMs and tensor memory has room for both
   const bool two = units * ks > sms && cols <= 256;
-  const int budget = two ? 110 * 1024 : MAX_DYN;
+  const int budget = two ? 112 * 1024 : MAX_DYN;
   int stages = (budget - 1024) / p.stage_bytes;
   if (stages > MX_MAX_STAGES) stages = MX_MAX_STAGES;
-  while (stages * p.stage_bytes < dump_bytes) ++stages;  // the sums reuse the ring
+  while (stages * p.stage_bytes < sum_bytes) ++stages;  // the sums reuse the ring
   if (stages < 2) stages = 2;
   if (stages > MX_MAX_STAGES || stages * p.stage_bytes + 1024 > MAX_DYN) return HYP_EINVAL;
   p.stages = stages;
@@ -426,11 +530,13 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(epi == EPI_SWIGLU_BF16 ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
+  const bool wide = epi == EPI_STORE_F32 || epi == EPI_RESID_F32;
+  p.vec = ldo % 4 == 0 && ((uintptr_t)out & (wide ? 15 : 7)) == 0;
   const int segments = (16 * p.KB + TERM_THREADS - 1) / TERM_THREADS;
   if (segments > 65535) return HYP_ECAPACITY;
   auto go = [&](auto kernel) {
-    return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, M, K / 8, p.KB, terms,
-                         t.tt, t.nb, t.block_bytes, scratch);
+    return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, K / 8, p.KB,
+                         terms, t.tt, t.nb, t.block_bytes, scratch);
   };
   HYP_CUDA_TRY(a_type == HYP_TYPE_F16 ? go(mx_terms_kernel<HYP_TYPE_F16>) : go(mx_terms_kernel<HYP_TYPE_BF16>));
   switch (epi) {

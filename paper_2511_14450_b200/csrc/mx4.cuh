@@ -93,6 +93,15 @@ __device__ __forceinline__ void load8(const void* p, float (&v)[8]) {
     }
   }
 }
+__device__ __forceinline__ void unpack8(uint4 r, bool f16, float (&v)[8]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = f16 ? half2_values(w[i]) : make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
 // Largest magnitude of eight values as its bits; infinities and NaN come out as 0x7f800000 or more.
 __device__ __forceinline__ uint32_t absmax_bits(const float (&v)[8]) {
   uint32_t m = 0;
