@@ -17,6 +17,7 @@
 //   warps 2-9  epilogue, lane = weight row.
 // Every mbarrier wait is bounded; the cluster barriers are reached by every thread of every CTA.
 #include <cuda.h>
+#include <math.h>
 
 #include "cache_ops.cuh"
 #include "gemm_tc.cuh"
@@ -29,24 +30,66 @@ namespace {
 
 constexpr int MX_EPI_WARPS = 8, MX_THREADS = 64 + 32 * MX_EPI_WARPS, MX_MAX_STAGES = 12, MX_A_BYTES = MX_ROWS * MX_BK;
 
-// How M tokens are cut: tiles of `tt` tokens, `nb` operand rows (terms x tokens, filled up to a multiple of 16).  `cap`: most rows.
-struct TokenTiles {
-  int tiles, tt, nb, sf_bytes;
+// How a product is cut.
+struct Plan {
+  int a_tiles;         // weight row tiles of a CTA (SwiGLU: gate and up)
+  int row_units;       // CTAs across the weight rows
+  int tiles, tt, nb;   // token tiles of tt tokens, nb operand rows each (terms x tokens, filled up to a multiple of 16)
+  int ksplit, sf_bytes;
   size_t block_bytes;  // terms of one (token tile, 128 k) with their scales
 };
-TokenTiles token_tiles(int M, int terms, int cap) {
-  TokenTiles t;
-  const int most = cap / terms / 8 * 8;
-  t.tiles = (M + most - 1) / most;
-  t.tt = ((M + t.tiles - 1) / t.tiles + 7) / 8 * 8;
-  t.tiles = (M + t.tt - 1) / t.tt;
-  t.nb = (t.tt * terms + 15) / 16 * 16;
-  t.sf_bytes = (t.nb + MX_ROWS - 1) / MX_ROWS * MX_SF_BYTES;
-  t.block_bytes = (size_t)t.nb * MX_BK + t.sf_bytes;
-  return t;
+constexpr int MX_MAX_DYN = 216 * 1024, MX_MORE_TILES = 3;
+// Tensor memory: one accumulator of 256 columns beside the scales, or two of 240.
+int row_cap(int a_tiles) { return a_tiles == 2 ? 240 : 256; }
+bool cut(Plan& p, int M, int N, int terms, int a_tiles, bool swiglu, int tiles) {
+  p.a_tiles = a_tiles;
+  p.row_units = (N + (swiglu ? 1 : a_tiles) * MX_ROWS - 1) / ((swiglu ? 1 : a_tiles) * MX_ROWS);
+  p.tt = ((M + tiles - 1) / tiles + 7) / 8 * 8;
+  p.tiles = (M + p.tt - 1) / p.tt;
+  p.nb = (p.tt * terms + 15) / 16 * 16;
+  p.sf_bytes = (p.nb + MX_ROWS - 1) / MX_ROWS * MX_SF_BYTES;
+  p.block_bytes = (size_t)p.nb * MX_BK + p.sf_bytes;
+  return p.nb <= row_cap(a_tiles);
 }
-// SwiGLU keeps two accumulators beside the scales in 512 columns of tensor memory.
-int row_cap(int epi) { return epi == EPI_SWIGLU_BF16 ? 240 : 256; }
+// The fewest tokens tiles that M can be cut into.
+int least_tiles(int M, int terms, int cap) {
+  const int most = cap / terms / 8 * 8;
+  return (M + most - 1) / most;
+}
+Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
+  const int sms = sm_count();
+  Plan best{}, p{};
+  if (M * (long long)terms <= 128) {
+    // Few tokens, bound by the weights' way from HBM: one CTA to an SM as far as the tiles can be divided that way (8 x 7680 x 5120 in two
+    // shares of K on 120 SMs 10.2 us, in four on all with two CTAs each 10.3; 32 x 17920 x 5120 with gate and up in one share 23.5, in two 39.6).
+    cut(best, M, N, terms, swiglu ? 2 : 1, swiglu, 1);
+    long long ks = sms / best.row_units;
+    if (ks > KB / 4) ks = KB / 4;
+    best.ksplit = ks > 8 ? 8 : ks < 1 ? 1 : (int)ks;
+    return best;
+  }
+  // Many tokens: the cheapest by a count of cycles.  A stage of 128 k takes 2 nb cycles of MMA for every row tile, or what its operands take
+  // from the L2 (about 40 bytes a cycle and SM); a CTA about 5000 to start and end, and its results.
+  double least = 0.0;
+  for (int a = swiglu ? 2 : 1; a <= 2; ++a) {
+    const int t0 = least_tiles(M, terms, row_cap(a));
+    for (int t = t0; t <= t0 + MX_MORE_TILES; ++t) {
+      if (!cut(p, M, N, terms, a, swiglu, t)) continue;
+      for (int ks = 1; ks <= 4; ++ks) {
+        if (ks > 1 && (ks > KB / 4 || a * p.tt * MX_ROWS * 4 > MX_MAX_DYN - 1024)) break;
+        const double stage = fmax(2.0 * a * p.nb, (a * MX_PACK_BYTES + (double)p.block_bytes) / 40.0);
+        const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * (ks > 1 ? 70.0 : 30.0);
+        const double waves = ceil((double)p.row_units * p.tiles * ks / sms);
+        if (least == 0.0 || waves * cta < least) {
+          least = waves * cta;
+          best = p;
+          best.ksplit = ks;
+        }
+      }
+    }
+  }
+  return best;
+}
 
 // ---------------------------------------------------------------------------------------------
 // activations to terms: four lanes take a block of 32 k of one token, eight values each
@@ -88,20 +131,31 @@ __device__ __forceinline__ uint32_t term_scale_at(int nb, int r, int c) {
 }
 
 constexpr int TERM_THREADS = 128;
-// grid (M, segments of 128 chunks of eight values)
-template <int TYPE>
+// grid (M, segments of 128 U chunks of eight values)
+template <int TYPE, int U>
 __global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int K8, int KB, int terms,
                                                                 int tt, int nb, size_t block_bytes, uint8_t* __restrict__ out) {
-  const int m = blockIdx.x, c = blockIdx.y * TERM_THREADS + threadIdx.x;
-  float v[1][8] = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+  const int m = blockIdx.x, c0 = blockIdx.y * (TERM_THREADS * U) + threadIdx.x;
+  float v[U][8];
   pdl_wait();
   pdl_trigger();
-  if (c < K8) load8<TYPE>(a + (m * stride + 8ll * c) * 2, v[0]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = c0 + u * TERM_THREADS;
+    if (c < K8) {
+      load8<TYPE>(a + (m * stride + 8ll * c) * 2, v[u]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+    }
+  }
   const int tile = m / tt, row = m - tile * tt;
-  uint8_t* blk = out + ((size_t)tile * KB + (c >> 4)) * block_bytes;
-  make_terms<1>(v, terms, [&](int, int t, uint2 codes, uint8_t scale) {
+  uint8_t* blk0 = out + (size_t)tile * KB * block_bytes;
+  make_terms<U>(v, terms, [&](int u, int t, uint2 codes, uint8_t scale) {
+    const int c = c0 + u * TERM_THREADS;
     if (c >= 16 * KB) return;
     const int r = t * tt + row;
+    uint8_t* blk = blk0 + (size_t)(c >> 4) * block_bytes;
     *reinterpret_cast<uint2*>(blk + term_at(r, c & 15)) = codes;
     if ((c & 3) == 0) blk[term_scale_at(nb, r, c & 15)] = scale;
   });
@@ -115,7 +169,7 @@ struct MxArgs {
   const uint8_t* terms;   // activations
   size_t block_bytes;
   int M, N, KB, ldo;
-  int tiles, token_tiles, tt, nb, n_terms, sf_bytes;
+  int tiles, row_units, token_tiles, tt, nb, n_terms;
   int stages, stage_bytes, ksplit, tmem_cols;
   uint32_t idesc;
   bool f16, vec;          // vec: four results at a time may be stored
@@ -196,11 +250,12 @@ __device__ __forceinline__ void mx_store(const MxArgs& p, int m, int n, float4 y
   }
 }
 
-template <int EPI>
-__global__ void __launch_bounds__(MX_THREADS)
+// A_TILES 2 without SwiGLU: two neighbouring row tiles, so that the terms' way from the L2 serves twice the products.
+template <int EPI, int A_TILES>
+__global__ void __launch_bounds__(MX_THREADS, 1)
 gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
-  constexpr bool SWIGLU = EPI == EPI_SWIGLU_BF16;
-  constexpr int A_TILES = SWIGLU ? 2 : 1;
+  constexpr bool SWIGLU = EPI == EPI_SWIGLU_BF16, DUAL = A_TILES == 2;
+  static_assert(!SWIGLU || DUAL, "gate and up");
   extern __shared__ uint8_t mx_smem[];
   __shared__ uint64_t bars[2 * MX_MAX_STAGES + 1];
   __shared__ uint32_t tmem_slot;
@@ -219,7 +274,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % (unsigned)p.ksplit);
   const int unit = (int)(blockIdx.x / (unsigned)p.ksplit);
-  const int tile = unit / p.token_tiles, tok = unit % p.token_tiles;  // the token tiles of a weight tile run side by side
+  const int tile = unit / p.token_tiles * (DUAL && !SWIGLU ? 2 : 1), tok = unit % p.token_tiles;  // the token tiles of a weight tile run side by side
   const int kb0 = (int)((long long)p.KB * rank / p.ksplit), kb1 = (int)((long long)p.KB * (rank + 1) / p.ksplit);
 
   if (threadIdx.x == 0) {
@@ -234,35 +289,38 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   const uint8_t* terms = p.terms + ((size_t)tok * p.KB + kb0) * p.block_bytes;
   // What a producing thread adds to the ring: `src` steps by `step` from k-block to k-block, `dst` and `bar` from stage to stage.
   const int n_kb = kb1 - kb0, n_first = min(S, n_kb);
-  const int line0 = (int)(((long long)tile * p.KB + kb0) * (MX_PACK_BYTES / 64)), up_lines = (int)((long long)p.tiles * p.KB * (MX_PACK_BYTES / 64));
+  const int line0 = (int)(((long long)tile * p.KB + kb0) * (MX_PACK_BYTES / 64)), up_lines = (SWIGLU ? p.tiles : tile + 1 < p.tiles ? 1 : 0) * p.KB * (MX_PACK_BYTES / 64);  // to the second row tile (behind the last: itself)
   auto load_w = [&](int line, uint32_t dst, uint32_t bar) {
     mbar_expect_tx(bar, A_TILES * MX_CODE_BYTES);  // a box counts by what it reads
     tma_load_2d(dst, &tm_w, 0, line, bar);
-    if (SWIGLU) tma_load_2d(dst + MX_A_BYTES, &tm_w, 0, line + up_lines, bar);
+    if (DUAL) tma_load_2d(dst + MX_A_BYTES, &tm_w, 0, line + up_lines, bar);
   };
   auto load_s = [&](const uint8_t* src, uint32_t dst, uint32_t bar) {
     mbar_expect_tx(bar, A_TILES * MX_SF_BYTES);
     bulk_load(dst + sfa_off, src, MX_SF_BYTES, bar);
-    if (SWIGLU) bulk_load(dst + sfa_off + MX_SF_BYTES, src + 64ll * up_lines, MX_SF_BYTES, bar);
+    if (DUAL) bulk_load(dst + sfa_off + MX_SF_BYTES, src + 64ll * up_lines, MX_SF_BYTES, bar);
   };
   const uint32_t term_bytes = (uint32_t)p.block_bytes;
   auto load_t = [&](const uint8_t* src, uint32_t dst, uint32_t bar) {
     mbar_expect_tx(bar, term_bytes);
     bulk_load(dst + b_off, src, term_bytes, bar);
   };
-  // One thread: all of the CTA's stages from `from` (at most S) on.
+  // A whole warp walks the CTA's stages from `from` (at most S) on, one lane issues.
   auto produce = [&](auto load, auto src, auto step, int from) {
     src += step * from;
     int stage = from == S ? 0 : from;
     uint32_t phase = from == S ? 0u : 1u;  // of the "empty" phase waited for; the first pass over the ring waits for nothing
     uint32_t dst = base + stage * p.stage_bytes;
     for (int i = from; i < n_kb; ++i) {
-      if (i >= S && !mbar_wait(empty_bar(stage), phase, abort_flag)) {
-        *abort_flag = 1;
-        atomicCAS(p.err, 0, 31);
+      if (i >= S && !__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase, abort_flag))) {
+        if (lane == 0) {
+          *abort_flag = 1;
+          atomicCAS(p.err, 0, 31);
+        }
         return false;
       }
-      load(src, dst, full_bar(stage));
+      if (elect_one()) load(src, dst, full_bar(stage));
+      __syncwarp();
       src += step;
       dst += p.stage_bytes;
       if (++stage == S) {
@@ -290,7 +348,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
 
   const int m0 = tok * p.tt, mt = min(p.tt, p.M - m0);
   if (warp == 0) {
-    if (lane == 0) produce(load_w, line0, MX_PACK_BYTES / 64, n_first);
+    produce(load_w, line0, MX_PACK_BYTES / 64, n_first);
   } else if (warp == 1) {
     // The whole warp walks the loop and one lane issues: so the operands stay in uniform registers (a lane on its own moves each of them there
     // for every instruction: 800 cycles a stage).
@@ -311,22 +369,22 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
       if (elect_one()) {
         // scales of this stage: in order behind the MMAs that still read the ones before
         mx_copy_scales(sfa, dsa0 + at);
-        if (SWIGLU) mx_copy_scales(sfa + 4, dsa0 + at + MX_SF_BYTES / 16);
+        if (DUAL) mx_copy_scales(sfa + 4, dsa0 + at + MX_SF_BYTES / 16);
         mx_copy_scales(sfb, dsb0 + at);
         if (two_sf) mx_copy_scales(sfb + 4, dsb0 + at + MX_SF_BYTES / 16);
         if (i == 0) {
           mx_mma<false>(tm, da, db, id0, sfa, sfb);
-          if (SWIGLU) mx_mma<false>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
+          if (DUAL) mx_mma<false>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
         } else {
           mx_mma<true>(tm, da, db, id0, sfa, sfb);
-          if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
+          if (DUAL) mx_mma<true>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
         }
         mx_mma<true>(tm, da + 2, db + 2, id1, sfa, sfb);
-        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 2, db + 2, id1, sfa + 4, sfb);
+        if (DUAL) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 2, db + 2, id1, sfa + 4, sfb);
         mx_mma<true>(tm, da + 4, db + 4, id2, sfa, sfb);
-        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 4, db + 4, id2, sfa + 4, sfb);
+        if (DUAL) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 4, db + 4, id2, sfa + 4, sfb);
         mx_mma<true>(tm, da + 6, db + 6, id3, sfa, sfb);
-        if (SWIGLU) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 6, db + 6, id3, sfa + 4, sfb);
+        if (DUAL) mx_mma<true>(acc2, da + MX_A_BYTES / 16 + 6, db + 6, id3, sfa + 4, sfb);
         tc_commit(empty_bar(stage));
         if (i == n_kb - 1) tc_commit(tfull_bar);
       }
@@ -340,98 +398,93 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
     }
   } else {
     bool ok = true;
-    // two of these warps issue copies first: a thread takes about 250 cycles for one, three to a stage would hold up the stream
-    if (warp == 2 && lane == 0) ok = produce(load_s, p.packed + 64ll * line0 + MX_CODE_BYTES, MX_PACK_BYTES, 0);
-    if (warp == 3 && lane == 0) ok = produce(load_t, terms, term_bytes, 0);
-    ok = __all_sync(0xffffffffu, ok);
-    // accumulators to shared memory, the terms added up (one CTA to a tile: SwiGLU applied); lane = weight row
-    const int row = 32 * (warp & 3) + lane;
-    const uint32_t t0 = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
+    // two of these warps issue copies first
+    if (warp == 2) ok = produce(load_s, p.packed + 64ll * line0 + MX_CODE_BYTES, MX_PACK_BYTES, 0);
+    if (warp == 3) ok = produce(load_t, terms, term_bytes, 0);
     ok = mbar_wait(tfull_bar, 0, abort_flag) && ok;
-    tc_fence_after();
     if (!ok && lane == 0) {
       *abort_flag = 1;
       atomicCAS(p.err, 0, 33);
     }
-    if (ok) {
-      constexpr int B = 2;  // groups of eight tokens in flight
-      for (int c = 8 * B * ((warp - 2) / 4); c < mt; c += 8 * B * (MX_EPI_WARPS / 4)) {  // two warps share a quarter of the lanes
-        float v[B][8], u[B][8];
+  }
+  // Results by way of shared memory: the accumulators with their terms added up (lane = weight row), then a warp to a token, four columns a
+  // lane, 512 bytes of a row at a time.  Shares of K leave all they have there and finish a part of the tokens each.
+  __syncthreads();
+  tc_fence_after();
+  auto leave = [&](int h, float* to, bool both) {  // accumulator h, or SwiGLU of both
+    const int row = 32 * (warp & 3) + lane;
+    const uint32_t t0 = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16) + h * p.nb;
+    constexpr int B = 2;  // groups of eight tokens in flight
+    for (int c = 8 * B * ((warp - 2) / 4); c < mt; c += 8 * B * (MX_EPI_WARPS / 4)) {  // two warps share a quarter of the lanes
+      float v[B][8], u[B][8];
+      for (int t = 0; t < p.n_terms; ++t) {
+        float w[B][8], x[B][8];
 #pragma unroll
         for (int i = 0; i < B; ++i) {
           if (c + 8 * i < p.tt) {
-            tmem_ld8(t0 + c + 8 * i, v[i]);
-            if (SWIGLU) tmem_ld8(t0 + p.nb + c + 8 * i, u[i]);
+            tmem_ld8(t0 + t * p.tt + c + 8 * i, w[i]);
+            if (SWIGLU && both) tmem_ld8(t0 + p.nb + t * p.tt + c + 8 * i, x[i]);
           }
         }
         tmem_ld_wait();
-        for (int t = 1; t < p.n_terms; ++t) {
-          float w[B][8], x[B][8];
 #pragma unroll
-          for (int i = 0; i < B; ++i) {
-            if (c + 8 * i < p.tt) {
-              tmem_ld8(t0 + t * p.tt + c + 8 * i, w[i]);
-              if (SWIGLU) tmem_ld8(t0 + p.nb + t * p.tt + c + 8 * i, x[i]);
-            }
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[i][j] = t == 0 ? w[i][j] : v[i][j] + w[i][j];
+            if (SWIGLU) u[i][j] = t == 0 ? x[i][j] : u[i][j] + x[i][j];
           }
-          tmem_ld_wait();
+      }
 #pragma unroll
-          for (int i = 0; i < B; ++i)
+      for (int i = 0; i < B; ++i) {
+        if (c + 8 * i < p.tt) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              v[i][j] += w[i][j];
-              if (SWIGLU) u[i][j] += x[i][j];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < B; ++i) {
-          if (c + 8 * i < p.tt) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int m = c + 8 * i + j;
-              if (SWIGLU && p.ksplit == 1) {
-                sums[m * MX_ROWS + row] = swiglu(v[i][j], u[i][j]);
-              } else {
-                sums[m * MX_ROWS + row] = v[i][j];
-                if (SWIGLU) sums[(p.tt + m) * MX_ROWS + row] = u[i][j];
-              }
-            }
-          }
+          for (int j = 0; j < 8; ++j) to[(c + 8 * i + j) * MX_ROWS + row] = SWIGLU && both ? swiglu(v[i][j], u[i][j]) : v[i][j];
         }
       }
     }
-  }
-  __syncthreads();
-  if (p.ksplit > 1) cluster_barrier();
-  // every warp finishes tokens, a lane four columns: 512 bytes of a row at a time
-  if (!abort_word) {
-    const int n = tile * MX_ROWS + 4 * lane;
-    if (n < p.N) {
-      if (p.ksplit == 1) {
+  };
+  if (p.ksplit == 1) {
+#pragma unroll
+    for (int h = 0; h < (SWIGLU ? 1 : A_TILES); ++h) {
+      if (warp >= 2 && !abort_word) leave(h, sums, true);
+      __syncthreads();
+      const int n = (tile + h) * MX_ROWS + 4 * lane;
+      if (n < p.N && !abort_word)
         for (int m = warp; m < mt; m += MX_THREADS / 32) mx_store<EPI>(p, m0 + m, n, *reinterpret_cast<const float4*>(sums + m * MX_ROWS + 4 * lane));
-      } else {
-        const uint32_t at = smem_u32(sums) + 16u * lane;
-        for (int m = rank + p.ksplit * warp; m < mt; m += p.ksplit * (MX_THREADS / 32)) {
-          float4 v[8], u[8];
+      if (h + 1 < A_TILES) __syncthreads();
+    }
+  } else {
+    if (warp >= 2 && !abort_word) {
+      leave(0, sums, false);
+      if (DUAL) leave(1, sums + p.tt * MX_ROWS, false);
+    }
+    __syncthreads();
+    cluster_barrier();
+    const int n = tile * MX_ROWS + 4 * lane;
+    if (n < p.N && !abort_word) {
+      const uint32_t at = smem_u32(sums) + 16u * lane;
+      for (int m = rank + p.ksplit * warp; m < mt; m += p.ksplit * (MX_THREADS / 32)) {
+        float4 v[8], u[8];
 #pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            v[r] = u[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < p.ksplit) {
-              v[r] = ld_cluster_v4(at + 512u * m, r);
-              if (SWIGLU) u[r] = ld_cluster_v4(at + 512u * (p.tt + m), r);
-            }
+        for (int r = 0; r < 8; ++r) {
+          v[r] = u[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r < p.ksplit) {
+            v[r] = ld_cluster_v4(at + 512u * m, r);
+            if (DUAL) u[r] = ld_cluster_v4(at + 512u * (p.tt + m), r);
           }
-          float4 y = v[0], z = u[0];
-#pragma unroll
-          for (int r = 1; r < 8; ++r) {
-            if (r < p.ksplit) {
-              y.x += v[r].x; y.y += v[r].y; y.z += v[r].z; y.w += v[r].w;
-              z.x += u[r].x; z.y += u[r].y; z.z += u[r].z; z.w += u[r].w;
-            }
-          }
-          if (SWIGLU) y = make_float4(swiglu(y.x, z.x), swiglu(y.y, z.y), swiglu(y.z, z.z), swiglu(y.w, z.w));
-          mx_store<EPI>(p, m0 + m, n, y);
         }
+        float4 y = v[0], z = u[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) {
+          if (r < p.ksplit) {
+            y.x += v[r].x; y.y += v[r].y; y.z += v[r].z; y.w += v[r].w;
+            z.x += u[r].x; z.y += u[r].y; z.z += u[r].z; z.w += u[r].w;
+          }
+        }
+        if (SWIGLU) y = make_float4(swiglu(y.x, z.x), swiglu(y.y, z.y), swiglu(y.z, z.z), swiglu(y.w, z.w));
+        mx_store<EPI>(p, m0 + m, n, y);
+        if (DUAL && !SWIGLU && n + MX_ROWS < p.N) mx_store<EPI>(p, m0 + m, n + MX_ROWS, z);
       }
     }
   }
@@ -446,42 +499,30 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   }
 }
 
-template <int EPI>
+template <int EPI, int A_TILES>
 int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
-  constexpr int A_TILES = EPI == EPI_SWIGLU_BF16 ? 2 : 1;
-  constexpr int MAX_DYN = 216 * 1024;
-  const int rc = allow_smem<gemm_mx4_kernel<EPI>>(MAX_DYN);
+  const int rc = allow_smem<gemm_mx4_kernel<EPI, A_TILES>>(MX_MAX_DYN);
   if (rc) return rc;
   int cols = 32;
   while (cols < A_TILES * (p.nb + 4) + 8) cols <<= 1;
   p.tmem_cols = cols;
   p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (int)p.block_bytes + 1023) / 1024 * 1024;
-  const int sms = sm_count();
-  const long long units = (long long)p.tiles * p.token_tiles;
-  // K shares: one CTA to an SM as far as the tiles can be divided that way, at least four k-blocks each; the shares' sums have to fit
-  long long ks = sms / units;
-  if (ks > p.KB / 4) ks = p.KB / 4;
-  if (ks > 8) ks = 8;
-  while (ks > 1 && A_TILES * p.tt * MX_ROWS * 4 > MAX_DYN - 1024) --ks;
-  if (ks < 1) ks = 1;
-  p.ksplit = (int)ks;
-  if (units * ks > 0x7fffffffll) return HYP_ECAPACITY;
-  const int sum_bytes = (ks > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
+  const long long ctas = (long long)p.row_units * p.token_tiles * p.ksplit;
+  if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
+  const int sum_bytes = (p.ksplit > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
   // two CTAs to an SM where there are more than SMs and tensor memory has room for both
-  const bool two = units * ks > sms && cols <= 256;
-  const int budget = two ? 112 * 1024 : MAX_DYN;
+  const int budget = ctas > sm_count() && cols <= 256 ? 112 * 1024 : MX_MAX_DYN;
   int stages = (budget - 1024) / p.stage_bytes;
   if (stages > MX_MAX_STAGES) stages = MX_MAX_STAGES;
-  while (stages * p.stage_bytes < sum_bytes) ++stages;  // the sums reuse the ring
   if (stages < 2) stages = 2;
-  if (stages > MX_MAX_STAGES || stages * p.stage_bytes + 1024 > MAX_DYN) return HYP_EINVAL;
   p.stages = stages;
+  int smem = (stages * p.stage_bytes > sum_bytes ? stages * p.stage_bytes : sum_bytes) + 1024;  // the sums reuse the ring
+  if (smem > MX_MAX_DYN) return HYP_EINVAL;
   // never more CTAs on an SM than tensor memory holds: one that waits for it would hold up its cluster
-  int smem = stages * p.stage_bytes + 1024;
   const int least = 228 * 1024 / (512 / cols + 1);
   if (smem < least) smem = least;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * ks));
+  cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(MX_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -492,58 +533,60 @@ int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
     attr[na].val.programmaticStreamSerializationAllowed = 1;
     ++na;
   }
-  if (ks > 1) {
+  if (p.ksplit > 1) {
     attr[na].id = cudaLaunchAttributeClusterDimension;
-    attr[na].val.clusterDim.x = (unsigned)ks;
+    attr[na].val.clusterDim.x = (unsigned)p.ksplit;
     attr[na].val.clusterDim.y = 1;
     attr[na].val.clusterDim.z = 1;
     ++na;
   }
   cfg.attrs = attr;
   cfg.numAttrs = na;
-  HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_mx4_kernel<EPI>, map, p));
+  HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_mx4_kernel<EPI, A_TILES>, map, p));
   return 1;
 }
 
 }  // namespace
 
 size_t mx4_scratch_bytes(int M, int K, int terms) {
-  // the two row caps cut the tokens differently: the larger of both
-  size_t most = 0;
-  for (int cap : {240, 256}) {
-    const TokenTiles t = token_tiles(M, terms, cap);
-    const size_t n = (size_t)t.tiles * mx_kb(K) * t.block_bytes;
-    if (n > most) most = n;
-  }
-  return most;
+  // whatever the plan: t tiles of at most M / t + 8 tokens, their operand rows filled up by 15 at most
+  const long long t = least_tiles(M, terms, 240) + MX_MORE_TILES, rows = (long long)M * terms + t * (8 * terms + 15);
+  return (size_t)mx_kb(K) * (rows * MX_BK + (rows / MX_ROWS + t) * MX_SF_BYTES);
 }
 
 int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t* packed, int M, int N, int K, int terms, int epi,
                     void* out, int ldo, uint8_t* scratch, cudaStream_t st) {
-  const TokenTiles t = token_tiles(M, terms, row_cap(epi));
+  const bool swiglu = epi == EPI_SWIGLU_BF16, wide = epi == EPI_STORE_F32 || epi == EPI_RESID_F32;
+  const Plan t = plan_for(M, N, mx_kb(K), terms, swiglu);
   MxArgs p{};
   p.packed = packed; p.terms = scratch; p.block_bytes = t.block_bytes;
   p.M = M; p.N = N; p.KB = mx_kb(K); p.ldo = ldo;
-  p.tiles = mx_row_tiles(N); p.token_tiles = t.tiles; p.tt = t.tt; p.nb = t.nb; p.n_terms = terms; p.sf_bytes = t.sf_bytes;
+  p.tiles = mx_row_tiles(N); p.row_units = t.row_units; p.token_tiles = t.tiles; p.tt = t.tt; p.nb = t.nb; p.n_terms = terms;
+  p.ksplit = t.ksplit;
   p.f16 = a_type == HYP_TYPE_F16; p.out = out; p.err = tc_err_flag_ptr();
+  p.vec = ldo % 4 == 0 && ((uintptr_t)out & (wide ? 15 : 7)) == 0;
   p.idesc = (5u << 7) | (0u << 10) | ((uint32_t)(t.nb >> 3) << 17) | (1u << 23) | ((uint32_t)(MX_ROWS >> 4) << 24);  // E2M1 x E4M3, power-of-two scales
   CUtensorMap map;
-  int rc = tc_make_mx4_map(&map, packed, (long long)(epi == EPI_SWIGLU_BF16 ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
+  int rc = tc_make_mx4_map(&map, packed, (long long)(swiglu ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
-  const bool wide = epi == EPI_STORE_F32 || epi == EPI_RESID_F32;
-  p.vec = ldo % 4 == 0 && ((uintptr_t)out & (wide ? 15 : 7)) == 0;
-  const int segments = (16 * p.KB + TERM_THREADS - 1) / TERM_THREADS;
+  const long long chunks = 16ll * p.KB;
+  const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs
+  const long long segments = (chunks + TERM_THREADS * (many ? 2 : 1) - 1) / (TERM_THREADS * (many ? 2 : 1));
   if (segments > 65535) return HYP_ECAPACITY;
   auto go = [&](auto kernel) {
     return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, K / 8, p.KB,
                          terms, t.tt, t.nb, t.block_bytes, scratch);
   };
-  HYP_CUDA_TRY(a_type == HYP_TYPE_F16 ? go(mx_terms_kernel<HYP_TYPE_F16>) : go(mx_terms_kernel<HYP_TYPE_BF16>));
+  if (a_type == HYP_TYPE_F16)
+    HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_F16, 2>) : go(mx_terms_kernel<HYP_TYPE_F16, 1>)));
+  else
+    HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_BF16, 2>) : go(mx_terms_kernel<HYP_TYPE_BF16, 1>)));
+  const bool dual = t.a_tiles == 2;
   switch (epi) {
-    case EPI_STORE_BF16: rc = launch_epi<EPI_STORE_BF16>(map, p, st); break;
-    case EPI_RESID_F32: rc = launch_epi<EPI_RESID_F32>(map, p, st); break;
-    case EPI_SWIGLU_BF16: rc = launch_epi<EPI_SWIGLU_BF16>(map, p, st); break;
-    case EPI_STORE_F32: rc = launch_epi<EPI_STORE_F32>(map, p, st); break;
+    case EPI_STORE_BF16: rc = dual ? launch_epi<EPI_STORE_BF16, 2>(map, p, st) : launch_epi<EPI_STORE_BF16, 1>(map, p, st); break;
+    case EPI_RESID_F32: rc = dual ? launch_epi<EPI_RESID_F32, 2>(map, p, st) : launch_epi<EPI_RESID_F32, 1>(map, p, st); break;
+    case EPI_SWIGLU_BF16: rc = launch_epi<EPI_SWIGLU_BF16, 2>(map, p, st); break;
+    case EPI_STORE_F32: rc = dual ? launch_epi<EPI_STORE_F32, 2>(map, p, st) : launch_epi<EPI_STORE_F32, 1>(map, p, st); break;
     default: return HYP_EINVAL;
   }
   return rc < 0 ? rc : rc + 1;
