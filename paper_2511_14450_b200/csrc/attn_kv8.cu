@@ -20,8 +20,9 @@ namespace hyp {
 
 namespace {
 
-constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32, K8_SLOTS = 2;
-constexpr int K8_PER_SM = 5, K8_WAVES = 4;  // resident CTAs; waves that a long context is cut for
+constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32;
+constexpr int K8_STEP = 2, K8_SLOTS = 2;    // pages that a warp takes at a time; ring slots of that many
+constexpr int K8_PER_SM = 3, K8_WAVES = 4;  // resident CTAs; waves that a long context is cut for
 constexpr float K8_GROWN = 256.f;
 
 struct Kv8Args {
@@ -40,7 +41,7 @@ struct Kv8Args {
 };
 
 template <int D>
-constexpr int kv8_smem() { return K8_WARPS * K8_SLOTS * 2 * kv8_half_page(D); }
+constexpr int kv8_smem() { return K8_WARPS * K8_SLOTS * K8_STEP * 2 * kv8_half_page(D); }
 
 // Four codes of one row to two operand registers: (0, 1) and (2, 3).
 template <int FMT>
@@ -99,7 +100,8 @@ __device__ __forceinline__ float lds32(uint32_t addr) {
 
 template <int D, int G, int FMT, bool CLUSTER>
 __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const Kv8Args a) {
-  constexpr int KS = D / 16, HALF = kv8_half_page(D), SLOT = 2 * HALF;
+  constexpr int KS = D / 16, HALF = kv8_half_page(D), PAGE = 2 * HALF, SLOT = K8_STEP * PAGE, T = K8_STEP;
+  static_assert(T == 2, "page ids come in pairs");
   extern __shared__ __align__(128) uint8_t k8_smem[];
   __shared__ uint64_t bars[K8_WARPS * K8_SLOTS];
   static_assert(kv8_smem<D>() >= (2 * K8_WARPS * 8 + K8_WARPS * G * D + 16 + G * D + 128) * 4, "the combine buffers reuse the ring");
@@ -109,24 +111,25 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   pdl_trigger();
 
   const int32_t* bt = a.table + (long long)b * a.table_stride;
-  int32_t ids_cur = 0;  // page ids of this warp's next 32 pages, one a lane; the first ones do not wait for the length
-  {
-    const int v = split + n_splits * (warp + K8_WARPS * lane);
-    if (v < a.table_stride) ids_cur = bt[v];
-  }
-  const int total = paged_total(a.ctx[b], a.table_stride), n_pages = (total + PG_PT - 1) / PG_PT;
+  // Ids of this warp's next 32 steps of two pages, one step a lane; the first ones do not wait for the length.
+  int2 ids_cur = make_int2(0, 0);
+  auto two_ids = [&](int step, int limit) {
+    return make_int2(T * step < limit ? bt[T * step] : 0, T * step + 1 < limit ? bt[T * step + 1] : 0);
+  };
+  ids_cur = two_ids(split + n_splits * (warp + K8_WARPS * lane), a.table_stride);
+  const int total = paged_total(a.ctx[b], a.table_stride), n_pages = (total + PG_PT - 1) / PG_PT, n_steps = (n_pages + T - 1) / T;
   // a shorter sequence uses no more splits than the plan's rule gives for its own length
   const int fair = max(a.wave_splits, (n_pages + 15) / 16);
-  const int used = n_pages > 64 * a.wave_splits ? n_splits : max(min(min(n_splits, fair), (n_pages + K8_WARPS - 1) / K8_WARPS), 1);
+  const int used = n_pages > 64 * a.wave_splits ? n_splits : max(min(min(n_splits, fair), (n_steps + K8_WARPS - 1) / K8_WARPS), 1);
   if (!CLUSTER && split >= used) {
     if (tid < G) *reinterpret_cast<float2*>(a.ml + (((size_t)b * a.Hq + kvh * G + tid) * a.n_slots + split) * 2) = make_float2(PG_NEG, 0.f);
     return;
   }
-  const int first = split + used * warp, stride_p = used * K8_WARPS;
-  const int my_n = split < used && first < n_pages ? (n_pages - first + stride_p - 1) / stride_p : 0;
-  auto load_ids = [&](int base) { return base + lane < my_n ? bt[first + stride_p * (base + lane)] : 0; };
+  const int first = split + used * warp, stride_s = used * K8_WARPS;
+  const int my_n = split < used && first < n_steps ? (n_steps - first + stride_s - 1) / stride_s : 0;
+  auto load_ids = [&](int base) { return base + lane < my_n ? two_ids(first + stride_s * (base + lane), n_pages) : make_int2(0, 0); };
   if (used != n_splits) ids_cur = load_ids(0);
-  int32_t ids_next = load_ids(32);
+  int2 ids_next = load_ids(32);
   const uint32_t my_bars = smem_u32(bars) + 8u * (warp * K8_SLOTS), my_ring = smem_u32(k8_smem) + (uint32_t)(warp * K8_SLOTS) * SLOT;
   const uint32_t page_bytes = 2u * a.Hkv * HALF, v_off = (uint32_t)a.Hkv * HALF;
   const uint8_t* head_base = a.pool + (size_t)kvh * HALF;
@@ -135,13 +138,19 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
       ids_cur = ids_next;
       ids_next = load_ids(i + 32);
     }
-    const int page = __shfl_sync(0xffffffffu, ids_cur, i & 31);
+    const int page0 = __shfl_sync(0xffffffffu, ids_cur.x, i & 31), page1 = __shfl_sync(0xffffffffu, ids_cur.y, i & 31);
     if (lane == 0) {
       const uint32_t dst = my_ring + slot * SLOT, bar = my_bars + 8u * slot;
-      mbar_expect_tx(bar, SLOT);
-      const uint8_t* src = head_base + (uint64_t)(uint32_t)page * page_bytes;
+      const bool both = T * (first + stride_s * i) + 1 < n_pages;  // the last step may hold one page
+      mbar_expect_tx(bar, both ? SLOT : PAGE);
+      const uint8_t* src = head_base + (uint64_t)(uint32_t)page0 * page_bytes;
       bulk_load(dst, src, HALF, bar);
       bulk_load(dst + HALF, src + v_off, HALF, bar);
+      if (both) {
+        src = head_base + (uint64_t)(uint32_t)page1 * page_bytes;
+        bulk_load(dst + PAGE, src, HALF, bar);
+        bulk_load(dst + PAGE + HALF, src + v_off, HALF, bar);
+      }
     }
   };
   if (lane == 0) {
@@ -173,62 +182,82 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   uint32_t phase = 0;
   for (int i = 0; i < my_n; ++i) {
     if (!mbar_wait(my_bars + 8u * slot, phase, nullptr)) { ok = false; break; }
-    const uint32_t kt = my_ring + slot * SLOT, vt = kt + HALF;
-    const int k0 = (first + stride_p * i) * PG_PT;
-    const bool partial = k0 + PG_PT > total;
+    const uint32_t at0 = my_ring + slot * SLOT;
+    const int k0 = T * (first + stride_s * i) * PG_PT;
+    const bool partial = k0 + T * PG_PT > total;
     if (FMT == HYP_KV8_E4M3 && partial) {  // a code behind the end may be a NaN, and a weight of 0 times NaN is not 0
-      for (int e = lane; e < D; e += 32)
-        if (k0 + e / (D / 16) >= total) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vt + (uint32_t)e * 16u), "r"(0u) : "memory");
+      for (int e = lane; e < T * D; e += 32)
+        if (k0 + e / (D / 16) >= total)
+          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at0 + HALF + (uint32_t)(e / D * PAGE + e % D * 16)), "r"(0u) : "memory");
       __syncwarp();
     }
-    // scores of keys g and g + 8 for heads 2tq, 2tq + 1
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    // scores of keys g and g + 8 of every page for heads 2tq, 2tq + 1
+    float s[T][4];
+#pragma unroll
+    for (int t = 0; t < T; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) {
-      const uint32_t at = kt + g * D + kv8_chunk<D>(tq + 4 * h, g);  // slots g and g + 8 have the same parity
-      const uint4 x = lds128(at), y = lds128(at + 8 * D);
-      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t a0, a1, a2, a3;
-        key_pair<FMT>(xw[j], a0, a2);
-        key_pair<FMT>(yw[j], a1, a3);
-        mma_f16_16816(s, a0, a1, a2, a3, qf[4 * h + j][0], qf[4 * h + j][1]);
+      for (int t = 0; t < T; ++t) {
+        const uint32_t at = at0 + t * PAGE + g * D + kv8_chunk<D>(tq + 4 * h, g);  // slots g and g + 8 have the same parity
+        const uint4 x = lds128(at), y = lds128(at + 8 * D);
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t a0, a1, a2, a3;
+          key_pair<FMT>(xw[j], a0, a2);
+          key_pair<FMT>(yw[j], a1, a3);
+          mma_f16_16816(s[t], a0, a1, a2, a3, qf[4 * h + j][0], qf[4 * h + j][1]);
+        }
       }
     }
-    const uint32_t sc = kt + 16 * D + 4 * g;
-    const float ks0 = lds32(sc) * sl2, ks1 = lds32(sc + 32) * sl2;
-    float vs0 = lds32(sc + HALF), vs1 = lds32(sc + HALF + 32);
-    float v[4], p[4], w[4];  // (key g, head 2tq), (g, 2tq + 1), (g + 8, 2tq), (g + 8, 2tq + 1)
+    // [page][(key g, head 2tq), (g, 2tq + 1), (g + 8, 2tq), (g + 8, 2tq + 1)]
+    float v[T][4], p[T][4], w[T][4], vs[T][2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = s[e] * (e < 2 ? ks0 : ks1);
-    if (partial) {  // keys behind the end: no weight, whatever their slots hold
-      if (k0 + g >= total) v[0] = v[1] = -INFINITY, vs0 = 0.f;
-      if (k0 + g + 8 >= total) v[2] = v[3] = -INFINITY, vs1 = 0.f;
+    for (int t = 0; t < T; ++t) {
+      const uint32_t sc = at0 + t * PAGE + 16 * D + 4 * g;
+      const float ks0 = lds32(sc) * sl2, ks1 = lds32(sc + 32) * sl2;
+      vs[t][0] = lds32(sc + HALF);
+      vs[t][1] = lds32(sc + HALF + 32);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[t][e] = s[t][e] * (e < 2 ? ks0 : ks1);
     }
+    if (partial) {  // keys behind the end: no weight, whatever their slots hold
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        if (k0 + t * PG_PT + g >= total) v[t][0] = v[t][1] = -INFINITY, vs[t][0] = 0.f;
+        if (k0 + t * PG_PT + g + 8 >= total) v[t][2] = v[t][3] = -INFINITY, vs[t][1] = 0.f;
+      }
+    }
+    float most = 0.f;
     auto weigh = [&] {  // (a scale times a reference may leave fp32: 0 times infinity would be NaN)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = ex2_approx(v[e] - m[e & 1]);
-        w[e] = p[e] * min_nan((e < 2 ? vs0 : vs1) * f[e & 1], 3e38f);
-      }
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[t][e] = ex2_approx(v[t][e] - m[e & 1]);
+          w[t][e] = p[t][e] * min_nan(vs[t][e >> 1] * f[e & 1], 3e38f);
+          most = fmaxf(most, fmaxf(p[t][e], w[t][e]));
+        }
     };
     weigh();
-    const float most = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
     if (__any_sync(0xffffffffu, most > K8_GROWN)) {  // new references: the largest score, the largest score + log2(scale)
-      // (values whose scale is below 2^-64 are zeros in fp16)
-      const float lv0 = fmaxf(lg2_approx(vs0), -64.f), lv1 = fmaxf(lg2_approx(vs1), -64.f);
       float corr2[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = fmaxf(v[h], v[2 + h]), top2 = fmaxf(v[h] + lv0, v[2 + h] + lv1);
+        float top = m[h], top2 = m2[h];
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {  // (values whose scale is below 2^-64 are zeros in fp16)
+            top = fmaxf(top, v[t][2 * k + h]);
+            top2 = fmaxf(top2, v[t][2 * k + h] + fmaxf(lg2_approx(vs[t][k]), -64.f));
+          }
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) {
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
           top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
         }
-        top = fmaxf(top, m[h]);
-        top2 = fmaxf(top2, m2[h]);
         l[h] *= ex2_approx(m[h] - top);
         corr2[h] = ex2_approx(m2[h] - top2);
         m[h] = top;
@@ -242,20 +271,24 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
       }
       weigh();
     }
-    l[0] += p[0] + p[2];
-    l[1] += p[1] + p[3];
-    const uint32_t b0 = transpose_8x8(pack_f16(w[0], w[1])), b1 = transpose_8x8(pack_f16(w[2], w[3]));
 #pragma unroll
-    for (int c2 = 0; c2 < KS / 2; ++c2) {
-      const int t = lane & 15;  // slots 0-7 and 8-15 of chunk 2 c2, then of the next one
-      uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
-      ldsm_x4_t(vt + t * D + kv8_chunk<D>(2 * c2 + (lane >> 4), t), r0, r1, r2, r3);
-      value_pair<FMT>(r0, a0, a1);
-      value_pair<FMT>(r1, a2, a3);
-      mma_f16_16816(o[2 * c2], a0, a1, a2, a3, b0, b1);
-      value_pair<FMT>(r2, a0, a1);
-      value_pair<FMT>(r3, a2, a3);
-      mma_f16_16816(o[2 * c2 + 1], a0, a1, a2, a3, b0, b1);
+    for (int t = 0; t < T; ++t) {
+      l[0] += p[t][0] + p[t][2];
+      l[1] += p[t][1] + p[t][3];
+      const uint32_t b0 = transpose_8x8(pack_f16(w[t][0], w[t][1])), b1 = transpose_8x8(pack_f16(w[t][2], w[t][3]));
+      const uint32_t vt = at0 + t * PAGE + HALF;
+#pragma unroll
+      for (int c2 = 0; c2 < KS / 2; ++c2) {
+        const int row = lane & 15;  // slots 0-7 and 8-15 of chunk 2 c2, then of the next one
+        uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+        ldsm_x4_t(vt + row * D + kv8_chunk<D>(2 * c2 + (lane >> 4), row), r0, r1, r2, r3);
+        value_pair<FMT>(r0, a0, a1);
+        value_pair<FMT>(r1, a2, a3);
+        mma_f16_16816(o[2 * c2], a0, a1, a2, a3, b0, b1);
+        value_pair<FMT>(r2, a0, a1);
+        value_pair<FMT>(r3, a2, a3);
+        mma_f16_16816(o[2 * c2 + 1], a0, a1, a2, a3, b0, b1);
+      }
     }
     __syncwarp();  // every lane's reads of the slot are done; hand it back to the copy engine
     if (i + K8_SLOTS < my_n) issue(i + K8_SLOTS, slot);
@@ -466,7 +499,7 @@ int kv8_splits(int n_seqs, int Hkv, int max_pages) {
   if (max_pages <= 4 * K8_WARPS) return 1;
   int want = wave_splits(n_seqs, Hkv);
   if (max_pages > 64 * want) want = (int)((K8_WAVES * K8_PER_SM * sm_count() + groups - 1) / groups);
-  const int cap = (max_pages + K8_WARPS - 1) / K8_WARPS;
+  const int cap = (max_pages + K8_STEP * K8_WARPS - 1) / (K8_STEP * K8_WARPS);
   if (want > cap) want = cap;
   return want > 64 ? 64 : want;
 }
