@@ -22,7 +22,7 @@ namespace {
 
 constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32;
 constexpr int K8_STEP = 2, K8_SLOTS = 2;    // pages that a warp takes at a time; ring slots of that many
-constexpr int K8_PER_SM = 3, K8_WAVES = 4;  // resident CTAs; waves that a long context is cut for
+constexpr int K8_PER_SM = 3, K8_WAVES = 5;  // resident CTAs; waves that a long context is cut for
 constexpr float K8_GROWN = 256.f;
 
 struct Kv8Args {
@@ -492,13 +492,15 @@ int wave_splits(int n_seqs, int Hkv) {
 }  // namespace
 
 int kv8_splits(int n_seqs, int Hkv, int max_pages) {
-  // Up to 16 pages: one CTA per sequence and KV head, which writes the result itself (the join is a launch of its own).  Short contexts:
-  // one wave.  Longer ones (more than 64 pages a CTA that way): about four waves, so that ragged batches even out.  At least one
-  // page per warp.
+  // Up to 16 pages: one CTA per sequence and KV head, which writes the result itself (the join is a launch of its own).  Short contexts, and
+  // long ones of few heads: one wave of CTAs, or just below (4 x 32768 tokens, 10 KV heads: 60.5 us in one wave, 62.7 / 65 / 67.3 in two to
+  // four).  Long contexts of more heads than a fourth of a wave: about five waves, so that ragged batches even out (64 ragged sequences of up to
+  // 8192, 8 heads: 111 us in one wave, 107.7 in three, 103 in five).  At least one step of two pages per warp.
   const long long groups = (long long)n_seqs * Hkv;
   if (max_pages <= 4 * K8_WARPS) return 1;
   int want = wave_splits(n_seqs, Hkv);
-  if (max_pages > 64 * want) want = (int)((K8_WAVES * K8_PER_SM * sm_count() + groups - 1) / groups);
+  if (want < 4 && max_pages > 64 * want) want = (int)(K8_WAVES * K8_PER_SM * sm_count() / groups);
+  if (want < 1) want = 1;
   const int cap = (max_pages + K8_STEP * K8_WARPS - 1) / (K8_STEP * K8_WARPS);
   if (want > cap) want = cap;
   return want > 64 ? 64 : want;

@@ -681,3 +681,27 @@ def test_prompt_through_the_8_bit_cache():
         # read back once more rounded: e4m3 values under a power of two are exact in fp16 unless subnormal
         assert ((out[r].double().view(hq, d) - want).abs() <= bound + 2.0 ** -9).all()
     assert ((last[0].double().view(hq, d) - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("heads,lens,extra", [((8, 2, 128), [3000, 0, 0, 1, 2999, 33, 32, 31, 0], 1200), ((2, 1, 64), [9001], 4000),
+                                              ((8, 1, 64), [5] * 60 + [6000] + [0] * 3, 2000), ((40, 10, 128), [4100, 17, 2050, 4096], 900),
+                                              ((3, 3, 64), [1, 1, 1], 6000), ((8, 8, 128), [16, 48, 47, 700], 3000)])
+def test_attention_even_runs(heads, fmt, lens, extra):
+    """Tables wide enough for runs across sequences: empty ones, one that holds everything, runs that end inside pages' pairs."""
+    check_attention(heads, fmt, lens, 51, extra)
+
+
+def test_attention_many_sequences():
+    """More sequences than share one list of runs."""
+    heads, fmt, n = (2, 1, 64), hyp.HYP_KV8_INT8, 600
+    c = Cache8([5, 70, 1000], 1, 64, fmt, 61, 0)
+    table = c.table.repeat(n // 3, 1)
+    q = normal(n, 128, seed=62).half()
+    out = attend(heads, fmt, q, c.pool, table, i32([4, 69, 999] * (n // 3)))
+    wide = torch.cat([table, table.new_zeros(n, 9000)], 1)                    # the same lengths in a table that is planned for more
+    again = attend(heads, fmt, q, c.pool, wide, i32([4, 69, 999] * (n // 3)))
+    for r in (out, again):
+        for i in list(range(0, 9)) + [n - 1, n - 2, n - 3, 300, 301, 302]:
+            want, bound = attention(q[i].double().view(2, 64), c.k[i % 3], c.v[i % 3])
+            assert ((r[i].double().view(2, 64) - want).abs() <= bound).all(), i
