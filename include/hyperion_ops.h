@@ -398,7 +398,7 @@ HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t
  * The softmax weights, times their values' scales, enter the value product as fp16 relative to (2^-8 of) the largest so far; results beyond
  * fp16 are infinities.  A key or value row with a NaN scale makes its sequence's results NaN, unless its weight is 0 in fp32.
  * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.
- * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small), HYP_ECUDA. */
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, more than 2^31 rows and heads to join), HYP_ECUDA. */
 HYP_API size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
 HYP_API int hyp_op_attn_decode_kv8(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* q, int64_t q_stride,
                                    const void* kv8_pages, const int32_t* block_table, int32_t max_pages_per_seq,

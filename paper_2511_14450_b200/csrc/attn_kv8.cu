@@ -444,6 +444,53 @@ __global__ void __launch_bounds__(K8_THREADS) kv8_merge_kernel(const float* __re
   }
 }
 
+// The same for up to K8_FEW rows of each of n_rows (sequence, query head): a warp joins them, all its loads on their way at once.
+constexpr int K8_FEW = 8;
+template <int D>
+__global__ void __launch_bounds__(K8_THREADS) kv8_merge_few_kernel(const float* __restrict__ acc, const float* __restrict__ ml, int n_slots,
+                                                                   int n_rows, __half* __restrict__ out) {
+  constexpr int V = D / 32;
+  const int lane = threadIdx.x & 31, row = blockIdx.x * K8_WARPS + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_trigger();
+  if (row >= n_rows) return;
+  const size_t first = (size_t)row * n_slots;
+  float r[K8_FEW][V];
+  float2 x[K8_FEW];
+#pragma unroll
+  for (int i = 0; i < K8_FEW; ++i) {
+    const size_t at = first + (i < n_slots ? i : 0);
+    x[i] = *reinterpret_cast<const float2*>(ml + at * 2);
+    const float* src = acc + at * D + V * lane;
+    if (V == 4) {
+      const float4 y = *reinterpret_cast<const float4*>(src);
+      r[i][0] = y.x; r[i][1] = y.y; r[i][2] = y.z; r[i][V - 1] = y.w;
+    } else {
+      const float2 y = *reinterpret_cast<const float2*>(src);
+      r[i][0] = y.x; r[i][1] = y.y;
+    }
+  }
+  float mx = PG_NEG, sum = 0.f, v[V];
+#pragma unroll
+  for (int i = 0; i < K8_FEW; ++i) mx = fmaxf(mx, x[i].x);
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = 0.f;
+#pragma unroll
+  for (int i = 0; i < K8_FEW; ++i) {
+    if (i >= n_slots || x[i].y == 0.f) continue;  // NaN is carried on
+    const float w = ex2_approx(x[i].x - mx);
+    sum = fmaf(w, x[i].y, sum);
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = fmaf(w, r[i][j], v[j]);
+  }
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
+  __half* to = out + (size_t)row * D + V * lane;
+  if (V == 4)
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_f16(v[0] * inv, v[1] * inv), pack_f16(v[2] * inv, v[V - 1] * inv));
+  else
+    *reinterpret_cast<uint32_t*>(to) = pack_f16(v[0] * inv, v[1] * inv);
+}
+
 template <int D, int G, int FMT, bool CLUSTER>
 int launch_one(const Kv8Args& a, int n_splits, int n_seqs, cudaStream_t st) {
   constexpr int smem = kv8_smem<D>();
@@ -471,10 +518,16 @@ template <int D, int G, int FMT>
 int launch_joined(Kv8Args a, int n_splits, int n_seqs, __half* out, cudaStream_t st) {
   const bool cluster = n_splits >= 2 && n_splits <= 8 && (long long)n_splits * a.Hkv * n_seqs <= (long long)K8_PER_SM * sm_count();
   if (n_splits == 1 || cluster) a.out = out;
+  else if ((long long)n_seqs * a.Hq > 0x7fffffffll) return HYP_ECAPACITY;  // rows to join
   if (cluster) return launch_one<D, G, FMT, true>(a, n_splits, n_seqs, st);
   const int rc = launch_one<D, G, FMT, false>(a, n_splits, n_seqs, st);
   if (rc < 0 || n_splits == 1) return rc;
-  HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_kernel<D>, dim3((unsigned)(n_seqs * a.Hq)), dim3(K8_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
+  const int rows = n_seqs * a.Hq;
+  if (a.n_slots <= K8_FEW)
+    HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_few_kernel<D>, dim3((unsigned)((rows + K8_WARPS - 1) / K8_WARPS)), dim3(K8_THREADS), (size_t)0, st, a.acc, a.ml,
+                               a.n_slots, rows, out));
+  else
+    HYP_CUDA_TRY(launch_pdl<2>(kv8_merge_kernel<D>, dim3((unsigned)rows), dim3(K8_THREADS), (size_t)0, st, a.acc, a.ml, a.n_slots, out));
   return rc + 1;
 }
 

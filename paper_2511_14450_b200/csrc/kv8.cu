@@ -46,6 +46,11 @@ __device__ __forceinline__ float row_scale(double amax) {
   const long long b = __double_as_longlong(amax);
   return pow2((int)(b >> 52) - 1023 - 8 + ((b & 0xfffffffffffffll) > 0xc000000000000ll ? 1 : 0));
 }
+template <int FMT>
+__device__ __forceinline__ float row_scale(float amax) {  // of values that were not rotated
+  if (FMT == HYP_KV8_INT8) return (float)((double)amax * (1.0 / 127.0));
+  return pow2(e4m3_exponent(__float_as_uint(amax)));
+}
 // x times an exact power of two, to fp32 rounded to odd, so that the rounding to E4M3 behind it is the only one.
 __device__ __forceinline__ float odd_product(double x, double inv) {
   const double y = x * inv;
@@ -124,7 +129,7 @@ struct WriteArgs {
 // used for the largest value of a row and where a code hangs on the rotation's roundings.  Those are two of half a step each, of a term and of
 // the sum; as both members of the row's pairs are kept, neither exceeds 1.42 times the row's largest magnitude: 2^-22 of it covers them.
 template <int D, int FMT, int TYPE>
-__global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
   constexpr int LANES = D / 4, PER = 32 / LANES, SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
   extern __shared__ __align__(128) uint8_t wr_smem[];
   __shared__ uint64_t bar_word;
@@ -187,8 +192,11 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
     const uint32_t top = __reduce_max_sync(mine, own_top);
     const bool bad = top >= 0x7f800000u;
     // the largest magnitude exactly: among the values whose fp32 form is within its error of the largest one
-    double amax = (double)__uint_as_float(top);
-    if (any_turn) {
+    float s = 0.f;
+    bool some = __uint_as_float(top) >= KV8_LEAST;
+    if (!any_turn) {
+      s = row_scale<FMT>(__uint_as_float(top));
+    } else {
       const float close = __uint_as_float(top) * (1.f - 0x1p-20f);
       double m = 0.0;
       if (turn && __uint_as_float(own_top) >= close) {
@@ -203,12 +211,14 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const WriteArgs a) {
 #pragma unroll
         for (int k = LANES / 2; k > 0; k >>= 1) best = fmax(best, __shfl_xor_sync(0xffffffffu, best, k));
       }
-      if (turn) amax = best;
-    }
-    float s = 0.f;
-    uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
-    if (!bad && amax >= (double)KV8_LEAST) {
+      const double amax = turn ? best : (double)__uint_as_float(top);
+      some = amax >= (double)KV8_LEAST;
       s = row_scale<FMT>(amax);
+    }
+    uint32_t w = FMT == HYP_KV8_INT8 ? 0x80808080u : 0u;
+    if (bad || !some) {
+      s = 0.f;
+    } else {
       if (!fast_codes<FMT>(x, turn ? __uint_as_float(top) * 0x1p-22f : 0.f, s, w)) {
         double xd[4];
 #pragma unroll
