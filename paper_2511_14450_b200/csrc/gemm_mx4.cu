@@ -56,32 +56,27 @@ int least_tiles(int M, int terms, int cap) {
   const int most = cap / terms / 8 * 8;
   return (M + most - 1) / most;
 }
+// CTAs that are on the GPU at once, one to an SM, in clusters of ks (which do not fill every group of SMs that shares a cluster's paths).
+int slots_for(int ks);
+// The cheapest cut by a count of cycles.  A stage of 128 k takes the longest of: its operands' way into the SM (about 40 bytes a cycle from the
+// L2), through shared memory (written and read, the weights spread to bytes, at about 100), the MMAs (at least 45 cycles each), and
+// the weights' way from HBM (3300 bytes a cycle for all).  A CTA takes about 5000 to start and end, and its results; shares of K meet in a cluster.
 Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
-  const int sms = sm_count();
   Plan best{}, p{};
-  if (M * (long long)terms <= 128) {
-    // Few tokens, bound by the weights' way from HBM: one CTA to an SM as far as the tiles can be divided that way (8 x 7680 x 5120 in two
-    // shares of K on 120 SMs 10.2 us, in four on all with two CTAs each 10.3; 32 x 17920 x 5120 with gate and up in one share 23.5, in two 39.6).
-    cut(best, M, N, terms, swiglu ? 2 : 1, swiglu, 1);
-    long long ks = sms / best.row_units;
-    if (ks > KB / 4) ks = KB / 4;
-    best.ksplit = ks > 8 ? 8 : ks < 1 ? 1 : (int)ks;
-    return best;
-  }
-  // Many tokens: the cheapest by a count of cycles.  A stage of 128 k takes 2 nb cycles of MMA for every row tile, or what its operands take
-  // from the L2 (about 40 bytes a cycle and SM); a CTA about 5000 to start and end, and its results.
   double least = 0.0;
   for (int a = swiglu ? 2 : 1; a <= 2; ++a) {
     const int t0 = least_tiles(M, terms, row_cap(a));
     for (int t = t0; t <= t0 + MX_MORE_TILES; ++t) {
       if (!cut(p, M, N, terms, a, swiglu, t)) continue;
-      for (int ks = 1; ks <= 4; ++ks) {
+      for (int ks = 1; ks <= 8; ++ks) {
         if (ks > 1 && (ks > KB / 4 || a * p.tt * MX_ROWS * 4 > MX_MAX_DYN - 1024)) break;
-        const double stage = fmax(2.0 * a * p.nb, (a * MX_PACK_BYTES + (double)p.block_bytes) / 40.0);
-        const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * (ks > 1 ? 70.0 : 30.0);
-        const double waves = ceil((double)p.row_units * p.tiles * ks / sms);
-        if (least == 0.0 || waves * cta < least) {
-          least = waves * cta;
+        const double ctas = (double)p.row_units * p.tiles * ks, slots = slots_for(ks), block = (double)p.block_bytes;
+        const double stage = fmax(fmax((a * MX_PACK_BYTES + block) / 40.0, (a * 2.0 * MX_A_BYTES + 2.0 * block) / 100.0),
+                                  fmax(a * fmax(180.0, 2.0 * p.nb), a * (double)MX_PACK_BYTES * fmin(ctas, slots) / p.tiles / 3300.0));
+        const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * 30.0 + (ks > 1 ? 1500.0 + a * p.tt * 40.0 : 0.0);
+        const double cost = ceil(ctas / slots) * cta;
+        if (least == 0.0 || cost < least) {
+          least = cost;
           best = p;
           best.ksplit = ks;
         }
@@ -544,6 +539,30 @@ int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   cfg.numAttrs = na;
   HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_mx4_kernel<EPI, A_TILES>, map, p));
   return 1;
+}
+
+int slots_for(int ks) {
+  static int known[64][9] = {};  // per device
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count();
+  if (known[dev][ks] == 0) {
+    int n = 0;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    cfg.gridDim = dim3((unsigned)ks * 64);
+    cfg.blockDim = dim3(MX_THREADS);
+    cfg.dynamicSmemBytes = 200 * 1024;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)ks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (ks == 1 || allow_smem<gemm_mx4_kernel<EPI_STORE_F32, 1>>(MX_MAX_DYN) != HYP_OK ||
+        cudaOccupancyMaxActiveClusters(&n, gemm_mx4_kernel<EPI_STORE_F32, 1>, &cfg) != cudaSuccess || n < 1)
+      n = sm_count() / ks;
+    known[dev][ks] = n * ks;
+  }
+  return known[dev][ks];
 }
 
 }  // namespace
