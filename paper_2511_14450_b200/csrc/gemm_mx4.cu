@@ -39,6 +39,7 @@ struct Plan {
   size_t block_bytes;  // terms of one (token tile, 128 k) with their scales
 };
 constexpr int MX_MAX_DYN = 216 * 1024, MX_MORE_TILES = 3;
+constexpr int OWN_CHUNKS = 2, OWN_BYTES = 64 * 1024;  // see launch_gemm_mx4
 // Tensor memory: one accumulator of 256 columns beside the scales, or two of 240.
 int row_cap(int a_tiles) { return a_tiles == 2 ? 240 : 256; }
 bool cut(Plan& p, int M, int N, int terms, int a_tiles, bool swiglu, int tiles) {
@@ -159,11 +160,16 @@ __global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* _
 // ---------------------------------------------------------------------------------------------
 // product
 // ---------------------------------------------------------------------------------------------
+// Bytes from one block of a CTA's own terms to the next (operands start on 1024 bytes).
+__host__ __device__ __forceinline__ uint32_t own_place(size_t block_bytes) { return ((uint32_t)block_bytes + 1023u) & ~1023u; }
+
 struct MxArgs {
   const uint8_t* packed;  // weights, for the scales
-  const uint8_t* terms;   // activations
+  const uint8_t* terms;   // activations in terms; OWN: as they are
+  const uint8_t* act;
+  long long act_stride;
   size_t block_bytes;
-  int M, N, KB, ldo;
+  int M, N, K8, KB, ldo;
   int tiles, row_units, token_tiles, tt, nb, n_terms;
   int stages, stage_bytes, ksplit, tmem_cols;
   uint32_t idesc;
@@ -245,25 +251,51 @@ __device__ __forceinline__ void mx_store(const MxArgs& p, int m, int n, float4 y
   }
 }
 
+// The terms of a CTA's tokens m0 .. m0 + mt - 1 for its n_kb blocks of 128 k; 32 MX_EPI_WARPS threads, a chunk of eight k at a time, the next
+// one's values on their way.
+__device__ __forceinline__ void own_terms(const MxArgs& p, uint8_t* to, int kb0, int n_kb, int m0, int mt, int t) {
+  constexpr int STEP = 32 * MX_EPI_WARPS;
+  const int all = 16 * p.tt * n_kb;  // a multiple of 128: whole warps, blocks of four lanes
+  auto fetch = [&](int i) {
+    const int c = i & 15, row = (i >> 4) % p.tt, ck = 16 * (kb0 + (i >> 4) / p.tt) + c;
+    return i < all && row < mt && ck < p.K8 ? *reinterpret_cast<const uint4*>(p.act + ((long long)(m0 + row) * p.act_stride + 8ll * ck) * 2) : make_uint4(0, 0, 0, 0);
+  };
+  uint4 raw = fetch(t);
+  for (int i = t; i < all; i += STEP) {
+    float v[1][8];
+    unpack8(raw, p.f16, v[0]);
+    raw = fetch(i + STEP);
+    const int c = i & 15, row = (i >> 4) % p.tt;
+    uint8_t* blk = to + (i >> 4) / p.tt * own_place(p.block_bytes);
+    make_terms<1>(v, p.n_terms, [&](int, int term, uint2 codes, uint8_t scale) {
+      const int r = term * p.tt + row;
+      *reinterpret_cast<uint2*>(blk + term_at(r, c)) = codes;
+      if ((c & 3) == 0) blk[term_scale_at(p.nb, r, c)] = scale;
+    });
+  }
+}
+
 // A_TILES 2 without SwiGLU: two neighbouring row tiles, so that the terms' way from the L2 serves twice the products.
-template <int EPI, int A_TILES>
+// OWN: a CTA's share of K is so small that it makes its terms itself, in a place of their own beside the ring: a launch less.
+template <int EPI, int A_TILES, bool OWN>
 __global__ void __launch_bounds__(MX_THREADS, 1)
 gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   constexpr bool SWIGLU = EPI == EPI_SWIGLU_BF16, DUAL = A_TILES == 2;
   static_assert(!SWIGLU || DUAL, "gate and up");
   extern __shared__ uint8_t mx_smem[];
-  __shared__ uint64_t bars[2 * MX_MAX_STAGES + 1];
+  __shared__ uint64_t bars[2 * MX_MAX_STAGES + 2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   const uint32_t base = (smem_u32(mx_smem) + 1023u) & ~1023u;
   uint8_t* ring = mx_smem + (base - smem_u32(mx_smem));
   float* sums = reinterpret_cast<float*>(ring);  // behind the main loop: [accumulator][token][128 rows]
   const int S = p.stages;
-  const uint32_t b_off = A_TILES * MX_A_BYTES, sfa_off = b_off + (uint32_t)p.block_bytes;  // terms, their scales, weight scales
+  // a stage: weights, terms with their scales (OWN: behind the ring), weight scales
+  const uint32_t b_off = A_TILES * MX_A_BYTES, sfa_off = b_off + (OWN ? 0u : (uint32_t)p.block_bytes);
   const uint32_t bar0 = smem_u32(bars);
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (MX_MAX_STAGES + s); };
-  const uint32_t tfull_bar = bar0 + 8u * (2 * MX_MAX_STAGES);
+  const uint32_t tfull_bar = bar0 + 8u * (2 * MX_MAX_STAGES), terms_bar = tfull_bar + 8;
   volatile int* abort_flag = &abort_word;
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -274,14 +306,15 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(full_bar(s), 3);  // codes, weight scales, terms
+      mbar_init(full_bar(s), OWN ? 2 : 3);  // codes, weight scales, terms
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(tfull_bar, 1);
+    mbar_init(terms_bar, MX_EPI_WARPS);
     abort_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const uint8_t* terms = p.terms + ((size_t)tok * p.KB + kb0) * p.block_bytes;
+  const uint8_t* terms = OWN ? nullptr : p.terms + ((size_t)tok * p.KB + kb0) * p.block_bytes;
   // What a producing thread adds to the ring: `src` steps by `step` from k-block to k-block, `dst` and `bar` from stage to stage.
   const int n_kb = kb1 - kb0, n_first = min(S, n_kb);
   const int line0 = (int)(((long long)tile * p.KB + kb0) * (MX_PACK_BYTES / 64)), up_lines = (SWIGLU ? p.tiles : tile + 1 < p.tiles ? 1 : 0) * p.KB * (MX_PACK_BYTES / 64);  // to the second row tile (behind the last: itself)
@@ -343,30 +376,42 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
 
   const int m0 = tok * p.tt, mt = min(p.tt, p.M - m0);
   if (warp == 0) {
-    produce(load_w, line0, MX_PACK_BYTES / 64, n_first);
+    if (OWN) {
+      // scales along with the codes: the other warps make terms
+      if (elect_one())
+        for (int i = 0; i < n_first; ++i) load_s(p.packed + 64ll * line0 + MX_CODE_BYTES + (size_t)i * MX_PACK_BYTES, base + i * p.stage_bytes, full_bar(i));
+      __syncwarp();
+      produce([&](int line, uint32_t dst, uint32_t bar) {
+        load_w(line, dst, bar);
+        load_s(p.packed + 64ll * line + MX_CODE_BYTES, dst, bar);
+      }, line0, MX_PACK_BYTES / 64, n_first);
+    } else {
+      produce(load_w, line0, MX_PACK_BYTES / 64, n_first);
+    }
   } else if (warp == 1) {
     // The whole warp walks the loop and one lane issues: so the operands stay in uniform registers (a lane on its own moves each of them there
     // for every instruction: 800 cycles a stage).
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0), ub = __shfl_sync(0xffffffffu, base, 0);
     const uint32_t sfa = tm + (uint32_t)(A_TILES * p.nb), sfb = sfa + 4 * A_TILES, step = (uint32_t)p.stage_bytes >> 4;
-    const uint64_t da0 = smem_desc(ub), db0 = smem_desc(ub + b_off), dsa0 = scales_desc(ub + sfa_off), dsb0 = scales_desc(ub + b_off + p.nb * MX_BK);
+    const uint32_t ut = OWN ? ub + S * p.stage_bytes : ub + b_off, t_step = OWN ? own_place(p.block_bytes) >> 4 : step;
+    const uint64_t da0 = smem_desc(ub), db0 = smem_desc(ut), dsa0 = scales_desc(ub + sfa_off), dsb0 = scales_desc(ut + p.nb * MX_BK);
     const uint32_t id0 = p.idesc, id1 = id0 | 1u << 29 | 1u << 4, id2 = id0 | 2u << 29 | 2u << 4, id3 = id0 | 3u << 29 | 3u << 4;  // byte of a scale word
     const uint32_t acc2 = tm + (uint32_t)p.nb;
     const bool two_sf = p.nb > MX_ROWS;
     int stage = 0;
-    uint32_t phase = 0, at = 0;  // at: the stage's place, in descriptor units
-    bool ok = true;
-    for (int i = 0; i < n_kb; ++i) {
+    uint32_t phase = 0, at = 0, t_at = 0;  // the places of the stage and of its terms, in descriptor units
+    bool ok = !OWN || __all_sync(0xffffffffu, mbar_wait(terms_bar, 0, abort_flag));
+    for (int i = 0; i < n_kb && ok; ++i) {
       ok = __all_sync(0xffffffffu, mbar_wait(full_bar(stage), phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const uint64_t da = da0 + at, db = db0 + at;
+      const uint64_t da = da0 + at, db = db0 + t_at;
       if (elect_one()) {
         // scales of this stage: in order behind the MMAs that still read the ones before
         mx_copy_scales(sfa, dsa0 + at);
         if (DUAL) mx_copy_scales(sfa + 4, dsa0 + at + MX_SF_BYTES / 16);
-        mx_copy_scales(sfb, dsb0 + at);
-        if (two_sf) mx_copy_scales(sfb + 4, dsb0 + at + MX_SF_BYTES / 16);
+        mx_copy_scales(sfb, dsb0 + t_at);
+        if (two_sf) mx_copy_scales(sfb + 4, dsb0 + t_at + MX_SF_BYTES / 16);
         if (i == 0) {
           mx_mma<false>(tm, da, db, id0, sfa, sfb);
           if (DUAL) mx_mma<false>(acc2, da + MX_A_BYTES / 16, db, id0, sfa + 4, sfb);
@@ -385,7 +430,13 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
       }
       __syncwarp();
       at += step;
-      if (++stage == S) { stage = 0; phase ^= 1u; at = 0; }
+      t_at += t_step;
+      if (++stage == S) {
+        stage = 0;
+        phase ^= 1u;
+        at = 0;
+        if (!OWN) t_at = 0;
+      }
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -394,8 +445,14 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   } else {
     bool ok = true;
     // two of these warps issue copies first
-    if (warp == 2) ok = produce(load_s, p.packed + 64ll * line0 + MX_CODE_BYTES, MX_PACK_BYTES, 0);
-    if (warp == 3) ok = produce(load_t, terms, term_bytes, 0);
+    if (!OWN && warp == 2) ok = produce(load_s, p.packed + 64ll * line0 + MX_CODE_BYTES, MX_PACK_BYTES, 0);
+    if (!OWN && warp == 3) ok = produce(load_t, terms, term_bytes, 0);
+    if (OWN) own_terms(p, ring + S * p.stage_bytes, kb0, n_kb, m0, mt, threadIdx.x - 64);
+    if (OWN) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(terms_bar);
+    }
     ok = mbar_wait(tfull_bar, 0, abort_flag) && ok;
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -494,24 +551,26 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   }
 }
 
-template <int EPI, int A_TILES>
-int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
-  const int rc = allow_smem<gemm_mx4_kernel<EPI, A_TILES>>(MX_MAX_DYN);
+template <int EPI, int A_TILES, bool OWN>
+int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
+  const int rc = allow_smem<gemm_mx4_kernel<EPI, A_TILES, OWN>>(MX_MAX_DYN);
   if (rc) return rc;
   int cols = 32;
   while (cols < A_TILES * (p.nb + 4) + 8) cols <<= 1;
   p.tmem_cols = cols;
-  p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (int)p.block_bytes + 1023) / 1024 * 1024;
+  p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (OWN ? 0 : (int)p.block_bytes) + 1023) / 1024 * 1024;
+  const int own_bytes = OWN ? (p.KB + p.ksplit - 1) / p.ksplit * (int)own_place(p.block_bytes) : 0;
   const long long ctas = (long long)p.row_units * p.token_tiles * p.ksplit;
   if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
   const int sum_bytes = (p.ksplit > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
   // two CTAs to an SM where there are more than SMs and tensor memory has room for both
   const int budget = ctas > sm_count() && cols <= 256 ? 112 * 1024 : MX_MAX_DYN;
-  int stages = (budget - 1024) / p.stage_bytes;
+  int stages = (budget - 1024 - own_bytes) / p.stage_bytes;
   if (stages > MX_MAX_STAGES) stages = MX_MAX_STAGES;
   if (stages < 2) stages = 2;
   p.stages = stages;
-  int smem = (stages * p.stage_bytes > sum_bytes ? stages * p.stage_bytes : sum_bytes) + 1024;  // the sums reuse the ring
+  const int ring = stages * p.stage_bytes + own_bytes;
+  int smem = (ring > sum_bytes ? ring : sum_bytes) + 1024;  // the sums reuse the ring
   if (smem > MX_MAX_DYN) return HYP_EINVAL;
   // never more CTAs on an SM than tensor memory holds: one that waits for it would hold up its cluster
   const int least = 228 * 1024 / (512 / cols + 1);
@@ -537,7 +596,7 @@ int launch_epi(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   }
   cfg.attrs = attr;
   cfg.numAttrs = na;
-  HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_mx4_kernel<EPI, A_TILES>, map, p));
+  HYP_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_mx4_kernel<EPI, A_TILES, OWN>, map, p));
   return 1;
 }
 
@@ -557,12 +616,27 @@ int slots_for(int ks) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (ks == 1 || allow_smem<gemm_mx4_kernel<EPI_STORE_F32, 1>>(MX_MAX_DYN) != HYP_OK ||
-        cudaOccupancyMaxActiveClusters(&n, gemm_mx4_kernel<EPI_STORE_F32, 1>, &cfg) != cudaSuccess || n < 1)
+    if (ks == 1 || allow_smem<gemm_mx4_kernel<EPI_STORE_F32, 1, false>>(MX_MAX_DYN) != HYP_OK ||
+        cudaOccupancyMaxActiveClusters(&n, gemm_mx4_kernel<EPI_STORE_F32, 1, false>, &cfg) != cudaSuccess || n < 1)
       n = sm_count() / ks;
     known[dev][ks] = n * ks;
   }
   return known[dev][ks];
+}
+
+template <int EPI, int A_TILES>
+int launch_epi(const CUtensorMap& map, MxArgs& p, bool own, cudaStream_t st) {
+  return own ? launch_own<EPI, A_TILES, true>(map, p, st) : launch_own<EPI, A_TILES, false>(map, p, st);
+}
+
+int launch_by_epi(int epi, bool dual, const CUtensorMap& map, MxArgs& p, bool own, cudaStream_t st) {
+  switch (epi) {
+    case EPI_STORE_BF16: return dual ? launch_epi<EPI_STORE_BF16, 2>(map, p, own, st) : launch_epi<EPI_STORE_BF16, 1>(map, p, own, st);
+    case EPI_RESID_F32: return dual ? launch_epi<EPI_RESID_F32, 2>(map, p, own, st) : launch_epi<EPI_RESID_F32, 1>(map, p, own, st);
+    case EPI_SWIGLU_BF16: return launch_epi<EPI_SWIGLU_BF16, 2>(map, p, own, st);
+    case EPI_STORE_F32: return dual ? launch_epi<EPI_STORE_F32, 2>(map, p, own, st) : launch_epi<EPI_STORE_F32, 1>(map, p, own, st);
+    default: return HYP_EINVAL;
+  }
 }
 
 }  // namespace
@@ -588,6 +662,15 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(swiglu ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
+  // Up to OWN_CHUNKS chunks a thread the CTAs make their terms themselves (one token, 512 x 256: 3.7 instead of 4.8 us); a chunk of three terms takes
+  // a warp about 0.9 us, so with three chunks and more a launch of their own is faster (6144 x 4096: 8.0 instead of 9.4 us).
+  const int share = (p.KB + p.ksplit - 1) / p.ksplit;
+  const bool own = t.tiles == 1 && 16ll * t.tt * share <= OWN_CHUNKS * 32 * MX_EPI_WARPS && share * (long long)own_place(t.block_bytes) <= OWN_BYTES &&
+                   (long long)t.row_units * t.ksplit <= sm_count();
+  if (own) {
+    p.act = (const uint8_t*)a; p.act_stride = a_stride; p.K8 = K / 8;
+    return launch_by_epi(epi, t.a_tiles == 2, map, p, true, st);
+  }
   const long long chunks = 16ll * p.KB;
   const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs
   const long long segments = (chunks + TERM_THREADS * (many ? 2 : 1) - 1) / (TERM_THREADS * (many ? 2 : 1));
@@ -600,14 +683,7 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
     HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_F16, 2>) : go(mx_terms_kernel<HYP_TYPE_F16, 1>)));
   else
     HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_BF16, 2>) : go(mx_terms_kernel<HYP_TYPE_BF16, 1>)));
-  const bool dual = t.a_tiles == 2;
-  switch (epi) {
-    case EPI_STORE_BF16: rc = dual ? launch_epi<EPI_STORE_BF16, 2>(map, p, st) : launch_epi<EPI_STORE_BF16, 1>(map, p, st); break;
-    case EPI_RESID_F32: rc = dual ? launch_epi<EPI_RESID_F32, 2>(map, p, st) : launch_epi<EPI_RESID_F32, 1>(map, p, st); break;
-    case EPI_SWIGLU_BF16: rc = launch_epi<EPI_SWIGLU_BF16, 2>(map, p, st); break;
-    case EPI_STORE_F32: rc = dual ? launch_epi<EPI_STORE_F32, 2>(map, p, st) : launch_epi<EPI_STORE_F32, 1>(map, p, st); break;
-    default: return HYP_EINVAL;
-  }
+  rc = launch_by_epi(epi, t.a_tiles == 2, map, p, false, st);
   return rc < 0 ? rc : rc + 1;
 }
 

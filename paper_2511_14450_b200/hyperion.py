@@ -648,14 +648,15 @@ def _types():
 
 def _matrix(where, name, t):
     """(device, type, rows, columns, address, row stride) of a matrix with dense rows, which may lie in a wider buffer."""
-    code = _types().get(t.dtype)
+    code = (_TYPES or _types()).get(t.dtype)
     dev, s = t.get_device(), t.shape
     if code is None or dev < 0 or len(s) != 2:
         _refuse(where, f"{name} must be a CUDA matrix of fp32, fp16 or bf16, not {t.dtype} {tuple(s)} on {t.device}")
+    rows, cols = s
     stride, one = t.stride()
-    if (one != 1 and s[1] > 1) or (stride < s[1] and s[0] > 1):
+    if (one != 1 and cols > 1) or (stride < cols and rows > 1):
         _refuse(where, f"{name} must have dense rows that do not overlap, not strides {t.stride()}")
-    return dev, code, s[0], s[1], t.data_ptr(), stride if s[0] > 1 else (s[1] + 7) // 8 * 8
+    return dev, code, rows, cols, t.data_ptr(), stride if rows > 1 else (cols + 7) // 8 * 8
 
 
 def hyp_op_mx4_quantize(x, codes, scales, stream=None):
@@ -676,8 +677,15 @@ def hyp_op_mx4_dequantize(codes, scales, out, stream=None):
     _launch(where, lib().hyp_op_mx4_dequantize, dev, stream, cp, sp, n, k, code, op, os_)
 
 
+_PACKED_BYTES = {}
+
+
 def hyp_op_mx4_packed_bytes(N: int, K: int, swiglu: bool) -> int:
-    return lib().hyp_op_mx4_packed_bytes(N, K, int(swiglu))
+    key = (N, K, swiglu)
+    n = _PACKED_BYTES.get(key)
+    if n is None:
+        n = _PACKED_BYTES[key] = lib().hyp_op_mx4_packed_bytes(N, K, int(swiglu))
+    return n
 
 
 def hyp_op_mx4_pack(codes, scales, swiglu: bool = False, stream=None):
@@ -728,7 +736,8 @@ def hyp_kv8_half_page_bytes(head_dim: int) -> int:
 
 
 def _pool8(where, t, dev, shape3):
-    _types()
+    if _U8 is None:
+        _types()
     s = t.shape
     if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous() or s[1:] != (2, shape3[1], 16 * shape3[2] + 64):
         _refuse(where, f"kv8_pages must be a contiguous uint8 page pool [pages, 2, {shape3[1]}, {16 * shape3[2] + 64}] on device {dev}, not "
