@@ -359,11 +359,18 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
     }
     return true;
   };
+  auto first_w = [&] {
+    if (threadIdx.x == 0)
+      for (int i = 0; i < n_first; ++i) load_w(line0 + i * (MX_PACK_BYTES / 64), base + i * p.stage_bytes, full_bar(i));
+  };
   __syncwarp();
-  if (threadIdx.x == 0)  // weights are no kernel's output: their first boxes go out before the wait
-    for (int i = 0; i < n_first; ++i) load_w(line0 + i * (MX_PACK_BYTES / 64), base + i * p.stage_bytes, full_bar(i));
+  // The kernel before this one is the one that made the terms (its own wait has seen the end of whatever wrote the weights): the first weights go
+  // out before the wait.  OWN: it may be any kernel.
+  if (!OWN) first_w();
   __syncwarp();
   pdl_wait();
+  if (OWN) first_w();
+  __syncwarp();
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(p.tmem_cols));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
@@ -561,7 +568,6 @@ int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (OWN ? 0 : (int)p.block_bytes) + 1023) / 1024 * 1024;
   const int own_bytes = OWN ? (p.KB + p.ksplit - 1) / p.ksplit * (int)own_place(p.block_bytes) : 0;
   const long long ctas = (long long)p.row_units * p.token_tiles * p.ksplit;
-  if (ctas > 0x7fffffffll) return HYP_ECAPACITY;
   const int sum_bytes = (p.ksplit > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
   // two CTAs to an SM where there are more than SMs and tensor memory has room for both
   const int budget = ctas > sm_count() && cols <= 256 ? 112 * 1024 : MX_MAX_DYN;
@@ -659,6 +665,7 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
   p.f16 = a_type == HYP_TYPE_F16; p.out = out; p.err = tc_err_flag_ptr();
   p.vec = ldo % 4 == 0 && ((uintptr_t)out & (wide ? 15 : 7)) == 0;
   p.idesc = (5u << 7) | (0u << 10) | ((uint32_t)(t.nb >> 3) << 17) | (1u << 23) | ((uint32_t)(MX_ROWS >> 4) << 24);  // E2M1 x E4M3, power-of-two scales
+  if ((long long)t.row_units * t.tiles * t.ksplit > 0x7fffffffll) return HYP_ECAPACITY;
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(swiglu ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
@@ -671,10 +678,9 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
     p.act = (const uint8_t*)a; p.act_stride = a_stride; p.K8 = K / 8;
     return launch_by_epi(epi, t.a_tiles == 2, map, p, true, st);
   }
-  const long long chunks = 16ll * p.KB;
+  const long long chunks = 16ll * p.KB;  // of a row: its segments fit the grid (K is at most 2^25)
   const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs
   const long long segments = (chunks + TERM_THREADS * (many ? 2 : 1) - 1) / (TERM_THREADS * (many ? 2 : 1));
-  if (segments > 65535) return HYP_ECAPACITY;
   auto go = [&](auto kernel) {
     return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, K / 8, p.KB,
                          terms, t.tt, t.nb, t.block_bytes, scratch);

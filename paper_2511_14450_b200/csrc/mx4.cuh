@@ -16,8 +16,8 @@ namespace hyp {
 constexpr int MX_ROWS = 128, MX_BK = 128, MX_BLOCK = 32;
 constexpr int MX_CODE_BYTES = MX_ROWS * MX_BK / 2, MX_SF_BYTES = 512;
 constexpr int MX_PACK_BYTES = MX_CODE_BYTES + MX_SF_BYTES;  // 136 lines of 64 bytes
-inline int mx_row_tiles(int N) { return (N + MX_ROWS - 1) / MX_ROWS; }
-inline int mx_kb(int K) { return (K + MX_BK - 1) / MX_BK; }
+inline int mx_row_tiles(int N) { return (N - 1) / MX_ROWS + 1; }
+inline int mx_kb(int K) { return (K - 1) / MX_BK + 1; }
 inline size_t mx4_packed_bytes(int N, int K, int halves) { return (size_t)halves * mx_row_tiles(N) * mx_kb(K) * MX_PACK_BYTES; }
 
 // Exponent e of the least power of two with amax <= 448 * 2^e, by amax's bits (finite, not negative); -127 at least.

@@ -127,7 +127,7 @@ template <template <int, int> class F, int U, typename... A>
 cudaError_t by_type(int type, A... a) {
   return type == HYP_TYPE_F32 ? F<HYP_TYPE_F32, U>::go(a...) : type == HYP_TYPE_F16 ? F<HYP_TYPE_F16, U>::go(a...) : F<HYP_TYPE_BF16, U>::go(a...);
 }
-dim3 matrix_grid(int N, int K8, int u) { return dim3((unsigned)((N + QW - 1) / QW), (unsigned)((K8 + 32 * u - 1) / (32 * u))); }
+dim3 matrix_grid(int N, int K8, int u) { return dim3((unsigned)((N - 1) / QW + 1), (unsigned)((K8 + 32 * u - 1) / (32 * u))); }
 template <int TYPE, int U>
 struct Quantize {
   static cudaError_t go(const void* x, int N, int K, long long stride, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
@@ -142,21 +142,17 @@ struct Dequantize {
                          K / 8, (K + MX_BLOCK - 1) / MX_BLOCK, (uint8_t*)out, stride);
   }
 };
-// segments of a row are the grid's second dimension
 bool wide_rows(int K) { return K > 1024; }
-bool grid_ok(int K) { return K / 8 <= 65535 * 128; }
 
 }  // namespace
 
 int launch_mx4_quantize(const void* x, int type, int N, int K, long long x_stride, uint8_t* codes, uint8_t* scales, cudaStream_t st) {
-  if (!grid_ok(K)) return HYP_ECAPACITY;
   HYP_CUDA_TRY((wide_rows(K) ? by_type<Quantize, 4>(type, x, N, K, x_stride, codes, scales, st)
                             : by_type<Quantize, 1>(type, x, N, K, x_stride, codes, scales, st)));
   return 1;
 }
 
 int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int N, int K, int type, void* out, long long out_stride, cudaStream_t st) {
-  if (!grid_ok(K)) return HYP_ECAPACITY;
   HYP_CUDA_TRY((wide_rows(K) ? by_type<Dequantize, 4>(type, codes, scales, N, K, out, out_stride, st)
                             : by_type<Dequantize, 1>(type, codes, scales, N, K, out, out_stride, st)));
   return 1;

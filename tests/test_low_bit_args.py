@@ -95,7 +95,7 @@ def test_cache_sizes_of_one_operator():
 
 @pytest.mark.parametrize("name", ["hyp_op_mx4_quantize", "hyp_op_mx4_dequantize", "hyp_op_mx4_pack", "hyp_op_gemm_mx4"])
 def test_matrix_sizes(name):
-    for kw in (dict(N=0), dict(N=-3), dict(K=0), dict(K=4), dict(K=60)):
+    for kw in (dict(N=0), dict(N=-3), dict(K=0), dict(K=4), dict(K=60), dict(K=(1 << 25) + 8), dict(K=-8)):
         assert call(name, **kw) == E, kw
 
 
@@ -113,7 +113,7 @@ def test_matrix_types_and_strides():
     assert need == 128 * 64 + 512 and call("hyp_op_mx4_pack", nbytes=need - 1) == CAP
     assert hyp.hyp_op_mx4_packed_bytes(129, 136, True) == 2 * 2 * 2 * need
     assert call("hyp_op_gemm_mx4", N=1 << 30, K=1 << 20, ldo=1 << 30) != hyp.HYP_OK
-    for n, k in ((0, 64), (5, 60), (1 << 30, 1 << 20)):
+    for n, k in ((0, 64), (5, 60), (1 << 30, 1 << 20), (2 ** 31 - 1, 64), (2 ** 31 - 1, 1 << 26), (128, 2 ** 31 - 8)):
         assert hyp.hyp_op_mx4_packed_bytes(n, k, False) == 0
     for m, k, t in ((0, 64, 1), (3, 60, 1), (3, 64, 0), (3, 64, 4), ((1 << 26) + 1, 64, 1)):
         assert hyp.hyp_op_gemm_mx4_scratch_bytes(m, k, t) == 0
