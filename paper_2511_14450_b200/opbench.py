@@ -8,6 +8,9 @@
     python -m paper_2511_14450_b200.opbench attn_scored --batch 4 --ctx 32768
     python -m paper_2511_14450_b200.opbench attn_shared --batch 32 --ctx 256 --prefix 2048
     python -m paper_2511_14450_b200.opbench kv_evict --batch 4 --ctx 4096 --keep 2048
+    python -m paper_2511_14450_b200.opbench gemm_mx4 --M 8 --N 17920 --K 5120 --terms 3 --epi swiglu
+    python -m paper_2511_14450_b200.opbench attn_kv8 --batch 4 --ctx 32768 --e4m3
+    python -m paper_2511_14450_b200.opbench kv8_write --batch 1 --rows 4096
     python -m paper_2511_14450_b200.opbench layer_gemms --M 512
     python -m paper_2511_14450_b200.opbench decode_stage --layers 2 --batch 8 --ctx 1024
     python -m paper_2511_14450_b200.opbench decode_stage --shape llama3 --layers 11 --batch 8 --ctx 1024
@@ -163,6 +166,60 @@ def kv_evict(batch, ctx, keep, in_place=False, Hq=40, Hkv=10, D=128, iters=20):
             "gbs": 2 * batch * min(ctx, keep) * 4 * Hkv * D / ms / 1e6}
 
 
+def gemm_mx4(M, N, K, terms, epi, iters=20):
+    """hyp_op_gemm_mx4 on a quantised N(0, 0.02) matrix; four copies rotated."""
+    swiglu = EPI[epi] == hyp.HYP_EPI_SWIGLU_BF16
+    rows = 2 * N if swiglu else N
+    codes = torch.empty(rows, K // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(rows, (K + 31) // 32, dtype=torch.uint8, device="cuda")
+    packed = []
+    for _ in range(4):
+        hyp.hyp_op_mx4_quantize((torch.randn(rows, K, device="cuda") * 0.02).bfloat16(), codes, scales)
+        packed.append(hyp.hyp_op_mx4_pack(codes, scales, swiglu))
+    a = torch.randn(M, K, device="cuda").half()
+    out = torch.zeros(M, N, dtype=torch.float16 if epi in ("bf16", "swiglu") else torch.float32, device="cuda")
+    scratch = torch.empty(hyp.hyp_op_gemm_mx4_scratch_bytes(M, K, terms), dtype=torch.uint8, device="cuda")
+    ms = _time(lambda i: hyp.hyp_op_gemm_mx4(a, packed[i % 4], N, terms, EPI[epi], out, scratch), iters)
+    return {"op": "gemm_mx4", "M": M, "N": N, "K": K, "terms": terms, "epi": epi, "us": ms * 1e3,
+            "weight_gbs": rows * K * 17 / 32 / ms / 1e6, "tflops": 2.0 * M * rows * K / ms / 1e9}
+
+
+def _cache8(rows, ctx, Hkv, D, fmt, copies):
+    """Pools of random codes under scales of 0.02 and the table of `rows` sequences."""
+    pages = (ctx + 15) // 16
+    table = torch.randperm(rows * pages, device="cuda").to(torch.int32).view(rows, pages).contiguous()
+    pools = []
+    for _ in range(copies):
+        p = torch.randint(0, 120, (rows * pages, 2, Hkv, 16 * D + 64), dtype=torch.uint8, device="cuda")
+        p[..., 16 * D:] = torch.full((16,), 0.02, device="cuda").view(torch.uint8)
+        pools.append(p)
+    return pools, table
+
+
+def attn_kv8(batch, ctx, fmt, Hq=40, Hkv=10, D=128, iters=20):
+    pools, table = _cache8(batch, ctx, Hkv, D, fmt, 2)
+    q = torch.randn(batch, Hq * D, device="cuda").half()
+    cl = torch.full((batch,), ctx - 1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(max(16, hyp.hyp_op_attn_kv8_scratch_bytes((Hq, Hkv, D), batch, table.shape[1])), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    ms = _time(lambda i: hyp.hyp_op_attn_decode_kv8((Hq, Hkv, D), fmt, q, pools[i % 2], table, cl, scratch, out), iters)
+    return {"op": "attn_kv8", "batch": batch, "ctx": ctx, "us": ms * 1e3, "kv_gbs": batch * ctx * 2 * Hkv * (D + 4) / ms / 1e6}
+
+
+def kv8_write(batch, rows, fmt, Hq=40, Hkv=10, D=128, iters=20):
+    """`rows` new tokens of each of `batch` sequences from fp32 q/k/v rows, rotated."""
+    pools, table = _cache8(batch, rows, Hkv, D, fmt, 2)
+    m = batch * rows
+    qkv = torch.randn(m, (Hq + 2 * Hkv) * D, device="cuda")
+    rope = torch.randn(rows, D // 2, 2, device="cuda")
+    cu = torch.arange(0, m + 1, rows, dtype=torch.int32, device="cuda")
+    ctx = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    q = torch.empty(m, Hq * D, dtype=torch.float16, device="cuda")
+    ms = _time(lambda i: hyp.hyp_op_kv8_write((Hq, Hkv, D), fmt, qkv, pools[i % 2], table, cu, ctx, rope, q), iters)
+    return {"op": "kv8_write", "batch": batch, "rows": rows, "us": ms * 1e3,
+            "gbs": m * ((Hq + 2 * Hkv) * D * 4 + Hq * D * 2 + 2 * Hkv * (D + 4)) / ms / 1e6}
+
+
 def _shape(name):
     from paper_2511_14450_b200 import inputs
     return inputs.llama3_8b_shape() if name == "llama3" else inputs.phi3_medium_shape()
@@ -219,7 +276,7 @@ def decode_stage(layers, batch, ctx, iters=20, shape="phi3"):
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("op", choices=["gemm", "attn_decode", "attn_prefill", "attn_decode_mod", "attn_prefill_mod", "attn_scored", "attn_shared",
-                                   "kv_evict", "layer_gemms", "decode_stage"])
+                                   "kv_evict", "gemm_mx4", "attn_kv8", "kv8_write", "layer_gemms", "decode_stage"])
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--shape", default="phi3", choices=["phi3", "llama3"], help="model shape of layer_gemms / decode_stage")
     ap.add_argument("--M", type=int, default=8)
@@ -235,7 +292,11 @@ def main():
     ap.add_argument("--prefix", type=int, default=2048, help="attn_shared: tokens of the shared prefix")
     ap.add_argument("--keep", type=int, default=512, help="kv_evict: tokens that stay")
     ap.add_argument("--in-place", action="store_true", help="kv_evict: the kept rows stay in their own pages")
+    ap.add_argument("--terms", type=int, default=3, help="gemm_mx4: 8-bit terms an activation")
+    ap.add_argument("--rows", type=int, default=1, help="kv8_write: new tokens a sequence")
+    ap.add_argument("--e4m3", action="store_true", help="attn_kv8, kv8_write: E4M3 codes (default: 8-bit integers)")
     a = ap.parse_args()
+    fmt = hyp.HYP_KV8_E4M3 if a.e4m3 else hyp.HYP_KV8_INT8
     if a.op == "gemm":
         out = [gemm(a.M, a.N, a.K, a.epi, a.iters)]
     elif a.op == "attn_decode":
@@ -252,6 +313,12 @@ def main():
         out = [attn_shared(a.batch, a.ctx, a.prefix, iters=a.iters)]
     elif a.op == "kv_evict":
         out = [kv_evict(a.batch, a.ctx, a.keep, a.in_place, iters=a.iters)]
+    elif a.op == "gemm_mx4":
+        out = [gemm_mx4(a.M, a.N, a.K, a.terms, a.epi, iters=a.iters)]
+    elif a.op == "attn_kv8":
+        out = [attn_kv8(a.batch, a.ctx, fmt, iters=a.iters)]
+    elif a.op == "kv8_write":
+        out = [kv8_write(a.batch, a.rows, fmt, iters=a.iters)]
     elif a.op == "decode_stage":
         out = [decode_stage(a.layers, a.batch, a.ctx, iters=a.iters, shape=a.shape)]
     else:
