@@ -90,7 +90,8 @@ Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
 // ---------------------------------------------------------------------------------------------
 // activations to terms: four lanes take a block of 32 k of one token, eight values each
 // ---------------------------------------------------------------------------------------------
-// U chunks at a time; calls put(chunk, term, codes, scale).  Every lane of the warp calls this.
+// U chunks at a time; calls put(chunk, term, codes, scale).  Every lane of the warp calls this.  Bound by issue slots where there are many, so
+// the power of two is formed from the bits: 0x1fffff more carries into the exponent exactly where the mantissa passes 1.75 (448 = 1.75 * 2^8).
 template <int U, typename Put>
 __device__ __forceinline__ void make_terms(float (&v)[U][8], int terms, Put put) {
   bool bad[U];
@@ -99,24 +100,27 @@ __device__ __forceinline__ void make_terms(float (&v)[U][8], int terms, Put put)
   for (int t = 0; t < terms; ++t) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      uint32_t top = absmax_bits(v[j]);
+      uint32_t top = __float_as_uint(absmax_nan(v[j]));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       bad[j] = bad[j] || top >= 0x7f800000u;
-      const int e = bad[j] ? 0 : e4m3_exponent(top);
-      const float inv = bad[j] ? 0.f : pow2(-e), scale = pow2(e);
-      uint32_t w[2] = {0u, 0u};
+      const int byte = max((int)((top + 0x1fffffu) >> 23) - 8, 0);  // exponent + 127 of the least power of two p with top <= 448 p
+      const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+      uint32_t w[2];
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const uint32_t q = bad[j] ? 0u : to_e4m3x2(v[j][2 * p] * inv, v[j][2 * p + 1] * inv);
-        w[p >> 1] |= q << (16 * (p & 1));
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t q0 = to_e4m3x2(v[j][4 * h] * inv, v[j][4 * h + 1] * inv), q1 = to_e4m3x2(v[j][4 * h + 2] * inv, v[j][4 * h + 3] * inv);
+        w[h] = __byte_perm(q0, q1, 0x5410);
         if (t + 1 < terms) {
-          const float2 f = half2_values(e4m3x2_to_half2(q));
-          v[j][2 * p] = fmaf(-f.x, scale, v[j][2 * p]);  // exact: what is left has fewer bits
-          v[j][2 * p + 1] = fmaf(-f.y, scale, v[j][2 * p + 1]);
+          const float scale = __uint_as_float(byte ? (uint32_t)byte << 23 : 0x00400000u);
+          const float2 f = half2_values(e4m3x2_to_half2(q0)), g = half2_values(e4m3x2_to_half2(q1));
+          v[j][4 * h] = fmaf(-f.x, scale, v[j][4 * h]);  // exact: what is left has fewer bits
+          v[j][4 * h + 1] = fmaf(-f.y, scale, v[j][4 * h + 1]);
+          v[j][4 * h + 2] = fmaf(-g.x, scale, v[j][4 * h + 2]);
+          v[j][4 * h + 3] = fmaf(-g.y, scale, v[j][4 * h + 3]);
         }
       }
-      put(j, t, make_uint2(w[0], w[1]), bad[j] ? 255 : (uint8_t)(e + 127));
+      put(j, t, make_uint2(w[0], w[1]), bad[j] ? 255 : (uint8_t)byte);  // under a NaN scale the codes do not matter
     }
   }
 }

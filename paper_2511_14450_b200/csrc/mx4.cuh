@@ -102,12 +102,16 @@ __device__ __forceinline__ void unpack8(uint4 r, bool f16, float (&v)[8]) {
     v[2 * i + 1] = f.y;
   }
 }
-// Largest magnitude of eight values as its bits; infinities and NaN come out as 0x7f800000 or more.
-__device__ __forceinline__ uint32_t absmax_bits(const float (&v)[8]) {
-  uint32_t m = 0;
+// Largest magnitude of eight values, NaN if one is.
+__device__ __forceinline__ float absmax_nan(const float (&v)[8]) {
+  float m[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  return m;
+  for (int i = 0; i < 8; ++i) m[i] = fabsf(v[i]);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < o; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m[i]) : "f"(m[i + o]));
+  return m[0];
 }
 
 int launch_mx4_quantize(const void* x, int type, int N, int K, long long x_stride, uint8_t* codes, uint8_t* scales, cudaStream_t st);

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(QT) mx4_quantize_kernel(const uint8_t* __restr
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    uint32_t m = absmax_bits(v[u]);
+    uint32_t m = __float_as_uint(absmax_nan(v[u]));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     const bool bad = m >= 0x7f800000u;
