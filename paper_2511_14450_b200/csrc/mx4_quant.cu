@@ -3,8 +3,8 @@
 // A warp takes a run of a row, a lane eight values at a time, so that four lanes hold a block of 32: the block's largest magnitude by
 // two shuffles, the exponent floor(log2 amax) - 2 from its bits (amax lands in [4, 8), where 6 is the largest code: what lies above
 // saturates), every value times the exact inverse power, rounded to E2M1 by the hardware conversion (nearest, ties to even).
-// Bound by HBM (one pass, 16-byte loads, up to four in flight a lane), next by issue slots: with a division by the row length in every
-// thread and eight values to a thread the two passes over 17920 x 5120 bf16 values took 65 + 52 us.
+// Bound by HBM: 17920 x 5120 bf16 values to codes and back, 464 MB in 79 us = 5.9 TB/s (one pass, 16-byte loads, up to four in flight a lane); next
+// by issue slots: with a division by the row length in every thread and eight values to a thread it took 114 us.
 #include "mx4.cuh"
 
 namespace hyp {
