@@ -372,7 +372,8 @@ HYP_API int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, con
 enum { HYP_KV8_INT8 = 0, HYP_KV8_E4M3 = 1 };
 
 /* Appends M new rows, packed sequence by sequence as hyp_op_attn_prefill takes them (a decode step: one row each): sequence i owns rows
- * cu_q[i] .. cu_q[i+1]-1 at positions ctx_lens[i], ctx_lens[i] + 1, ...; keys and values are quantised and written, queries go to q_out.
+ * cu_q[i] .. cu_q[i+1]-1 (ascending from 0) at positions ctx_lens[i], ctx_lens[i] + 1, ...; keys and values are quantised and written, queries
+ * go to q_out.
  *   qkv         [M, stride] of `type` (HYP_TYPE_*): [Q heads | K heads | V heads], stride >= (n_q_heads + 2 n_kv_heads) * head_dim, a
  *               multiple of 8, 16-byte aligned
  *   rope_table  fp32 [rope_positions, head_dim / 2, 2] (cos, sin), 16-byte aligned: queries and keys are rotated (pairs i, i + head_dim / 2)

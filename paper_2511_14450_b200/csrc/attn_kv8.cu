@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   int slot = 0;
   uint32_t phase = 0;
   for (int i = 0; i < my_n; ++i) {
-    if (!mbar_wait(my_bars + 8u * slot, phase, nullptr)) { ok = false; break; }
+    if (!__all_sync(0xffffffffu, mbar_wait(my_bars + 8u * slot, phase, nullptr))) { ok = false; break; }
     const uint32_t at0 = my_ring + slot * SLOT;
     const int k0 = T * (first + stride_s * i) * PG_PT;
     const bool partial = k0 + T * PG_PT > total;

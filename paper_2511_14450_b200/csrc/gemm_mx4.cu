@@ -62,21 +62,23 @@ int least_tiles(int M, int terms, int cap) {
   const int most = cap / terms / 8 * 8;
   return (M + most - 1) / most;
 }
-// CTAs that are on the GPU at once, one to an SM, in clusters of ks (which do not fill every group of SMs that shares a cluster's paths).
-int slots_for(int ks);
+// CTAs that are on the GPU at once, one to an SM, in clusters of ks = 1 .. 8 (which do not fill every group of SMs that shares a cluster's
+// paths); of the current device.
+const int* slots_by_ks();
 // The cheapest cut by a count of cycles.  A stage of 128 k takes the longest of: its operands' way into the SM (about 40 bytes a cycle from the
 // L2), through shared memory (written and read, the weights spread to bytes, at about 100), the MMAs (at least 45 cycles each), and
 // the weights' way from HBM (3300 bytes a cycle for all).  A CTA takes about 5000 to start and end, and its results; shares of K meet in a cluster.
 Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
   Plan best{}, p{};
   double least = 0.0;
+  const int* slots_of = slots_by_ks();
   for (int a = swiglu ? 2 : 1; a <= 2; ++a) {
     const int t0 = least_tiles(M, terms, row_cap(a));
     for (int t = t0; t <= t0 + MX_MORE_TILES; ++t) {
       if (!cut(p, M, N, terms, a, swiglu, t)) continue;
       for (int ks = 1; ks <= 8; ++ks) {
         if (ks > 1 && (ks > KB / 4 || a * p.tt * MX_ROWS * 4 > MX_MAX_DYN - 1024)) break;
-        const double ctas = (double)p.row_units * p.tiles * ks, slots = slots_for(ks), block = (double)p.block_bytes;
+        const double ctas = (double)p.row_units * p.tiles * ks, slots = slots_of[ks], block = (double)p.block_bytes;
         const double stage = fmax(fmax((a * MX_PACK_BYTES + block) / 40.0, (a * 2.0 * MX_A_BYTES + 2.0 * block) / 100.0),
                                   fmax(a * fmax(180.0, 2.0 * p.nb), a * (double)MX_PACK_BYTES * fmin(ctas, slots) / p.tiles / 3300.0));
         const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * 30.0 + (ks > 1 ? 1500.0 + a * p.tt * 40.0 : 0.0);
@@ -615,11 +617,11 @@ int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   return 1;
 }
 
-int slots_for(int ks) {
+const int* slots_by_ks() {
   static int known[64][9] = {};  // per device
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count();
-  if (known[dev][ks] == 0) {
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
+  for (int ks = 1; ks <= 8 && known[dev][ks] == 0; ++ks) {
     int n = 0;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
@@ -636,7 +638,7 @@ int slots_for(int ks) {
       n = sm_count() / ks;
     known[dev][ks] = n * ks;
   }
-  return known[dev][ks];
+  return known[dev];
 }
 
 template <int EPI, int A_TILES>
@@ -654,6 +656,19 @@ int launch_by_epi(int epi, bool dual, const CUtensorMap& map, MxArgs& p, bool ow
   }
 }
 
+// A program calls with a few sizes again and again, and weighing the cuts takes 1-2 us of the host.
+Plan known_plan(int M, int N, int KB, int terms, bool swiglu) {
+  struct Entry {
+    int M, N, KB, terms;
+    bool swiglu;
+    Plan plan;
+  };
+  static thread_local Entry table[16] = {};
+  Entry& e = table[((unsigned)M * 31u + (unsigned)N / 16u + (unsigned)KB * 7u + (unsigned)terms) % 16u];
+  if (e.M != M || e.N != N || e.KB != KB || e.terms != terms || e.swiglu != swiglu) e = Entry{M, N, KB, terms, swiglu, plan_for(M, N, KB, terms, swiglu)};
+  return e.plan;
+}
+
 }  // namespace
 
 size_t mx4_scratch_bytes(int M, int K, int terms) {
@@ -665,7 +680,7 @@ size_t mx4_scratch_bytes(int M, int K, int terms) {
 int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t* packed, int M, int N, int K, int terms, int epi,
                     void* out, int ldo, uint8_t* scratch, cudaStream_t st) {
   const bool swiglu = epi == EPI_SWIGLU_BF16, wide = epi == EPI_STORE_F32 || epi == EPI_RESID_F32;
-  const Plan t = plan_for(M, N, mx_kb(K), terms, swiglu);
+  const Plan t = known_plan(M, N, mx_kb(K), terms, swiglu);
   MxArgs p{};
   p.packed = packed; p.terms = scratch; p.block_bytes = t.block_bytes;
   p.M = M; p.N = N; p.KB = mx_kb(K); p.ldo = ldo;

@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
   }
   const int seq = sequence_of(a.cu, a.n_seqs, row, lane);
   const long long pos = (long long)a.ctx[seq] + (row - a.cu[seq]);
-  const bool kept = pos >= 0 && pos < (long long)a.table_stride * 16;
+  const bool kept = row >= a.cu[seq] && pos >= 0 && pos < (long long)a.table_stride * 16;
   const int slot = (int)(pos & 15);
   uint8_t* page = a.pool + (kept ? (size_t)a.table[(long long)seq * a.table_stride + (pos >> 4)] * 2 * a.Hkv * kv8_half_page(D) : 0);
   float cs[8];  // (cos, sin) of this lane's four pairs, the sine with the sign of its term
@@ -163,11 +163,9 @@ __global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
   }
   const int code_at = slot * D + kv8_chunk<D>(l >> 2, slot) + 4 * (l & 3);
   __syncthreads();  // the barrier is set up
-  if (!mbar_wait(bar, 0, nullptr)) {
-    if (threadIdx.x == 0) {
-      atomicCAS(a.err, 0, 35);
-      mbar_wait(bar, 0, nullptr);
-    }
+  if (!__all_sync(0xffffffffu, mbar_wait(bar, 0, nullptr))) {  // the lanes go on together, or not at all
+    if (lane == 0) atomicCAS(a.err, 0, 35);
+    if (threadIdx.x == 0) mbar_wait(bar, 0, nullptr);
     return;
   }
   const uint8_t* mine_at = wr_smem + 4 * l * SIZE;
