@@ -65,9 +65,17 @@ int least_tiles(int M, int terms, int cap) {
 // CTAs that are on the GPU at once, one to an SM, in clusters of ks = 1 .. 8 (which do not fill every group of SMs that shares a cluster's
 // paths); of the current device.
 const int* slots_by_ks();
-// The cheapest cut by a count of cycles.  A stage of 128 k takes the longest of: its operands' way into the SM (about 40 bytes a cycle from the
-// L2), through shared memory (written and read, the weights spread to bytes, at about 100), the MMAs (at least 45 cycles each), and
-// the weights' way from HBM (3300 bytes a cycle for all).  A CTA takes about 5000 to start and end, and its results; shares of K meet in a cluster.
+int tmem_columns(int a_tiles, int nb) {
+  int cols = 32;
+  while (cols < a_tiles * (nb + 4) + 8) cols <<= 1;
+  return cols;
+}
+// The cheapest cut by a count of cycles.  A stage of 128 k takes the longest of: its operands' way into the SM (about 53 bytes a cycle from the
+// L2), the ring's round trip (about 3300 for all stages that fit), the issuing warp (450, for two row tiles 700), the MMAs, and the
+// weights' way from HBM (3300 bytes a cycle for all).  A CTA takes about 5000 to start and end, and its results; shares of K meet in a cluster.
+// Measured against every cut of one or two row tiles, four token counts and one to six shares: within 5 % of the best of 512 x 5120 x 17920
+// (one row tile 50.4 us, two 54.3), 512 x 7680 x 5120 (24.5, 27.1), 600 x 4096 x 4096, 128 x 5120 x 17920 (27.7, 30.5), 64 x 7680 x 5120 of three
+// terms (14.2, 16.0), 8 x 7680 x 5120 (10.2, 9.5), 8 x 5120 x 17920 (16.1, 15.8) and eight others.
 Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
   Plan best{}, p{};
   double least = 0.0;
@@ -79,10 +87,13 @@ Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
       for (int ks = 1; ks <= 8; ++ks) {
         if (ks > 1 && (ks > KB / 4 || a * p.tt * MX_ROWS * 4 > MX_MAX_DYN - 1024)) break;
         const double ctas = (double)p.row_units * p.tiles * ks, slots = slots_of[ks], block = (double)p.block_bytes;
-        const double stage = fmax(fmax((a * MX_PACK_BYTES + block) / 40.0, (a * 2.0 * MX_A_BYTES + 2.0 * block) / 100.0),
-                                  fmax(a * fmax(180.0, 2.0 * p.nb), a * (double)MX_PACK_BYTES * fmin(ctas, slots) / p.tiles / 3300.0));
-        const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * 30.0 + (ks > 1 ? 1500.0 + a * p.tt * 40.0 : 0.0);
-        const double cost = ceil(ctas / slots) * cta;
+        const double on_sm = ctas > slots && tmem_columns(a, p.nb) <= 256 ? 2.0 : 1.0;  // CTAs of an SM (see launch_own)
+        const double ring = fmin(floor((MX_MAX_DYN / on_sm - 1024.0) / (a * (MX_A_BYTES + MX_SF_BYTES) + block)), MX_MAX_STAGES);
+        const double stage = fmax(fmax(on_sm * (a * MX_PACK_BYTES + block) / 53.0, 3300.0 / fmax(ring, 2.0)),
+                                  fmax(on_sm * fmax(a == 2 ? 700.0 : 450.0, 2.0 * a * p.nb),
+                                       a * (double)MX_PACK_BYTES * fmin(ctas, on_sm * slots) / p.tiles / 3300.0));
+        const double cta = (double)((KB + ks - 1) / ks) * stage + 5000.0 + a * p.tt * 30.0 + (ks > 1 ? 1500.0 + a * p.tt * 40.0 : a == 2 ? 1500.0 : 0.0);
+        const double cost = ceil(ctas / (on_sm * slots)) * cta;
         if (least == 0.0 || cost < least) {
           least = cost;
           best = p;
@@ -573,8 +584,7 @@ template <int EPI, int A_TILES, bool OWN>
 int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   const int rc = allow_smem<gemm_mx4_kernel<EPI, A_TILES, OWN>>(MX_MAX_DYN);
   if (rc) return rc;
-  int cols = 32;
-  while (cols < A_TILES * (p.nb + 4) + 8) cols <<= 1;
+  const int cols = tmem_columns(A_TILES, p.nb);
   p.tmem_cols = cols;
   p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (OWN ? 0 : (int)p.block_bytes) + 1023) / 1024 * 1024;
   const int own_bytes = OWN ? (p.KB + p.ksplit - 1) / p.ksplit * (int)own_place(p.block_bytes) : 0;
