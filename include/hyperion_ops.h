@@ -326,7 +326,7 @@ enum { HYP_TYPE_F32 = 0, HYP_TYPE_F16 = 1, HYP_TYPE_BF16 = 2 };
  *               2^-149, in bf16 down to 2^-133).
  *   x, out  [N, K] of `type` (HYP_TYPE_*), rows x_stride / out_stride elements apart, 16-byte aligned; strides multiples of 8 (fp32: 4)
  *   codes   uint8 [N, K / 2], 16-byte aligned;  scales uint8 [N, ceil(K / 32)]
- * K a multiple of 8, at most 2^25, N >= 1.  Errors: HYP_EINVAL, HYP_ECUDA. */
+ * K a multiple of 8, at most 2^25, 1 <= N <= 2^31 - 8.  Errors: HYP_EINVAL, HYP_ECUDA. */
 HYP_API int hyp_op_mx4_quantize(const void* x, int32_t type, int32_t N, int32_t K, int64_t x_stride, void* codes, void* scales,
                                 void* stream);
 HYP_API int hyp_op_mx4_dequantize(const void* codes, const void* scales, int32_t N, int32_t K, int32_t type, void* out,
@@ -350,7 +350,7 @@ HYP_API int hyp_op_mx4_pack(const void* codes, const void* scales, int32_t N, in
  *   out       [M, ldo], ldo >= N; HYP_EPI_RESID_F32 adds to it
  *   scratch   at least hyp_op_gemm_mx4_scratch_bytes(M, K, terms) bytes (0 on bad arguments), 128-byte aligned; needs no initialisation;
  *             calls whose kernels can overlap need one each
- * 1 <= M <= 2^26, N >= 1, K a multiple of 8, at most 2^25, terms 1 .. 3; `out` overlaps no other operand.  An activation row that holds an infinity or NaN gives
+ * 1 <= M <= 2^26, 1 <= N <= 2^31 - 8, K a multiple of 8, at most 2^25, terms 1 .. 3; `out` overlaps no other operand.  An activation row that holds an infinity or NaN gives
  * NaN, as does a weight row with a scale of 255.  Sums are formed in the same order on every run.  The first call on a device allocates one
  * word there for error reporting: make it before capturing a graph.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, matrix too large), HYP_ECUDA. */

@@ -21,8 +21,8 @@ Kv8View view(const hyp_attn_shape* s, int32_t format, int32_t n_seqs, const void
   return Kv8View{(uint8_t*)pool, table, table_stride, n_seqs, s->n_q_heads, s->n_kv_heads, s->head_dim, format};
 }
 bool type_ok(int32_t t) { return t == HYP_TYPE_F32 || t == HYP_TYPE_F16 || t == HYP_TYPE_BF16; }
-// (up to 2^25 columns: what the grids' second dimension takes)
-bool matrix_ok(int32_t N, int32_t K) { return N >= 1 && K >= 8 && K <= (1 << 25) && K % 8 == 0; }
+// (up to 2^25 columns: what the grids' second dimension takes; 2^31 - 8 rows: whole CTAs of eight count them in 31 bits)
+bool matrix_ok(int32_t N, int32_t K) { return N >= 1 && N <= 0x7ffffff8 && K >= 8 && K <= (1 << 25) && K % 8 == 0; }
 // The tensor map counts lines of 64 bytes in 31 bits.
 bool mx4_lines_ok(int32_t N, int32_t K, int halves) {
   return (long long)halves * mx_row_tiles(N) * mx_kb(K) * (MX_PACK_BYTES / 64) <= 0x7fffffffll;

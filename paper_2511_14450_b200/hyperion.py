@@ -631,6 +631,7 @@ def hyp_op_attn_decode_shared(shape3, q, kv_pages, cu_group, prefix_table, prefi
 # --------------------------------------------------------------------------------------------
 HYP_TYPE_F32, HYP_TYPE_F16, HYP_TYPE_BF16 = range(3)
 _U8 = None
+_INT_MAX = 2 ** 31 - 1
 _TYPES = {}
 
 
@@ -656,6 +657,8 @@ def _matrix(where, name, t):
     stride, one = t.stride()
     if (one != 1 and cols > 1) or (stride < cols and rows > 1):
         _refuse(where, f"{name} must have dense rows that do not overlap, not strides {t.stride()}")
+    if rows > _INT_MAX or cols > _INT_MAX:
+        _refuse(where, f"{name} {tuple(s)} has more rows or columns than an int32 counts")
     return dev, code, rows, cols, t.data_ptr(), stride if rows > 1 else (cols + 7) // 8 * 8
 
 
@@ -718,7 +721,7 @@ def hyp_op_gemm_mx4(a, w_packed, N: int, terms: int, epilogue: int, out, scratch
     dev, code, m, k, ap, as_ = _matrix(where, "a", a)
     odev, ocode, om, on, op, os_ = _matrix(where, "out", out)
     swiglu = epilogue == HYP_EPI_SWIGLU_BF16
-    if odev != dev or om != m or on < N or ocode != (code if swiglu or epilogue == HYP_EPI_STORE_BF16 else HYP_TYPE_F32):
+    if odev != dev or om != m or on < N or os_ > _INT_MAX or ocode != (code if swiglu or epilogue == HYP_EPI_STORE_BF16 else HYP_TYPE_F32):
         _refuse(where, f"out {out.dtype} {tuple(out.shape)} on {out.device} does not fit {m} rows of {N} results of epilogue {epilogue}")
     nbytes = hyp_op_mx4_packed_bytes(N, k, swiglu)
     if w_packed.dtype is not _U8 or w_packed.get_device() != dev or not w_packed.is_contiguous() or w_packed.nbytes < max(nbytes, 1):

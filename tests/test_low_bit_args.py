@@ -99,6 +99,21 @@ def test_matrix_sizes(name):
         assert call(name, **kw) == E, kw
 
 
+@pytest.mark.parametrize("name", ["hyp_op_mx4_quantize", "hyp_op_mx4_dequantize", "hyp_op_mx4_pack", "hyp_op_gemm_mx4"])
+def test_rows_that_whole_ctas_cannot_count(name):
+    assert call(name, N=2 ** 31 - 7, K=8, ldo=2 ** 31 - 1) == E if name == "hyp_op_gemm_mx4" else call(name, N=2 ** 31 - 7, K=8) == E
+
+
+def test_binding_refuses_sizes_beyond_31_bits():
+    class Wide:                                             # what the binding asks of a tensor, without its memory
+        dtype, shape, device = torch.float16, (2 ** 32 + 5, 8), "cuda:0"
+        get_device, stride, data_ptr = (lambda self: 0), (lambda self: (8, 1)), (lambda self: P)
+    refused(hyp._matrix, "here", "x", Wide())
+    Wide.shape = (2, 2 ** 31)
+    Wide.stride = lambda self: (2 ** 31, 1)
+    refused(hyp._matrix, "here", "x", Wide())
+
+
 def test_matrix_types_and_strides():
     for name in ("hyp_op_mx4_quantize", "hyp_op_mx4_dequantize"):
         for kw in (dict(type=3), dict(type=-1), dict(stride=63), dict(stride=66), dict(type=1, stride=68), dict(type=2, stride=60)):
