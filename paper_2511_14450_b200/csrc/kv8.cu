@@ -120,16 +120,18 @@ struct WriteArgs {
   int* err;
 };
 
-// grid (M, shares of the heads).  One bulk copy brings a CTA's heads of a row to shared memory while the warps look up the row's sequence, page
+// grid (M, shares of the heads); ROPE: rotates.  One bulk copy brings a CTA's heads of a row to shared memory while the warps look up the row's sequence, page
 // and angles; then D / 4 lanes take a head, four values each.
-//   Bound by HBM for prompts (4096 fp32 rows of 60 heads of 128: 179 MB in 32 us, 5.6 TB/s), by latency for single tokens (8 rows: 2.5 us).
-// Loads by the warps themselves, one head ahead, had 24 KB on their way on an SM: 46 us.
+//   Bound by HBM for prompts (4096 fp32 rows of 60 heads of 128: 179 MB in 31 us, 5.8 TB/s), by latency for single tokens (8 rows: 2.5 us).
+// Loads by the warps themselves, one head ahead, had 24 KB on their way on an SM: 46 us.  Warps hide a head's chain of steps, so registers are
+// what counts: a rotation that is decided at run time costs 7-10 % (33 us; rows that are not rotated 9.9 instead of 8.1 for 2500), a CTA that walks
+// over rows with the next one's look-ups ahead (64 registers) 55-80 %.
 //   Codes have to be those of the exact value.  Exact arithmetic on every value costs more than the memory (in fp64 76 us for 4096 rows of 60
 // heads, issue slots 84 % busy), so values are rotated and rounded in fp32, and fp64, in which products of fp32 numbers are exact, is
 // used for the largest value of a row and where a code hangs on the rotation's roundings.  Those are two of half a step each, of a term and of
 // the sum; as both members of the row's pairs are kept, neither exceeds 1.42 times the row's largest magnitude: 2^-22 of it covers them.
-template <int D, int FMT, int TYPE>
-__global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
+template <int D, int FMT, int TYPE, bool ROPE>
+__global__ void __launch_bounds__(256, ROPE ? 6 : 8) kv8_write_kernel(const WriteArgs a) {
   constexpr int LANES = D / 4, PER = 32 / LANES, SIZE = TYPE == HYP_TYPE_F32 ? 4 : 2;
   extern __shared__ __align__(128) uint8_t wr_smem[];
   __shared__ uint64_t bar_word;
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
   const int slot = (int)(pos & 15);
   uint8_t* page = a.pool + (kept ? (size_t)a.table[(long long)seq * a.table_stride + (pos >> 4)] * 2 * a.Hkv * kv8_half_page(D) : 0);
   float cs[8];  // (cos, sin) of this lane's four pairs, the sine with the sign of its term
-  if (a.rope) {
+  if (ROPE) {
     const long long at = min(max(pos, 0ll), (long long)a.rope_positions - 1);
     const float4* t = reinterpret_cast<const float4*>(a.rope + (at * (D / 2) + 4 * (l % (LANES / 2))) * 2);
     const float4 t0 = t[0], t1 = t[1];
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(256, 6) kv8_write_kernel(const WriteArgs a) {
   for (int h0 = h_lo + warp * PER; h0 < h_hi; h0 += 8 * PER) {  // the warp's lanes stay together
     const int head = h0 + sub;
     const bool in = head < h_hi;
-    const bool any_turn = a.rope && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
+    const bool any_turn = ROPE && h0 < a.Hq + a.Hkv, turn = any_turn && head < a.Hq + a.Hkv;
     float v[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};  // own values and the other members of their pairs, D / 2 away
     if (in) load4<TYPE>(mine_at + (head - h_lo) * (D * SIZE), v);
     if (turn && in) load4<TYPE>(mine_at + (head - h_lo) * (D * SIZE) + other, o);
@@ -297,7 +299,9 @@ int write_go(WriteArgs a, cudaStream_t st) {
   if (y < least) y = least;
   a.per = ((heads + y - 1) / y + PER - 1) / PER * PER;
   y = (heads + a.per - 1) / a.per;
-  HYP_CUDA_TRY(launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE>, dim3((unsigned)a.M, (unsigned)y), dim3(256), (size_t)a.per * HEAD, st, a));
+  const dim3 grid((unsigned)a.M, (unsigned)y);
+  HYP_CUDA_TRY((a.rope ? launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE, true>, grid, dim3(256), (size_t)a.per * HEAD, st, a)
+                       : launch_pdl<2>(kv8_write_kernel<D, FMT, TYPE, false>, grid, dim3(256), (size_t)a.per * HEAD, st, a)));
   return 1;
 }
 template <int D, int FMT>
