@@ -18,8 +18,8 @@
 //   warps 2-9  epilogue, lane = weight row.
 // Few tokens: bound by the weights' way: from HBM for large matrices (32 rows, gate and up 17920 x 5120: 98 MB in 16 us of main loop, 23.4 us in
 // all), through shared memory, where the spread weights are written and read at twice their size, for small ones (8 rows, 7680 x 5120:
-// 9.6 us, 5 of them launches, terms, start and end).  Many tokens: by the operands' way from the L2 (512 x 5120 x 17920, one term: 54 us =
-// 1.75 PFLOP/s, tensor pipe 60 % busy; 2048 x 7680 x 5120: 85 us = 1.9).
+// 9.6 us, 5 of them launches, terms, start and end).  Many tokens: by the operands' way from the L2 (512 x 5120 x 17920, one term: 51 us =
+// 1.85 PFLOP/s, tensor pipe 62 % busy during the product; 2048 x 7680 x 5120: 82 us = 1.97; 2048 x 5120 x 17920: 170 us = 2.2).
 // Every mbarrier wait is bounded; the cluster barriers are reached by every thread of every CTA.
 #include <cuda.h>
 #include <math.h>
@@ -108,20 +108,34 @@ Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
 // ---------------------------------------------------------------------------------------------
 // activations to terms: four lanes take a block of 32 k of one token, eight values each
 // ---------------------------------------------------------------------------------------------
-// U chunks at a time; calls put(chunk, term, codes, scale).  Every lane of the warp calls this.  Bound by issue slots where there are many, so
-// the power of two is formed from the bits: 0x1fffff more carries into the exponent exactly where the mantissa passes 1.75 (448 = 1.75 * 2^8).
+// The largest magnitude of a block's 32 values, as fp32 bits, from the 16-bit values of its four lanes, two at a time.
+__device__ __forceinline__ uint32_t block_top(uint4 raw, bool f16) {
+  constexpr uint32_t ABS = 0x7fff7fffu;
+  uint32_t m = __vmaxu2(__vmaxu2(raw.x & ABS, raw.y & ABS), __vmaxu2(raw.z & ABS, raw.w & ABS));
+  m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  m = max(m & 0xffffu, m >> 16);
+  return f16 ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))) : m << 16;
+}
+// U chunks at a time, their blocks' largest magnitudes in `tops`; calls put(chunk, term, codes, scale).  Every lane of the warp calls this.  Issue
+// slots count where there are many (108 instructions a chunk; with fp32 maxima and a loop over the terms 205: 128 rows of two terms 17.3 instead of 16.6 us
+// in all), so the power of two is formed from the bits: 0x1fffff more carries into the exponent exactly where the mantissa passes 1.75 (448 = 1.75 * 2^8).
 template <int U, typename Put>
-__device__ __forceinline__ void make_terms(float (&v)[U][8], int terms, Put put) {
+__device__ __forceinline__ void make_terms(float (&v)[U][8], const uint32_t (&tops)[U], int terms, Put put) {
   bool bad[U];
 #pragma unroll
-  for (int j = 0; j < U; ++j) bad[j] = false;
-  for (int t = 0; t < terms; ++t) {
+  for (int j = 0; j < U; ++j) bad[j] = tops[j] >= 0x7f800000u;
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    if (t >= terms) break;
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      uint32_t top = __float_as_uint(absmax_nan(v[j]));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      bad[j] = bad[j] || top >= 0x7f800000u;
+      uint32_t top = tops[j];
+      if (t > 0) {
+        top = __float_as_uint(absmax_nan(v[j]));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      }
       const int byte = max((int)((top + 0x1fffffu) >> 23) - 8, 0);  // exponent + 127 of the least power of two p with top <= 448 p
       const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
       uint32_t w[2];
@@ -149,27 +163,27 @@ __device__ __forceinline__ uint32_t term_scale_at(int nb, int r, int c) {
 }
 
 constexpr int TERM_THREADS = 128;
-// grid (M, segments of 128 U chunks of eight values)
-template <int TYPE, int U>
-__global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int K8, int KB, int terms,
-                                                                int tt, int nb, size_t block_bytes, uint8_t* __restrict__ out) {
+// grid (M, segments of 128 U chunks of eight values).  512 x 17920, one term: 8 us of the product's 51 (9.6 on cold caches: read 18 MB, write 9).
+template <int TYPE, int U, int TERMS>
+__global__ void __launch_bounds__(TERM_THREADS) mx_terms_kernel(const uint8_t* __restrict__ a, long long stride, int K8, int KB, int tt,
+                                                                int nb, size_t block_bytes, uint8_t* __restrict__ out) {
   const int m = blockIdx.x, c0 = blockIdx.y * (TERM_THREADS * U) + threadIdx.x;
-  float v[U][8];
+  uint4 raw[U];
   pdl_wait();
   pdl_trigger();
+  const uint4* src = reinterpret_cast<const uint4*>(a + m * stride * 2) + c0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) raw[u] = c0 + u * TERM_THREADS < K8 ? src[u * TERM_THREADS] : make_uint4(0u, 0u, 0u, 0u);
+  float v[U][8];
+  uint32_t tops[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int c = c0 + u * TERM_THREADS;
-    if (c < K8) {
-      load8<TYPE>(a + (m * stride + 8ll * c) * 2, v[u]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
-    }
+    unpack8(raw[u], TYPE == HYP_TYPE_F16, v[u]);
+    tops[u] = block_top(raw[u], TYPE == HYP_TYPE_F16);
   }
   const int tile = m / tt, row = m - tile * tt;
   uint8_t* blk0 = out + (size_t)tile * KB * block_bytes;
-  make_terms<U>(v, terms, [&](int u, int t, uint2 codes, uint8_t scale) {
+  make_terms<U>(v, tops, TERMS, [&](int u, int t, uint2 codes, uint8_t scale) {
     const int c = c0 + u * TERM_THREADS;
     if (c >= 16 * KB) return;
     const int r = t * tt + row;
@@ -286,10 +300,11 @@ __device__ __forceinline__ void own_terms(const MxArgs& p, uint8_t* to, int kb0,
   for (int i = t; i < all; i += STEP) {
     float v[1][8];
     unpack8(raw, p.f16, v[0]);
+    const uint32_t tops[1] = {block_top(raw, p.f16)};
     raw = fetch(i + STEP);
     const int c = i & 15, row = (i >> 4) % p.tt;
     uint8_t* blk = to + (i >> 4) / p.tt * own_place(p.block_bytes);
-    make_terms<1>(v, p.n_terms, [&](int, int term, uint2 codes, uint8_t scale) {
+    make_terms<1>(v, tops, p.n_terms, [&](int, int term, uint2 codes, uint8_t scale) {
       const int r = term * p.tt + row;
       *reinterpret_cast<uint2*>(blk + term_at(r, c)) = codes;
       if ((c & 3) == 0) blk[term_scale_at(p.nb, r, c)] = scale;
@@ -713,16 +728,17 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
     return launch_by_epi(epi, t.a_tiles == 2, map, p, true, st);
   }
   const long long chunks = 16ll * p.KB;  // of a row: its segments fit the grid (K is at most 2^25)
-  const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs
+  const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs (512 x 5120 x 17920 51 us, one chunk 55, four 51; 128 rows 28, 29, 31)
   const long long segments = (chunks + TERM_THREADS * (many ? 2 : 1) - 1) / (TERM_THREADS * (many ? 2 : 1));
   auto go = [&](auto kernel) {
     return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, K / 8, p.KB,
-                         terms, t.tt, t.nb, t.block_bytes, scratch);
+                         t.tt, t.nb, t.block_bytes, scratch);
   };
-  if (a_type == HYP_TYPE_F16)
-    HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_F16, 2>) : go(mx_terms_kernel<HYP_TYPE_F16, 1>)));
-  else
-    HYP_CUDA_TRY((many ? go(mx_terms_kernel<HYP_TYPE_BF16, 2>) : go(mx_terms_kernel<HYP_TYPE_BF16, 1>)));
+  auto by_chunks = [&](auto two, auto one) { return many ? go(two) : go(one); };
+#define HYP_F(T, N) \
+  if (a_type == T && terms == N) HYP_CUDA_TRY(by_chunks(mx_terms_kernel<T, 2, N>, mx_terms_kernel<T, 1, N>));
+  HYP_F(HYP_TYPE_F16, 1) HYP_F(HYP_TYPE_F16, 2) HYP_F(HYP_TYPE_F16, 3) HYP_F(HYP_TYPE_BF16, 1) HYP_F(HYP_TYPE_BF16, 2) HYP_F(HYP_TYPE_BF16, 3)
+#undef HYP_F
   rc = launch_by_epi(epi, t.a_tiles == 2, map, p, false, st);
   return rc < 0 ? rc : rc + 1;
 }
