@@ -122,9 +122,9 @@ struct WriteArgs {
 
 // grid (M, shares of the heads); ROPE: rotates.  One bulk copy brings a CTA's heads of a row to shared memory while the warps look up the row's sequence, page
 // and angles; then D / 4 lanes take a head, four values each.
-//   Bound by HBM for prompts (4096 fp32 rows of 60 heads of 128: 179 MB in 31 us, 5.8 TB/s), by latency for single tokens (8 rows: 2.5 us).
+//   Bound by HBM for prompts (4096 fp32 rows of 60 heads of 128: 179 MB in 31-32 us, 5.6-5.8 TB/s), by latency for single tokens (8 rows: 2.5 us).
 // Loads by the warps themselves, one head ahead, had 24 KB on their way on an SM: 46 us.  Warps hide a head's chain of steps, so registers are
-// what counts: a rotation that is decided at run time costs 7-10 % (33 us; rows that are not rotated 9.9 instead of 8.1 for 2500), a CTA that walks
+// what counts: a rotation that is decided at run time costs 7-10 % (34 us; rows that are not rotated 9.9 instead of 8.1 for 2500), a CTA that walks
 // over rows with the next one's look-ups ahead (64 registers) 55-80 %.
 //   Codes have to be those of the exact value.  Exact arithmetic on every value costs more than the memory (in fp64 76 us for 4096 rows of 60
 // heads, issue slots 84 % busy), so values are rotated and rounded in fp32, and fp64, in which products of fp32 numbers are exact, is
