@@ -44,7 +44,7 @@ struct Plan {
   size_t block_bytes;  // terms of one (token tile, 128 k) with their scales
 };
 constexpr int MX_MAX_DYN = 216 * 1024, MX_MORE_TILES = 3;
-constexpr int OWN_CHUNKS = 2, OWN_BYTES = 64 * 1024;  // see launch_gemm_mx4
+constexpr int OWN_TERMS = 4, OWN_BYTES = 64 * 1024;  // see launch_gemm_mx4
 // Tensor memory: one accumulator of 256 columns beside the scales, or two of 240.
 int row_cap(int a_tiles) { return a_tiles == 2 ? 240 : 256; }
 bool cut(Plan& p, int M, int N, int terms, int a_tiles, bool swiglu, int tiles) {
@@ -291,20 +291,21 @@ __device__ __forceinline__ void mx_store(const MxArgs& p, int m, int n, float4 y
 // one's values on their way.
 __device__ __forceinline__ void own_terms(const MxArgs& p, uint8_t* to, int kb0, int n_kb, int m0, int mt, int t) {
   constexpr int STEP = 32 * MX_EPI_WARPS;
-  const int all = 16 * p.tt * n_kb;  // a multiple of 128: whole warps, blocks of four lanes
+  const int all = 16 * mt * n_kb;  // blocks of four lanes; rows behind the last token hold anything, their columns are not read
   auto fetch = [&](int i) {
-    const int c = i & 15, row = (i >> 4) % p.tt, ck = 16 * (kb0 + (i >> 4) / p.tt) + c;
-    return i < all && row < mt && ck < p.K8 ? *reinterpret_cast<const uint4*>(p.act + ((long long)(m0 + row) * p.act_stride + 8ll * ck) * 2) : make_uint4(0, 0, 0, 0);
+    const int c = i & 15, row = (i >> 4) % mt, ck = 16 * (kb0 + (i >> 4) / mt) + c;
+    return i < all && ck < p.K8 ? *reinterpret_cast<const uint4*>(p.act + ((long long)(m0 + row) * p.act_stride + 8ll * ck) * 2) : make_uint4(0, 0, 0, 0);
   };
   uint4 raw = fetch(t);
-  for (int i = t; i < all; i += STEP) {
+  for (int i = t; (i & ~31) < all; i += STEP) {  // the warp's lanes stay together
     float v[1][8];
     unpack8(raw, p.f16, v[0]);
     const uint32_t tops[1] = {block_top(raw, p.f16)};
     raw = fetch(i + STEP);
-    const int c = i & 15, row = (i >> 4) % p.tt;
-    uint8_t* blk = to + (i >> 4) / p.tt * own_place(p.block_bytes);
+    const int c = i & 15, row = (i >> 4) % mt;
+    uint8_t* blk = to + (i >> 4) / mt * own_place(p.block_bytes);
     make_terms<1>(v, tops, p.n_terms, [&](int, int term, uint2 codes, uint8_t scale) {
+      if (i >= all) return;
       const int r = term * p.tt + row;
       *reinterpret_cast<uint2*>(blk + term_at(r, c)) = codes;
       if ((c & 3) == 0) blk[term_scale_at(p.nb, r, c)] = scale;
@@ -718,10 +719,12 @@ int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(swiglu ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
-  // Up to OWN_CHUNKS chunks a thread the CTAs make their terms themselves (one token, 512 x 256: 3.7 instead of 4.8 us); a chunk of three terms takes
-  // a warp about 0.9 us, so with three chunks and more a launch of their own is faster (6144 x 4096: 8.0 instead of 9.4 us).
+  // Up to OWN_TERMS terms a thread (of a chunk each) the CTAs make their terms themselves (one token, 512 x 256 of three: 3.6 instead of 4.4 us, 7680 x 5120
+  // 8.9, 9.3; three tokens, 1000 x 2000 of two: 4.8, 5.7); with more, a launch of their own is faster (two tokens, 7680 x 5120 of three: 9.3
+  // instead of 9.6).
   const int share = (p.KB + p.ksplit - 1) / p.ksplit;
-  const bool own = t.tiles == 1 && 16ll * t.tt * share <= OWN_CHUNKS * 32 * MX_EPI_WARPS && share * (long long)own_place(t.block_bytes) <= OWN_BYTES &&
+  const int own_threads = 32 * MX_EPI_WARPS;
+  const bool own = t.tiles == 1 && (16ll * M * share + own_threads - 1) / own_threads * terms <= OWN_TERMS && share * (long long)own_place(t.block_bytes) <= OWN_BYTES &&
                    (long long)t.row_units * t.ksplit <= sm_count();
   if (own) {
     p.act = (const uint8_t*)a; p.act_stride = a_stride; p.K8 = K / 8;
