@@ -183,6 +183,22 @@ def test_product(m, n, k, dtype, terms):
         assert (err <= bound + rest).all(), float((err / bound).max())
 
 
+@pytest.mark.parametrize("n,k", [(1000, 2000), (130, 5120), (700, 4104), (96, 40)])
+@pytest.mark.parametrize("m,dtype,terms", [(1, torch.float16, 3), (1, torch.bfloat16, 2), (2, torch.float16, 2), (3, torch.bfloat16, 1),
+                                           (5, torch.float16, 3), (7, torch.bfloat16, 2)])
+def test_product_of_few_tokens(n, k, m, dtype, terms):
+    """Fewer tokens than a tile has places for, behind a product that left NaN wherever it kept its operands."""
+    codes, scales = weights(n, k, seed=n)
+    product(torch.full((8, k), math.nan, dtype=dtype, device="cuda"), codes, scales, n, 3, hyp.HYP_EPI_STORE_F32, torch.empty(8, n, device="cuda"))
+    a = normal(m, k, seed=m + k).to(dtype)
+    out = torch.full((m + 1, n), 9.0, device="cuda")
+    product(a, codes, scales, n, terms, hyp.HYP_EPI_STORE_F32, out[:m])
+    ok()
+    w, held = values(codes, scales, k), in_terms(a, terms)
+    assert ((out[:m].double() - held @ w.T).abs() <= product_bound(held, w, k)).all()
+    assert (out[m:] == 9.0).all()
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 100, 64), (8, 688, 256), (33, 200, 688), (129, 136, 520), (500, 130, 256)])
 @pytest.mark.parametrize("dtype,terms", [(torch.float16, 3), (torch.bfloat16, 1)])
 def test_product_epilogues(m, n, k, dtype, terms):
