@@ -8,7 +8,8 @@
 //   1024 and one packed subtraction, E4M3 by the hardware conversion; both exact.  The order of the dimensions inside a product is that
 //   in which a lane reads 16 bytes of a key's row; the queries are fetched in the same order.
 //   A key's scale multiplies its score in fp32.  A value's scale goes into its weight: w = p * scale * 2^(m - m2), with references m for
-//   the scores and m2 for score + log2(scale), so that the fp16 weights are relative to the largest one, whatever the scales are.
+//   the scores and m2 for score + log2(scale), so that the fp16 weights are relative to the largest one, whatever the scales are.  What is kept
+//   is m2 - m: beside a score of 1e9 and more m2 itself would have lost log2(scale) to rounding.
 //   Both references move only when a weight outgrows 2^8 (one vote a step instead of shuffles and a rescaled O).
 // A warp takes two pages a step: their chains of products run side by side (8 x 1024 tokens 9.9 -> 8.7 us).
 // Weights are rounded to fp16 (2^-11 of each); sums, references and O are fp32.  Bound by HBM: 4 x 32768 tokens of 10 KV heads of 128 5.7 TB/s
@@ -27,6 +28,9 @@ constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32;
 constexpr int K8_STEP = 2, K8_SLOTS = 2;    // pages that a warp takes at a time; ring slots of that many
 constexpr int K8_PER_SM = 3, K8_WAVES = 5;  // resident CTAs; waves that a long context is cut for
 constexpr float K8_GROWN = 256.f;
+// "No key seen yet".  A key's fp32 scale takes scores down to -FLT_MAX, so nothing finite is below every one of them; at the bottom itself a
+// reference that has not moved is as good as one that has.
+constexpr float K8_NONE = -3.402823466e38f;
 
 struct Kv8Args {
   const __half* q;  // row b at q + b * q_stride
@@ -125,7 +129,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   const int fair = max(a.wave_splits, (n_pages + 15) / 16);
   const int used = n_pages > 64 * a.wave_splits ? n_splits : max(min(min(n_splits, fair), (n_steps + K8_WARPS - 1) / K8_WARPS), 1);
   if (!CLUSTER && split >= used) {
-    if (tid < G) *reinterpret_cast<float2*>(a.ml + (((size_t)b * a.Hq + kvh * G + tid) * a.n_slots + split) * 2) = make_float2(PG_NEG, 0.f);
+    if (tid < G) *reinterpret_cast<float2*>(a.ml + (((size_t)b * a.Hq + kvh * G + tid) * a.n_slots + split) * 2) = make_float2(K8_NONE, 0.f);
     return;
   }
   const int first = split + used * warp, stride_s = used * K8_WARPS;
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   float o[KS][4];  // 16-byte chunk c of the head: (dims 16c + 2g, + 1) x (heads 2tq, 2tq + 1)
 #pragma unroll
   for (int c = 0; c < KS; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
-  float m[2] = {PG_NEG, PG_NEG}, m2[2] = {PG_NEG, PG_NEG}, f[2] = {1.f, 1.f}, l[2] = {0.f, 0.f};  // of heads 2tq, 2tq + 1
+  float m[2] = {K8_NONE, K8_NONE}, d2[2] = {0.f, 0.f}, f[2] = {1.f, 1.f}, l[2] = {0.f, 0.f};  // of heads 2tq, 2tq + 1; d2 = m2 - m, f = 2^-d2
 
   bool ok = true;
   int slot = 0;
@@ -248,24 +252,24 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
       float corr2[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = m[h], top2 = m2[h];
+        float top = m[h];
+#pragma unroll
+        for (int t = 0; t < T; ++t) top = fmaxf(top, fmaxf(v[t][h], v[t][2 + h]));
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float down = m[h] - top;  // (may leave fp32 to -infinity: the old sums are nothing then)
+        float d = down + d2[h];
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {  // (values whose scale is below 2^-64 are zeros in fp16)
-            top = fmaxf(top, v[t][2 * k + h]);
-            top2 = fmaxf(top2, v[t][2 * k + h] + fmaxf(lg2_approx(vs[t][k]), -64.f));
-          }
+          for (int k = 0; k < 2; ++k) d = fmaxf(d, v[t][2 * k + h] - top + fmaxf(lg2_approx(vs[t][k]), -64.f));  // (values whose scale is below 2^-64 are zeros in fp16)
 #pragma unroll
-        for (int x = 4; x < 32; x <<= 1) {
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-          top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
-        }
-        l[h] *= ex2_approx(m[h] - top);
-        corr2[h] = ex2_approx(m2[h] - top2);
+        for (int x = 4; x < 32; x <<= 1) d = fmaxf(d, __shfl_xor_sync(0xffffffffu, d, x));
+        l[h] *= ex2_approx(down);
+        corr2[h] = ex2_approx(down + d2[h] - d);
         m[h] = top;
-        m2[h] = top2;
-        f[h] = ex2_approx(top - top2);
+        d2[h] = d;
+        f[h] = ex2_approx(-d);
       }
 #pragma unroll
       for (int c = 0; c < KS; ++c) {
@@ -312,7 +316,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
-    const float back = ex2_approx(m2[h] - m[h]);  // O in units of 2^m
+    const float back = ex2_approx(d2[h]);  // O in units of 2^m
     const int head = 2 * tq + h;
     if (head < G) {
       if (g == 0) {
@@ -327,7 +331,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
   __syncthreads();
   for (int e = tid; e < G * D; e += K8_THREADS) {
     const int gq = e / D, dd = e % D;
-    float mx = PG_NEG;
+    float mx = K8_NONE;
 #pragma unroll
     for (int w = 0; w < K8_WARPS; ++w) mx = fmaxf(mx, sm_m[w * 8 + gq]);
     float lsum = 0.f, acc = 0.f;
@@ -367,7 +371,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
       float ov[8];
 #pragma unroll
       for (int sp = 0; sp < 8; ++sp) ov[sp] = sp < n_splits ? ld_cluster_f32(smem_u32(ex_o + e), sp) : 0.f;
-      float mx = PG_NEG, lsum = 0.f, acc = 0.f;
+      float mx = K8_NONE, lsum = 0.f, acc = 0.f;
 #pragma unroll
       for (int sp = 0; sp < 8; ++sp)
         if (sp < n_splits) mx = fmaxf(mx, all_m[gq * 8 + sp]);
@@ -399,7 +403,7 @@ __global__ void __launch_bounds__(K8_THREADS) kv8_merge_kernel(const float* __re
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int s = lane + 32 * k;
-    const float2 x = s < n_slots ? *reinterpret_cast<const float2*>(ml + (row0 + s) * 2) : make_float2(PG_NEG, 0.f);
+    const float2 x = s < n_slots ? *reinterpret_cast<const float2*>(ml + (row0 + s) * 2) : make_float2(K8_NONE, 0.f);
     m[k] = x.x;
     l[k] = x.y;
   }
@@ -473,7 +477,7 @@ __global__ void __launch_bounds__(K8_THREADS) kv8_merge_few_kernel(const float* 
       r[i][0] = y.x; r[i][1] = y.y;
     }
   }
-  float mx = PG_NEG, sum = 0.f, v[V];
+  float mx = K8_NONE, sum = 0.f, v[V];
 #pragma unroll
   for (int i = 0; i < K8_FEW; ++i) mx = fmaxf(mx, x[i].x);
 #pragma unroll

@@ -1,0 +1,69 @@
+"""Operators in few bits at the edges of what they are documented for, against definitions in 64 bits.  Tolerances: those derived in
+test_gpu_low_bit.py, or given beside the test."""
+import math
+
+import pytest
+import torch
+
+from paper_2511_14450_b200 import hyperion as hyp
+from tests import test_gpu_low_bit as low
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = low.FORMATS
+i32, normal, ok = low.i32, low.normal, low.ok
+
+
+def cache8(x, fmt, extra=0):
+    """Pool, table and the held values (fp64) of one sequence of rows x [tokens, 2, n_kv_heads, D]; a page that nobody owns lies in front,
+    slots behind the end hold NaN."""
+    l, _, hkv, d = x.shape
+    pages = (l + 15) // 16
+    codes, scales = low.quantized8(x.double(), fmt)
+    held = low.numbers(codes, fmt) * scales.double()[..., None]
+    c = torch.full((pages * 16, 2, hkv, d), 0xFF, dtype=torch.uint8, device="cuda")
+    s = torch.full((pages * 16, 2, hkv), math.nan, device="cuda")
+    c[:l], s[:l] = codes, scales
+    c, s = c.view(pages, 16, 2, hkv, d).permute(0, 2, 3, 1, 4), s.view(pages, 16, 2, hkv).permute(0, 2, 3, 1)
+    pool = torch.full((pages + 1, 2, hkv, 16 * d + 64), 0xFF, dtype=torch.uint8, device="cuda")
+    pool[1:] = low.half_page(c.contiguous(), s.contiguous(), d)
+    table = torch.cat([torch.arange(1, pages + 1, device="cuda"), torch.zeros(extra, device="cuda")]).to(torch.int32).view(1, -1)
+    return pool, table, held
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("size", [1e28, 1e31, 2.0 ** 100, 1e35])
+@pytest.mark.parametrize("heads,l,extra", [((4, 2, 64), 1, 0), ((8, 1, 128), 17, 0), ((8, 2, 128), 700, 0), ((4, 1, 64), 5000, 0), ((2, 2, 64), 40, 300),
+                                           ((2, 2, 64), 9000, 0)])
+def test_attention_over_very_negative_scores(fmt, size, heads, l, extra):
+    """Keys whose scores lie far below what fp16 keys could give, all of them alike: the result is the values' mean, whatever the scales of the
+    values (up to 2^6 apart both ways).  One launch, a cluster's join and a join of its own."""
+    hq, hkv, d = heads
+    x = normal(l, 2, hkv, d, seed=l)
+    x[:, 0] = -(normal(1, hkv, d, seed=1).abs() + 0.5) * size
+    x[:, 1] *= torch.exp2(torch.randint(-6, 7, (l, hkv, 1), generator=low.gen(2), device="cuda").float())
+    pool, table, held = cache8(x, fmt, extra)
+    q = (normal(1, hq * d, seed=3).abs() + 0.1).half() / 64
+    out = low.attend(heads, fmt, q, pool, table, i32([l - 1]))[0].double().view(hq, d)
+    v = held[:, 1].repeat_interleave(hq // hkv, 1)
+    want, mean = v.mean(0), v.abs().mean(0)
+    # equal weights: half a step of each and of the result; weights below fp16's normal range as in test_gpu_low_bit.attention
+    bound = 2.0 ** -11 * (want.abs() + mean) * 1.01 + 2.0 ** -18 * mean + 2.0 ** -25 * 4 * v.abs().amax((0, 2)).view(hq, 1) + 2.0 ** -25
+    assert (out.abs().amax() > 0) and ((out - want).abs() <= bound).all(), float(((out - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("l,at", [(3, 1), (300, 299), (4000, 1777)])
+def test_attention_largest_of_very_negative_scores(fmt, l, at):
+    """Scores of -1e33 but for one of about -1e29: that key has all of the weight, also where its value is small beside the others'."""
+    heads = (8, 2, 128)
+    hq, hkv, d = heads
+    x = normal(l, 2, hkv, d, seed=l)
+    x[:, 0] = -(normal(1, hkv, d, seed=1).abs() + 0.5) * 1e33
+    x[at, 0] *= 1e-4
+    x[at, 1] *= 2.0 ** -9
+    pool, table, held = cache8(x, fmt)
+    q = (normal(1, hq * d, seed=3).abs() + 0.1).half()
+    out = low.attend(heads, fmt, q, pool, table, i32([l - 1]))[0].double().view(hq, d)
+    want = held[at, 1].repeat_interleave(hq // hkv, 0)
+    assert ((out - want).abs() <= 2.0 ** -10 * 1.01 * want.abs() + 2.0 ** -25).all()
