@@ -10,9 +10,9 @@
 //   A key's scale multiplies its score in fp32.  A value's scale goes into its weight: w = p * scale * 2^(m - m2), with references m for
 //   the scores and m2 for score + log2(scale), so that the fp16 weights are relative to the largest one, whatever the scales are.  What is kept
 //   is m2 - m: beside a score of 1e9 and more m2 itself would have lost log2(scale) to rounding.
-//   Both references move only when a weight outgrows 2^8 (one vote a step instead of shuffles and a rescaled O).
+//   Both references move only when a weight outgrows 2^15 (one vote a step instead of shuffles and a rescaled O).
 // A warp takes two pages a step: their chains of products run side by side (8 x 1024 tokens 9.9 -> 8.7 us).
-// Weights are rounded to fp16 (2^-11 of each); sums, references and O are fp32.  Bound by HBM: 4 x 32768 tokens of 10 KV heads of 128 5.7 TB/s
+// Weights are rounded to fp16 (2^-11 of each, or 2^-32 of the warp's largest so far); sums, references and O are fp32.  Bound by HBM: 4 x 32768 tokens of 10 KV heads of 128 5.7 TB/s
 // of cache, where the same copies without the arithmetic reach 5.8; 64 ragged sequences of up to 8192 5.6 (6.0); 8 x 1024 one wave of
 // latencies, 8.7 us (6.4).  Neither more CTAs (six of 80 registers) nor the conversions taken out changed the long ones.
 #include "attn_paged.cuh"
@@ -27,7 +27,10 @@ namespace {
 constexpr int K8_WARPS = 4, K8_THREADS = K8_WARPS * 32;
 constexpr int K8_STEP = 2, K8_SLOTS = 2;    // pages that a warp takes at a time; ring slots of that many
 constexpr int K8_PER_SM = 3, K8_WAVES = 5;  // resident CTAs; waves that a long context is cut for
-constexpr float K8_GROWN = 256.f;
+// The value reference moves so that the largest weight times scale is 2^K8_HEAD, and a weight may grow to 2^15 (fp16 ends at 2^16) before it moves again:
+// what lies 2^21 below the largest is still a normal fp16 number and steps of 2^-31 of it are left below that.  With the largest at 1 a million small weights beside a
+// large one could lose, or count twice, 3 % of the result.
+constexpr float K8_HEAD = 7.f, K8_GROWN = 32768.f;
 // "No key seen yet".  A key's fp32 scale takes scores down to -FLT_MAX, so nothing finite is below every one of them; at the bottom itself a
 // reference that has not moved is as good as one that has.
 constexpr float K8_NONE = -3.402823466e38f;
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(K8_THREADS, K8_PER_SM) attn_kv8_kernel(const K
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) d = fmaxf(d, v[t][2 * k + h] - top + fmaxf(lg2_approx(vs[t][k]), -64.f));  // (values whose scale is below 2^-64 are zeros in fp16)
+          for (int k = 0; k < 2; ++k) d = fmaxf(d, v[t][2 * k + h] - top + (fmaxf(lg2_approx(vs[t][k]), -64.f) - K8_HEAD));  // (values whose scale is below 2^-64 are zeros in fp16)
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) d = fmaxf(d, __shfl_xor_sync(0xffffffffu, d, x));
         l[h] *= ex2_approx(down);

@@ -67,3 +67,25 @@ def test_attention_largest_of_very_negative_scores(fmt, l, at):
     out = low.attend(heads, fmt, q, pool, table, i32([l - 1]))[0].double().view(hq, d)
     want = held[at, 1].repeat_interleave(hq // hkv, 0)
     assert ((out - want).abs() <= 2.0 ** -10 * 1.01 * want.abs() + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("fmt,key", [(hyp.HYP_KV8_INT8, -144.0), (hyp.HYP_KV8_E4M3, -144.0), (hyp.HYP_KV8_INT8, -136.0)])
+def test_attention_many_small_weights_beside_a_large_one(fmt, key):
+    """40000 keys a warp with weights of e^-18 (or e^-17) beside one of 1: just below (or above) 2^-25 of the largest.  Their values sit in a
+    dimension of their own, so that what they lose is seen.  No term of the bound grows with the length."""
+    heads, n, pages = (8, 8, 64), 300, 10000
+    x = torch.zeros(32, 2, 8, 64, device="cuda")
+    x[:, 0, :, 0], x[:, 1, :, 1] = key, 1.0
+    x[0, 0], x[0, 1] = 0.0, 0.0
+    x[0, 1, :, 0] = 1.0
+    pool, two, held = cache8(x, fmt)                                     # a page with the large key in front, one without
+    table = two[:, 1:].expand(n, pages).contiguous()
+    table[:, 0:8:2] = two[0, 0]                                          # one of each warp's
+    q = torch.zeros(n, 8, 64, device="cuda", dtype=torch.float16)
+    q[:, :, 0] = 1.0
+    out = low.attend(heads, fmt, q.view(n, -1), pool, table, i32([16 * pages - 1] * n)).double().view(n, 8, 64)
+    small = math.exp(float(held[1, 0, 0, 0]) / 8) * (16 * pages - 4)
+    want = torch.zeros(64, dtype=torch.float64, device="cuda")
+    want[0], want[1] = 4 / (4 + small), small / (4 + small)
+    assert float(want[1]) > 2.0 ** -11
+    assert ((out - want).abs() <= 2.0 ** -10 * 1.01 * want + 2.0 ** -15).all(), float((out - want).abs().max())
