@@ -593,7 +593,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-EncodeTiledFn encode_fn() {
+EncodeTiledFn driver_encode() {
   static EncodeTiledFn fn = nullptr;
   if (!fn) {
     void* p = nullptr;
@@ -604,6 +604,18 @@ EncodeTiledFn encode_fn() {
   }
   return fn;
 }
+
+// The driver's call wants a context, and a thread whose first CUDA work this is has none yet: cudaSetDevice gives it the device's own.
+CUresult encode_in_context(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+                           const cuuint32_t* box, const cuuint32_t* estr, CUtensorMapInterleave interleave, CUtensorMapSwizzle swizzle,
+                           CUtensorMapL2promotion l2, CUtensorMapFloatOOBfill fill) {
+  CUresult r = driver_encode()(map, type, rank, base, dims, strides, box, estr, interleave, swizzle, l2, fill);
+  int dev = 0;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess)
+    r = driver_encode()(map, type, rank, base, dims, strides, box, estr, interleave, swizzle, l2, fill);
+  return r;
+}
+EncodeTiledFn encode_fn() { return driver_encode() ? encode_in_context : nullptr; }
 
 int encode_map(CUtensorMap* map, const void* ptr, int rows, int K, int box_rows, bool f16) {
   EncodeTiledFn enc = encode_fn();

@@ -89,3 +89,49 @@ def test_attention_many_small_weights_beside_a_large_one(fmt, key):
     want[0], want[1] = 4 / (4 + small), small / (4 + small)
     assert float(want[1]) > 2.0 ** -11
     assert ((out - want).abs() <= 2.0 ** -10 * 1.01 * want + 2.0 ** -15).all(), float((out - want).abs().max())
+
+
+def in_a_new_thread(call):
+    """Runs `call` as a new thread's first work with CUDA; its exception, if it raised one."""
+    import threading
+    raised = []
+
+    def body():
+        try:
+            call()
+        except Exception as e:  # noqa: BLE001 - handed to the test
+            raised.append(e)
+    torch.cuda.synchronize()
+    t = threading.Thread(target=body)
+    t.start()
+    t.join()
+    return raised[0] if raised else None
+
+
+@pytest.mark.parametrize("m", [1, 8, 300])
+def test_product_as_first_work_of_a_thread(m):
+    n, k = 700, 5120
+    codes, scales = low.weights(n, k, seed=1)
+    packed = hyp.hyp_op_mx4_pack(codes, scales)
+    a, out = normal(m, k, seed=2).half(), torch.zeros(m, n, device="cuda")
+    scratch = torch.empty(hyp.hyp_op_gemm_mx4_scratch_bytes(m, k, 3), dtype=torch.uint8, device="cuda")
+    assert in_a_new_thread(lambda: hyp.hyp_op_gemm_mx4(a, packed, n, 3, hyp.HYP_EPI_STORE_F32, out, scratch)) is None
+    ok()
+    held, w = low.in_terms(a, 3), low.values(codes, scales, k)
+    assert ((out.double() - held @ w.T).abs() <= low.product_bound(held, w, k)).all()
+
+
+@pytest.mark.parametrize("f16", [False, True])
+def test_16_bit_product_as_first_work_of_a_thread(f16):
+    """The operators in 16 bits describe their operands in the same way."""
+    m, n, k = 300, 256, 512
+    w = normal(n, k, seed=1, std=0.05).bfloat16()
+    a = normal(m, k, seed=2).to(torch.float16 if f16 else torch.bfloat16)
+    packed = hyp.hyp_op_pack_weight(w, n, False, f16=f16)
+    out = torch.zeros(m, n, device="cuda")
+    fn = hyp.hyp_op_gemm_f16 if f16 else hyp.hyp_op_gemm
+    stream = torch.cuda.current_stream()
+    assert in_a_new_thread(lambda: fn(a, packed, n, hyp.HYP_EPI_STORE_F32, out, stream)) is None
+    ok()
+    want = a.double() @ w.double().T
+    assert ((out.double() - want).abs() <= k * 2.0 ** -23 * (a.double().abs() @ w.double().abs().T)).all()
