@@ -24,6 +24,8 @@
 #include <cuda.h>
 #include <math.h>
 
+#include <mutex>
+
 #include "cache_ops.cuh"
 #include "gemm_tc.cuh"
 #include "mx4.cuh"
@@ -643,27 +645,37 @@ int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
   return 1;
 }
 
-const int* slots_by_ks() {
-  static int known[64][9] = {};  // per device
+int current_device() {
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
-  for (int ks = 1; ks <= 8 && known[dev][ks] == 0; ++ks) {
-    int n = 0;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr;
-    cfg.gridDim = dim3((unsigned)ks * 64);
-    cfg.blockDim = dim3(MX_THREADS);
-    cfg.dynamicSmemBytes = 200 * 1024;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)ks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (ks == 1 || allow_smem<gemm_mx4_kernel<EPI_STORE_F32, 1, false>>(MX_MAX_DYN) != HYP_OK ||
-        cudaOccupancyMaxActiveClusters(&n, gemm_mx4_kernel<EPI_STORE_F32, 1, false>, &cfg) != cudaSuccess || n < 1)
-      n = sm_count() / ks;
-    known[dev][ks] = n * ks;
-  }
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 ? dev : 0;
+}
+
+const int* slots_by_ks() {
+  static int known[64][9];
+  static std::once_flag asked[64];  // a second thread's first call waits: a plan weighed by half of the table would cut K another way
+  const int dev = current_device();
+  std::call_once(asked[dev], [dev] {
+    for (int ks = 1; ks <= 8; ++ks) {
+      int n = 0;
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute attr;
+      cfg.gridDim = dim3((unsigned)ks * 64);
+      cfg.blockDim = dim3(MX_THREADS);
+      cfg.dynamicSmemBytes = 200 * 1024;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = (unsigned)ks;
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      if (ks > 1 && (allow_smem<gemm_mx4_kernel<EPI_STORE_F32, 1, false>>(MX_MAX_DYN) != HYP_OK ||
+                     cudaOccupancyMaxActiveClusters(&n, gemm_mx4_kernel<EPI_STORE_F32, 1, false>, &cfg) != cudaSuccess)) {
+        n = 0;
+        cudaGetLastError();  // the question was refused: no error of the launch that asks
+      }
+      if (n < 1) n = sm_count() / ks;
+      known[dev][ks] = n * ks;
+    }
+  });
   return known[dev];
 }
 
@@ -685,13 +697,15 @@ int launch_by_epi(int epi, bool dual, const CUtensorMap& map, MxArgs& p, bool ow
 // A program calls with a few sizes again and again, and weighing the cuts takes 1-2 us of the host.
 Plan known_plan(int M, int N, int KB, int terms, bool swiglu) {
   struct Entry {
-    int M, N, KB, terms;
+    int M, N, KB, terms, dev;
     bool swiglu;
     Plan plan;
   };
   static thread_local Entry table[16] = {};
   Entry& e = table[((unsigned)M * 31u + (unsigned)N / 16u + (unsigned)KB * 7u + (unsigned)terms) % 16u];
-  if (e.M != M || e.N != N || e.KB != KB || e.terms != terms || e.swiglu != swiglu) e = Entry{M, N, KB, terms, swiglu, plan_for(M, N, KB, terms, swiglu)};
+  const int dev = current_device();
+  if (e.M != M || e.N != N || e.KB != KB || e.terms != terms || e.dev != dev || e.swiglu != swiglu)
+    e = Entry{M, N, KB, terms, dev, swiglu, plan_for(M, N, KB, terms, swiglu)};
   return e.plan;
 }
 

@@ -135,3 +135,42 @@ def test_16_bit_product_as_first_work_of_a_thread(f16):
     ok()
     want = a.double() @ w.double().T
     assert ((out.double() - want).abs() <= k * 2.0 ** -23 * (a.double().abs() @ w.double().abs().T)).all()
+
+
+# Eight threads whose first products, on streams and buffers of their own, start together in a fresh process.
+FIRST_CALLS = """
+import threading
+import torch
+from paper_2511_14450_b200 import hyperion as hyp
+from tests import test_gpu_low_bit as low
+n, k, m = 700, 5120, 8
+pool = torch.zeros(1, 2, 1, 1088, device="cuda", dtype=torch.uint8)
+low.attend((2, 1, 64), 0, torch.zeros(1, 128, device="cuda").half(), pool, low.i32([[0]]), low.i32([0]))
+packed = hyp.hyp_op_mx4_pack(*low.weights(n, k, 1))
+a = low.normal(m, k, seed=2).half()
+outs = [torch.zeros(m, n, device="cuda") for _ in range(8)]
+scratch = [torch.empty(hyp.hyp_op_gemm_mx4_scratch_bytes(m, k, 3), dtype=torch.uint8, device="cuda") for _ in range(8)]
+streams = [torch.cuda.Stream() for _ in range(8)]
+torch.cuda.synchronize()
+gate = threading.Barrier(8)
+def call(i):
+    gate.wait()
+    hyp.hyp_op_gemm_mx4(a, packed, n, 3, hyp.HYP_EPI_STORE_F32, outs[i], scratch[i], streams[i])
+threads = [threading.Thread(target=call, args=(i,)) for i in range(8)]
+for t in threads: t.start()
+for t in threads: t.join()
+low.ok()
+assert outs[0].abs().max() > 0
+print("alike", sum(torch.equal(outs[0], o) for o in outs))
+"""
+
+
+def test_product_first_calls_of_many_threads():
+    """All threads cut K alike: their sums are the same to the bit."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert r.stdout.split() == ["alike", "8"]
