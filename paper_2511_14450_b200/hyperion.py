@@ -349,15 +349,26 @@ def hyp_tune(key: int, value: int):
     _check(lib().hyp_tune(key, value), "hyp_tune")
 
 
+def _packed_buffer(nbytes: int, device, stream):
+    """Bytes that a kernel on `stream` fills, from that stream's own memory: what another stream has freed it may still be using."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def hyp_op_pack_weight(w, N: int, swiglu: bool, stream=None, f16: bool = False):
     """Packed copy of a bf16 [N (2N for SwiGLU), K] weight matrix, as hyp_op_gemm reads it (a uint8 tensor);
-    f16: the values converted to fp16 on the way (hyp_op_pack_weight_f16, for hyp_op_gemm_f16)."""
-    import torch
+    f16: the values converted to fp16 on the way (hyp_op_pack_weight_f16, for hyp_op_gemm_f16).  The copy is memory of `stream`:
+    for use on another stream, as with any tensor, wait for it and tell the allocator (record_stream)."""
     K = w.shape[1]
     nbytes = lib().hyp_op_weight_packed_bytes(N, K, int(swiglu))
     if nbytes == 0:
         raise HyperionError(HYP_EINVAL, "hyp_op_weight_packed_bytes")
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=w.device)
+    packed = _packed_buffer(nbytes, w.device, stream)
     name = "hyp_op_pack_weight_f16" if f16 else "hyp_op_pack_weight"
     _check(getattr(lib(), name)(_ptr(w), N, K, int(swiglu), _ptr(packed), nbytes, _stream_handle(stream)), name)
     return packed
@@ -693,8 +704,7 @@ def hyp_op_mx4_packed_bytes(N: int, K: int, swiglu: bool) -> int:
 
 def hyp_op_mx4_pack(codes, scales, swiglu: bool = False, stream=None):
     """The packed copy (a uint8 tensor) of codes [N, K / 2] and scales [N, ceil(K / 32)], for hyp_op_gemm_mx4; SwiGLU: 2N rows of
-    each, gate rows then up rows."""
-    import torch
+    each, gate rows then up rows.  Memory of `stream`, as hyp_op_pack_weight's."""
     where = "hyp_op_mx4_pack"
     _types()
     dev, s = codes.get_device(), codes.shape
@@ -706,7 +716,7 @@ def hyp_op_mx4_pack(codes, scales, swiglu: bool = False, stream=None):
     nbytes = hyp_op_mx4_packed_bytes(n, k, swiglu)
     if not nbytes:
         _refuse(where, f"no matrix of {n} rows and {k} columns")
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    packed = _packed_buffer(nbytes, codes.device, stream)
     _launch(where, lib().hyp_op_mx4_pack, dev, stream, cp, sp, n, k, int(swiglu), packed.data_ptr(), nbytes)
     return packed
 

@@ -174,3 +174,38 @@ def test_product_first_calls_of_many_threads():
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
     assert r.stdout.split() == ["alike", "8"]
+
+
+def behind_queued_work(pack, raw):
+    """`pack` on a stream of its own, while the current stream still has to write a freed block of the size that the copy needs."""
+    want = pack(None).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                                       # about 0.1 s
+    block = torch.empty_like(want)
+    block.fill_(0xAA)
+    del block
+    got = pack(side.cuda_stream if raw else side)
+    torch.cuda.synchronize()
+    return got, want
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("swiglu", [False, True])
+def test_pack_of_4_bit_weights_on_another_stream(swiglu, raw):
+    codes, scales = low.weights(1400, 4096, seed=1)
+    got, want = behind_queued_work(lambda s: hyp.hyp_op_mx4_pack(codes, scales, swiglu, stream=s), raw)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("f16", [False, True])
+def test_pack_of_16_bit_weights_on_another_stream(f16, raw):
+    w = normal(1400, 1024, seed=1).bfloat16()
+    got, want = behind_queued_work(lambda s: hyp.hyp_op_pack_weight(w, 1400, False, stream=s, f16=f16), raw)
+    assert torch.equal(got, want)
+
+
+def test_pack_on_the_default_stream_by_its_address():
+    codes, scales = low.weights(200, 512, seed=1)
+    assert torch.equal(hyp.hyp_op_mx4_pack(codes, scales, stream=0), hyp.hyp_op_mx4_pack(codes, scales))
