@@ -38,11 +38,19 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int n, int row, in
   return lo;
 }
 
-// Scale of a row from its largest magnitude.  int8: amax / 127 rounded to fp32 (the fp64 product with the rounded 1 / 127 is off by
-// 2^-52; a quotient of a 24-bit amax is never that near to a border).  e4m3: the least power of two p with amax <= 448 p.
+// Scale of a row from its largest magnitude.  int8: amax / 127 rounded to fp32 once.  The product with the rounded 1 / 127 is less than a step
+// of fp64 off the quotient, which never lies that near to the middle of two fp32 numbers for a 24-bit amax, but does for one in 2^27 or so of
+// 53 bits: a product that came out as a middle goes a step to where the quotient lies.  e4m3: the least power of two p with amax <= 448 p.
 template <int FMT>
 __device__ __forceinline__ float row_scale(double amax) {
-  if (FMT == HYP_KV8_INT8) return (float)(amax * (1.0 / 127.0));
+  if (FMT == HYP_KV8_INT8) {
+    double q = amax * (1.0 / 127.0);
+    if ((__double2loint(q) & 0x1fffffff) == 0x10000000) {
+      const double rest = fma(-127.0, q, amax);  // its sign is exact
+      q = __longlong_as_double(__double_as_longlong(q) + (rest > 0.0 ? 1 : rest < 0.0 ? -1 : 0));
+    }
+    return (float)q;
+  }
   const long long b = __double_as_longlong(amax);
   return pow2((int)(b >> 52) - 1023 - 8 + ((b & 0xfffffffffffffll) > 0xc000000000000ll ? 1 : 0));
 }

@@ -209,3 +209,36 @@ def test_pack_of_16_bit_weights_on_another_stream(f16, raw):
 def test_pack_on_the_default_stream_by_its_address():
     codes, scales = low.weights(200, 512, seed=1)
     assert torch.equal(hyp.hyp_op_mx4_pack(codes, scales, stream=0), hyp.hyp_op_mx4_pack(codes, scales))
+
+
+def fp32_nearest(x):
+    """The fp32 number nearest to a fraction, ties to even."""
+    from fractions import Fraction
+    import numpy as np
+    f = np.float32(float(x))
+    near = [np.nextafter(f, np.float32(-np.inf)), f, np.nextafter(f, np.float32(np.inf))]
+    return float(min(near, key=lambda v: (abs(Fraction(float(v)) - x), int(v.view(np.uint32)) & 1)))
+
+
+def test_write_scales_of_rotated_rows_next_to_a_border():
+    """Largest magnitudes of 127 M +- 2^-22 and 127 M, M an odd number of 25 bits: a 127th of them lies half a step of fp64, or nothing, away
+    from the middle between two fp32 numbers."""
+    from fractions import Fraction
+    heads, n, d = (1, 1, 64), 300, 64
+    ks = [3355445 + 2 * 43 * i for i in range(n)]
+    tab = torch.zeros(n, d // 2, 2, device="cuda")
+    tab[:, 0, 0], tab[:, 0, 1] = torch.tensor(ks, device="cuda").float(), -2.0 ** -22
+    qkv = torch.zeros(3 * n, 3 * d, device="cuda")
+    qkv[:, d] = 635.0                                                    # 635 k - b sin
+    for i, b in enumerate((1.0, 0.0, -1.0)):
+        qkv[i * n:(i + 1) * n, d + d // 2] = b
+    pages = (n + 15) // 16
+    table = torch.arange(3 * pages, dtype=torch.int32, device="cuda").view(3, pages)
+    pool = torch.zeros(3 * pages, 2, 1, 16 * d + 64, dtype=torch.uint8, device="cuda")
+    hyp.hyp_op_kv8_write(heads, hyp.HYP_KV8_INT8, qkv, pool, table, i32([0, n, 2 * n, 3 * n]), i32([0, 0, 0]), tab)
+    ok()
+    got = pool[:, 0, 0, 16 * d:].contiguous().view(torch.float32).view(3, -1)[:, :n].cpu()
+    want = torch.tensor([[fp32_nearest((Fraction(635 * k) + b * Fraction(1, 1 << 22)) / 127) for k in ks] for b in (1, 0, -1)])
+    assert torch.equal(got, want), int((got != want).sum())
+    codes = pool[:, 0, 0, :16 * d].reshape(3, -1, d)[:, :n]
+    assert (codes[:, :, 0] == 255).all() and (codes[:, :, 1:32] == 128).all()
