@@ -770,8 +770,12 @@ def hyp_op_kv8_write(shape3, fmt: int, qkv, kv8_pages, block_table, cu_q, ctx_le
     ctx, n = _rows(where, "ctx_lens", ctx_lens, _I32, dev, ())
     table, pages = _rows(where, "block_table", block_table, _I32, dev, (n,))
     cu = _dense(where, "cu_q", cu_q, _I32, dev, (n + 1,))
-    rope = 0 if rope_table is None else rope_table.shape[0]
-    rp = None if rope_table is None else _dense(where, "rope_table", rope_table, _F32, dev, (rope, shape3[2] // 2, 2))
+    rope, rp = 0, None
+    if rope_table is not None:
+        rope = rope_table.shape[0] if rope_table.dim() else 0
+        rp = _dense(where, "rope_table", rope_table, _F32, dev, (rope, shape3[2] // 2, 2))
+        if rope < 1:                                            # its address is that of no table at all
+            _refuse(where, "rope_table holds no position")
     op = None if q_out is None else _dense(where, "q_out", q_out, _F16, dev, (m, shape3[0] * shape3[2]))
     _launch(where, lib().hyp_op_kv8_write, dev, stream, sh, fmt, n, m, qp, code, qs, rp, rope, pool, table, pages, cu, ctx, op)
 
