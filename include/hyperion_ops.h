@@ -392,7 +392,7 @@ HYP_API int hyp_op_kv8_write(const hyp_attn_shape* shape, int32_t format, int32_
  * and the other operators over the fp16 cache.  Values are code times scale rounded once; beyond +-65504 they saturate.
  *   first  DEVICE int32 [n_seqs] or NULL (0);  lens DEVICE int32 [n_seqs]; both clamped to what both tables' rows can name
  *   dst_pages fp16 pool, 16-byte aligned;  dst_table int32 [n_seqs, dst_pages_per_seq].  Other slots are left as they were.
- * Errors: HYP_EINVAL, HYP_ECUDA. */
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (both tables' rows name more than 2^31 - 2^16 half pages of a head), HYP_ECUDA. */
 HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* kv8_pages, const int32_t* block_table,
                             int32_t max_pages_per_seq, const int32_t* first, const int32_t* lens, void* dst_pages,
                             const int32_t* dst_table, int32_t dst_pages_per_seq, void* stream);

@@ -105,6 +105,9 @@ extern "C" int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int3
   if (!shape_ok(shape, format) || !kv8_pages || !block_table || !lens || !dst_pages || !dst_table) return HYP_EINVAL;
   if (!count_ok(n_seqs) || !pages_ok(max_pages_per_seq) || !pages_ok(dst_pages_per_seq)) return HYP_EINVAL;
   if (!aligned(kv8_pages, 16) || !aligned(dst_pages, 16)) return HYP_EINVAL;
+  // a sequence's half pages, and the step of the warps that share them, are counted in 31 bits
+  const int64_t pages = max_pages_per_seq < dst_pages_per_seq ? max_pages_per_seq : dst_pages_per_seq;
+  if (pages * 2 * shape->n_kv_heads > 0x7fffffff - (1 << 16)) return HYP_ECAPACITY;
   return finish(launch_kv8_read(view(shape, format, n_seqs, kv8_pages, block_table, max_pages_per_seq), first, lens, (__half*)dst_pages,
                                 dst_table, dst_pages_per_seq, (cudaStream_t)stream));
 }

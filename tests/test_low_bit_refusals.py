@@ -43,3 +43,10 @@ def test_rope_tables_that_fit_reach_the_launch(monkeypatch):
     write_with(None)
     rope = [(a[11], a[12]) for a in calls]                       # the table's address and positions
     assert rope == [(args.P, 5), (None, 0)]
+
+
+@pytest.mark.parametrize("hkv,pages,dpages", [(16, 1 << 26, 1 << 26), (32767, 32769, 1 << 26), (32767, 1 << 26, 32769), (64, 1 << 24, 1 << 24)])
+def test_read_of_more_half_pages_than_31_bits_count(hkv, pages, dpages):
+    """The warps' steps over a sequence's half pages would have wrapped around: refused by the sizes, whatever the lengths are."""
+    assert args.call("hyp_op_kv8_read", shape=args.shape(hkv, hkv, 64), pages=pages, dpages=dpages) == CAP
+    assert args.call("hyp_op_kv8_read", shape=args.shape(hkv, hkv, 64), pages=0, dpages=dpages) == E
