@@ -358,6 +358,13 @@ HYP_API size_t hyp_op_gemm_mx4_scratch_bytes(int32_t M, int32_t K, int32_t terms
 HYP_API int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, const void* w_packed, int32_t M, int32_t N, int32_t K,
                             int32_t terms, int32_t epilogue, void* out, int32_t ldo, void* scratch, size_t scratch_bytes, void* stream);
 
+/* How hyp_op_gemm_mx4 cuts a product on the current device (a function of the sizes alone; nothing is launched).
+ *   plan  int32 [8]: weight row tiles (of 128) of a CTA; token tiles; shares of K, one to a CTA of a cluster; CTAs; stages of 128 k that a CTA's ring
+ *         holds; CTAs that an SM holds at once; 1 where the CTAs make the terms of the activations themselves; else the chunks of eight
+ *         values that a thread of the terms' launch takes
+ * Errors: HYP_EINVAL, HYP_ECAPACITY (matrix too large). */
+HYP_API int hyp_op_gemm_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t terms, int32_t epilogue, int32_t* plan);
+
 /* The paged cache in 8 bits.  Pool uint8 [n_pages][2 (K then V)][n_kv_heads][16 * head_dim + 64], 16-byte aligned: a half page of a head
  * is 16 token rows of head_dim one-byte codes, then the 16 tokens' scales (fp32).  At head_dim 128 the 16-byte chunk c of slot t's row
  * sits at chunk position c ^ (4 * (t & 1)).

@@ -46,7 +46,7 @@ struct Plan {
   size_t block_bytes;  // terms of one (token tile, 128 k) with their scales
 };
 constexpr int MX_MAX_DYN = 216 * 1024, MX_MORE_TILES = 3;
-constexpr int OWN_TERMS = 4, OWN_BYTES = 64 * 1024;  // see launch_gemm_mx4
+constexpr int OWN_TERMS = 4, OWN_BYTES = 64 * 1024;  // see launch_for
 // Tensor memory: one accumulator of 256 columns beside the scales, or two of 240.
 int row_cap(int a_tiles) { return a_tiles == 2 ? 240 : 256; }
 bool cut(Plan& p, int M, int N, int terms, int a_tiles, bool swiglu, int tiles) {
@@ -89,7 +89,7 @@ Plan plan_for(int M, int N, int KB, int terms, bool swiglu) {
       for (int ks = 1; ks <= 8; ++ks) {
         if (ks > 1 && (ks > KB / 4 || a * p.tt * MX_ROWS * 4 > MX_MAX_DYN - 1024)) break;
         const double ctas = (double)p.row_units * p.tiles * ks, slots = slots_of[ks], block = (double)p.block_bytes;
-        const double on_sm = ctas > slots && tmem_columns(a, p.nb) <= 256 ? 2.0 : 1.0;  // CTAs of an SM (see launch_own)
+        const double on_sm = ctas > slots && tmem_columns(a, p.nb) <= 256 ? 2.0 : 1.0;  // CTAs of an SM (see launch_for)
         const double ring = fmin(floor((MX_MAX_DYN / on_sm - 1024.0) / (a * (MX_A_BYTES + MX_SF_BYTES) + block)), MX_MAX_STAGES);
         const double stage = fmax(fmax(on_sm * (a * MX_PACK_BYTES + block) / 53.0, 3300.0 / fmax(ring, 2.0)),
                                   fmax(on_sm * fmax(a == 2 ? 700.0 : 450.0, 2.0 * a * p.nb),
@@ -598,32 +598,22 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap tm_w, const MxArgs p) {
   }
 }
 
+// What a launch needs beside the cut.
+struct Launch {
+  Plan plan;
+  long long ctas;
+  int tmem_cols, stages, stage_bytes, smem;
+  bool own, many;  // the CTAs make their terms; else the terms' launch takes two chunks a thread
+};
+
 template <int EPI, int A_TILES, bool OWN>
-int launch_own(const CUtensorMap& map, MxArgs& p, cudaStream_t st) {
+int launch_own(const CUtensorMap& map, const MxArgs& p, const Launch& l, cudaStream_t st) {
   const int rc = allow_smem<gemm_mx4_kernel<EPI, A_TILES, OWN>>(MX_MAX_DYN);
   if (rc) return rc;
-  const int cols = tmem_columns(A_TILES, p.nb);
-  p.tmem_cols = cols;
-  p.stage_bytes = (A_TILES * (MX_A_BYTES + MX_SF_BYTES) + (OWN ? 0 : (int)p.block_bytes) + 1023) / 1024 * 1024;
-  const int own_bytes = OWN ? (p.KB + p.ksplit - 1) / p.ksplit * (int)own_place(p.block_bytes) : 0;
-  const long long ctas = (long long)p.row_units * p.token_tiles * p.ksplit;
-  const int sum_bytes = (p.ksplit > 1 ? A_TILES : 1) * p.tt * MX_ROWS * 4;
-  // two CTAs to an SM where there are more than SMs and tensor memory has room for both
-  const int budget = ctas > sm_count() && cols <= 256 ? 112 * 1024 : MX_MAX_DYN;
-  int stages = (budget - 1024 - own_bytes) / p.stage_bytes;
-  if (stages > MX_MAX_STAGES) stages = MX_MAX_STAGES;
-  if (stages < 2) stages = 2;
-  p.stages = stages;
-  const int ring = stages * p.stage_bytes + own_bytes;
-  int smem = (ring > sum_bytes ? ring : sum_bytes) + 1024;  // the sums reuse the ring
-  if (smem > MX_MAX_DYN) return HYP_EINVAL;
-  // never more CTAs on an SM than tensor memory holds: one that waits for it would hold up its cluster
-  const int least = 228 * 1024 / (512 / cols + 1);
-  if (smem < least) smem = least;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.gridDim = dim3((unsigned)l.ctas);
   cfg.blockDim = dim3(MX_THREADS);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = l.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int na = 0;
@@ -680,16 +670,17 @@ const int* slots_by_ks() {
 }
 
 template <int EPI, int A_TILES>
-int launch_epi(const CUtensorMap& map, MxArgs& p, bool own, cudaStream_t st) {
-  return own ? launch_own<EPI, A_TILES, true>(map, p, st) : launch_own<EPI, A_TILES, false>(map, p, st);
+int launch_epi(const CUtensorMap& map, const MxArgs& p, const Launch& l, cudaStream_t st) {
+  return l.own ? launch_own<EPI, A_TILES, true>(map, p, l, st) : launch_own<EPI, A_TILES, false>(map, p, l, st);
 }
 
-int launch_by_epi(int epi, bool dual, const CUtensorMap& map, MxArgs& p, bool own, cudaStream_t st) {
+int launch_by_epi(int epi, const CUtensorMap& map, const MxArgs& p, const Launch& l, cudaStream_t st) {
+  const bool dual = l.plan.a_tiles == 2;
   switch (epi) {
-    case EPI_STORE_BF16: return dual ? launch_epi<EPI_STORE_BF16, 2>(map, p, own, st) : launch_epi<EPI_STORE_BF16, 1>(map, p, own, st);
-    case EPI_RESID_F32: return dual ? launch_epi<EPI_RESID_F32, 2>(map, p, own, st) : launch_epi<EPI_RESID_F32, 1>(map, p, own, st);
-    case EPI_SWIGLU_BF16: return launch_epi<EPI_SWIGLU_BF16, 2>(map, p, own, st);
-    case EPI_STORE_F32: return dual ? launch_epi<EPI_STORE_F32, 2>(map, p, own, st) : launch_epi<EPI_STORE_F32, 1>(map, p, own, st);
+    case EPI_STORE_BF16: return dual ? launch_epi<EPI_STORE_BF16, 2>(map, p, l, st) : launch_epi<EPI_STORE_BF16, 1>(map, p, l, st);
+    case EPI_RESID_F32: return dual ? launch_epi<EPI_RESID_F32, 2>(map, p, l, st) : launch_epi<EPI_RESID_F32, 1>(map, p, l, st);
+    case EPI_SWIGLU_BF16: return launch_epi<EPI_SWIGLU_BF16, 2>(map, p, l, st);
+    case EPI_STORE_F32: return dual ? launch_epi<EPI_STORE_F32, 2>(map, p, l, st) : launch_epi<EPI_STORE_F32, 1>(map, p, l, st);
     default: return HYP_EINVAL;
   }
 }
@@ -709,6 +700,37 @@ Plan known_plan(int M, int N, int KB, int terms, bool swiglu) {
   return e.plan;
 }
 
+// 0 stages: no room (no plan asks for it)
+Launch launch_for(int M, int N, int KB, int terms, bool swiglu) {
+  Launch l{};
+  l.plan = known_plan(M, N, KB, terms, swiglu);
+  const Plan& t = l.plan;
+  l.ctas = (long long)t.row_units * t.tiles * t.ksplit;
+  // Up to OWN_TERMS terms a thread (of a chunk each) the CTAs make their terms themselves (one token, 512 x 256 of three: 3.6 instead of 4.4 us, 7680 x 5120
+  // 8.9, 9.3; three tokens, 1000 x 2000 of two: 4.8, 5.7); with more, a launch of their own is faster (two tokens, 7680 x 5120 of three: 9.3
+  // instead of 9.6).
+  const int share = (KB + t.ksplit - 1) / t.ksplit, own_threads = 32 * MX_EPI_WARPS;
+  l.own = t.tiles == 1 && (16ll * M * share + own_threads - 1) / own_threads * terms <= OWN_TERMS &&
+          share * (long long)own_place(t.block_bytes) <= OWN_BYTES && (long long)t.row_units * t.ksplit <= sm_count();
+  l.many = !l.own && 16ll * M * KB > 1 << 18;  // two chunks a thread: half the CTAs (512 x 5120 x 17920 51 us, one chunk 55, four 51; 128 rows 28, 29, 31)
+  l.tmem_cols = tmem_columns(t.a_tiles, t.nb);
+  l.stage_bytes = (t.a_tiles * (MX_A_BYTES + MX_SF_BYTES) + (l.own ? 0 : (int)t.block_bytes) + 1023) / 1024 * 1024;
+  const int own_bytes = l.own ? share * (int)own_place(t.block_bytes) : 0;
+  const int sum_bytes = (t.ksplit > 1 ? t.a_tiles : 1) * t.tt * MX_ROWS * 4;
+  // two CTAs to an SM where there are more than SMs and tensor memory has room for both
+  const int budget = l.ctas > sm_count() && l.tmem_cols <= 256 ? 112 * 1024 : MX_MAX_DYN;
+  l.stages = (budget - 1024 - own_bytes) / l.stage_bytes;
+  if (l.stages > MX_MAX_STAGES) l.stages = MX_MAX_STAGES;
+  if (l.stages < 2) l.stages = 2;
+  const int ring = l.stages * l.stage_bytes + own_bytes;
+  l.smem = (ring > sum_bytes ? ring : sum_bytes) + 1024;  // the sums reuse the ring
+  if (l.smem > MX_MAX_DYN) l.stages = 0;
+  // never more CTAs on an SM than tensor memory holds: one that waits for it would hold up its cluster
+  const int least = 228 * 1024 / (512 / l.tmem_cols + 1);
+  if (l.smem < least) l.smem = least;
+  return l;
+}
+
 }  // namespace
 
 size_t mx4_scratch_bytes(int M, int K, int terms) {
@@ -717,46 +739,47 @@ size_t mx4_scratch_bytes(int M, int K, int terms) {
   return (size_t)mx_kb(K) * (rows * MX_BK + (rows / MX_ROWS + t) * MX_SF_BYTES);
 }
 
+void mx4_plan(int M, int N, int K, int terms, bool swiglu, int32_t (&plan)[8]) {
+  const Launch l = launch_for(M, N, mx_kb(K), terms, swiglu);
+  const int32_t v[8] = {l.plan.a_tiles, l.plan.tiles, l.plan.ksplit, (int32_t)(l.ctas > 0x7fffffffll ? 0x7fffffff : l.ctas), l.stages,
+                        228 * 1024 / (l.smem + 1024), l.own, l.own ? 0 : l.many ? 2 : 1};
+  for (int i = 0; i < 8; ++i) plan[i] = v[i];
+}
+
 int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t* packed, int M, int N, int K, int terms, int epi,
                     void* out, int ldo, uint8_t* scratch, cudaStream_t st) {
   const bool swiglu = epi == EPI_SWIGLU_BF16, wide = epi == EPI_STORE_F32 || epi == EPI_RESID_F32;
-  const Plan t = known_plan(M, N, mx_kb(K), terms, swiglu);
+  const Launch l = launch_for(M, N, mx_kb(K), terms, swiglu);
+  const Plan& t = l.plan;
+  if (l.stages == 0) return HYP_EINVAL;
   MxArgs p{};
   p.packed = packed; p.terms = scratch; p.block_bytes = t.block_bytes;
   p.M = M; p.N = N; p.KB = mx_kb(K); p.ldo = ldo;
   p.tiles = mx_row_tiles(N); p.row_units = t.row_units; p.token_tiles = t.tiles; p.tt = t.tt; p.nb = t.nb; p.n_terms = terms;
-  p.ksplit = t.ksplit;
+  p.ksplit = t.ksplit; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.tmem_cols = l.tmem_cols;
   p.f16 = a_type == HYP_TYPE_F16; p.out = out; p.err = tc_err_flag_ptr();
   p.vec = ldo % 4 == 0 && ((uintptr_t)out & (wide ? 15 : 7)) == 0;
   p.idesc = (5u << 7) | (0u << 10) | ((uint32_t)(t.nb >> 3) << 17) | (1u << 23) | ((uint32_t)(MX_ROWS >> 4) << 24);  // E2M1 x E4M3, power-of-two scales
-  if ((long long)t.row_units * t.tiles * t.ksplit > 0x7fffffffll) return HYP_ECAPACITY;
+  if (l.ctas > 0x7fffffffll) return HYP_ECAPACITY;
   CUtensorMap map;
   int rc = tc_make_mx4_map(&map, packed, (long long)(swiglu ? 2 : 1) * p.tiles * p.KB * (MX_PACK_BYTES / 64));
   if (rc) return rc;
-  // Up to OWN_TERMS terms a thread (of a chunk each) the CTAs make their terms themselves (one token, 512 x 256 of three: 3.6 instead of 4.4 us, 7680 x 5120
-  // 8.9, 9.3; three tokens, 1000 x 2000 of two: 4.8, 5.7); with more, a launch of their own is faster (two tokens, 7680 x 5120 of three: 9.3
-  // instead of 9.6).
-  const int share = (p.KB + p.ksplit - 1) / p.ksplit;
-  const int own_threads = 32 * MX_EPI_WARPS;
-  const bool own = t.tiles == 1 && (16ll * M * share + own_threads - 1) / own_threads * terms <= OWN_TERMS && share * (long long)own_place(t.block_bytes) <= OWN_BYTES &&
-                   (long long)t.row_units * t.ksplit <= sm_count();
-  if (own) {
+  if (l.own) {
     p.act = (const uint8_t*)a; p.act_stride = a_stride; p.K8 = K / 8;
-    return launch_by_epi(epi, t.a_tiles == 2, map, p, true, st);
+    return launch_by_epi(epi, map, p, l, st);
   }
   const long long chunks = 16ll * p.KB;  // of a row: its segments fit the grid (K is at most 2^25)
-  const bool many = M * chunks > 1 << 18;  // two chunks a thread: half the CTAs (512 x 5120 x 17920 51 us, one chunk 55, four 51; 128 rows 28, 29, 31)
-  const long long segments = (chunks + TERM_THREADS * (many ? 2 : 1) - 1) / (TERM_THREADS * (many ? 2 : 1));
+  const long long segments = (chunks + TERM_THREADS * (l.many ? 2 : 1) - 1) / (TERM_THREADS * (l.many ? 2 : 1));
   auto go = [&](auto kernel) {
     return launch_pdl<2>(kernel, dim3((unsigned)M, (unsigned)segments), dim3(TERM_THREADS), (size_t)0, st, (const uint8_t*)a, a_stride, K / 8, p.KB,
                          t.tt, t.nb, t.block_bytes, scratch);
   };
-  auto by_chunks = [&](auto two, auto one) { return many ? go(two) : go(one); };
+  auto by_chunks = [&](auto two, auto one) { return l.many ? go(two) : go(one); };
 #define HYP_F(T, N) \
   if (a_type == T && terms == N) HYP_CUDA_TRY(by_chunks(mx_terms_kernel<T, 2, N>, mx_terms_kernel<T, 1, N>));
   HYP_F(HYP_TYPE_F16, 1) HYP_F(HYP_TYPE_F16, 2) HYP_F(HYP_TYPE_F16, 3) HYP_F(HYP_TYPE_BF16, 1) HYP_F(HYP_TYPE_BF16, 2) HYP_F(HYP_TYPE_BF16, 3)
 #undef HYP_F
-  rc = launch_by_epi(epi, t.a_tiles == 2, map, p, false, st);
+  rc = launch_by_epi(epi, map, p, l, st);
   return rc < 0 ? rc : rc + 1;
 }
 

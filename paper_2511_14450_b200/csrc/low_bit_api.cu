@@ -71,6 +71,17 @@ extern "C" size_t hyp_op_gemm_mx4_scratch_bytes(int32_t M, int32_t K, int32_t te
   return mx4_scratch_bytes(M, K, terms);
 }
 
+extern "C" int hyp_op_gemm_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t terms, int32_t epilogue, int32_t* plan) {
+  if (!plan || !matrix_ok(N, K) || M < 1 || M > (1 << 26) || terms < 1 || terms > 3) return HYP_EINVAL;
+  if (epilogue < HYP_EPI_STORE_BF16 || epilogue > HYP_EPI_STORE_F32) return HYP_EINVAL;
+  const bool swiglu = epilogue == HYP_EPI_SWIGLU_BF16;
+  if (!mx4_lines_ok(N, K, swiglu ? 2 : 1)) return HYP_ECAPACITY;
+  int32_t v[8];
+  mx4_plan(M, N, K, terms, swiglu, v);
+  for (int i = 0; i < 8; ++i) plan[i] = v[i];
+  return HYP_OK;
+}
+
 extern "C" int hyp_op_gemm_mx4(const void* a, int32_t a_type, int64_t a_stride, const void* w_packed, int32_t M, int32_t N, int32_t K,
                                int32_t terms, int32_t epilogue, void* out, int32_t ldo, void* scratch, size_t scratch_bytes, void* stream) {
   if (!a || !w_packed || !out || !scratch || (a_type != HYP_TYPE_F16 && a_type != HYP_TYPE_BF16)) return HYP_EINVAL;

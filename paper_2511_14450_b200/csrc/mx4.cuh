@@ -119,6 +119,7 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int N, in
 int launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, int N, int K, int halves, uint8_t* packed, cudaStream_t st);
 
 size_t mx4_scratch_bytes(int M, int K, int terms);
+void mx4_plan(int M, int N, int K, int terms, bool swiglu, int32_t (&plan)[8]);  // as hyp_op_gemm_mx4_plan
 int launch_gemm_mx4(const void* a, int a_type, long long a_stride, const uint8_t* packed, int M, int N, int K, int terms, int epi,
                     void* out, int ldo, uint8_t* scratch, cudaStream_t st);
 

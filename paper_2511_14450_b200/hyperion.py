@@ -112,6 +112,7 @@ SIGNATURES = {
     "hyp_op_mx4_packed_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     "hyp_op_mx4_pack": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hyp_op_gemm_mx4_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "hyp_op_gemm_mx4_plan": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]),
     "hyp_op_gemm_mx4": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hyp_op_kv8_write": (C.c_int, [C.POINTER(hyp_attn_shape), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int64,
@@ -723,6 +724,16 @@ def hyp_op_mx4_pack(codes, scales, swiglu: bool = False, stream=None):
 
 def hyp_op_gemm_mx4_scratch_bytes(M: int, K: int, terms: int) -> int:
     return lib().hyp_op_gemm_mx4_scratch_bytes(M, K, terms)
+
+
+_PLAN = ("row_tiles", "token_tiles", "shares", "ctas", "stages", "per_sm", "own_terms", "chunks")
+
+
+def hyp_op_gemm_mx4_plan(M: int, N: int, K: int, terms: int, epilogue: int) -> dict:
+    """How hyp_op_gemm_mx4 cuts a product on the current device."""
+    plan = (C.c_int32 * 8)()
+    _check(lib().hyp_op_gemm_mx4_plan(M, N, K, terms, epilogue, plan), "hyp_op_gemm_mx4_plan")
+    return dict(zip(_PLAN, plan))
 
 
 def hyp_op_gemm_mx4(a, w_packed, N: int, terms: int, epilogue: int, out, scratch, stream=None):
