@@ -406,7 +406,8 @@ HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t
 
 /* hyp_op_attn_decode over the 8-bit cache (keys and values 0 .. ctx_lens[b], the new token's included; -1: nothing, the row is zeros).
  * The softmax weights, times their values' scales, enter the value product as fp16, off by 2^-11 of each or by 2^-32 of the largest so far, whichever is
- * more; results beyond fp16 are infinities.  A score q . k that leaves fp32 counts as an infinity: NaN, or no weight.  A key or value row with a NaN scale makes its sequence's results NaN, unless its weight is 0 in fp32.
+ * more; results beyond fp16 are infinities.  A score q . k that leaves fp32 counts as an infinity: NaN, or no weight.  A key or
+ * value row with a NaN scale makes its sequence's results NaN, whatever its weight.
  * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, more than 2^31 rows and heads to join), HYP_ECUDA. */
 HYP_API size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);

@@ -242,3 +242,33 @@ def test_write_scales_of_rotated_rows_next_to_a_border():
     assert torch.equal(got, want), int((got != want).sum())
     codes = pool[:, 0, 0, :16 * d].reshape(3, -1, d)[:, :n]
     assert (codes[:, :, 0] == 255).all() and (codes[:, :, 1:32] == 128).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("l,at", [(40, 39), (5000, 3)])
+@pytest.mark.parametrize("part", [0, 1])
+def test_attention_nan_row_of_no_weight(fmt, l, at, part):
+    """A key or value row with a NaN scale makes its sequence's results NaN, a value row whose weight is nothing beside the others' as well."""
+    heads = (4, 2, 64)
+    x = normal(l, 2, 2, 64, seed=l)
+    x[:, 0] = 0.0
+    x[at, 0] = -3000.0                                                   # e^-24000 of the others' weight
+    pool, table, held = cache8(x, fmt)
+    q = torch.ones(1, 256, device="cuda", dtype=torch.float16)
+    out = low.attend(heads, fmt, q, pool, table, i32([l - 1]))[0].double().view(4, 64)
+    keep = torch.arange(l, device="cuda") != at
+    want = held[keep, 1].mean(0).repeat_interleave(2, 0)
+    assert ((out - want).abs() <= 2.0 ** -10 * held[:, 1].abs().amax()).all()
+    pool[int(table[0, at // 16]), part, 1, 16 * 64 + 4 * (at % 16):16 * 64 + 4 * (at % 16) + 4] = 0xFF
+    again = low.attend(heads, fmt, q, pool, table, i32([l - 1]))[0].double().view(4, 64)
+    assert torch.isnan(again[2:]).all() and torch.equal(again[:2], out[:2])
+
+
+@pytest.mark.parametrize("heads,lens,extra", [((40, 10, 128), [1024] * 8, 0), ((8, 2, 128), [2500, 3, 700], 0), ((8, 8, 128), [300] * 40, 200)])
+def test_attention_is_the_same_on_every_run(heads, lens, extra):
+    hq, hkv, d = heads
+    c = low.Cache8(lens, hkv, d, hyp.HYP_KV8_INT8, 71, extra)
+    q, ctx = normal(len(lens), hq * d, seed=72).half(), i32([l - 1 for l in lens])
+    first = low.attend(heads, hyp.HYP_KV8_INT8, q, c.pool, c.table, ctx)
+    for _ in range(5):
+        assert torch.equal(low.attend(heads, hyp.HYP_KV8_INT8, q, c.pool, c.table, ctx), first)
