@@ -345,6 +345,8 @@ HYP_API int hyp_op_mx4_pack(const void* codes, const void* scales, int32_t N, in
  * power of two of its own per row and block of 32 k: term 1 is a rounded to 4 significant bits, the next ones what is left.  terms = 3 holds
  * fp16 values, terms = 2 bf16 values (up to 2^-17, for three terms 2^-25, of their block's largest magnitude); terms = 1 is an 8-bit
  * product, off by up to 2^-4 of every activation.  The term's power of two is the least p with amax <= 448 p.
+ * Every term is a product of its own.  Against hyp_op_gemm_f16 on the same matrix in fp16 one term is faster at any number of rows, two up to about 256, three
+ * up to about 128 (512 x 5120 x 17920: 50, 87 and 110 us against 82).
  *   a         HYP_TYPE_F16 or HYP_TYPE_BF16 [M, K], rows a_stride elements apart (a multiple of 8), 16-byte aligned
  *   w_packed  from hyp_op_mx4_pack for the same N, K and swiglu = (epilogue == HYP_EPI_SWIGLU_BF16)
  *   out       [M, ldo], ldo >= N; HYP_EPI_RESID_F32 adds to it
@@ -372,8 +374,8 @@ HYP_API int hyp_op_gemm_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t terms,
  *                 integer nearest to value / scale, ties to even
  *   HYP_KV8_E4M3  value = code * scale; scale = the least power of two p with amax <= 448 p, code the E4M3 number nearest to value / scale,
  *                 ties to even
- * A row with amax < 2^-118 is zeros under a scale of 0; one that holds an infinity or NaN, or whose rotation leaves fp32, gets a NaN scale: it
- * reads back as NaN.
+ * A row with amax < 2^-118 is zeros under a scale of 0; one that holds an infinity or NaN, or whose rotation (a term of it too) leaves fp32,
+ * gets a NaN scale: it reads back as NaN.
  * Lengths, tables and streams as for the operators over the fp16 cache above; the first call of hyp_op_kv8_write or hyp_op_attn_decode_kv8 on a device
  * allocates one word there: make it before capturing a graph. */
 enum { HYP_KV8_INT8 = 0, HYP_KV8_E4M3 = 1 };
@@ -396,7 +398,8 @@ HYP_API int hyp_op_kv8_write(const hyp_attn_shape* shape, int32_t format, int32_
                              void* q_out, void* stream);
 
 /* Tokens first[i] .. lens[i] - 1 of every sequence to the same slots of fp16 pages (the layout at the top of this file), for prefill attention
- * and the other operators over the fp16 cache.  Values are code times scale rounded once; beyond +-65504 they saturate.
+ * and the other operators over the fp16 cache.  Values are code times scale, rounded to fp32 and then to fp16; beyond +-65504
+ * they saturate.
  *   first  DEVICE int32 [n_seqs] or NULL (0);  lens DEVICE int32 [n_seqs]; both clamped to what both tables' rows can name
  *   dst_pages fp16 pool, 16-byte aligned;  dst_table int32 [n_seqs, dst_pages_per_seq].  Other slots are left as they were.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (both tables' rows name more than 2^31 - 2^16 half pages of a head), HYP_ECUDA. */
@@ -408,7 +411,8 @@ HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t
  * The softmax weights, times their values' scales, enter the value product as fp16, off by 2^-11 of each or by 2^-32 of the largest so far, whichever is
  * more; results beyond fp16 are infinities.  A score q . k that leaves fp32 counts as an infinity: NaN, or no weight.  A key or
  * value row with a NaN scale makes its sequence's results NaN, whatever its weight.
- * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.
+ * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.  Fewer sequences are split further
+ * and may need more: a buffer for any batch size holds the largest of its sizes.
  * Errors: HYP_EINVAL, HYP_ECAPACITY (scratch too small, more than 2^31 rows and heads to join), HYP_ECUDA. */
 HYP_API size_t hyp_op_attn_kv8_scratch_bytes(const hyp_attn_shape* shape, int32_t n_seqs, int32_t max_pages_per_seq);
 HYP_API int hyp_op_attn_decode_kv8(const hyp_attn_shape* shape, int32_t format, int32_t n_seqs, const void* q, int64_t q_stride,

@@ -131,9 +131,11 @@ struct WriteArgs {
 // grid (M, shares of the heads); ROPE: rotates.  One bulk copy brings a CTA's heads of a row to shared memory while the warps look up the row's sequence, page
 // and angles; then D / 4 lanes take a head, four values each.
 //   Bound by HBM for prompts (4096 fp32 rows of 60 heads of 128: 179 MB in 31-32 us, 5.6-5.8 TB/s), by latency for single tokens (8 rows: 2.5 us).
-// Loads by the warps themselves, one head ahead, had 24 KB on their way on an SM: 46 us.  Warps hide a head's chain of steps, so registers are
-// what counts: a rotation that is decided at run time costs 7-10 % (34 us; rows that are not rotated 9.9 instead of 8.1 for 2500), a CTA that walks
-// over rows with the next one's look-ups ahead (64 registers) 55-80 %.
+// Loads by the warps themselves, one head ahead, had 24 KB on their way on an SM: 46 us.  Warps hide a head's chain of steps: a rotation that
+// is decided at run time costs 7-10 % (34 us; rows that are not rotated 9.9 instead of 8.1 for 2500), a CTA that walks over rows with the next one's
+// look-ups ahead (64 registers) 55-80 %.  Six CTAs to an SM (rotating; eight otherwise) leave 40 (32) registers, for which most rotating forms, and the int8 ones at
+// D = 64, spill 8 or 16 bytes.  With five (seven) append and read of 4096 rows of 60 heads, fp32, take 42.3 instead of 41.6 us in int8, 40.1 instead of 41.8 in
+// e4m3, bf16 in int8 40.3, 40.9; 4096 rows of 40 heads of 64, bf16 in int8, 22.4, 20.7.
 //   Codes have to be those of the exact value.  Exact arithmetic on every value costs more than the memory (in fp64 76 us for 4096 rows of 60
 // heads, issue slots 84 % busy), so values are rotated and rounded in fp32, and fp64, in which products of fp32 numbers are exact, is
 // used for the largest value of a row and where a code hangs on the rotation's roundings.  Those are two of half a step each, of a term and of
