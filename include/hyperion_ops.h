@@ -409,7 +409,7 @@ HYP_API int hyp_op_kv8_read(const hyp_attn_shape* shape, int32_t format, int32_t
 
 /* hyp_op_attn_decode over the 8-bit cache (keys and values 0 .. ctx_lens[b], the new token's included; -1: nothing, the row is zeros).
  * The softmax weights, times their values' scales, enter the value product as fp16, off by 2^-11 of each or by 2^-32 of the largest so far, whichever is
- * more; results beyond fp16 are infinities.  A score q . k that leaves fp32 counts as an infinity: NaN, or no weight.  A key or
+ * more, and a softmax weight below 2^-112 of the largest may count as none; results beyond fp16 are infinities.  A score q . k that leaves fp32 counts as an infinity: NaN, or no weight.  A key or
  * value row with a NaN scale makes its sequence's results NaN, whatever its weight.
  * scratch: hyp_op_attn_kv8_scratch_bytes(...) bytes (0 on bad arguments), 16-byte aligned, as for the operators above.  Fewer sequences are split further
  * and may need more: a buffer for any batch size holds the largest of its sizes.
